@@ -13,6 +13,13 @@
  *   fr_unpack_verify  transfer buffer -> tensors, list of failing chunks
  *   fr_diff           chunks whose fingerprints differ
  *
+ * and over the optimizer step that makes the state, the same bits on every
+ * replica:
+ *
+ *   fr_grad_clip      norm of all gradients, non-finite count, clip factor
+ *   fr_adamw_step     AdamW over many tensors at once, moments in 32 or 8 bits
+ *   fr_opt_convert    moments from 32 bits to 8 and back
+ *
  * All device work runs in hand-written CUDA kernels for sm_103a.  There is no
  * CPU fallback: without a usable GPU every call returns FR_ERR_CUDA.
  *
@@ -333,6 +340,138 @@ fr_status fr_shard_pieces(uint64_t n_elems, uint32_t elem_bytes, uint32_t n_dst,
 #define FR_STATIC_MAX_SEGMENTS 131072
 fr_status fr_fingerprint_static(const fr_tensor* tensors, uint64_t n_tensors, uint64_t chunk_bytes,
                                 fr_fp* out_dev, void* stream);
+
+/* ---------------------------------------------------------------- optimizer step */
+
+/* The step that turns the state after step i into the state after step i+1:
+ * the one that the step tags of Sec. III-E bracket.  Data-parallel replicas
+ * stay comparable (fr_diff) and interchangeable (fr_restore) only if every
+ * one of them computes the same bits, so each result here is a function of
+ * the tensor list, its values and the call's arguments alone: not of
+ * addresses, alignment, the SM count or the order in which blocks run.
+ *
+ * One fr_opt_tensor is one parameter tensor and what training keeps for it,
+ * `n` elements of each.  A plan may hold parts of it: fr_grad_clip needs the
+ * gradients, fr_opt_convert the moments (m and v, both or neither),
+ * fr_adamw_step the weights, the gradients and the moments; a pointer that no
+ * call needs is NULL, in all of a plan's tensors or in some.
+ *
+ *   weight   what the model computes with: FR_DT_BF16 or FR_DT_F32
+ *   grad     FR_DT_BF16 or FR_DT_F32
+ *   master   fp32 copy of a bf16 weight; the step updates it and writes its
+ *            rounding (to nearest even) to the weight.  NULL: the weight itself
+ *            is the parameter
+ *   m, v     first and second moment, state_dtype FR_DT_F32, or FR_DT_BYTES: 8-bit
+ *            codes, with one exponent byte per FR_OPT_BLOCK elements in m_exp
+ *            and v_exp (ceil(n / FR_OPT_BLOCK) bytes each).  All zero bytes
+ *            is the zero moment of a first step
+ *   lr_scale, decay_scale   the tensor's factors on the learning rate and on the
+ *            weight decay (0: a norm or bias that does not decay)
+ *
+ * Any alignment to the element size is allowed (else FR_ERR_ALIGNMENT);
+ * 16-byte-aligned tensors are the fastest.  No two buffers may overlap.
+ *
+ * 8-bit moments.  A block is FR_OPT_BLOCK consecutive elements from the
+ * tensor's start (the last one shorter).  With A the largest bit pattern of
+ * |x| in it, its exponent byte is E = max((A + 0xFFFFF) >> 23, 16 for m, 32
+ * for v), a biased fp32 exponent at or above every element's.  m: bit 7 is
+ * the sign, bits 0-6 the code c; v: the whole byte is c.  With base = 8 (E -
+ * 15) for m and 8 (E - 31) for v, c > 0 stands for the fp32 number of pattern
+ * (c + base) << 20: three fraction bits, over the 15 (m) or 31 (v) binades
+ * below the block's top.  c = 0 is zero.  Coding adds to the pattern of |x|
+ * what the rounding gives below bit 20 and cuts there; what falls below code 1
+ * becomes 0 in m, and code 1 in v if it is not zero (a second moment rounded
+ * to zero would make the next step explode).  A block with an Inf or NaN gets
+ * E = 255, and all its elements read as NaN.
+ *
+ * Rounding to fewer bits: FR_ROUND_NEAREST (ties to even) or FR_ROUND_RANDOM,
+ * up with the probability that makes the mean exact: with beta2 = 0.999 a
+ * second moment changes by less than half a step of its code per update, so
+ * that to nearest it would stand still.  The random bits come from a counter:
+ * a function of seed, step, the tensor's index in the plan and the element's
+ * index, so replicas draw the same.  FR_ROUND_RANDOM also rounds a bf16
+ * weight without a master. */
+#define FR_OPT_BLOCK 256
+
+typedef enum { FR_ROUND_NEAREST = 0, FR_ROUND_RANDOM = 1 } fr_rounding;
+
+typedef struct {
+  void* weight;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  uint8_t* m_exp; /* 8-bit moments only, else NULL */
+  uint8_t* v_exp;
+  uint64_t n;     /* elements */
+  uint32_t weight_dtype;
+  uint32_t grad_dtype;
+  uint32_t state_dtype;
+  uint32_t flags; /* 0 */
+  float lr_scale;
+  float decay_scale;
+} fr_opt_tensor;
+
+typedef struct fr_opt_s* fr_opt;
+
+/* Plan the step over `n_tensors` tensors (host array, copied; a tensor of 0
+ * elements is allowed).  As with fr_plan_create, the plan is bound to the
+ * current device and to the tensors' addresses, it allocates here and nowhere
+ * else, and one stream at a time may use it.
+ * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT, FR_ERR_CUDA. */
+fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt* out);
+
+/* Tensors, elements and FR_OPT_BLOCK blocks of a plan (host; any may be NULL). */
+fr_status fr_opt_info(fr_opt plan, uint64_t* n_tensors, uint64_t* n_elems, uint64_t* n_blocks);
+
+/* Free the plan and its device memory (synchronizes the device first). */
+void fr_opt_destroy(fr_opt plan);
+
+/* What fr_grad_clip finds, in device memory, 16 bytes. */
+typedef struct {
+  float norm;         /* grad_scale * sqrt(sum of squares of the finite gradients)      */
+  float scale;        /* grad_scale * min(1, max_norm / norm); 0 if any is non-finite   */
+  uint64_t nonfinite; /* gradients whose exponent field is all ones                     */
+} fr_clip;
+
+/* Norm of all the plan's gradients, the number of non-finite ones, and the
+ * factor by which fr_adamw_step multiplies each gradient.  `grad_scale` (finite,
+ * > 0) undoes a loss scale or a gradient accumulation; `max_norm` > 0,
+ * INFINITY for no clipping.  Sums of squares neither overflow nor underflow.
+ * Reads the gradients once.  With the parameters spread over several ranks or
+ * plans, add their norms' squares and their counts and write the record by a
+ * kernel of your own.  `out_dev`: 8-byte aligned.
+ * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
+fr_status fr_grad_clip(fr_opt plan, float max_norm, float grad_scale, fr_clip* out_dev, void* stream);
+
+/* One step's numbers.  0 <= beta1, beta2 < 1, eps > 0, lr and weight_decay
+ * >= 0, all finite; step counts from 1 (a skipped step does not count). */
+typedef struct {
+  double lr, beta1, beta2, eps, weight_decay;
+  uint64_t step;
+  uint64_t seed;     /* FR_ROUND_RANDOM: the same on all replicas */
+  uint32_t rounding; /* fr_rounding */
+  uint32_t reserved; /* 0 */
+} fr_adamw;
+
+/* AdamW, in fp32, per element with h = scale * gradient:
+ *   m <- beta1 m + (1 - beta1) h,   v <- beta2 v + (1 - beta2) h h
+ *   p <- p - lr lr_scale ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *                         + weight_decay decay_scale p)
+ * m and v each by separately rounded products and sums (so 8-bit codes are
+ * the same bits wherever they are computed); p uses them before they are coded.
+ * `clip_dev`: the record of fr_grad_clip, read on the device: its scale, and
+ * if its nonfinite is not 0 the step leaves every byte as it is.  NULL: scale 1.
+ * In a CUDA graph the numbers in `hyper` are those of the capture.
+ * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
+fr_status fr_adamw_step(fr_opt plan, const fr_adamw* hyper, const fr_clip* clip_dev, void* stream);
+
+/* Write the moments of `dst` from those of `src`, tensor by tensor of equal
+ * size: FR_DT_F32 to FR_DT_BYTES (`rounding`, and `seed` with step 0; a
+ * negative second moment counts as zero) or FR_DT_BYTES to FR_DT_F32 (both
+ * ignored).  The two plans need one element type each, not the same one.
+ * Errors: FR_ERR_INVALID_ARG, FR_ERR_PLAN_MISMATCH (other sizes), FR_ERR_CUDA. */
+fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t seed, void* stream);
 
 /* ---------------------------------------------------------------- status */
 

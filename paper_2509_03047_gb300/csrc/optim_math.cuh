@@ -1,0 +1,100 @@
+// optim_math.cuh -- arithmetic of the optimizer step that its kernels share:
+// the update, the 8-bit moments' code, the random bits of a rounding.
+//
+// Every operation is written as the one rounding that it is (no contraction
+// is left to the compiler), so all kernels and paths give the same bits.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include <cstdint>
+
+#include "optim.h"
+
+namespace frk {
+
+// ---- 8-bit moments (the format is described in flashrec.h)
+
+constexpr int kSpanM = 15, kSpanV = 31;  // binades below a block's top
+
+// A block's exponent from the largest bit pattern of |x| in it.  The largest
+// code is reached whichever way its element is rounded: 0xFFFFF is the most
+// that a rounding adds.
+__device__ __forceinline__ uint32_t block_exponent(uint32_t top, int span) {
+  const uint32_t e = (min(top, 0x7F800000u) + 0xFFFFFu) >> 23;
+  return max(e, static_cast<uint32_t>(span + 1));
+}
+__device__ __forceinline__ int code_base(uint32_t e, int span) {
+  return static_cast<int>(max(e, static_cast<uint32_t>(span + 1)) - span) << 3;
+}
+
+__device__ __forceinline__ uint32_t round_nearest(uint32_t bits) { return 0x7FFFFu + ((bits >> 20) & 1u); }
+
+// r: what the rounding adds below bit 20.
+__device__ __forceinline__ uint32_t encode_m(float x, uint32_t r, uint32_t e) {
+  const uint32_t bits = __float_as_uint(x);
+  const int c = static_cast<int>(((bits & 0x7FFFFFFFu) + r) >> 20) - code_base(e, kSpanM);
+  return c < 1 || e == 255 ? 0u : static_cast<uint32_t>(c) | ((bits >> 24) & 0x80u);
+}
+__device__ __forceinline__ uint32_t encode_v(float x, uint32_t r, uint32_t e) {
+  const uint32_t bits = __float_as_uint(x) & 0x7FFFFFFFu;
+  const int c = static_cast<int>((bits + r) >> 20) - code_base(e, kSpanV);
+  return bits == 0 || e == 255 ? 0u : static_cast<uint32_t>(max(c, 1));
+}
+__device__ __forceinline__ float decode_m(uint32_t code, uint32_t e) {
+  const uint32_t c = code & 0x7Fu;
+  const uint32_t bits = c ? ((c + code_base(e, kSpanM)) << 20) | ((code & 0x80u) << 24) : 0u;
+  return e == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(bits);
+}
+__device__ __forceinline__ float decode_v(uint32_t code, uint32_t e) {
+  const uint32_t bits = code ? (code + code_base(e, kSpanV)) << 20 : 0u;
+  return e == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(bits);
+}
+
+// ---- random bits
+//
+// A counter-based generator: two rounds of multiplication and shift over the
+// index of a pair of elements, keyed by 64 bits per tensor, then one product
+// for each number that is taken.  The factors are the golden ratio's and, from
+// L'Ecuyer, "Tables of linear congruential generators of different sizes and
+// good lattice structure" (1999) and its successors, multipliers modulo 2^32.
+struct RandomKey {
+  uint32_t lo, hi;
+};
+__device__ __forceinline__ RandomKey random_key(uint64_t key, uint32_t tensor) {
+  const uint64_t k = mix64(key + tensor * 0x9E3779B97F4A7C15ull);
+  return {static_cast<uint32_t>(k), static_cast<uint32_t>(k >> 32)};
+}
+__device__ __forceinline__ uint32_t random_pair(RandomKey k, uint64_t pair) {
+  uint32_t u = static_cast<uint32_t>(pair) * 0x9E3779B1u + (k.lo ^ (static_cast<uint32_t>(pair >> 32) * 0x85EBCA77u));
+  u ^= u >> 16;
+  u = u * 2891336453u + k.hi;
+  return u ^ (u >> 15);
+}
+// 32 bits of the pair's first or second element: the high half rounds v, the low half m.
+__device__ __forceinline__ uint32_t random_moments(uint32_t u, int odd) { return u * (odd ? 741103597u : 1597334677u); }
+// The pair's weights: 16 bits each, the high half for the first.
+__device__ __forceinline__ uint32_t random_weights(uint32_t u) { return u * 747796405u; }
+
+// ---- the update
+
+struct Hyper {
+  float b1, c1, b2, c2, scale;  // scale: of the gradient
+  float lr, decay, eps, m_fix, v_fix;
+};
+
+// New moments, each product and sum rounded by itself.
+__device__ __forceinline__ void update_moments(const Hyper& h, float grad, float& m, float& v) {
+  const float g = __fmul_rn(grad, h.scale);
+  m = __fadd_rn(__fmul_rn(m, h.b1), __fmul_rn(g, h.c1));
+  v = __fadd_rn(__fmul_rn(v, h.b2), __fmul_rn(__fmul_rn(g, g), h.c2));
+}
+
+// The parameter from the new moments.
+__device__ __forceinline__ float update_param(const Hyper& h, float p, float m, float v) {
+  const float below = __fmaf_rn(__fsqrt_rn(v), h.v_fix, h.eps);
+  const float u = __fmaf_rn(__fdiv_rn(m, below), h.m_fix, __fmul_rn(p, h.decay));
+  return __fmaf_rn(-h.lr, u, p);
+}
+
+}  // namespace frk

@@ -28,6 +28,9 @@ FR_ERR_CUDA = 7
 
 FR_DT_BYTES, FR_DT_BF16, FR_DT_F32 = 0, 1, 2
 FP_ENTRY_BYTES = 16
+FR_OPT_BLOCK = 256
+FR_ROUND_NEAREST, FR_ROUND_RANDOM = 0, 1
+CLIP_BYTES = 16
 
 _TORCH_TO_FR = {torch.bfloat16: FR_DT_BF16, torch.float32: FR_DT_F32, torch.uint8: FR_DT_BYTES,
                 torch.int8: FR_DT_BYTES}
@@ -41,6 +44,21 @@ class fr_tensor(ctypes.Structure):
 class fr_piece(ctypes.Structure):
     _fields_ = [("source", ctypes.c_uint32), ("reserved", ctypes.c_uint32), ("src_off", ctypes.c_uint64),
                 ("dst_off", ctypes.c_uint64), ("nbytes", ctypes.c_uint64)]
+
+
+class fr_opt_tensor(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("n", ctypes.c_uint64), ("weight_dtype", ctypes.c_uint32), ("grad_dtype", ctypes.c_uint32),
+                ("state_dtype", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("lr_scale", ctypes.c_float),
+                ("decay_scale", ctypes.c_float)]
+
+
+class fr_adamw(ctypes.Structure):
+    """One step's numbers; a training loop keeps one and counts `step` up."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double), ("step", ctypes.c_uint64), ("seed", ctypes.c_uint64),
+                ("rounding", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
 
 
 class FlashrecError(RuntimeError):
@@ -80,6 +98,13 @@ def _load() -> ctypes.CDLL:
     L.fr_resend_fp.argtypes = [vp, vp, vp, u64, u64p, vp, vp, vp, vp]
     L.fr_restore_multi.argtypes = [ctypes.POINTER(vp), u32, vp, vp, u64, u32, vp, u64, vp, vp,
                                    ctypes.POINTER(vp), vp]
+    L.fr_opt_create.argtypes = [ctypes.POINTER(fr_opt_tensor), u64, ctypes.POINTER(vp)]
+    L.fr_opt_info.argtypes = [vp, u64p, u64p, u64p]
+    L.fr_opt_destroy.argtypes = [vp]
+    L.fr_opt_destroy.restype = None
+    L.fr_grad_clip.argtypes = [vp, ctypes.c_float, ctypes.c_float, vp, vp]
+    L.fr_adamw_step.argtypes = [vp, ctypes.POINTER(fr_adamw), vp, vp]
+    L.fr_opt_convert.argtypes = [vp, vp, u32, u64, vp]
     L.fr_status_str.argtypes = [ctypes.c_int]
     L.fr_status_str.restype = ctypes.c_char_p
     L.fr_last_error.argtypes = []
@@ -89,7 +114,8 @@ def _load() -> ctypes.CDLL:
                  "fr_unpack_verify", "fr_diff", "fr_sync_status", "fr_version", "fr_fingerprint_static",
                  "fr_plan_create_batched", "fr_plan_batch", "fr_pack_batch", "fr_unpack_verify_batch",
                  "fr_unpack_collect", "fr_resend", "fr_restore", "fr_shard_pieces", "fr_pack_fp", "fr_unpack_verify_fp",
-                 "fr_restore_fp", "fr_resend_fp", "fr_restore_multi"]:
+                 "fr_restore_fp", "fr_resend_fp", "fr_restore_multi", "fr_opt_create", "fr_opt_info", "fr_grad_clip",
+                 "fr_adamw_step", "fr_opt_convert"]:
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -326,6 +352,118 @@ def fr_fingerprint_static(tensors: Sequence[torch.Tensor], chunk_bytes: int, out
                                      _stream(stream)), "fr_fingerprint_static")
 
 
+# ---------------------------------------------------------------- optimizer step
+
+_FLOATS = {torch.bfloat16: FR_DT_BF16, torch.float32: FR_DT_F32}
+_MOMENTS = {torch.float32: FR_DT_F32, torch.uint8: FR_DT_BYTES}
+_F32 = {torch.float32: FR_DT_F32}
+_U8 = {torch.uint8: FR_DT_BYTES}
+
+
+def _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scale):
+    """(fr_opt_tensor array, its length): 11 words per tensor, filled column by column."""
+    lists = [("weights", weights, _FLOATS, 1), ("grads", grads, _FLOATS, 1), ("masters", masters, _F32, 1),
+             ("m", m, _MOMENTS, 1), ("v", v, _MOMENTS, 1), ("m_exp", m_exp, _U8, FR_OPT_BLOCK),
+             ("v_exp", v_exp, _U8, FR_OPT_BLOCK)]
+    given = [x for _, x, _, _ in lists if x is not None]
+    if not given:
+        raise ValueError("a plan needs weights, gradients or moments")
+    count = len(given[0])
+    sizes = [None] * count
+    columns, codes = [], {}
+    for name, tensors, allowed, per in lists:
+        if tensors is None:
+            columns.append([0] * count)
+            codes[name] = [0] * count
+            continue
+        if len(tensors) != count:
+            raise ValueError("%s holds %d tensors, not %d" % (name, len(tensors), count))
+        column, code = [], []
+        for i, t in enumerate(tensors):
+            if t is None:
+                column.append(0)
+                code.append(0)
+                continue
+            n = t.numel()
+            if n and not t.is_cuda:
+                raise ValueError("%s[%d] is not on a CUDA device" % (name, i))
+            if not t.is_contiguous():
+                raise ValueError("%s[%d] is not contiguous" % (name, i))
+            c = allowed.get(t.dtype)
+            if c is None:
+                raise ValueError("%s[%d]: unsupported dtype %s" % (name, i, t.dtype))
+            if per == 1:
+                if sizes[i] is None:
+                    sizes[i] = n
+                elif sizes[i] != n:
+                    raise ValueError("%s[%d] holds %d elements, not %d" % (name, i, n, sizes[i]))
+            elif n != -(-(sizes[i] or 0) // per):
+                raise ValueError("%s[%d] holds %d bytes, one per block of %d is needed" % (name, i, n, per))
+            column.append(t.data_ptr() if n else 0)
+            code.append(c)
+        columns.append(column)
+        codes[name] = code
+    if any(a != b for a, b in zip(codes["m"], codes["v"])):
+        raise ValueError("m and v differ in type")
+
+    def factors(x):
+        x = array.array("f", [1.0] * count if x is None else x)
+        if len(x) != count:
+            raise ValueError("%d factors for %d tensors" % (len(x), count))
+        return array.array("I", x.tobytes())
+
+    words = array.array("Q", bytes(8 * 11 * max(count, 1)))
+    for k, column in enumerate(columns):
+        words[k:11 * count:11] = array.array("Q", column)
+    words[7:11 * count:11] = array.array("Q", [n or 0 for n in sizes])
+    words[8:11 * count:11] = array.array("Q", [w | g << 32 for w, g in zip(codes["weights"], codes["grads"])])
+    words[9:11 * count:11] = array.array("Q", codes["m"])
+    words[10:11 * count:11] = array.array("Q", [a | b << 32 for a, b in zip(factors(lr_scale), factors(decay_scale))])
+    return (fr_opt_tensor * max(count, 1)).from_buffer(words), count
+
+
+def fr_opt_create(weights=None, grads=None, m=None, v=None, masters=None, m_exp=None, v_exp=None, lr_scale=None,
+                  decay_scale=None):
+    """Plan over lists of contiguous CUDA tensors (a list, or an entry, may be None; factors default to 1).  Moments
+    are fp32, or uint8 codes with one uint8 exponent per FR_OPT_BLOCK elements.  Returns the opaque handle (int)."""
+    arr, count = _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scale)
+    h = ctypes.c_void_p()
+    _check(lib.fr_opt_create(arr, count, ctypes.byref(h)), "fr_opt_create")
+    return h.value
+
+
+def fr_opt_info(plan):
+    """(tensors, elements, blocks)"""
+    t, n, b = ctypes.c_uint64(), ctypes.c_uint64(), ctypes.c_uint64()
+    _check(lib.fr_opt_info(plan, ctypes.byref(t), ctypes.byref(n), ctypes.byref(b)), "fr_opt_info")
+    return t.value, n.value, b.value
+
+
+def fr_opt_destroy(plan) -> None:
+    if plan:
+        lib.fr_opt_destroy(plan)
+
+
+def _record(t: torch.Tensor) -> int:
+    if not t.is_cuda or not t.is_contiguous() or t.nbytes < CLIP_BYTES:
+        raise ValueError("a clip record is %d bytes of CUDA memory" % CLIP_BYTES)
+    return t.data_ptr()
+
+
+def fr_grad_clip(plan, max_norm: float, grad_scale: float, out: torch.Tensor, stream=None) -> None:
+    """`out`: CUDA tensor of 16 bytes, the fr_clip record (see clip_view)."""
+    _check(lib.fr_grad_clip(plan, max_norm, grad_scale, _record(out), _stream(stream)), "fr_grad_clip")
+
+
+def fr_adamw_step(plan, hyper: fr_adamw, clip: Optional[torch.Tensor] = None, stream=None) -> None:
+    _check(lib.fr_adamw_step(plan, hyper, None if clip is None else _record(clip), _stream(stream)), "fr_adamw_step")
+
+
+def fr_opt_convert(src, dst, rounding: int = FR_ROUND_NEAREST, seed: int = 0, stream=None) -> None:
+    """The moments of plan `dst` from those of plan `src`, 32 bits to 8 or back."""
+    _check(lib.fr_opt_convert(src, dst, rounding, seed, _stream(stream)), "fr_opt_convert")
+
+
 # ---------------------------------------------------------------- convenience
 
 def fr_shard_pieces(n_elems: int, elem_bytes: int, n_dst: int, rank: int, n_src: int):
@@ -436,3 +574,50 @@ def diff(a: torch.Tensor, b: torch.Tensor, cap: Optional[int] = None, stream=Non
     fr_diff(a, b, n, out, count, stream)
     k = int(count.item())
     return out[: min(k, cap)], k
+
+
+def clip_view(record: torch.Tensor):
+    """(norm, scale, nonfinite) of an fr_clip record, as views of one element each."""
+    b = record.view(torch.uint8).view(-1)
+    return b[0:4].view(torch.float32), b[4:8].view(torch.float32), b[8:16].view(torch.int64)
+
+
+class OptPlan:
+    """A plan of the optimizer step over lists of CUDA tensors (arguments as fr_opt_create)."""
+
+    def __init__(self, weights=None, grads=None, m=None, v=None, masters=None, m_exp=None, v_exp=None, lr_scale=None,
+                 decay_scale=None):
+        lists = [weights, grads, m, v, masters, m_exp, v_exp]
+        self.buffers = [None if x is None else list(x) for x in lists]  # the plan holds their addresses
+        first = next((t for x in self.buffers if x for t in x if t is not None), None)
+        self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
+        self.handle = None
+        self.handle = fr_opt_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale)
+        self.n_tensors, self.n_elems, self.n_blocks = fr_opt_info(self.handle)
+
+    def close(self) -> None:
+        if self.handle:
+            fr_opt_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def new_clip(self) -> torch.Tensor:
+        return torch.zeros(CLIP_BYTES, dtype=torch.uint8, device=self.device)
+
+    def clip(self, max_norm: float = float("inf"), grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
+             stream=None) -> torch.Tensor:
+        """fr_grad_clip: returns the record, for step()."""
+        out = self.new_clip() if out is None else out
+        fr_grad_clip(self.handle, max_norm, grad_scale, out, stream)
+        return out
+
+    def step(self, hyper: fr_adamw, clip: Optional[torch.Tensor] = None, stream=None) -> None:
+        fr_adamw_step(self.handle, hyper, clip, stream)
+
+    def convert_to(self, dst: "OptPlan", rounding: int = FR_ROUND_NEAREST, seed: int = 0, stream=None) -> None:
+        fr_opt_convert(self.handle, dst.handle, rounding, seed, stream)
