@@ -1,10 +1,9 @@
 // optim.h -- the optimizer step's plan tables and kernel launchers (internal
 // to libflashrec).
 //
-// Work is counted in blocks of kOptBlock elements from each tensor's start, a
-// warp's unit: eight elements per lane.  A launch cuts the concatenated blocks
-// of its tensors into one contiguous range per warp, so the warps take equal
-// times whatever the tensor sizes.
+// Work is counted in blocks of kOptBlock elements from each tensor's start:
+// what a warp takes at a time, eight elements per lane.  A launch's blocks are
+// those of its tensors one after the other, in units of consecutive blocks.
 #pragma once
 
 #include <cstdint>
@@ -39,30 +38,25 @@ struct OptDesc {        // 96 bytes: one tensor that has elements
 };
 static_assert(sizeof(OptDesc) == 96, "OptDesc layout");
 
-// Tensors in order, and for each warp of a launch the tensor that its range
-// starts in: warp w of n_warps takes the blocks [n_blocks * w / n_warps,
-// n_blocks * (w + 1) / n_warps).
+// Tensors in order, and for each unit the tensor that it starts in.
 struct OptWork {
   const OptDesc* tensors;
   const uint32_t* start;
-  uint32_t n_blocks;
-  uint32_t n_warps;
+  uint32_t n_blocks, n_units, unit_blocks;
 };
-__host__ __device__ inline uint32_t opt_range(uint32_t n_blocks, uint32_t n_warps, uint32_t w) {
-  return static_cast<uint32_t>(static_cast<uint64_t>(n_blocks) * w / n_warps);
-}
 
 constexpr int kOptWarps = 8;  // per CTA, in every kernel here
 
 // ---- the norm
 
-// A launch's sums are added in an order that the warps' ranges decide, so how
-// many there are follows from the sizes alone, not from the GPU: four blocks
-// per warp at least, and 8 CTAs for each of a GB300's 152 SMs at most.
-constexpr uint32_t kClipCtas = 8 * 152;
-inline uint32_t clip_ctas(uint64_t n_blocks) {
-  const uint64_t c = (n_blocks + 4 * kOptWarps - 1) / (4 * kOptWarps);
-  return c < 1 ? 1 : c < kClipCtas ? static_cast<uint32_t>(c) : kClipCtas;
+// A launch's sums are added in an order that units and CTAs decide, so both
+// follow from the sizes alone, not from the GPU: at most 4 CTAs for each of a
+// GB300's 152 SMs, about four units for each, of 2 to 16 blocks per warp.
+constexpr uint32_t kClipUnit = 16 * kOptWarps;
+constexpr uint32_t kClipCtas = 4 * 152;
+inline uint32_t clip_unit(uint64_t n_blocks) {
+  const uint64_t per_warp = n_blocks / (4 * kClipCtas * kOptWarps);
+  return static_cast<uint32_t>(per_warp < 2 ? 2 : per_warp < 16 ? per_warp : 16) * kOptWarps;
 }
 struct ClipPartial {  // of one CTA
   double sumsq;
@@ -75,7 +69,7 @@ struct ClipParams {
   double grad_scale, max_norm;
   fr_clip* out;
 };
-cudaError_t launch_clip(const ClipParams& p, int n_ctas, cudaStream_t s);
+cudaError_t launch_clip(const ClipParams& p, cudaStream_t s);
 
 // ---- the step
 
@@ -83,10 +77,10 @@ cudaError_t launch_clip(const ClipParams& p, int n_ctas, cudaStream_t s);
 enum : int { kWeightF32 = 0, kWeightBf16 = 1, kWeightMaster = 2 };  // the parameter: fp32 weight, bf16 weight, master
 struct StepClass {
   int weight;
-  bool bf16_grad, eight, aligned;
-  int index() const { return ((weight * 2 + bf16_grad) * 2 + eight) * 2 + aligned; }
+  bool bf16_grad, eight;
+  int index() const { return (weight * 2 + bf16_grad) * 2 + eight; }
 };
-constexpr int kStepClasses = 3 * 2 * 2 * 2;
+constexpr int kStepClasses = 3 * 2 * 2;
 
 struct StepParams {
   OptWork work;
@@ -94,11 +88,11 @@ struct StepParams {
   float b1, c1, b2, c2;        // beta1, 1 - beta1, beta2, 1 - beta2
   float lr, decay, eps;
   float m_fix, v_fix;          // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  uint32_t exact;              // 1: eps is too small for the approximations of update_param (optim_math.cuh)
   uint32_t random;             // 1: FR_ROUND_RANDOM
   uint64_t key;                // of the random bits: mix64(mix64(seed) + step)
 };
-cudaError_t launch_step(const StepClass& c, const StepParams& p, int n_ctas, cudaStream_t s);
-int step_ctas_per_sm(const StepClass& c);
+cudaError_t launch_step(const StepClass& c, const StepParams& p, cudaStream_t s);
 
 // ---- conversion
 
@@ -108,8 +102,7 @@ struct ConvertParams {
   uint32_t random;
   uint64_t key;
 };
-constexpr int kConvertCtasPerSm = 4;
-cudaError_t launch_convert(const ConvertParams& p, int n_ctas, cudaStream_t s);
+cudaError_t launch_convert(const ConvertParams& p, cudaStream_t s);
 
 // splitmix64's output function (Steele, Lea, Flood, "Fast splittable
 // pseudorandom number generators", OOPSLA 2014).

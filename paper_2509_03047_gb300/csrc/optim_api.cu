@@ -1,6 +1,6 @@
 // optim_api.cu -- the C ABI of the optimizer step (declared in
 // include/flashrec.h) and its planner: the tensors of each launch in one list,
-// with the tensor in which each warp's range of blocks starts.
+// cut into units of blocks.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,7 @@ struct WorkList {
   std::vector<OptDesc> tensors;
   std::vector<uint32_t> start;
   uint64_t n_blocks = 0;
-  int n_ctas = 0;
+  uint32_t unit_blocks = kOptWarps;
   OptDesc* d_tensors = nullptr;
   uint32_t* d_start = nullptr;
 
@@ -31,16 +31,15 @@ struct WorkList {
     n_blocks += d.n_blocks;
     tensors.push_back(d);
   }
-  // At most `most` CTAs, one block per warp at least.
-  void cut(uint32_t most) {
-    n_ctas = static_cast<int>(std::max<uint64_t>(1, std::min<uint64_t>(most, (n_blocks + kOptWarps - 1) / kOptWarps)));
-    const uint32_t n_warps = static_cast<uint32_t>(n_ctas) * kOptWarps;
-    start.resize(n_warps);
+  // Into units of `blocks`.
+  void cut(uint32_t blocks) {
+    unit_blocks = blocks;
+    const uint64_t n_units = (n_blocks + unit_blocks - 1) / unit_blocks;
+    start.resize(n_units);
     size_t t = 0;
-    for (uint32_t w = 0; w < n_warps; ++w) {
-      const uint32_t b = opt_range(static_cast<uint32_t>(n_blocks), n_warps, w);
-      while (t + 1 < tensors.size() && tensors[t + 1].first <= b) ++t;
-      start[w] = static_cast<uint32_t>(t);
+    for (uint64_t u = 0; u < n_units; ++u) {
+      while (t + 1 < tensors.size() && tensors[t + 1].first <= u * unit_blocks) ++t;
+      start[u] = static_cast<uint32_t>(t);
     }
   }
   void place(PlanMemory& mem) {
@@ -48,7 +47,8 @@ struct WorkList {
     mem.table(&d_start, start);
   }
   OptWork work() const {
-    return {d_tensors, d_start, static_cast<uint32_t>(n_blocks), static_cast<uint32_t>(n_ctas) * kOptWarps};
+    return {d_tensors, d_start, static_cast<uint32_t>(n_blocks), static_cast<uint32_t>((n_blocks + unit_blocks - 1) / unit_blocks),
+            unit_blocks};
   }
 };
 
@@ -114,7 +114,7 @@ OptDesc describe(const fr_opt_tensor& x, uint64_t index) {
   return d;
 }
 
-fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors, int n_sm) {
+fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
   for (uint64_t t = 0; t < n_tensors; ++t) {
     const fr_opt_tensor& x = tensors[t];
     p->sizes.push_back(x.n);
@@ -129,7 +129,6 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors, i
       c.weight = x.master ? kWeightMaster : x.weight_dtype == FR_DT_BF16 ? kWeightBf16 : kWeightF32;
       c.bf16_grad = x.grad_dtype == FR_DT_BF16;
       c.eight = x.state_dtype == FR_DT_BYTES;
-      c.aligned = d.aligned;
       p->classes[c.index()] = c;
       p->step[c.index()].add(d);
     } else {
@@ -140,20 +139,20 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors, i
     if (x.m) (x.state_dtype == FR_DT_BYTES ? p->eight : p->thirty_two) = true;
   }
   PlanMemory mem;
-  p->clip.cut(clip_ctas(p->clip.n_blocks));
+  p->clip.cut(clip_unit(p->clip.n_blocks));
   p->clip.place(mem);
   if (p->moments) {
-    p->convert.cut(static_cast<uint32_t>(n_sm * kConvertCtasPerSm));
+    p->convert.cut(kOptWarps);
     p->convert.place(mem);
   }
   if (p->params)
     for (int c = 0; c < kStepClasses; ++c) {
       if (p->step[c].n_blocks == 0) continue;
-      p->step[c].cut(static_cast<uint32_t>(n_sm * step_ctas_per_sm(p->classes[c])));
+      p->step[c].cut(kOptWarps);
       p->step[c].place(mem);
     }
   mem.table(&p->d_done, std::vector<uint32_t>(1, 0));
-  mem.scratch(&p->d_partials, static_cast<uint64_t>(p->clip.n_ctas));
+  mem.scratch(&p->d_partials, kClipCtas);
   const cudaError_t e = mem.commit(&p->d_memory);
   // The device has them now.
   auto drop = [](WorkList& l) {
@@ -189,18 +188,16 @@ fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt
   }
   if (blocks >= (1ull << 32) - 1) return report_invalid(me, "too many elements");
 
-  int dev = 0, n_sm = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return report_cuda("cudaGetDevice", e);
-  e = cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return report_cuda("cudaDeviceGetAttribute", e);
 
   fr_opt p = new (std::nothrow) fr_opt_s;
   if (p == nullptr) return report_invalid(me, "out of host memory");
   p->device = dev;
   fr_status st;
   try {
-    st = fill_opt(p, tensors, n_tensors, n_sm);
+    st = fill_opt(p, tensors, n_tensors);
   } catch (const std::bad_alloc&) {
     st = report_invalid(me, "out of host memory");
   }
@@ -247,7 +244,7 @@ fr_status fr_grad_clip(fr_opt p, float max_norm, float grad_scale, fr_clip* out_
   cp.grad_scale = grad_scale;
   cp.max_norm = max_norm;
   cp.out = out_dev;
-  const cudaError_t e = launch_clip(cp, p->clip.n_ctas, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_clip(cp, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? FR_OK : report_cuda("clip kernel launch", e);
 }
 
@@ -279,12 +276,13 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   sp.eps = static_cast<float>(h->eps);
   sp.m_fix = static_cast<float>(1.0 / (1.0 - std::pow(h->beta1, static_cast<double>(h->step))));
   sp.v_fix = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(h->beta2, static_cast<double>(h->step))));
+  sp.exact = sp.eps < 0x1p-39f * sp.v_fix;
   sp.random = h->rounding == FR_ROUND_RANDOM;
   sp.key = mix64(mix64(h->seed) + h->step);
   for (int c = 0; c < kStepClasses; ++c) {
     if (p->step[c].n_blocks == 0) continue;
     sp.work = p->step[c].work();
-    const cudaError_t e = launch_step(p->classes[c], sp, p->step[c].n_ctas, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_step(p->classes[c], sp, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return report_cuda("step kernel launch", e);
   }
   return FR_OK;
@@ -311,7 +309,7 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
   cp.to_eight = dst->eight;
   cp.random = rounding == FR_ROUND_RANDOM;
   cp.key = mix64(mix64(seed));
-  const cudaError_t e = launch_convert(cp, src->convert.n_ctas, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_convert(cp, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? FR_OK : report_cuda("convert kernel launch", e);
 }
 

@@ -1,5 +1,10 @@
-// optim_block.cuh -- a warp's block of 256 elements: loads, stores, random bits,
-// coding of 8-bit moments.
+// optim_block.cuh -- a warp's block of 256 elements: walking the units, loads,
+// stores, random bits, coding of 8-bit moments.
+//
+// A whole block whose buffers are aligned moves as vectors: lane l has the
+// elements 8 l ... 8 l + 7.  Any other block moves element by element, lane l
+// with the elements l, l + 32, ..., those past the tensor's end read as zero.
+// Both give the same bits.
 #pragma once
 
 #include "optim.h"
@@ -7,118 +12,196 @@
 
 namespace frk {
 
-// The eight elements of a lane, in an aligned tensor lane * 8 + j, else j * 32
-// + lane (single elements, coalesced).
-template <bool Aligned>
-__device__ __forceinline__ int place(int lane, int j) {
-  return Aligned ? lane * kOptLane + j : j * 32 + lane;
+// The tensor of block b of a launch, from the one that b's unit starts in.
+__device__ __forceinline__ uint32_t tensor_of(const OptWork& w, uint32_t t, uint32_t b) {
+  while (b - w.tensors[t].first >= w.tensors[t].n_blocks) ++t;
+  return t;
 }
 
-// Loads and stores of a lane's elements [0, left) of a block; elements past the
-// end read as zero.
-template <bool Aligned>
-__device__ __forceinline__ void load(const float* p, int lane, int left, float (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    const float4 a = reinterpret_cast<const float4*>(p)[lane * 2], b = reinterpret_cast<const float4*>(p)[lane * 2 + 1];
-    x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j) x[j] = place<Aligned>(lane, j) < left ? p[place<Aligned>(lane, j)] : 0.0f;
+// ---- vectors
+
+template <class T>
+__device__ __forceinline__ T load_vector(const T* p) {
+  T r;
+  if constexpr (sizeof(T) == 16)
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(reinterpret_cast<uint32_t*>(&r)[0]), "=r"(reinterpret_cast<uint32_t*>(&r)[1]),
+                   "=r"(reinterpret_cast<uint32_t*>(&r)[2]), "=r"(reinterpret_cast<uint32_t*>(&r)[3])
+                 : "l"(p));
+  else
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];"
+                 : "=r"(reinterpret_cast<uint32_t*>(&r)[0]), "=r"(reinterpret_cast<uint32_t*>(&r)[1])
+                 : "l"(p));
+  return r;
 }
-template <bool Aligned>
-__device__ __forceinline__ void store(float* p, int lane, int left, const float (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    reinterpret_cast<float4*>(p)[lane * 2] = make_float4(x[0], x[1], x[2], x[3]);
-    reinterpret_cast<float4*>(p)[lane * 2 + 1] = make_float4(x[4], x[5], x[6], x[7]);
-    return;
+
+// A lane's eight elements as they lie in memory.
+struct RawF32 {
+  uint4 a, b;
+  __device__ __forceinline__ void load(const void* block, int lane) {
+    a = load_vector(static_cast<const uint4*>(block) + 2 * lane);
+    b = load_vector(static_cast<const uint4*>(block) + 2 * lane + 1);
   }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j)
-    if (place<Aligned>(lane, j) < left) p[place<Aligned>(lane, j)] = x[j];
-}
-template <bool Aligned>
-__device__ __forceinline__ void load(const uint16_t* p, int lane, int left, float (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    const uint4 a = reinterpret_cast<const uint4*>(p)[lane];
+  __device__ __forceinline__ void get(Pair (&x)[4]) const {
+    x[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
+    x[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
+    x[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
+    x[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+  }
+};
+struct RawBf16 {
+  uint4 a;
+  __device__ __forceinline__ void load(const void* block, int lane) { a = load_vector(static_cast<const uint4*>(block) + lane); }
+  __device__ __forceinline__ void get(Pair (&x)[4]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      x[2 * j] = __uint_as_float(w[j] << 16);
-      x[2 * j + 1] = __uint_as_float(w[j] & 0xFFFF0000u);
-    }
-    return;
+    for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
   }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j)
-    x[j] = place<Aligned>(lane, j) < left ? __uint_as_float(static_cast<uint32_t>(p[place<Aligned>(lane, j)]) << 16) : 0.0f;
+};
+struct RawCodes {
+  uint2 a;
+  __device__ __forceinline__ void load(const void* block, int lane) { a = load_vector(static_cast<const uint2*>(block) + lane); }
+};
+__device__ __forceinline__ void store_f32(float* block, int lane, const Pair (&x)[4]) {
+  float4* p = reinterpret_cast<float4*>(block) + 2 * lane;
+  p[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+  p[1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
 }
-template <bool Aligned>
-__device__ __forceinline__ void store(uint16_t* p, int lane, int left, const uint16_t (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = x[2 * j] | static_cast<uint32_t>(x[2 * j + 1]) << 16;
-    reinterpret_cast<uint4*>(p)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j)
-    if (place<Aligned>(lane, j) < left) p[place<Aligned>(lane, j)] = x[j];
-}
-template <bool Aligned>
-__device__ __forceinline__ void load(const uint8_t* p, int lane, int left, uint32_t (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    const uint2 a = reinterpret_cast<const uint2*>(p)[lane];
-#pragma unroll
-    for (int j = 0; j < kOptLane; ++j) x[j] = ((j < 4 ? a.x : a.y) >> (8 * (j & 3))) & 0xFFu;
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j) x[j] = place<Aligned>(lane, j) < left ? p[place<Aligned>(lane, j)] : 0u;
-}
-template <bool Aligned>
-__device__ __forceinline__ void store(uint8_t* p, int lane, int left, const uint32_t (&x)[kOptLane]) {
-  if (Aligned && left >= (lane + 1) * kOptLane) {
-    reinterpret_cast<uint2*>(p)[lane] = make_uint2(x[0] | x[1] << 8 | x[2] << 16 | x[3] << 24, x[4] | x[5] << 8 | x[6] << 16 | x[7] << 24);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < kOptLane; ++j)
-    if (place<Aligned>(lane, j) < left) p[place<Aligned>(lane, j)] = static_cast<uint8_t>(x[j]);
+__device__ __forceinline__ void store_bf16(uint16_t* block, int lane, const uint32_t (&w)[4]) {
+  reinterpret_cast<uint4*>(block)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The random bits of a lane's elements: for the moments, and for a bf16 weight.
-template <bool Aligned>
-__device__ __forceinline__ void random_bits(RandomKey key, uint64_t first, int lane, uint32_t (&moments)[kOptLane],
-                                            uint32_t (&weights)[kOptLane]) {
+// Four codes of a block of exponent e < 255 as values: two at a time as bf16
+// patterns (a code's three fraction bits fit), zero codes without the base.
+template <bool Signed>
+__device__ __forceinline__ void decode4(uint32_t w, uint32_t e, Pair& x, Pair& y) {
+  const uint32_t base = static_cast<uint32_t>(code_base(e, Signed ? kSpanM : kSpanV)) << 4;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint32_t two = __byte_perm(w, 0, k ? 0x4342 : 0x4140);
+    const uint32_t c = Signed ? two & 0x007F007Fu : two;
+    uint32_t h = c * 16 + __vminu2(c, 0x00010001u) * base;
+    if (Signed) h += (two & 0x00800080u) * 256;
+    (k ? y : x) = make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u));
+  }
+}
+
+// Codes of four values of a block of exponent e, r: what rounding adds to each
+// below bit 20.  The rounded patterns' high halves, two at a time, less the
+// base.  Unsigned: code 1 at least, so zeros are left to the caller.
+template <bool Signed>
+__device__ __forceinline__ uint32_t encode4(Pair x, Pair y, const uint32_t (&r)[4], uint32_t e) {
+  const uint32_t base = static_cast<uint32_t>(code_base(e, Signed ? kSpanM : kSpanV)) * 0x00010001u;
+  const uint32_t s0 = __float_as_uint(x.x) + r[0], s1 = __float_as_uint(x.y) + r[1];
+  const uint32_t s2 = __float_as_uint(y.x) + r[2], s3 = __float_as_uint(y.y) + r[3];
+  const uint32_t h0 = __byte_perm(s0, s1, 0x7632), h1 = __byte_perm(s2, s3, 0x7632);
+  const uint32_t least = Signed ? base : base + 0x00010001u;
+  const uint32_t c0 = __vmaxu2((h0 >> 4) & 0x07FF07FFu, least) - base, c1 = __vmaxu2((h1 >> 4) & 0x07FF07FFu, least) - base;
+  const uint32_t c = __byte_perm(c0, c1, 0x6420);
+  if (!Signed) return c;
+  return c | (__byte_perm(h0, h1, 0x7531) & (c + 0x7F7F7F7Fu) & 0x80808080u);
+}
+
+// Largest bit pattern of |x| over the warp; a NaN's is above all others.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+__device__ __forceinline__ uint32_t warp_max(uint32_t x) { return __reduce_max_sync(0xFFFFFFFFu, x); }
+__device__ __forceinline__ uint32_t block_top(const Pair (&x)[4]) {
+  const float a = max3(x[0].x, x[0].y, x[1].x), b = max3(x[1].y, x[2].x, x[2].y);
+  return warp_max(__float_as_uint(max3(max3(a, b, x[3].x), x[3].y, 0.0f)));
+}
+
+// A lane's random bits of a whole block: u of each pair of elements.
+__device__ __forceinline__ void random_pairs(RandomKey key, uint64_t first, int lane, uint32_t (&u)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) u[j] = random_pair(key, (first >> 1) + lane * 4 + j);
+}
+
+// Codes a whole block's moments and stores them; u: the lane's random_pairs.
+template <bool Signed, bool Random>
+__device__ __forceinline__ void store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes, uint8_t* exponent, int lane) {
+  const uint32_t e = block_exponent(block_top(x), Signed ? kSpanM : kSpanV);
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint32_t r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (Random) {
+        const uint32_t q = random_moments(u[2 * k + j / 2], j & 1);
+        r[j] = (Signed ? q & 0xFFFFu : q >> 16) << 4;
+      } else {
+        const Pair y = x[2 * k + j / 2];
+        r[j] = round_nearest(__float_as_uint(j & 1 ? y.y : y.x));
+      }
+    }
+    w[k] = encode4<Signed>(x[2 * k], x[2 * k + 1], r, e);
+  }
+  if (!Signed) {  // second moments that are zero: whole rows, or none
+    const float least = fminf(fminf(fminf(x[0].x, x[0].y), fminf(x[1].x, x[1].y)), fminf(fminf(x[2].x, x[2].y), fminf(x[3].x, x[3].y)));
+    if (least == 0.0f)
+#pragma unroll
+      for (int j = 0; j < kOptLane; ++j)
+        if ((j & 1 ? x[j / 2].y : x[j / 2].x) == 0.0f) w[j / 4] &= ~(0xFFu << 8 * (j & 3));
+  }
+  if (e == 255) w[0] = w[1] = 0;
+  reinterpret_cast<uint2*>(codes)[lane] = make_uint2(w[0], w[1]);
+  if (lane == 0) *exponent = static_cast<uint8_t>(e);
+}
+
+// ---- element by element
+
+template <class T>
+__device__ __forceinline__ float to_float(T x) {
+  if constexpr (sizeof(T) == 2)
+    return __uint_as_float(static_cast<uint32_t>(x) << 16);
+  else
+    return x;
+}
+template <class T>
+__device__ __forceinline__ void load_any(const void* block, int lane, int left, float (&x)[kOptLane]) {
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j) x[j] = j * 32 + lane < left ? to_float(static_cast<const T*>(block)[j * 32 + lane]) : 0.0f;
+}
+template <class T>
+__device__ __forceinline__ void store_any(T* block, int lane, int left, const T (&x)[kOptLane]) {
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j)
+    if (j * 32 + lane < left) block[j * 32 + lane] = x[j];
+}
+template <bool Signed>
+__device__ __forceinline__ void load_codes_any(const uint8_t* block, uint32_t e, int lane, int left, float (&x)[kOptLane]) {
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j) {
-    const uint64_t i = first + place<Aligned>(lane, j);
-    const int odd = static_cast<int>(i & 1);
-    const uint32_t u = random_pair(key, i >> 1), w = random_weights(u);
-    moments[j] = random_moments(u, odd);
-    weights[j] = odd ? w & 0xFFFFu : w >> 16;
+    const uint32_t c = j * 32 + lane < left ? block[j * 32 + lane] : 0u;
+    x[j] = Signed ? decode_m(c, e) : decode_v(c, e);
+    if (j * 32 + lane >= left) x[j] = 0.0f;
   }
 }
-
-__device__ __forceinline__ uint32_t warp_max(uint32_t x) { return __reduce_max_sync(0xFFFFFFFFu, x); }
-
-// Codes a block's moments and stores them; rnd: the lane's random bits, shifted so that the low half counts.
-template <bool Aligned, bool Signed>
-__device__ __forceinline__ void store_moments(const float (&x)[kOptLane], const uint32_t (&rnd)[kOptLane], bool random,
-                                              uint8_t* codes, uint8_t* exponent, int lane, int left) {
-  uint32_t top = 0;
+// random: the tensor's key counts
+template <bool Signed>
+__device__ __forceinline__ void store_codes_any(const float (&x)[kOptLane], bool random, RandomKey key, uint64_t first, uint8_t* codes,
+                                                uint8_t* exponent, int lane, int left) {
+  uint32_t top = 0, c[kOptLane];
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
   const uint32_t e = block_exponent(warp_max(top), Signed ? kSpanM : kSpanV);
-  uint32_t c[kOptLane];
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j) {
-    const uint32_t r = random ? (rnd[j] & 0xFFFFu) << 4 : round_nearest(__float_as_uint(x[j]));
+    const uint64_t i = first + j * 32 + lane;
+    uint32_t r = round_nearest(__float_as_uint(x[j]));
+    if (random) {
+      const uint32_t q = random_moments(random_pair(key, i >> 1), static_cast<int>(i & 1));
+      r = (Signed ? q & 0xFFFFu : q >> 16) << 4;
+    }
     c[j] = Signed ? encode_m(x[j], r, e) : encode_v(x[j], r, e);
   }
-  store<Aligned>(codes, lane, left, c);
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j)
+    if (j * 32 + lane < left) codes[j * 32 + lane] = static_cast<uint8_t>(c[j]);
   if (lane == 0) *exponent = static_cast<uint8_t>(e);
 }
 

@@ -2,23 +2,27 @@
 // the factor that clips them, in one launch.
 //
 // A lane squares the eight elements that it has of each block into two fp32
-// sums, which a float pair takes up error-free every kClipSeg blocks: 64
-// squares are added in fp32 at a time, at most.  A segment whose fp32 sum is
+// sums, which a float pair takes up error-free after the warp's blocks of a
+// unit: at most 64 squares are added in fp32 at a time.  A sum that is
 // not finite (a NaN or Inf, or an overflow) or so small that squares may have
 // lost bits to underflow is added again by the lanes concerned, element by
 // element in fp64, the non-finite ones counted and left out.  Warps, then CTAs,
 // then the partial sums of all CTAs are added in fp64 in a fixed order; the CTA
 // that is last to finish adds those.
+//
+// Which lane has which element does not depend on the address (the order of the
+// sums must not): off the 16-byte boundary a lane loads the granules around its
+// elements and shifts them out.
 #include <cmath>
 
 #include "kernels.h"
-#include "optim.h"
+#include "optim_block.cuh"
 
 namespace frk {
 
 namespace {
 
-constexpr uint32_t kClipSeg = 16;
+static_assert(kClipUnit / kOptWarps * kOptLane / 2 <= 64, "squares in one fp32 sum");
 
 template <bool Bf16>
 __device__ __forceinline__ float element(const void* p, uint64_t i) {
@@ -26,66 +30,106 @@ __device__ __forceinline__ float element(const void* p, uint64_t i) {
 }
 
 struct LaneSums {
-  float hi = 0.0f, lo = 0.0f;  // of segments added in fp32
-  double exact = 0.0;          // of segments added in fp64
+  float hi = 0.0f, lo = 0.0f;  // of sums in fp32
+  double exact = 0.0;          // of sums in fp64
   uint32_t nonfinite = 0;
 };
 
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  float2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;"
-      : "=l"(reinterpret_cast<uint64_t&>(r))
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
-  return r;
+// Granules of 16 bytes around a lane's eight elements.
+template <bool Bf16, bool Shifted>
+struct Granules {
+  static constexpr int kWords = Bf16 ? 4 : 8, kLoaded = kWords / 4 + Shifted;
+  uint4 g[kLoaded];
+  // at: address of the first element, floored to a granule's
+  __device__ __forceinline__ void load(uint64_t at) {
+#pragma unroll
+    for (int k = 0; k < kLoaded; ++k) g[k] = load_vector(reinterpret_cast<const uint4*>(at) + k);
+  }
+  // shift: bytes from there to the first element
+  __device__ __forceinline__ void words(uint32_t shift, uint32_t (&w)[kWords]) const {
+    uint32_t a[4 * kLoaded];
+#pragma unroll
+    for (int k = 0; k < kLoaded; ++k) a[4 * k] = g[k].x, a[4 * k + 1] = g[k].y, a[4 * k + 2] = g[k].z, a[4 * k + 3] = g[k].w;
+    if constexpr (Shifted) {
+      // by 8 bytes, then 4, then 2
+#pragma unroll
+      for (int i = 0; i < kWords + 2; ++i) a[i] = shift & 8 ? a[i + 2 < 4 * kLoaded ? i + 2 : i] : a[i];
+#pragma unroll
+      for (int i = 0; i < kWords + 1; ++i) a[i] = shift & 4 ? a[i + 1] : a[i];
+      if (Bf16)
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) a[i] = shift & 2 ? __funnelshift_r(a[i], a[i + 1], 16) : a[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) w[i] = a[i];
+  }
+};
+
+template <bool Bf16>
+__device__ __forceinline__ void add_words(const uint32_t (&w)[Bf16 ? 4 : 8], Pair& sum, uint32_t& any) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    Pair x;
+    if (Bf16) {
+      x = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+      any |= w[j];
+    } else {
+      x = make_float2(__uint_as_float(w[Bf16 ? 0 : 2 * j]), __uint_as_float(w[Bf16 ? 0 : 2 * j + 1]));
+      any |= w[Bf16 ? 0 : 2 * j] | w[Bf16 ? 0 : 2 * j + 1];
+    }
+    sum = fma2(x, x, sum);
+  }
 }
 
-// Blocks [first, first + count) of one tensor, count <= kClipSeg.
-template <bool Bf16>
-__device__ __forceinline__ void add_segment(const OptDesc& d, uint32_t first, uint32_t count, int lane, LaneSums& s) {
-  float2 sum = make_float2(0.0f, 0.0f);
+// The warp's blocks [block, stop) of one tensor, every kOptWarps-th.
+template <bool Bf16, bool Shifted>
+__device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_t block, uint32_t stop, int lane, LaneSums& s) {
+  constexpr int kAhead = Bf16 ? 8 : 4;  // blocks loaded at a time
+  constexpr int kBytes = Bf16 ? 2 : 4;
+  Pair sum = pair(0.0f);
   uint32_t any = 0;  // a bit set: some element is not +0
-  for (uint32_t k = 0; k < count; ++k) {
-    const uint64_t at = static_cast<uint64_t>(first + k) * kOptBlock + lane * kOptLane;
-    if (d.aligned && at + kOptLane <= d.n) {
-      if (Bf16) {
-        const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(d.grad) + at);
-        const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  const uint32_t shift = Shifted ? static_cast<uint32_t>(reinterpret_cast<uint64_t>(grad)) % 16 : 0;
+  const uint64_t base = reinterpret_cast<uint64_t>(grad) - shift + lane * kOptLane * kBytes;
+  const uint32_t whole = static_cast<uint32_t>(min(n / kOptBlock, static_cast<uint64_t>(stop)));
+  uint32_t b = block;
+  for (; b + (kAhead - 1) * kOptWarps < whole; b += kAhead * kOptWarps) {
+    Granules<Bf16, Shifted> r[kAhead];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float2 x = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
-          sum = fma2(x, x, sum);
-          any |= w[j];
-        }
-      } else {
-        const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(d.grad) + at);
+    for (int k = 0; k < kAhead; ++k) r[k].load(base + static_cast<uint64_t>(b + k * kOptWarps) * kOptBlock * kBytes);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const float4 a = q[j];
-          const float2 x = make_float2(a.x, a.y), y = make_float2(a.z, a.w);
-          sum = fma2(x, x, sum);
-          sum = fma2(y, y, sum);
-          any |= __float_as_uint(a.x) | __float_as_uint(a.y) | __float_as_uint(a.z) | __float_as_uint(a.w);
-        }
-      }
+    for (int k = 0; k < kAhead; ++k) {
+      uint32_t w[Bf16 ? 4 : 8];
+      r[k].words(shift, w);
+      add_words<Bf16>(w, sum, any);
+    }
+  }
+  for (; b < stop; b += kOptWarps) {
+    const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
+    if (b < whole) {
+      Granules<Bf16, Shifted> r;
+      uint32_t w[Bf16 ? 4 : 8];
+      r.load(base + static_cast<uint64_t>(b) * kOptBlock * kBytes);
+      r.words(shift, w);
+      add_words<Bf16>(w, sum, any);
     } else {
 #pragma unroll
       for (int j = 0; j < kOptLane; j += 2) {
-        float2 x;
-        x.x = at + j < d.n ? element<Bf16>(d.grad, at + j) : 0.0f;
-        x.y = at + j + 1 < d.n ? element<Bf16>(d.grad, at + j + 1) : 0.0f;
+        Pair x;
+        x.x = at + j < n ? element<Bf16>(grad, at + j) : 0.0f;
+        x.y = at + j + 1 < n ? element<Bf16>(grad, at + j + 1) : 0.0f;
         sum = fma2(x, x, sum);
         any |= __float_as_uint(x.x) | __float_as_uint(x.y);
       }
     }
   }
   const float t = __fadd_rn(sum.x, sum.y);
-  // A square below 2^-126 is off by 2^-150 at most: nothing beside 2^-90.  (At
-  // 2^96 a segment the pair does not overflow: a lane has fewer than 2^31.)
+  // A square below 2^-126 is off by 2^-150 at most: nothing beside 2^-90.  (Of
+  // sums below 2^96 the pair does not overflow: a lane has fewer than 2^31.)
   if (!(t < 0x1p96f) || (t < 0x1p-90f && any != 0)) {
-    for (uint32_t k = 0; k < count; ++k) {
-      const uint64_t at = static_cast<uint64_t>(first + k) * kOptBlock + lane * kOptLane;
-      for (int j = 0; j < kOptLane && at + j < d.n; ++j) {
-        const float x = element<Bf16>(d.grad, at + j);
+    for (b = block; b < stop; b += kOptWarps) {
+      const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
+      for (int j = 0; j < kOptLane && at + j < n; ++j) {
+        const float x = element<Bf16>(grad, at + j);
         if ((__float_as_uint(x) & 0x7F800000u) == 0x7F800000u)
           ++s.nonfinite;
         else
@@ -122,26 +166,27 @@ __device__ __forceinline__ ClipPartial cta_sum(double sum, uint64_t count, ClipP
   return all;
 }
 
-__global__ void __launch_bounds__(32 * kOptWarps) clip_kernel(const ClipParams p) {
+__global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kOptWarps];
   __shared__ bool last;
   wait_for_kernel_before();
   const int lane = threadIdx.x % 32;
-  const uint32_t w = blockIdx.x * kOptWarps + threadIdx.x / 32;
-  uint32_t b = opt_range(p.work.n_blocks, p.work.n_warps, w);
-  const uint32_t end = opt_range(p.work.n_blocks, p.work.n_warps, w + 1);
   LaneSums s;
-  if (b < end) {
-    for (uint32_t t = p.work.start[w]; b < end; ++t) {
-      const OptDesc d = p.work.tensors[t];
+  const uint32_t warp = threadIdx.x / 32;
+  for (uint32_t u = blockIdx.x; u < p.work.n_units; u += gridDim.x) {
+    const uint32_t end = min((u + 1) * p.work.unit_blocks, p.work.n_blocks);
+    uint32_t b = u * p.work.unit_blocks + warp;
+    for (uint32_t t = p.work.start[u]; b < end; ++t) {
+      const OptDesc& d = p.work.tensors[t];
       const uint32_t stop = min(end, d.first + d.n_blocks);
-      for (; b < stop; b += min(kClipSeg, stop - b)) {
-        const uint32_t count = min(kClipSeg, stop - b);
-        if (d.bf16_grad)
-          add_segment<true>(d, b - d.first, count, lane, s);
-        else
-          add_segment<false>(d, b - d.first, count, lane, s);
-      }
+      if (b >= stop) continue;
+      const uint32_t from = b - d.first, to = stop - d.first;
+      const bool shifted = reinterpret_cast<uint64_t>(d.grad) % 16 != 0;
+      if (d.bf16_grad)
+        shifted ? add_blocks<true, true>(d.grad, d.n, from, to, lane, s) : add_blocks<true, false>(d.grad, d.n, from, to, lane, s);
+      else
+        shifted ? add_blocks<false, true>(d.grad, d.n, from, to, lane, s) : add_blocks<false, false>(d.grad, d.n, from, to, lane, s);
+      b += (to - from + kOptWarps - 1) / kOptWarps * kOptWarps;
     }
   }
   const ClipPartial mine = cta_sum(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact, s.nonfinite, warps);
@@ -172,8 +217,9 @@ __global__ void __launch_bounds__(32 * kOptWarps) clip_kernel(const ClipParams p
 
 }  // namespace
 
-cudaError_t launch_clip(const ClipParams& p, int n_ctas, cudaStream_t s) {
-  return launch_chained(clip_kernel, n_ctas, 32 * kOptWarps, 0, s, p);
+cudaError_t launch_clip(const ClipParams& p, cudaStream_t s) {
+  const uint32_t n_ctas = p.work.n_units < 1 ? 1 : p.work.n_units < kClipCtas ? p.work.n_units : kClipCtas;
+  return launch_chained(clip_kernel, static_cast<int>(n_ctas), 32 * kOptWarps, 0, s, p);
 }
 
 }  // namespace frk

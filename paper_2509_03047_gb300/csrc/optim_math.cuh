@@ -76,25 +76,67 @@ __device__ __forceinline__ uint32_t random_moments(uint32_t u, int odd) { return
 // The pair's weights: 16 bits each, the high half for the first.
 __device__ __forceinline__ uint32_t random_weights(uint32_t u) { return u * 747796405u; }
 
+// ---- pairs: two fp32 products per instruction, each rounded as a single one
+
+using Pair = float2;
+__device__ __forceinline__ Pair pair(float x) { return make_float2(x, x); }
+#define FR_PAIR(x) reinterpret_cast<const uint64_t&>(x)
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(FR_PAIR(a)), "l"(FR_PAIR(b)));
+  return r;
+}
+// (add.rn.f32x2 of a product is contracted to a fused multiply-add by CUDA 13.0's
+// assembler, with and without -fmad=false; two single additions are not.)
+__device__ __forceinline__ Pair add2(Pair a, Pair b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(FR_PAIR(a)), "l"(FR_PAIR(b)), "l"(FR_PAIR(c)));
+  return r;
+}
+#undef FR_PAIR
+
 // ---- the update
 
 struct Hyper {
   float b1, c1, b2, c2, scale;  // scale: of the gradient
   float lr, decay, eps, m_fix, v_fix;
+  bool exact;
 };
 
 // New moments, each product and sum rounded by itself.
-__device__ __forceinline__ void update_moments(const Hyper& h, float grad, float& m, float& v) {
-  const float g = __fmul_rn(grad, h.scale);
-  m = __fadd_rn(__fmul_rn(m, h.b1), __fmul_rn(g, h.c1));
-  v = __fadd_rn(__fmul_rn(v, h.b2), __fmul_rn(__fmul_rn(g, g), h.c2));
+__device__ __forceinline__ void update_moments(const Hyper& h, Pair grad, Pair& m, Pair& v) {
+  const Pair g = mul2(grad, pair(h.scale));
+  m = add2(mul2(m, pair(h.b1)), mul2(g, pair(h.c1)));
+  v = add2(mul2(v, pair(h.b2)), mul2(mul2(g, g), pair(h.c2)));
 }
 
-// The parameter from the new moments.
-__device__ __forceinline__ float update_param(const Hyper& h, float p, float m, float v) {
-  const float below = __fmaf_rn(__fsqrt_rn(v), h.v_fix, h.eps);
-  const float u = __fmaf_rn(__fdiv_rn(m, below), h.m_fix, __fmul_rn(p, h.decay));
-  return __fmaf_rn(-h.lr, u, p);
+// The parameter from the new moments.  The square root and the reciprocal are
+// the hardware's approximations, 2^-23 off at most: under lr they are nothing
+// beside the parameter's own rounding, and the correctly rounded ones take 20
+// more instructions per element.  Subnormal second moments count as zero there,
+// which is under 2^-63 v_fix of a denominator of at least eps; an eps too small for that
+// (below 2^-39 v_fix) takes the correctly rounded ones.
+__device__ __forceinline__ float approx_sqrt(float x) {
+  float r;
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float approx_reciprocal(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ Pair update_param(const Hyper& h, Pair p, Pair m, Pair v) {
+  Pair u;
+  if (h.exact) {
+    const Pair below = fma2(make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y)), pair(h.v_fix), pair(h.eps));
+    u = make_float2(__fdiv_rn(m.x, below.x), __fdiv_rn(m.y, below.y));
+  } else {
+    const Pair below = fma2(make_float2(approx_sqrt(v.x), approx_sqrt(v.y)), pair(h.v_fix), pair(h.eps));
+    u = mul2(m, make_float2(approx_reciprocal(below.x), approx_reciprocal(below.y)));
+  }
+  return fma2(fma2(u, pair(h.m_fix), mul2(p, pair(h.decay))), pair(-h.lr), p);
 }
 
 }  // namespace frk
