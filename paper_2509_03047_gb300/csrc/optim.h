@@ -18,7 +18,7 @@ constexpr int kOptBlock = FR_OPT_BLOCK;
 constexpr int kOptLane = kOptBlock / 32;  // elements of a block per lane
 static_assert(kOptBlock == 256, "eight elements per lane");
 
-struct OptDesc {        // 96 bytes: one tensor that has elements
+struct OptDesc {        // 96 bytes: one tensor that has elements, or a part of it
   void* weight;
   const void* grad;
   float* master;
@@ -34,7 +34,7 @@ struct OptDesc {        // 96 bytes: one tensor that has elements
   float lr_scale;
   float decay_scale;
   uint32_t aligned;     // every buffer that it has starts at a vector's boundary
-  uint32_t unused;
+  uint32_t skipped;     // elements of the plan's tensor before this one's first
 };
 static_assert(sizeof(OptDesc) == 96, "OptDesc layout");
 
@@ -46,14 +46,15 @@ struct OptWork {
 };
 
 constexpr int kOptWarps = 8;  // per CTA, in every kernel here
+constexpr uint32_t kSms = 152;  // of a GB300
 
 // ---- the norm
 
 // A launch's sums are added in an order that units and CTAs decide, so both
-// follow from the sizes alone, not from the GPU: at most 4 CTAs for each of a
-// GB300's 152 SMs, about four units for each, of 2 to 16 blocks per warp.
+// follow from the sizes alone, not from the GPU: at most 4 CTAs per SM, about
+// four units for each, of 2 to 16 blocks per warp.
 constexpr uint32_t kClipUnit = 16 * kOptWarps;
-constexpr uint32_t kClipCtas = 4 * 152;
+constexpr uint32_t kClipCtas = 4 * kSms;
 inline uint32_t clip_unit(uint64_t n_blocks) {
   const uint64_t per_warp = n_blocks / (4 * kClipCtas * kOptWarps);
   return static_cast<uint32_t>(per_warp < 2 ? 2 : per_warp < 16 ? per_warp : 16) * kOptWarps;
@@ -82,16 +83,30 @@ struct StepClass {
 };
 constexpr int kStepClasses = 3 * 2 * 2;
 
+using Pair = float2;
+
+struct StepNumbers {
+  Pair b1, c1, b2, c2;  // beta1, 1 - beta1, beta2, 1 - beta2
+  Pair m_fix, v_fix;    // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  Pair eps;
+};
 struct StepParams {
   OptWork work;
   const fr_clip* clip;         // may be null
-  float b1, c1, b2, c2;        // beta1, 1 - beta1, beta2, 1 - beta2
-  float lr, decay, eps;
-  float m_fix, v_fix;          // 1 / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+  StepNumbers numbers;
+  float lr, decay;
   uint32_t exact;              // 1: eps is too small for the approximations of update_param (optim_math.cuh)
   uint32_t random;             // 1: FR_ROUND_RANDOM
   uint64_t key;                // of the random bits: mix64(mix64(seed) + step)
 };
+// CTAs of eight warps per SM, what the registers of a lane's elements allow.
+constexpr int step_ctas(bool eight) { return eight ? 3 : 4; }
+// Consecutive blocks per warp.
+inline uint32_t step_blocks(bool eight, uint64_t n_blocks) {
+  if (!eight) return 1;
+  const uint64_t warps = kSms * step_ctas(true) * kOptWarps, b = n_blocks / (2 * warps);
+  return static_cast<uint32_t>(b < 1 ? 1 : b < 8 ? b : 8);
+}
 cudaError_t launch_step(const StepClass& c, const StepParams& p, cudaStream_t s);
 
 // ---- conversion
@@ -102,6 +117,13 @@ struct ConvertParams {
   uint32_t random;
   uint64_t key;
 };
+#ifndef FR_TO8
+#define FR_TO8 2
+#endif
+#ifndef FR_TO32
+#define FR_TO32 4
+#endif
+constexpr int convert_blocks(bool to_eight) { return to_eight ? FR_TO8 : FR_TO32; }
 cudaError_t launch_convert(const ConvertParams& p, cudaStream_t s);
 
 // splitmix64's output function (Steele, Lea, Flood, "Fast splittable

@@ -70,10 +70,11 @@ struct fr_opt_s {
 
 namespace {
 
+Pair twice(double x) { return make_float2(static_cast<float>(x), static_cast<float>(x)); }
 bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 uint64_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : dtype == FR_DT_BF16 ? 2 : 1; }
-// The boundary on which a lane's eight elements can move as vectors of 16 bytes (codes: 8).
-uint64_t vector_bytes(uint32_t dtype) { return dtype == FR_DT_BYTES ? 8 : 16; }
+// The boundary on which a lane's eight elements move as one vector.
+uint64_t vector_bytes(uint32_t dtype) { return kOptLane * type_bytes(dtype); }
 
 // A tensor's descriptor, or why it has none.
 const char* check(const fr_opt_tensor& x, bool& misaligned) {
@@ -110,8 +111,41 @@ OptDesc describe(const fr_opt_tensor& x, uint64_t index) {
   d.lr_scale = x.lr_scale;
   d.decay_scale = x.decay_scale;
   d.aligned = (!x.weight || on(x.weight, vector_bytes(x.weight_dtype))) && (!x.grad || on(x.grad, vector_bytes(x.grad_dtype))) &&
-              on(x.master, 16) && on(x.m, x.m ? vector_bytes(x.state_dtype) : 1) && on(x.v, x.v ? vector_bytes(x.state_dtype) : 1);
+              on(x.master, vector_bytes(FR_DT_F32)) && on(x.m, x.m ? vector_bytes(x.state_dtype) : 1) && on(x.v, x.v ? vector_bytes(x.state_dtype) : 1);
   return d;
+}
+
+// The elements of a tensor of the step before the first at which every buffer is
+// on a vector's boundary, so that the rest of it moves as vectors: the views of
+// flat groups start at any element, but at the same one in each.  0: none, or
+// all are already, or the rest would not do: blocks of 8-bit moments start with
+// the tensor, random bits of bf16 weights belong to pairs.
+uint64_t head_elems(const fr_opt_tensor& x, const StepClass& c) {
+  if (c.eight) return 0;
+  auto to_boundary = [](const void* p, uint32_t dtype) {
+    const uint64_t v = vector_bytes(dtype);
+    return (v - reinterpret_cast<uintptr_t>(p) % v) % v / type_bytes(dtype);
+  };
+  const uint64_t head = to_boundary(x.weight, x.weight_dtype);
+  if (to_boundary(x.grad, x.grad_dtype) != head || to_boundary(x.m, FR_DT_F32) != head || to_boundary(x.v, FR_DT_F32) != head) return 0;
+  if (x.master && to_boundary(x.master, FR_DT_F32) != head) return 0;
+  return c.weight == kWeightBf16 && head % 2 ? 0 : head;
+}
+
+OptDesc part(const OptDesc& d, const fr_opt_tensor& x, uint64_t first, uint64_t n) {
+  fr_opt_tensor y = x;
+  auto advance = [&](const void* p, uint32_t dtype) {
+    return const_cast<uint8_t*>(static_cast<const uint8_t*>(p)) + first * type_bytes(dtype);
+  };
+  y.weight = advance(x.weight, x.weight_dtype);
+  y.grad = advance(x.grad, x.grad_dtype);
+  if (x.master) y.master = reinterpret_cast<float*>(advance(x.master, FR_DT_F32));
+  y.m = advance(x.m, FR_DT_F32);
+  y.v = advance(x.v, FR_DT_F32);
+  y.n = n;
+  OptDesc r = describe(y, d.tensor);
+  r.skipped = static_cast<uint32_t>(first);
+  return r;
 }
 
 fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
@@ -130,7 +164,13 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
       c.bf16_grad = x.grad_dtype == FR_DT_BF16;
       c.eight = x.state_dtype == FR_DT_BYTES;
       p->classes[c.index()] = c;
-      p->step[c.index()].add(d);
+      const uint64_t head = head_elems(x, c);
+      if (head > 0 && head < x.n) {
+        p->step[c.index()].add(part(d, x, 0, head));
+        p->step[c.index()].add(part(d, x, head, x.n - head));
+      } else {
+        p->step[c.index()].add(d);
+      }
     } else {
       p->params = false;
     }
@@ -142,13 +182,13 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
   p->clip.cut(clip_unit(p->clip.n_blocks));
   p->clip.place(mem);
   if (p->moments) {
-    p->convert.cut(kOptWarps);
+    p->convert.cut(convert_blocks(!p->eight) * kOptWarps);
     p->convert.place(mem);
   }
   if (p->params)
     for (int c = 0; c < kStepClasses; ++c) {
       if (p->step[c].n_blocks == 0) continue;
-      p->step[c].cut(kOptWarps);
+      p->step[c].cut(step_blocks(p->classes[c].eight, p->step[c].n_blocks) * kOptWarps);
       p->step[c].place(mem);
     }
   mem.table(&p->d_done, std::vector<uint32_t>(1, 0));
@@ -186,7 +226,7 @@ fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt
     }
     blocks += (tensors[t].n + kOptBlock - 1) / kOptBlock;
   }
-  if (blocks >= (1ull << 32) - 1) return report_invalid(me, "too many elements");
+  if (blocks + n_tensors >= (1ull << 32) - 1) return report_invalid(me, "too many elements");  // (a head may be a block of its own)
 
   int dev = 0;
   const cudaError_t e = cudaGetDevice(&dev);
@@ -267,16 +307,16 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
   StepParams sp;
   sp.clip = clip_dev;
-  sp.b1 = static_cast<float>(h->beta1);
-  sp.c1 = static_cast<float>(1.0 - h->beta1);
-  sp.b2 = static_cast<float>(h->beta2);
-  sp.c2 = static_cast<float>(1.0 - h->beta2);
+  sp.numbers.b1 = twice(h->beta1);
+  sp.numbers.c1 = twice(1.0 - h->beta1);
+  sp.numbers.b2 = twice(h->beta2);
+  sp.numbers.c2 = twice(1.0 - h->beta2);
   sp.lr = static_cast<float>(h->lr);
   sp.decay = static_cast<float>(h->weight_decay);
-  sp.eps = static_cast<float>(h->eps);
-  sp.m_fix = static_cast<float>(1.0 / (1.0 - std::pow(h->beta1, static_cast<double>(h->step))));
-  sp.v_fix = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(h->beta2, static_cast<double>(h->step))));
-  sp.exact = sp.eps < 0x1p-39f * sp.v_fix;
+  sp.numbers.eps = twice(h->eps);
+  sp.numbers.m_fix = twice(1.0 / (1.0 - std::pow(h->beta1, static_cast<double>(h->step))));
+  sp.numbers.v_fix = twice(1.0 / std::sqrt(1.0 - std::pow(h->beta2, static_cast<double>(h->step))));
+  sp.exact = sp.numbers.eps.x < 0x1p-39f * sp.numbers.v_fix.x;
   sp.random = h->rounding == FR_ROUND_RANDOM;
   sp.key = mix64(mix64(h->seed) + h->step);
   for (int c = 0; c < kStepClasses; ++c) {

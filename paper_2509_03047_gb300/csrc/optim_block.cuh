@@ -20,38 +20,32 @@ __device__ __forceinline__ uint32_t tensor_of(const OptWork& w, uint32_t t, uint
 
 // ---- vectors
 
-template <class T>
-__device__ __forceinline__ T load_vector(const T* p) {
-  T r;
-  if constexpr (sizeof(T) == 16)
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                 : "=r"(reinterpret_cast<uint32_t*>(&r)[0]), "=r"(reinterpret_cast<uint32_t*>(&r)[1]),
-                   "=r"(reinterpret_cast<uint32_t*>(&r)[2]), "=r"(reinterpret_cast<uint32_t*>(&r)[3])
-                 : "l"(p));
-  else
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];"
-                 : "=r"(reinterpret_cast<uint32_t*>(&r)[0]), "=r"(reinterpret_cast<uint32_t*>(&r)[1])
-                 : "l"(p));
+__device__ __forceinline__ uint4 load_16(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
   return r;
 }
 
-// A lane's eight elements as they lie in memory.
+// A lane's eight elements as they lie in memory.  (32 bytes go by one
+// instruction: two of 16 bytes, each lane's beside one another, write at 4.7
+// TB/s where this does at 7.0.)
 struct RawF32 {
-  uint4 a, b;
-  __device__ __forceinline__ void load(const void* block, int lane) {
-    a = load_vector(static_cast<const uint4*>(block) + 2 * lane);
-    b = load_vector(static_cast<const uint4*>(block) + 2 * lane + 1);
+  static constexpr int kBytes = 4;
+  uint32_t a[8];
+  __device__ __forceinline__ void load(const void* p) {
+    asm volatile("ld.global.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7])
+                 : "l"(p));
   }
   __device__ __forceinline__ void get(Pair (&x)[4]) const {
-    x[0] = make_float2(__uint_as_float(a.x), __uint_as_float(a.y));
-    x[1] = make_float2(__uint_as_float(a.z), __uint_as_float(a.w));
-    x[2] = make_float2(__uint_as_float(b.x), __uint_as_float(b.y));
-    x[3] = make_float2(__uint_as_float(b.z), __uint_as_float(b.w));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(a[2 * j]), __uint_as_float(a[2 * j + 1]));
   }
 };
 struct RawBf16 {
+  static constexpr int kBytes = 2;
   uint4 a;
-  __device__ __forceinline__ void load(const void* block, int lane) { a = load_vector(static_cast<const uint4*>(block) + lane); }
+  __device__ __forceinline__ void load(const void* p) { a = load_16(p); }
   __device__ __forceinline__ void get(Pair (&x)[4]) const {
     const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
@@ -59,16 +53,23 @@ struct RawBf16 {
   }
 };
 struct RawCodes {
+  static constexpr int kBytes = 1;
   uint2 a;
-  __device__ __forceinline__ void load(const void* block, int lane) { a = load_vector(static_cast<const uint2*>(block) + lane); }
+  __device__ __forceinline__ void load(const void* p) {
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "l"(p));
+  }
 };
-__device__ __forceinline__ void store_f32(float* block, int lane, const Pair (&x)[4]) {
-  float4* p = reinterpret_cast<float4*>(block) + 2 * lane;
-  p[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
-  p[1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+__device__ __forceinline__ void store_f32(void* p, const Pair (&x)[4]) {
+  asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y),
+               "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y), "l"(p)
+               : "memory");
 }
-__device__ __forceinline__ void store_bf16(uint16_t* block, int lane, const uint32_t (&w)[4]) {
-  reinterpret_cast<uint4*>(block)[lane] = make_uint4(w[0], w[1], w[2], w[3]);
+__device__ __forceinline__ void store_bf16(void* p, const uint32_t (&w)[4]) { *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+
+// A lane's place in a block of a buffer.
+template <int Bytes>
+__device__ __forceinline__ uint8_t* lane_at(const void* buffer, uint32_t block, int lane) {
+  return static_cast<uint8_t*>(const_cast<void*>(buffer)) + (static_cast<uint64_t>(block) * kOptBlock + lane * kOptLane) * Bytes;
 }
 
 // Four codes of a block of exponent e < 255 as values: two at a time as bf16
@@ -120,9 +121,10 @@ __device__ __forceinline__ void random_pairs(RandomKey key, uint64_t first, int 
   for (int j = 0; j < 4; ++j) u[j] = random_pair(key, (first >> 1) + lane * 4 + j);
 }
 
-// Codes a whole block's moments and stores them; u: the lane's random_pairs.
+// Codes a whole block's moments and stores them at the lane's place; returns the
+// exponent.  u: the lane's random_pairs.
 template <bool Signed, bool Random>
-__device__ __forceinline__ void store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes, uint8_t* exponent, int lane) {
+__device__ __forceinline__ uint32_t store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes) {
   const uint32_t e = block_exponent(block_top(x), Signed ? kSpanM : kSpanV);
   uint32_t w[2];
 #pragma unroll
@@ -148,9 +150,29 @@ __device__ __forceinline__ void store_codes(const Pair (&x)[4], const uint32_t (
         if ((j & 1 ? x[j / 2].y : x[j / 2].x) == 0.0f) w[j / 4] &= ~(0xFFu << 8 * (j & 3));
   }
   if (e == 255) w[0] = w[1] = 0;
-  reinterpret_cast<uint2*>(codes)[lane] = make_uint2(w[0], w[1]);
-  if (lane == 0) *exponent = static_cast<uint8_t>(e);
+  *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
+  return e;
 }
+
+// The exponents of a warp's consecutive blocks, one per lane: read before the
+// first block's stores, written after the last's.  (A load from a sector with a
+// store under way waits for it, and 32 blocks share a sector: block by block,
+// four blocks a warp took twice the time of one.)
+struct Exponents {
+  uint32_t m, v;
+  __device__ __forceinline__ void load(const uint8_t* me, const uint8_t* ve, int count, int lane) {
+    m = v = 0;
+    if (lane < count) m = me[lane], v = ve[lane];
+  }
+  __device__ __forceinline__ void store(uint8_t* me, uint8_t* ve, int count, int lane) const {
+    if (lane < count) me[lane] = static_cast<uint8_t>(m), ve[lane] = static_cast<uint8_t>(v);
+  }
+  __device__ __forceinline__ uint32_t of_m(int k) const { return __shfl_sync(0xFFFFFFFFu, m, k); }
+  __device__ __forceinline__ uint32_t of_v(int k) const { return __shfl_sync(0xFFFFFFFFu, v, k); }
+  __device__ __forceinline__ void set(int k, int lane, uint32_t em, uint32_t ev) {
+    if (lane == k) m = em, v = ev;
+  }
+};
 
 // ---- element by element
 

@@ -43,7 +43,7 @@ struct Granules {
   // at: address of the first element, floored to a granule's
   __device__ __forceinline__ void load(uint64_t at) {
 #pragma unroll
-    for (int k = 0; k < kLoaded; ++k) g[k] = load_vector(reinterpret_cast<const uint4*>(at) + k);
+    for (int k = 0; k < kLoaded; ++k) g[k] = load_16(reinterpret_cast<const uint4*>(at) + k);
   }
   // shift: bytes from there to the first element
   __device__ __forceinline__ void words(uint32_t shift, uint32_t (&w)[kWords]) const {
@@ -169,6 +169,8 @@ __device__ __forceinline__ ClipPartial cta_sum(double sum, uint64_t count, ClipP
 __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kOptWarps];
   __shared__ bool last;
+  uint32_t t = blockIdx.x < p.work.n_units ? p.work.start[blockIdx.x] : 0;  // (the plan's tables: nothing writes them)
+  asm volatile("prefetch.global.L1 [%0];" ::"l"(p.work.tensors + t));
   wait_for_kernel_before();
   const int lane = threadIdx.x % 32;
   LaneSums s;
@@ -176,7 +178,8 @@ __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_co
   for (uint32_t u = blockIdx.x; u < p.work.n_units; u += gridDim.x) {
     const uint32_t end = min((u + 1) * p.work.unit_blocks, p.work.n_blocks);
     uint32_t b = u * p.work.unit_blocks + warp;
-    for (uint32_t t = p.work.start[u]; b < end; ++t) {
+    if (u != blockIdx.x) t = p.work.start[u];
+    for (; b < end; ++t) {
       const OptDesc& d = p.work.tensors[t];
       const uint32_t stop = min(end, d.first + d.n_blocks);
       if (b >= stop) continue;

@@ -1,4 +1,6 @@
 // optim_convert.cu -- moments from 32 bits to 8 and back.
+#include <type_traits>
+
 #include "kernels.h"
 #include "optim.h"
 #include "optim_block.cuh"
@@ -10,39 +12,45 @@ namespace {
 // A negative second moment counts as zero, a NaN stays one.
 __device__ __forceinline__ float not_negative(float x) { return x < 0.0f ? 0.0f : fabsf(x); }
 
+// A whole block's loads.
+template <bool ToEight>
+struct Raw {
+  std::conditional_t<ToEight, RawF32, RawCodes> m, v;
+  uint32_t em, ev;
+  __device__ __forceinline__ void load(const OptDesc& s, uint32_t block, int lane) {
+    m.load(lane_at<ToEight ? 4 : 1>(s.m, block, lane));
+    v.load(lane_at<ToEight ? 4 : 1>(s.v, block, lane));
+    if (!ToEight) em = s.m_exp[block], ev = s.v_exp[block];
+  }
+};
+
 template <bool ToEight, bool Random>
-__device__ __forceinline__ void convert_whole(const OptDesc& s, const OptDesc& d, uint32_t block, RandomKey key, int lane) {
+__device__ __forceinline__ void convert_whole(const Raw<ToEight>& r, const OptDesc& d, uint32_t block, RandomKey key, int lane) {
   const uint64_t first = static_cast<uint64_t>(block) * kOptBlock;
   Pair m[4], v[4];
   if constexpr (ToEight) {
-    RawF32 raw_m, raw_v;
-    raw_m.load(static_cast<const float*>(s.m) + first, lane);
-    raw_v.load(static_cast<const float*>(s.v) + first, lane);
-    raw_m.get(m);
-    raw_v.get(v);
+    r.m.get(m);
+    r.v.get(v);
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = make_float2(not_negative(v[j].x), not_negative(v[j].y));
     uint32_t u[4];
     if (Random) random_pairs(key, first, lane, u);
-    store_codes<true, Random>(m, u, static_cast<uint8_t*>(d.m) + first, d.m_exp + block, lane);
-    store_codes<false, Random>(v, u, static_cast<uint8_t*>(d.v) + first, d.v_exp + block, lane);
+    const uint32_t em = store_codes<true, Random>(m, u, lane_at<1>(d.m, block, lane));
+    const uint32_t ev = store_codes<false, Random>(v, u, lane_at<1>(d.v, block, lane));
+    if (lane == 0) d.m_exp[block] = static_cast<uint8_t>(em), d.v_exp[block] = static_cast<uint8_t>(ev);
   } else {
-    RawCodes raw_m, raw_v;
-    raw_m.load(static_cast<const uint8_t*>(s.m) + first, lane);
-    raw_v.load(static_cast<const uint8_t*>(s.v) + first, lane);
-    const uint32_t em = s.m_exp[block], ev = s.v_exp[block];
-    decode4<true>(raw_m.a.x, em, m[0], m[1]);
-    decode4<true>(raw_m.a.y, em, m[2], m[3]);
-    decode4<false>(raw_v.a.x, ev, v[0], v[1]);
-    decode4<false>(raw_v.a.y, ev, v[2], v[3]);
+    decode4<true>(r.m.a.x, r.em, m[0], m[1]);
+    decode4<true>(r.m.a.y, r.em, m[2], m[3]);
+    decode4<false>(r.v.a.x, r.ev, v[0], v[1]);
+    decode4<false>(r.v.a.y, r.ev, v[2], v[3]);
     const Pair nan = pair(__uint_as_float(0x7FC00000u));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if (em == 255) m[j] = nan;
-      if (ev == 255) v[j] = nan;
+      if (r.em == 255) m[j] = nan;
+      if (r.ev == 255) v[j] = nan;
     }
-    store_f32(static_cast<float*>(d.m) + first, lane, m);
-    store_f32(static_cast<float*>(d.v) + first, lane, v);
+    store_f32(lane_at<4>(d.m, block, lane), m);
+    store_f32(lane_at<4>(d.v, block, lane), v);
   }
 }
 
@@ -68,20 +76,40 @@ __device__ __noinline__ void convert_any(const OptDesc* from, const OptDesc* to,
 }
 
 template <bool ToEight, bool Random>
-__global__ void __launch_bounds__(32 * kOptWarps, 4) convert_kernel(const __grid_constant__ ConvertParams p) {
-  wait_for_kernel_before();
+__global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_constant__ ConvertParams p) {
+  constexpr int kBlocks = convert_blocks(ToEight);
   const int lane = threadIdx.x % 32;
-  const uint32_t b = blockIdx.x * kOptWarps + threadIdx.x / 32;
+  uint32_t b = blockIdx.x * (kBlocks * kOptWarps) + threadIdx.x / 32;
   if (b >= p.src.n_blocks) return;
-  const uint32_t t = tensor_of(p.src, p.src.start[blockIdx.x], b);
-  const OptDesc s = p.src.tensors[t], d = p.dst.tensors[t];
+  uint32_t t = tensor_of(p.src, p.src.start[blockIdx.x], b);
+  OptDesc s = p.src.tensors[t], d = p.dst.tensors[t];  // (the plans' tables: nothing writes them)
+  wait_for_kernel_before();
   RandomKey key = {0, 0};
   if (Random) key = random_key(p.key, s.tensor);
-  const uint32_t block = b - s.first;
-  if (s.aligned && d.aligned && block < s.n / kOptBlock)
-    convert_whole<ToEight, Random>(s, d, block, key, lane);
-  else
-    convert_any<ToEight, Random>(p.src.tensors + t, p.dst.tensors + t, block, key, lane);
+  if (s.aligned && d.aligned && b - s.first + (kBlocks - 1) * kOptWarps < s.n / kOptBlock) {
+    Raw<ToEight> r[kBlocks];
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) r[k].load(s, b - s.first + k * kOptWarps, lane);
+#pragma unroll
+    for (int k = 0; k < kBlocks; ++k) convert_whole<ToEight, Random>(r[k], d, b - s.first + k * kOptWarps, key, lane);
+    return;
+  }
+#pragma unroll 1
+  for (int k = 0;;) {
+    const uint32_t block = b - s.first;
+    if (s.aligned && d.aligned && block < s.n / kOptBlock) {
+      Raw<ToEight> r;
+      r.load(s, block, lane);
+      convert_whole<ToEight, Random>(r, d, block, key, lane);
+    } else {
+      convert_any<ToEight, Random>(p.src.tensors + t, p.dst.tensors + t, block, key, lane);
+    }
+    b += kOptWarps;
+    if (++k == kBlocks || b >= p.src.n_blocks) return;
+    t = tensor_of(p.src, t, b);
+    s = p.src.tensors[t], d = p.dst.tensors[t];
+    if (Random) key = random_key(p.key, s.tensor);
+  }
 }
 
 }  // namespace

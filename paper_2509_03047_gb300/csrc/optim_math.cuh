@@ -78,7 +78,6 @@ __device__ __forceinline__ uint32_t random_weights(uint32_t u) { return u * 7477
 
 // ---- pairs: two fp32 products per instruction, each rounded as a single one
 
-using Pair = float2;
 __device__ __forceinline__ Pair pair(float x) { return make_float2(x, x); }
 #define FR_PAIR(x) reinterpret_cast<const uint64_t&>(x)
 __device__ __forceinline__ Pair mul2(Pair a, Pair b) {
@@ -98,17 +97,18 @@ __device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
 
 // ---- the update
 
+// What a step's numbers are multiplied in as: the launch's, twice each so that
+// the pairs come from constant memory, and the tensor's own.
 struct Hyper {
-  float b1, c1, b2, c2, scale;  // scale: of the gradient
-  float lr, decay, eps, m_fix, v_fix;
-  bool exact;
+  const StepNumbers& n;
+  float scale, lr, decay;  // scale: of the gradient
 };
 
 // New moments, each product and sum rounded by itself.
 __device__ __forceinline__ void update_moments(const Hyper& h, Pair grad, Pair& m, Pair& v) {
   const Pair g = mul2(grad, pair(h.scale));
-  m = add2(mul2(m, pair(h.b1)), mul2(g, pair(h.c1)));
-  v = add2(mul2(v, pair(h.b2)), mul2(mul2(g, g), pair(h.c2)));
+  m = add2(mul2(m, h.n.b1), mul2(g, h.n.c1));
+  v = add2(mul2(v, h.n.b2), mul2(mul2(g, g), h.n.c2));
 }
 
 // The parameter from the new moments.  The square root and the reciprocal are
@@ -128,15 +128,14 @@ __device__ __forceinline__ float approx_reciprocal(float x) {
   return r;
 }
 __device__ __forceinline__ Pair update_param(const Hyper& h, Pair p, Pair m, Pair v) {
-  Pair u;
-  if (h.exact) {
-    const Pair below = fma2(make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y)), pair(h.v_fix), pair(h.eps));
-    u = make_float2(__fdiv_rn(m.x, below.x), __fdiv_rn(m.y, below.y));
-  } else {
-    const Pair below = fma2(make_float2(approx_sqrt(v.x), approx_sqrt(v.y)), pair(h.v_fix), pair(h.eps));
-    u = mul2(m, make_float2(approx_reciprocal(below.x), approx_reciprocal(below.y)));
-  }
-  return fma2(fma2(u, pair(h.m_fix), mul2(p, pair(h.decay))), pair(-h.lr), p);
+  const Pair below = fma2(make_float2(approx_sqrt(v.x), approx_sqrt(v.y)), h.n.v_fix, h.n.eps);
+  const Pair u = mul2(m, make_float2(approx_reciprocal(below.x), approx_reciprocal(below.y)));
+  return fma2(fma2(u, h.n.m_fix, mul2(p, pair(h.decay))), pair(-h.lr), p);
+}
+__device__ __forceinline__ Pair update_param_exactly(const Hyper& h, Pair p, Pair m, Pair v) {
+  const Pair below = fma2(make_float2(__fsqrt_rn(v.x), __fsqrt_rn(v.y)), h.n.v_fix, h.n.eps);
+  const Pair u = make_float2(__fdiv_rn(m.x, below.x), __fdiv_rn(m.y, below.y));
+  return fma2(fma2(u, h.n.m_fix, mul2(p, pair(h.decay))), pair(-h.lr), p);
 }
 
 }  // namespace frk

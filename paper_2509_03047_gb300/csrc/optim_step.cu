@@ -25,33 +25,57 @@ __device__ __forceinline__ uint32_t nearest_bf16x2(Pair x) {
   return r;
 }
 
+__device__ __forceinline__ Hyper hyper(const StepParams& p, float scale, const OptDesc& d) {
+  return {p.numbers, scale, __fmul_rn(p.lr, d.lr_scale), __fmul_rn(p.decay, d.decay_scale)};
+}
+
 template <int Weight, bool Bf16Grad, bool Eight, bool Random>
 struct Step {
   using RawGrad = std::conditional_t<Bf16Grad, RawBf16, RawF32>;
   using RawParam = std::conditional_t<Weight == kWeightBf16, RawBf16, RawF32>;
   using RawMoment = std::conditional_t<Eight, RawCodes, RawF32>;
-  static constexpr int kGradBytes = Bf16Grad ? 2 : 4, kMomentBytes = Eight ? 1 : 4;
+  static constexpr int kGradBytes = RawGrad::kBytes, kMomentBytes = RawMoment::kBytes, kWeightBytes = Weight == kWeightF32 ? 4 : 2;
 
-  static __device__ __forceinline__ void whole(const Hyper& h, const OptDesc& d, uint32_t block, RandomKey key, int lane) {
-    const uint64_t first = static_cast<uint64_t>(block) * kOptBlock;
-    uint8_t* const m_at = static_cast<uint8_t*>(d.m) + first * kMomentBytes;
-    uint8_t* const v_at = static_cast<uint8_t*>(d.v) + first * kMomentBytes;
-    RawGrad raw_g;
-    RawParam raw_p;
-    RawMoment raw_m, raw_v;
-    raw_g.load(static_cast<const uint8_t*>(d.grad) + first * kGradBytes, lane);
-    raw_m.load(m_at, lane);
-    raw_v.load(v_at, lane);
-    raw_p.load(Weight == kWeightMaster ? static_cast<const void*>(d.master + first)
-                                       : static_cast<const uint8_t*>(d.weight) + first * (Weight == kWeightBf16 ? 2 : 4), lane);
+  // The lane's places in a block.
+  struct Places {
+    const uint8_t* g;
+    uint8_t *p, *w, *m, *v;  // w: the weight, where it is not the parameter
+    __device__ __forceinline__ Places(const OptDesc& d, uint32_t block, int lane) {
+      g = lane_at<kGradBytes>(d.grad, block, lane);
+      p = lane_at<RawParam::kBytes>(Weight == kWeightMaster ? d.master : d.weight, block, lane);
+      w = lane_at<2>(d.weight, block, lane);
+      m = lane_at<kMomentBytes>(d.m, block, lane);
+      v = lane_at<kMomentBytes>(d.v, block, lane);
+    }
+    __device__ __forceinline__ void next() {
+      g += kOptBlock * kGradBytes;
+      p += kOptBlock * RawParam::kBytes;
+      w += kOptBlock * 2;
+      m += kOptBlock * kMomentBytes;
+      v += kOptBlock * kMomentBytes;
+    }
+  };
+  // A whole block's loads, `ahead` blocks further.
+  struct Raw {
+    RawGrad g;
+    RawParam p;
+    RawMoment m, v;
+    __device__ __forceinline__ void load(const Places& at, int ahead) {
+      g.load(at.g + ahead * (kOptBlock * kGradBytes));
+      m.load(at.m + ahead * (kOptBlock * kMomentBytes));
+      v.load(at.v + ahead * (kOptBlock * kMomentBytes));
+      p.load(at.p + ahead * (kOptBlock * RawParam::kBytes));
+    }
+  };
+  // The rest of it; first: its first element's index, em and ev: its exponents, old and new.
+  static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, uint64_t first, RandomKey key, int lane, const Raw& r,
+                                                uint32_t& em, uint32_t& ev) {
     Pair g[4], p[4], m[4], v[4];
     if constexpr (Eight) {
-      const uint32_t em = d.m_exp[block], ev = d.v_exp[block];
-      __syncwarp();  // every lane has read the exponents before one writes them
-      decode4<true>(raw_m.a.x, em, m[0], m[1]);
-      decode4<true>(raw_m.a.y, em, m[2], m[3]);
-      decode4<false>(raw_v.a.x, ev, v[0], v[1]);
-      decode4<false>(raw_v.a.y, ev, v[2], v[3]);
+      decode4<true>(r.m.a.x, em, m[0], m[1]);
+      decode4<true>(r.m.a.y, em, m[2], m[3]);
+      decode4<false>(r.v.a.x, ev, v[0], v[1]);
+      decode4<false>(r.v.a.y, ev, v[2], v[3]);
       if (em == 255 || ev == 255) {  // (rare) a block that has lost its moments
         const float nan = __uint_as_float(0x7FC00000u);
 #pragma unroll
@@ -61,11 +85,11 @@ struct Step {
         }
       }
     } else {
-      raw_m.get(m);
-      raw_v.get(v);
+      r.m.get(m);
+      r.v.get(v);
     }
-    raw_g.get(g);
-    raw_p.get(p);
+    r.g.get(g);
+    r.p.get(p);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       update_moments(h, g[j], m[j], v[j]);
@@ -73,41 +97,79 @@ struct Step {
     }
     uint32_t u[4];
     if (Random) random_pairs(key, first, lane, u);
-    if (Weight == kWeightMaster) store_f32(d.master + first, lane, p);
-    if (Weight == kWeightF32) {
-      store_f32(static_cast<float*>(d.weight) + first, lane, p);
-    } else {
+    if (Weight == kWeightBf16) {
       uint32_t w[4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) w[j] = Random && Weight == kWeightBf16 ? random_bf16x2(p[j], u[j]) : nearest_bf16x2(p[j]);
-      store_bf16(static_cast<uint16_t*>(d.weight) + first, lane, w);
+      for (int j = 0; j < 4; ++j) w[j] = Random ? random_bf16x2(p[j], u[j]) : nearest_bf16x2(p[j]);
+      store_bf16(at.p, w);
+    } else {
+      store_f32(at.p, p);
+      if (Weight == kWeightMaster) {
+        uint32_t w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = nearest_bf16x2(p[j]);
+        store_bf16(at.w, w);
+      }
     }
     if constexpr (Eight) {
-      store_codes<true, Random>(m, u, m_at, d.m_exp + block, lane);
-      store_codes<false, Random>(v, u, v_at, d.v_exp + block, lane);
+      em = store_codes<true, Random>(m, u, at.m);
+      ev = store_codes<false, Random>(v, u, at.v);
     } else {
-      store_f32(reinterpret_cast<float*>(m_at), lane, m);
-      store_f32(reinterpret_cast<float*>(v_at), lane, v);
+      store_f32(at.m, m);
+      store_f32(at.v, v);
     }
   }
 
-  static __device__ __noinline__ void any(const Hyper h, const OptDesc* tensor, uint32_t block, RandomKey key, int lane) {
-    const OptDesc d = *tensor;
+  // `count` whole blocks one after the other, one loaded ahead.  Not unrolled:
+  // the code must stay in the instruction cache.
+  static __device__ __forceinline__ void whole(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
+    Places at(d, block, lane);
+    uint64_t first = static_cast<uint64_t>(block) * kOptBlock + d.skipped;
+    Raw r;
+    r.load(at, 0);
+    uint32_t em = 0, ev = 0;
+    if (!Eight) {
+      finish(h, at, first, key, lane, r, em, ev);
+      return;
+    }
+    Exponents e;
+    e.load(d.m_exp + block, d.v_exp + block, count, lane);
+#pragma unroll 1
+    for (int k = 0;;) {
+      Raw next;
+      if (k + 1 < count) next.load(at, 1);
+      em = e.of_m(k), ev = e.of_v(k);
+      finish(h, at, first, key, lane, r, em, ev);
+      e.set(k, lane, em, ev);
+      if (++k == count) break;
+      r = next;
+      first += kOptBlock;
+      at.next();
+    }
+    e.store(d.m_exp + block, d.v_exp + block, count, lane);
+  }
+
+  // Any block of tensor t, element by element.
+  static __device__ __noinline__ void any(const StepParams& p, float scale, uint32_t t, uint32_t block) {
+    const OptDesc d = p.work.tensors[t];
+    const int lane = threadIdx.x % 32;
+    const Hyper h = hyper(p, scale, d);
+    RandomKey key = {0, 0};
+    if (Random) key = random_key(p.key, d.tensor);
     const uint64_t first = static_cast<uint64_t>(block) * kOptBlock;
     const int left = static_cast<int>(min(d.n - first, static_cast<uint64_t>(kOptBlock)));
     uint8_t* const m_at = static_cast<uint8_t*>(d.m) + first * kMomentBytes;
     uint8_t* const v_at = static_cast<uint8_t*>(d.v) + first * kMomentBytes;
-    float g[kOptLane], p[kOptLane], m[kOptLane], v[kOptLane];
+    float g[kOptLane], x[kOptLane], m[kOptLane], v[kOptLane];
     load_any<std::conditional_t<Bf16Grad, uint16_t, float>>(static_cast<const uint8_t*>(d.grad) + first * kGradBytes, lane, left, g);
     if (Weight == kWeightMaster)
-      load_any<float>(d.master + first, lane, left, p);
+      load_any<float>(d.master + first, lane, left, x);
     else if (Weight == kWeightBf16)
-      load_any<uint16_t>(static_cast<const uint16_t*>(d.weight) + first, lane, left, p);
+      load_any<uint16_t>(static_cast<const uint16_t*>(d.weight) + first, lane, left, x);
     else
-      load_any<float>(static_cast<const float*>(d.weight) + first, lane, left, p);
+      load_any<float>(static_cast<const float*>(d.weight) + first, lane, left, x);
     if (Eight) {
       const uint32_t em = d.m_exp[block], ev = d.v_exp[block];
-      __syncwarp();
       load_codes_any<true>(m_at, em, lane, left, m);
       load_codes_any<false>(v_at, ev, lane, left, v);
     } else {
@@ -118,18 +180,18 @@ struct Step {
     for (int j = 0; j < kOptLane; j += 2) {
       Pair a = make_float2(m[j], m[j + 1]), b = make_float2(v[j], v[j + 1]);
       update_moments(h, make_float2(g[j], g[j + 1]), a, b);
-      const Pair q = update_param(h, make_float2(p[j], p[j + 1]), a, b);
-      m[j] = a.x, m[j + 1] = a.y, v[j] = b.x, v[j + 1] = b.y, p[j] = q.x, p[j + 1] = q.y;
+      const Pair old = make_float2(x[j], x[j + 1]), q = p.exact ? update_param_exactly(h, old, a, b) : update_param(h, old, a, b);
+      m[j] = a.x, m[j + 1] = a.y, v[j] = b.x, v[j + 1] = b.y, x[j] = q.x, x[j + 1] = q.y;
     }
-    if (Weight == kWeightMaster) store_any<float>(d.master + first, lane, left, p);
+    if (Weight == kWeightMaster) store_any<float>(d.master + first, lane, left, x);
     if (Weight == kWeightF32) {
-      store_any<float>(static_cast<float*>(d.weight) + first, lane, left, p);
+      store_any<float>(static_cast<float*>(d.weight) + first, lane, left, x);
     } else {
       uint16_t w[kOptLane];
 #pragma unroll
       for (int j = 0; j < kOptLane; ++j) {
-        const uint64_t i = first + j * 32 + lane;
-        const Pair twice = pair(p[j]);  // (the pair's half that counts)
+        const uint64_t i = first + d.skipped + j * 32 + lane;
+        const Pair twice = pair(x[j]);  // (the pair's half that counts)
         const uint32_t both = Random && Weight == kWeightBf16 ? random_bf16x2(twice, random_pair(key, i >> 1)) : nearest_bf16x2(twice);
         w[j] = static_cast<uint16_t>(i & 1 ? both >> 16 : both);
       }
@@ -146,30 +208,38 @@ struct Step {
 };
 
 template <int Weight, bool Bf16Grad, bool Eight, bool Random>
-__global__ void __launch_bounds__(32 * kOptWarps, 4) step_kernel(const __grid_constant__ StepParams p) {
-  wait_for_kernel_before();
+__global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight)) step_kernel(const __grid_constant__ StepParams p) {
   using S = Step<Weight, Bf16Grad, Eight, Random>;
+  const uint32_t per_warp = Eight ? p.work.unit_blocks / kOptWarps : 1;
   const int lane = threadIdx.x % 32;
-  const uint32_t b = blockIdx.x * kOptWarps + threadIdx.x / 32;
-  if (b >= p.work.n_blocks) return;
-  const uint32_t t = tensor_of(p.work, p.work.start[blockIdx.x], b);
-  const OptDesc d = p.work.tensors[t];
-  Hyper h;
-  h.scale = 1.0f;
+  uint32_t b = (blockIdx.x * kOptWarps + threadIdx.x / 32) * per_warp;
+  const uint32_t end = min(b + per_warp, p.work.n_blocks);
+  if (b >= end) return;
+  uint32_t t = tensor_of(p.work, p.work.start[blockIdx.x], b);
+  OptDesc d = p.work.tensors[t];  // (the plan's tables: nothing writes them)
+  wait_for_kernel_before();
+  float scale = 1.0f;
   if (p.clip != nullptr) {
     if (p.clip->nonfinite != 0) return;
-    h.scale = p.clip->scale;
+    scale = p.clip->scale;
   }
-  h.b1 = p.b1, h.c1 = p.c1, h.b2 = p.b2, h.c2 = p.c2, h.eps = p.eps, h.m_fix = p.m_fix, h.v_fix = p.v_fix, h.exact = p.exact;
-  h.lr = __fmul_rn(p.lr, d.lr_scale);
-  h.decay = __fmul_rn(p.decay, d.decay_scale);
-  RandomKey key = {0, 0};
-  if (Random) key = random_key(p.key, d.tensor);
-  const uint32_t block = b - d.first;
-  if (d.aligned && block < d.n / kOptBlock)
-    S::whole(h, d, block, key, lane);
-  else
-    S::any(h, p.work.tensors + t, block, key, lane);
+#pragma unroll 1
+  for (;;) {
+    const uint32_t block = b - d.first, whole = d.aligned && !p.exact ? static_cast<uint32_t>(d.n / kOptBlock) : 0;
+    if (block < whole) {
+      RandomKey key = {0, 0};
+      if (Random) key = random_key(p.key, d.tensor);
+      const uint32_t count = Eight ? min(end - b, whole - block) : 1;
+      S::whole(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
+      b += count;
+    } else {
+      S::any(p, scale, t, block);
+      ++b;
+    }
+    if (b >= end) return;
+    t = tensor_of(p.work, t, b);
+    d = p.work.tensors[t];
+  }
 }
 
 template <class F>
