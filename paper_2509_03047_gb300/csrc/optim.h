@@ -3,7 +3,7 @@
 //
 // Work is counted in blocks of kOptBlock elements from each tensor's start:
 // what a warp takes at a time, eight elements per lane.  A launch's blocks are
-// those of its tensors one after the other, in units of consecutive blocks.
+// those of its tensors one after the other.
 #pragma once
 
 #include <cstdint>
@@ -38,11 +38,12 @@ struct OptDesc {        // 96 bytes: one tensor that has elements, or a part of 
 };
 static_assert(sizeof(OptDesc) == 96, "OptDesc layout");
 
-// Tensors in order, and for each unit the tensor that it starts in.
+// Tensors in order, and for each CTA the tensor that its first block is in (the
+// norm: for each segment).
 struct OptWork {
   const OptDesc* tensors;
   const uint32_t* start;
-  uint32_t n_blocks, n_units, unit_blocks;
+  uint32_t n_blocks, n_starts;
 };
 
 constexpr int kOptWarps = 8;  // per CTA, in every kernel here
@@ -50,12 +51,14 @@ constexpr uint32_t kSms = 152;  // of a GB300
 
 // ---- the norm
 
-// A launch's sums are added in an order that units and CTAs decide, so both
+// A launch's sums are added in an order that segments and CTAs decide, so both
 // follow from the sizes alone, not from the GPU: at most 4 CTAs per SM, about
-// four units for each, of 2 to 16 blocks per warp.
-constexpr uint32_t kClipUnit = 16 * kOptWarps;
+// four segments for each, of 2 to 16 blocks per warp.  CTA c of g takes the
+// segments c, c + g, ..., its warps a segment's blocks in turn.  (One range of
+// blocks per CTA: an 8B rank's 2 GB 287 us, so 276.)
+constexpr uint32_t kClipSegment = 16 * kOptWarps;
 constexpr uint32_t kClipCtas = 4 * kSms;
-inline uint32_t clip_unit(uint64_t n_blocks) {
+inline uint32_t clip_segment(uint64_t n_blocks) {
   const uint64_t per_warp = n_blocks / (4 * kClipCtas * kOptWarps);
   return static_cast<uint32_t>(per_warp < 2 ? 2 : per_warp < 16 ? per_warp : 16) * kOptWarps;
 }
@@ -65,9 +68,11 @@ struct ClipPartial {  // of one CTA
 };
 struct ClipParams {
   OptWork work;
-  ClipPartial* partials;
+  uint32_t segment;        // blocks
+  ClipPartial* partials;  // one per CTA
   uint32_t* done;  // CTAs that have written theirs; zero before a launch and after it
-  double grad_scale, max_norm;
+  double grad_scale;
+  float max_norm;
   fr_clip* out;
 };
 cudaError_t launch_clip(const ClipParams& p, cudaStream_t s);
@@ -97,14 +102,17 @@ struct StepParams {
   float lr, decay;
   uint32_t exact;              // 1: eps is too small for the approximations of update_param (optim_math.cuh)
   uint32_t random;             // 1: FR_ROUND_RANDOM
+  uint32_t per_warp;           // consecutive blocks
   uint64_t key;                // of the random bits: mix64(mix64(seed) + step)
 };
-// CTAs of eight warps per SM, what the registers of a lane's elements allow.
-constexpr int step_ctas(bool eight) { return eight ? 3 : 4; }
+// CTAs of eight warps per SM, what the registers of a lane's elements allow: of
+// the 8-bit classes the one that loads least is as fast with 64 as with 80 (GPT-2
+// small 207 us with 4 CTAs, 211 with 3; with a master 326 and 299).
+constexpr int step_ctas(bool eight, int weight, bool bf16_grad) { return eight && !(weight == kWeightBf16 && bf16_grad) ? 3 : 4; }
 // Consecutive blocks per warp.
 inline uint32_t step_blocks(bool eight, uint64_t n_blocks) {
   if (!eight) return 1;
-  const uint64_t warps = kSms * step_ctas(true) * kOptWarps, b = n_blocks / (2 * warps);
+  const uint64_t warps = kSms * 3 * kOptWarps, b = n_blocks / (2 * warps);
   return static_cast<uint32_t>(b < 1 ? 1 : b < 8 ? b : 8);
 }
 cudaError_t launch_step(const StepClass& c, const StepParams& p, cudaStream_t s);
@@ -117,13 +125,10 @@ struct ConvertParams {
   uint32_t random;
   uint64_t key;
 };
-#ifndef FR_TO8
-#define FR_TO8 2
-#endif
-#ifndef FR_TO32
-#define FR_TO32 4
-#endif
-constexpr int convert_blocks(bool to_eight) { return to_eight ? FR_TO8 : FR_TO32; }
+// Blocks per warp, loaded together (one, two, three, four of GPT-2 small: to 8
+// bits 239, 193, 192, 202 us, back 185, 179, 180, 180; of 18 million elements in
+// 2,000 tensors 40, 36, 38, 43 and 33 for each).
+constexpr int kConvertBlocks = 2;
 cudaError_t launch_convert(const ConvertParams& p, cudaStream_t s);
 
 // splitmix64's output function (Steele, Lea, Flood, "Fast splittable

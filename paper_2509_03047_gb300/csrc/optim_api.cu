@@ -1,6 +1,6 @@
 // optim_api.cu -- the C ABI of the optimizer step (declared in
 // include/flashrec.h) and its planner: the tensors of each launch in one list,
-// cut into units of blocks.
+// with the tensor that each CTA's first block is in.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -22,7 +22,7 @@ struct WorkList {
   std::vector<OptDesc> tensors;
   std::vector<uint32_t> start;
   uint64_t n_blocks = 0;
-  uint32_t unit_blocks = kOptWarps;
+  uint32_t n_starts = 0;
   OptDesc* d_tensors = nullptr;
   uint32_t* d_start = nullptr;
 
@@ -31,25 +31,25 @@ struct WorkList {
     n_blocks += d.n_blocks;
     tensors.push_back(d);
   }
-  // Into units of `blocks`.
-  void cut(uint32_t blocks) {
-    unit_blocks = blocks;
-    const uint64_t n_units = (n_blocks + unit_blocks - 1) / unit_blocks;
-    start.resize(n_units);
+  // For CTAs whose first blocks are first(0) <= first(1) <= ...
+  template <class F>
+  void cut(uint64_t ctas, F&& first) {
+    n_starts = static_cast<uint32_t>(ctas);
+    start.resize(n_starts);
     size_t t = 0;
-    for (uint64_t u = 0; u < n_units; ++u) {
-      while (t + 1 < tensors.size() && tensors[t + 1].first <= u * unit_blocks) ++t;
-      start[u] = static_cast<uint32_t>(t);
+    for (uint32_t c = 0; c < n_starts; ++c) {
+      while (t + 1 < tensors.size() && tensors[t + 1].first <= first(c)) ++t;
+      start[c] = static_cast<uint32_t>(t);
     }
+  }
+  void cut_every(uint64_t blocks) {
+    cut((n_blocks + blocks - 1) / blocks, [&](uint32_t c) { return c * blocks; });
   }
   void place(PlanMemory& mem) {
     mem.table(&d_tensors, tensors);
     mem.table(&d_start, start);
   }
-  OptWork work() const {
-    return {d_tensors, d_start, static_cast<uint32_t>(n_blocks), static_cast<uint32_t>((n_blocks + unit_blocks - 1) / unit_blocks),
-            unit_blocks};
-  }
+  OptWork work() const { return {d_tensors, d_start, static_cast<uint32_t>(n_blocks), n_starts}; }
 };
 
 }  // namespace
@@ -179,16 +179,16 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
     if (x.m) (x.state_dtype == FR_DT_BYTES ? p->eight : p->thirty_two) = true;
   }
   PlanMemory mem;
-  p->clip.cut(clip_unit(p->clip.n_blocks));
+  p->clip.cut_every(clip_segment(p->clip.n_blocks));
   p->clip.place(mem);
   if (p->moments) {
-    p->convert.cut(convert_blocks(!p->eight) * kOptWarps);
+    p->convert.cut_every(kConvertBlocks * kOptWarps);
     p->convert.place(mem);
   }
   if (p->params)
     for (int c = 0; c < kStepClasses; ++c) {
       if (p->step[c].n_blocks == 0) continue;
-      p->step[c].cut(step_blocks(p->classes[c].eight, p->step[c].n_blocks) * kOptWarps);
+      p->step[c].cut_every(step_blocks(p->classes[c].eight, p->step[c].n_blocks) * kOptWarps);
       p->step[c].place(mem);
     }
   mem.table(&p->d_done, std::vector<uint32_t>(1, 0));
@@ -279,6 +279,7 @@ fr_status fr_grad_clip(fr_opt p, float max_norm, float grad_scale, fr_clip* out_
   if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
   ClipParams cp;
   cp.work = p->clip.work();
+  cp.segment = clip_segment(p->clip.n_blocks);
   cp.partials = p->d_partials;
   cp.done = p->d_done;
   cp.grad_scale = grad_scale;
@@ -322,6 +323,7 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   for (int c = 0; c < kStepClasses; ++c) {
     if (p->step[c].n_blocks == 0) continue;
     sp.work = p->step[c].work();
+    sp.per_warp = step_blocks(p->classes[c].eight, p->step[c].n_blocks);
     const cudaError_t e = launch_step(p->classes[c], sp, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return report_cuda("step kernel launch", e);
   }

@@ -1,4 +1,4 @@
-// optim_block.cuh -- a warp's block of 256 elements: walking the units, loads,
+// optim_block.cuh -- a warp's block of 256 elements: finding its tensor, loads,
 // stores, random bits, coding of 8-bit moments.
 //
 // A whole block whose buffers are aligned moves as vectors: lane l has the
@@ -12,7 +12,7 @@
 
 namespace frk {
 
-// The tensor of block b of a launch, from the one that b's unit starts in.
+// The tensor of block b of a launch, from one that is not after it.
 __device__ __forceinline__ uint32_t tensor_of(const OptWork& w, uint32_t t, uint32_t b) {
   while (b - w.tensors[t].first >= w.tensors[t].n_blocks) ++t;
   return t;
@@ -72,35 +72,46 @@ __device__ __forceinline__ uint8_t* lane_at(const void* buffer, uint32_t block, 
   return static_cast<uint8_t*>(const_cast<void*>(buffer)) + (static_cast<uint64_t>(block) * kOptBlock + lane * kOptLane) * Bytes;
 }
 
-// Four codes of a block of exponent e < 255 as values: two at a time as bf16
-// patterns (a code's three fraction bits fit), zero codes without the base.
+// Four codes of a block of exponent e (span < e < 255) as values: two at a time
+// as bf16 patterns (a code's three fraction bits fit), zero codes without the
+// base.
 template <bool Signed>
 __device__ __forceinline__ void decode4(uint32_t w, uint32_t e, Pair& x, Pair& y) {
-  const uint32_t base = static_cast<uint32_t>(code_base(e, Signed ? kSpanM : kSpanV)) << 4;
+  const uint32_t base = code_base(e, Signed ? kSpanM : kSpanV) * 16;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const uint32_t two = __byte_perm(w, 0, k ? 0x4342 : 0x4140);
-    const uint32_t c = Signed ? two & 0x007F007Fu : two;
-    uint32_t h = c * 16 + __vminu2(c, 0x00010001u) * base;
-    if (Signed) h += (two & 0x00800080u) * 256;
+    uint32_t h;
+    if (Signed) {  // the bytes in the high halves' places: the sign is where it belongs
+      const uint32_t two = __byte_perm(w, 0, k ? 0x3424 : 0x1404), c = (two >> 4) & 0x07F007F0u;
+      h = (c + __vminu2(c, 0x00010001u) * base) | (two & 0x80008000u);
+    } else {
+      const uint32_t two = __byte_perm(w, 0, k ? 0x4342 : 0x4140);
+      h = two * 16 + __vminu2(two, 0x00010001u) * base;
+    }
     (k ? y : x) = make_float2(__uint_as_float(h << 16), __uint_as_float(h & 0xFFFF0000u));
   }
 }
 
-// Codes of four values of a block of exponent e, r: what rounding adds to each
-// below bit 20.  The rounded patterns' high halves, two at a time, less the
-// base.  Unsigned: code 1 at least, so zeros are left to the caller.
+// Two values' patterns rounded and cut at bit 20, in 12 bits each with the sign.
+template <bool Random>
+__device__ __forceinline__ uint32_t cut2(Pair x, uint32_t r) {
+  const uint32_t a = __float_as_uint(x.x), b = __float_as_uint(x.y);
+  if (!Random) return (__byte_perm(a + round_nearest(a), b + round_nearest(b), 0x7632) >> 4) & 0x0FFF0FFFu;
+  // r: 16 random bits for each.  Four bits down, the cut is where a conversion to
+  // bf16 that rounds by given bits has it, and the patterns are small numbers.
+  uint32_t h;
+  asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(h) : "f"(__uint_as_float(b >> 4)), "f"(__uint_as_float(a >> 4)), "r"(r));
+  return h;
+}
+
+// Codes of four values of a block of exponent e, from their cut patterns.
+// Unsigned: code 1 at least, so zeros are left to the caller.
 template <bool Signed>
-__device__ __forceinline__ uint32_t encode4(Pair x, Pair y, const uint32_t (&r)[4], uint32_t e) {
-  const uint32_t base = static_cast<uint32_t>(code_base(e, Signed ? kSpanM : kSpanV)) * 0x00010001u;
-  const uint32_t s0 = __float_as_uint(x.x) + r[0], s1 = __float_as_uint(x.y) + r[1];
-  const uint32_t s2 = __float_as_uint(y.x) + r[2], s3 = __float_as_uint(y.y) + r[3];
-  const uint32_t h0 = __byte_perm(s0, s1, 0x7632), h1 = __byte_perm(s2, s3, 0x7632);
-  const uint32_t least = Signed ? base : base + 0x00010001u;
-  const uint32_t c0 = __vmaxu2((h0 >> 4) & 0x07FF07FFu, least) - base, c1 = __vmaxu2((h1 >> 4) & 0x07FF07FFu, least) - base;
-  const uint32_t c = __byte_perm(c0, c1, 0x6420);
-  if (!Signed) return c;
-  return c | (__byte_perm(h0, h1, 0x7531) & (c + 0x7F7F7F7Fu) & 0x80808080u);
+__device__ __forceinline__ uint32_t encode4(uint32_t h0, uint32_t h1, uint32_t e) {
+  const uint32_t base = code_base(e, Signed ? kSpanM : kSpanV) * 0x00010001u;
+  if (!Signed) return __byte_perm(__vmaxu2(h0, base + 0x00010001u) - base, __vmaxu2(h1, base + 0x00010001u) - base, 0x6420);
+  const uint32_t c = __byte_perm(__vmaxu2(h0 & 0x07FF07FFu, base) - base, __vmaxu2(h1 & 0x07FF07FFu, base) - base, 0x6420);
+  return c | ((__byte_perm(h0, h1, 0x7531) * 16) & (c + 0x7F7F7F7Fu) & 0x80808080u);  // no zero has a sign
 }
 
 // Largest bit pattern of |x| over the warp; a NaN's is above all others.
@@ -115,10 +126,16 @@ __device__ __forceinline__ uint32_t block_top(const Pair (&x)[4]) {
   return warp_max(__float_as_uint(max3(max3(a, b, x[3].x), x[3].y, 0.0f)));
 }
 
-// A lane's random bits of a whole block: u of each pair of elements.
-__device__ __forceinline__ void random_pairs(RandomKey key, uint64_t first, int lane, uint32_t (&u)[4]) {
+// A lane's random bits of a whole block: those of its four pairs of elements, from the first one's counter.
+__device__ __forceinline__ void random_pairs(RandomKey key, uint32_t counter, uint32_t (&u)[4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) u[j] = random_pair(key, (first >> 1) + lane * 4 + j);
+  for (int j = 0; j < 4; ++j) u[j] = random_mix(key, counter + j * kRandomStep);
+}
+
+__device__ __forceinline__ float min3(float a, float b, float c) {
+  float r;
+  asm("min.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 // Codes a whole block's moments and stores them at the lane's place; returns the
@@ -126,30 +143,19 @@ __device__ __forceinline__ void random_pairs(RandomKey key, uint64_t first, int 
 template <bool Signed, bool Random>
 __device__ __forceinline__ uint32_t store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes) {
   const uint32_t e = block_exponent(block_top(x), Signed ? kSpanM : kSpanV);
-  uint32_t w[2];
+  uint32_t h[4], w[2];
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    uint32_t r[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (Random) {
-        const uint32_t q = random_moments(u[2 * k + j / 2], j & 1);
-        r[j] = (Signed ? q & 0xFFFFu : q >> 16) << 4;
-      } else {
-        const Pair y = x[2 * k + j / 2];
-        r[j] = round_nearest(__float_as_uint(j & 1 ? y.y : y.x));
-      }
-    }
-    w[k] = encode4<Signed>(x[2 * k], x[2 * k + 1], r, e);
-  }
+  for (int j = 0; j < 4; ++j)
+    h[j] = cut2<Random>(x[j], Random ? __byte_perm(random_moments(u[j], 0), random_moments(u[j], 1), Signed ? 0x5410 : 0x7632) : 0u);
+  w[0] = encode4<Signed>(h[0], h[1], e);
+  w[1] = encode4<Signed>(h[2], h[3], e);
   if (!Signed) {  // second moments that are zero: whole rows, or none
-    const float least = fminf(fminf(fminf(x[0].x, x[0].y), fminf(x[1].x, x[1].y)), fminf(fminf(x[2].x, x[2].y), fminf(x[3].x, x[3].y)));
-    if (least == 0.0f)
+    if (min3(min3(x[0].x, x[0].y, x[1].x), min3(x[1].y, x[2].x, x[2].y), fminf(x[3].x, x[3].y)) == 0.0f)
 #pragma unroll
       for (int j = 0; j < kOptLane; ++j)
         if ((j & 1 ? x[j / 2].y : x[j / 2].x) == 0.0f) w[j / 4] &= ~(0xFFu << 8 * (j & 3));
   }
-  if (e == 255) w[0] = w[1] = 0;
+  if (e >= 255) w[0] = w[1] = 0;
   *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
   return e;
 }
@@ -163,9 +169,10 @@ struct Exponents {
   __device__ __forceinline__ void load(const uint8_t* me, const uint8_t* ve, int count, int lane) {
     m = v = 0;
     if (lane < count) m = me[lane], v = ve[lane];
+    m = read_exponent(m, kSpanM), v = read_exponent(v, kSpanV);
   }
   __device__ __forceinline__ void store(uint8_t* me, uint8_t* ve, int count, int lane) const {
-    if (lane < count) me[lane] = static_cast<uint8_t>(m), ve[lane] = static_cast<uint8_t>(v);
+    if (lane < count) me[lane] = stored_exponent(m), ve[lane] = stored_exponent(v);
   }
   __device__ __forceinline__ uint32_t of_m(int k) const { return __shfl_sync(0xFFFFFFFFu, m, k); }
   __device__ __forceinline__ uint32_t of_v(int k) const { return __shfl_sync(0xFFFFFFFFu, v, k); }
@@ -195,7 +202,8 @@ __device__ __forceinline__ void store_any(T* block, int lane, int left, const T 
     if (j * 32 + lane < left) block[j * 32 + lane] = x[j];
 }
 template <bool Signed>
-__device__ __forceinline__ void load_codes_any(const uint8_t* block, uint32_t e, int lane, int left, float (&x)[kOptLane]) {
+__device__ __forceinline__ void load_codes_any(const uint8_t* block, uint32_t exponent, int lane, int left, float (&x)[kOptLane]) {
+  const uint32_t e = read_exponent(exponent, Signed ? kSpanM : kSpanV);
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j) {
     const uint32_t c = j * 32 + lane < left ? block[j * 32 + lane] : 0u;
@@ -224,7 +232,7 @@ __device__ __forceinline__ void store_codes_any(const float (&x)[kOptLane], bool
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j)
     if (j * 32 + lane < left) codes[j * 32 + lane] = static_cast<uint8_t>(c[j]);
-  if (lane == 0) *exponent = static_cast<uint8_t>(e);
+  if (lane == 0) *exponent = stored_exponent(e);
 }
 
 }  // namespace frk

@@ -3,7 +3,7 @@
 //
 // A lane squares the eight elements that it has of each block into two fp32
 // sums, which a float pair takes up error-free after the warp's blocks of a
-// unit: at most 64 squares are added in fp32 at a time.  A sum that is
+// segment: at most 64 squares are added in fp32 at a time.  A sum that is
 // not finite (a NaN or Inf, or an overflow) or so small that squares may have
 // lost bits to underflow is added again by the lanes concerned, element by
 // element in fp64, the non-finite ones counted and left out.  Warps, then CTAs,
@@ -22,7 +22,7 @@ namespace frk {
 
 namespace {
 
-static_assert(kClipUnit / kOptWarps * kOptLane / 2 <= 64, "squares in one fp32 sum");
+static_assert(kClipSegment / kOptWarps * kOptLane / 2 <= 64, "squares in one fp32 sum");
 
 template <bool Bf16>
 __device__ __forceinline__ float element(const void* p, uint64_t i) {
@@ -34,6 +34,14 @@ struct LaneSums {
   double exact = 0.0;          // of sums in fp64
   uint32_t nonfinite = 0;
 };
+
+// (hi, lo) += (h, l), error-free in hi (Knuth's TwoSum), to 2^-44 in all.
+__device__ __forceinline__ void add_to_pair(float& hi, float& lo, float h, float l) {
+  const float s = __fadd_rn(hi, h), back = __fsub_rn(s, hi);
+  const float e = __fadd_rn(__fadd_rn(__fsub_rn(hi, __fsub_rn(s, back)), __fsub_rn(h, back)), __fadd_rn(lo, l));
+  hi = __fadd_rn(s, e);
+  lo = __fsub_rn(e, __fsub_rn(hi, s));
+}
 
 // Granules of 16 bytes around a lane's eight elements.
 template <bool Bf16, bool Shifted>
@@ -84,7 +92,7 @@ __device__ __forceinline__ void add_words(const uint32_t (&w)[Bf16 ? 4 : 8], Pai
 // The warp's blocks [block, stop) of one tensor, every kOptWarps-th.
 template <bool Bf16, bool Shifted>
 __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_t block, uint32_t stop, int lane, LaneSums& s) {
-  constexpr int kAhead = Bf16 ? 8 : 4;  // blocks loaded at a time
+  constexpr int kAhead = (Bf16 ? 8 : 4) / (Shifted ? 2 : 1);  // blocks loaded at a time
   constexpr int kBytes = Bf16 ? 2 : 4;
   Pair sum = pair(0.0f);
   uint32_t any = 0;  // a bit set: some element is not +0
@@ -138,52 +146,59 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
     }
     return;
   }
-  // TwoSum of hi and each half
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const float x = half ? sum.y : sum.x;
-    const float r = __fadd_rn(s.hi, x), back = __fsub_rn(r, s.hi);
-    s.lo = __fadd_rn(s.lo, __fadd_rn(__fsub_rn(s.hi, __fsub_rn(r, back)), __fsub_rn(x, back)));
-    s.hi = r;
-  }
+  add_to_pair(s.hi, s.lo, sum.x, 0.0f);
+  add_to_pair(s.hi, s.lo, sum.y, 0.0f);
 }
 
-// Sums over a CTA, in thread 0, in an order that the thread count fixes.
-__device__ __forceinline__ ClipPartial cta_sum(double sum, uint64_t count, ClipPartial* warps) {
+// A warp's sum, in lane 0; the fp64 pipe is narrow, so as float pairs where no lane has a sum in fp64.
+__device__ __forceinline__ double warp_sum(const LaneSums& s) {
+  if (__any_sync(0xFFFFFFFFu, s.exact != 0.0)) {
+    double d = static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact;
+#pragma unroll
+    for (int k = 16; k > 0; k /= 2) d += __shfl_down_sync(0xFFFFFFFFu, d, k);
+    return d;
+  }
+  float hi = s.hi, lo = s.lo;
 #pragma unroll
   for (int k = 16; k > 0; k /= 2) {
-    sum += __shfl_down_sync(0xFFFFFFFFu, sum, k);
-    count += __shfl_down_sync(0xFFFFFFFFu, count, k);
+    const float h = __shfl_down_sync(0xFFFFFFFFu, hi, k), l = __shfl_down_sync(0xFFFFFFFFu, lo, k);
+    add_to_pair(hi, lo, h, l);
   }
-  if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = {sum, count};
-  __syncthreads();
-  ClipPartial all = {0.0, 0};
-  if (threadIdx.x == 0)
-    for (int k = 0; k < kOptWarps; ++k) {
-      all.sumsq += warps[k].sumsq;
-      all.nonfinite += warps[k].nonfinite;
-    }
-  return all;
+  return static_cast<double>(hi) + static_cast<double>(lo);
+}
+
+__device__ __forceinline__ uint64_t warp_count(uint64_t n) {
+#pragma unroll
+  for (int k = 16; k > 0; k /= 2) n += __shfl_down_sync(0xFFFFFFFFu, n, k);
+  return n;
+}
+
+// sqrt(x) to 2^-44: one step of Newton's from fp32's, of x over a power of four.
+__device__ __forceinline__ double square_root(double x) {
+  if (x == 0.0) return 0.0;
+  const int k = (ilogb(x) & ~1);
+  const double s = scalbn(x, -k), y = static_cast<double>(rsqrtf(static_cast<float>(s))), r = s * y;
+  return scalbn(r + 0.5 * y * fma(-r, r, s), k / 2);
 }
 
 __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kOptWarps];
-  __shared__ bool last;
-  uint32_t t = blockIdx.x < p.work.n_units ? p.work.start[blockIdx.x] : 0;  // (the plan's tables: nothing writes them)
-  asm volatile("prefetch.global.L1 [%0];" ::"l"(p.work.tensors + t));
+  uint32_t t = 0;
+  if (p.work.n_blocks) {  // (the plan's tables: nothing writes them)
+    t = p.work.start[blockIdx.x];
+    asm volatile("prefetch.global.L1 [%0];" ::"l"(p.work.tensors + t));
+  }
   wait_for_kernel_before();
   const int lane = threadIdx.x % 32;
-  LaneSums s;
   const uint32_t warp = threadIdx.x / 32;
-  for (uint32_t u = blockIdx.x; u < p.work.n_units; u += gridDim.x) {
-    const uint32_t end = min((u + 1) * p.work.unit_blocks, p.work.n_blocks);
-    uint32_t b = u * p.work.unit_blocks + warp;
-    if (u != blockIdx.x) t = p.work.start[u];
-    for (; b < end; ++t) {
+  LaneSums s;
+  for (uint32_t k = blockIdx.x; k < p.work.n_starts; k += gridDim.x) {
+    const uint32_t end = min((k + 1) * p.segment, p.work.n_blocks);
+    if (k != blockIdx.x) t = p.work.start[k];
+    for (uint32_t b = k * p.segment + warp; b < end;) {
+      t = tensor_of(p.work, t, b);
       const OptDesc& d = p.work.tensors[t];
-      const uint32_t stop = min(end, d.first + d.n_blocks);
-      if (b >= stop) continue;
-      const uint32_t from = b - d.first, to = stop - d.first;
+      const uint32_t from = b - d.first, to = min(end - d.first, d.n_blocks);
       const bool shifted = reinterpret_cast<uint64_t>(d.grad) % 16 != 0;
       if (d.bf16_grad)
         shifted ? add_blocks<true, true>(d.grad, d.n, from, to, lane, s) : add_blocks<true, false>(d.grad, d.n, from, to, lane, s);
@@ -192,28 +207,46 @@ __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_co
       b += (to - from + kOptWarps - 1) / kOptWarps * kOptWarps;
     }
   }
-  const ClipPartial mine = cta_sum(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact, s.nonfinite, warps);
-  if (threadIdx.x == 0) {
-    p.partials[blockIdx.x] = mine;
-    __threadfence();
-    last = atomicInc(p.done, gridDim.x - 1) == gridDim.x - 1;  // wraps to zero with the last
-    __threadfence();
-  }
+  const double sum_of_warp = warp_sum(s);
+  const uint32_t count_of_warp = __reduce_add_sync(0xFFFFFFFFu, s.nonfinite);  // (a warp has fewer than 2^32 elements)
+  if (lane == 0) warps[warp] = {sum_of_warp, count_of_warp};
   __syncthreads();
-  if (!last) return;
+  if (warp != 0) return;
+  ClipPartial mine = {0.0, 0};
+  if (lane < kOptWarps) mine = warps[lane];
+  static_assert(kOptWarps == 8, "three halvings");
+#pragma unroll
+  for (int k = kOptWarps / 2; k > 0; k /= 2) {
+    mine.sumsq += __shfl_down_sync(0xFFFFFFFFu, mine.sumsq, k);
+    mine.nonfinite += __shfl_down_sync(0xFFFFFFFFu, mine.nonfinite, k);
+  }
+  uint32_t before = 0;
+  if (lane == 0) {
+    p.partials[blockIdx.x] = mine;
+    // releases the partial sum, and acquires the others' for the last; wraps to zero with it
+    asm volatile("atom.inc.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(before) : "l"(p.done), "r"(gridDim.x - 1) : "memory");
+  }
+  if (__shfl_sync(0xFFFFFFFFu, before, 0) != gridDim.x - 1) return;
+  __syncwarp();
   double sum = 0.0;
   uint64_t count = 0;
-  for (uint32_t i = threadIdx.x; i < gridDim.x; i += 32 * kOptWarps) {
-    sum += __ldcg(&p.partials[i].sumsq);
-    count += __ldcg(&p.partials[i].nonfinite);
+  constexpr int kMost = (kClipCtas + 31) / 32;
+#pragma unroll
+  for (int k = 0; k < kMost; ++k) {
+    const uint32_t i = k * 32 + lane;
+    if (i < gridDim.x) {
+      sum += __ldcg(&p.partials[i].sumsq);
+      count += __ldcg(&p.partials[i].nonfinite);
+    }
   }
-  const ClipPartial all = cta_sum(sum, count, warps);
-  if (threadIdx.x == 0) {
-    const double norm = p.grad_scale * sqrt(all.sumsq);
+#pragma unroll
+  for (int k = 16; k > 0; k /= 2) sum += __shfl_down_sync(0xFFFFFFFFu, sum, k);
+  count = warp_count(count);
+  if (lane == 0) {
     fr_clip r;
-    r.norm = static_cast<float>(norm);
-    r.scale = all.nonfinite ? 0.0f : static_cast<float>(p.grad_scale * (norm > p.max_norm ? p.max_norm / norm : 1.0));
-    r.nonfinite = all.nonfinite;
+    r.norm = static_cast<float>(p.grad_scale * square_root(sum));
+    r.scale = count ? 0.0f : r.norm > p.max_norm ? __fmul_rn(static_cast<float>(p.grad_scale), __fdiv_rn(p.max_norm, r.norm)) : static_cast<float>(p.grad_scale);
+    r.nonfinite = count;
     *p.out = r;
   }
 }
@@ -221,7 +254,7 @@ __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_co
 }  // namespace
 
 cudaError_t launch_clip(const ClipParams& p, cudaStream_t s) {
-  const uint32_t n_ctas = p.work.n_units < 1 ? 1 : p.work.n_units < kClipCtas ? p.work.n_units : kClipCtas;
+  const uint32_t n_ctas = p.work.n_starts < 1 ? 1 : p.work.n_starts < kClipCtas ? p.work.n_starts : kClipCtas;
   return launch_chained(clip_kernel, static_cast<int>(n_ctas), 32 * kOptWarps, 0, s, p);
 }
 

@@ -20,7 +20,7 @@ struct Raw {
   __device__ __forceinline__ void load(const OptDesc& s, uint32_t block, int lane) {
     m.load(lane_at<ToEight ? 4 : 1>(s.m, block, lane));
     v.load(lane_at<ToEight ? 4 : 1>(s.v, block, lane));
-    if (!ToEight) em = s.m_exp[block], ev = s.v_exp[block];
+    if (!ToEight) em = read_exponent(s.m_exp[block], kSpanM), ev = read_exponent(s.v_exp[block], kSpanV);
   }
 };
 
@@ -34,10 +34,10 @@ __device__ __forceinline__ void convert_whole(const Raw<ToEight>& r, const OptDe
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = make_float2(not_negative(v[j].x), not_negative(v[j].y));
     uint32_t u[4];
-    if (Random) random_pairs(key, first, lane, u);
+    if (Random) random_pairs(key, random_counter(key, (first >> 1) + 4 * lane), u);
     const uint32_t em = store_codes<true, Random>(m, u, lane_at<1>(d.m, block, lane));
     const uint32_t ev = store_codes<false, Random>(v, u, lane_at<1>(d.v, block, lane));
-    if (lane == 0) d.m_exp[block] = static_cast<uint8_t>(em), d.v_exp[block] = static_cast<uint8_t>(ev);
+    if (lane == 0) d.m_exp[block] = stored_exponent(em), d.v_exp[block] = stored_exponent(ev);
   } else {
     decode4<true>(r.m.a.x, r.em, m[0], m[1]);
     decode4<true>(r.m.a.y, r.em, m[2], m[3]);
@@ -77,7 +77,7 @@ __device__ __noinline__ void convert_any(const OptDesc* from, const OptDesc* to,
 
 template <bool ToEight, bool Random>
 __global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_constant__ ConvertParams p) {
-  constexpr int kBlocks = convert_blocks(ToEight);
+  constexpr int kBlocks = kConvertBlocks;
   const int lane = threadIdx.x % 32;
   uint32_t b = blockIdx.x * (kBlocks * kOptWarps) + threadIdx.x / 32;
   if (b >= p.src.n_blocks) return;
@@ -115,10 +115,10 @@ __global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_co
 }  // namespace
 
 cudaError_t launch_convert(const ConvertParams& p, cudaStream_t s) {
-  const int n_ctas = static_cast<int>(p.src.n_units);
-  if (!p.to_eight) return launch_chained(convert_kernel<false, false>, n_ctas, 32 * kOptWarps, 0, s, p);
-  if (p.random) return launch_chained(convert_kernel<true, true>, n_ctas, 32 * kOptWarps, 0, s, p);
-  return launch_chained(convert_kernel<true, false>, n_ctas, 32 * kOptWarps, 0, s, p);
+  const int n_starts = static_cast<int>(p.src.n_starts);
+  if (!p.to_eight) return launch_chained(convert_kernel<false, false>, n_starts, 32 * kOptWarps, 0, s, p);
+  if (p.random) return launch_chained(convert_kernel<true, true>, n_starts, 32 * kOptWarps, 0, s, p);
+  return launch_chained(convert_kernel<true, false>, n_starts, 32 * kOptWarps, 0, s, p);
 }
 
 }  // namespace frk

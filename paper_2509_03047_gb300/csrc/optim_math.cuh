@@ -17,29 +17,27 @@ namespace frk {
 
 constexpr int kSpanM = 15, kSpanV = 31;  // binades below a block's top
 
-// A block's exponent from the largest bit pattern of |x| in it.  The largest
-// code is reached whichever way its element is rounded: 0xFFFFF is the most
-// that a rounding adds.
-__device__ __forceinline__ uint32_t block_exponent(uint32_t top, int span) {
-  const uint32_t e = (min(top, 0x7F800000u) + 0xFFFFFu) >> 23;
-  return max(e, static_cast<uint32_t>(span + 1));
-}
-__device__ __forceinline__ int code_base(uint32_t e, int span) {
-  return static_cast<int>(max(e, static_cast<uint32_t>(span + 1)) - span) << 3;
-}
+// A block's exponent from the largest bit pattern of |x| in it (256 for some
+// NaNs, stored as 255).  The largest code is reached whichever way its element
+// is rounded: 0xFFFFF is the most that a rounding adds.
+__device__ __forceinline__ uint32_t block_exponent(uint32_t top, int span) { return max((top + 0xFFFFFu) >> 23, static_cast<uint32_t>(span + 1)); }
+__device__ __forceinline__ uint8_t stored_exponent(uint32_t e) { return static_cast<uint8_t>(min(e, 255u)); }
+// An exponent byte as it is read: written by somebody else it may be below its floor.
+__device__ __forceinline__ uint32_t read_exponent(uint32_t e, int span) { return max(e, static_cast<uint32_t>(span + 1)); }
+__device__ __forceinline__ uint32_t code_base(uint32_t e, int span) { return (e - span) * 8; }
 
 __device__ __forceinline__ uint32_t round_nearest(uint32_t bits) { return 0x7FFFFu + ((bits >> 20) & 1u); }
 
 // r: what the rounding adds below bit 20.
 __device__ __forceinline__ uint32_t encode_m(float x, uint32_t r, uint32_t e) {
   const uint32_t bits = __float_as_uint(x);
-  const int c = static_cast<int>(((bits & 0x7FFFFFFFu) + r) >> 20) - code_base(e, kSpanM);
-  return c < 1 || e == 255 ? 0u : static_cast<uint32_t>(c) | ((bits >> 24) & 0x80u);
+  const int c = static_cast<int>(((bits & 0x7FFFFFFFu) + r) >> 20) - static_cast<int>(code_base(e, kSpanM));
+  return c < 1 || e >= 255 ? 0u : static_cast<uint32_t>(c) | ((bits >> 24) & 0x80u);
 }
 __device__ __forceinline__ uint32_t encode_v(float x, uint32_t r, uint32_t e) {
   const uint32_t bits = __float_as_uint(x) & 0x7FFFFFFFu;
-  const int c = static_cast<int>((bits + r) >> 20) - code_base(e, kSpanV);
-  return bits == 0 || e == 255 ? 0u : static_cast<uint32_t>(max(c, 1));
+  const int c = static_cast<int>((bits + r) >> 20) - static_cast<int>(code_base(e, kSpanV));
+  return bits == 0 || e >= 255 ? 0u : static_cast<uint32_t>(max(c, 1));
 }
 __device__ __forceinline__ float decode_m(uint32_t code, uint32_t e) {
   const uint32_t c = code & 0x7Fu;
@@ -65,12 +63,16 @@ __device__ __forceinline__ RandomKey random_key(uint64_t key, uint32_t tensor) {
   const uint64_t k = mix64(key + tensor * 0x9E3779B97F4A7C15ull);
   return {static_cast<uint32_t>(k), static_cast<uint32_t>(k >> 32)};
 }
-__device__ __forceinline__ uint32_t random_pair(RandomKey k, uint64_t pair) {
-  uint32_t u = static_cast<uint32_t>(pair) * 0x9E3779B1u + (k.lo ^ (static_cast<uint32_t>(pair >> 32) * 0x85EBCA77u));
+constexpr uint32_t kRandomStep = 0x9E3779B1u;  // from a pair's counter to the next one's
+__device__ __forceinline__ uint32_t random_counter(RandomKey k, uint64_t pair) {
+  return static_cast<uint32_t>(pair) * kRandomStep + (k.lo ^ (static_cast<uint32_t>(pair >> 32) * 0x85EBCA77u));
+}
+__device__ __forceinline__ uint32_t random_mix(RandomKey k, uint32_t u) {
   u ^= u >> 16;
   u = u * 2891336453u + k.hi;
   return u ^ (u >> 15);
 }
+__device__ __forceinline__ uint32_t random_pair(RandomKey k, uint64_t pair) { return random_mix(k, random_counter(k, pair)); }
 // 32 bits of the pair's first or second element: the high half rounds v, the low half m.
 __device__ __forceinline__ uint32_t random_moments(uint32_t u, int odd) { return u * (odd ? 741103597u : 1597334677u); }
 // The pair's weights: 16 bits each, the high half for the first.

@@ -67,9 +67,9 @@ struct Step {
       p.load(at.p + ahead * (kOptBlock * RawParam::kBytes));
     }
   };
-  // The rest of it; first: its first element's index, em and ev: its exponents, old and new.
-  static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, uint64_t first, RandomKey key, int lane, const Raw& r,
-                                                uint32_t& em, uint32_t& ev) {
+  // The rest of it; em and ev: its exponents, old and new.
+  static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, uint32_t counter, RandomKey key, const Raw& r, uint32_t& em,
+                                                uint32_t& ev) {
     Pair g[4], p[4], m[4], v[4];
     if constexpr (Eight) {
       decode4<true>(r.m.a.x, em, m[0], m[1]);
@@ -96,7 +96,7 @@ struct Step {
       p[j] = update_param(h, p[j], m[j], v[j]);
     }
     uint32_t u[4];
-    if (Random) random_pairs(key, first, lane, u);
+    if (Random) random_pairs(key, counter, u);
     if (Weight == kWeightBf16) {
       uint32_t w[4];
 #pragma unroll
@@ -124,12 +124,13 @@ struct Step {
   // the code must stay in the instruction cache.
   static __device__ __forceinline__ void whole(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
     Places at(d, block, lane);
-    uint64_t first = static_cast<uint64_t>(block) * kOptBlock + d.skipped;
+    // (a run does not pass a multiple of 2^32 pairs: see run_length)
+    uint32_t counter = random_counter(key, (static_cast<uint64_t>(block) * kOptBlock + d.skipped) / 2 + 4 * lane);
     Raw r;
     r.load(at, 0);
     uint32_t em = 0, ev = 0;
     if (!Eight) {
-      finish(h, at, first, key, lane, r, em, ev);
+      finish(h, at, counter, key, r, em, ev);
       return;
     }
     Exponents e;
@@ -139,11 +140,11 @@ struct Step {
       Raw next;
       if (k + 1 < count) next.load(at, 1);
       em = e.of_m(k), ev = e.of_v(k);
-      finish(h, at, first, key, lane, r, em, ev);
+      finish(h, at, counter, key, r, em, ev);
       e.set(k, lane, em, ev);
       if (++k == count) break;
       r = next;
-      first += kOptBlock;
+      counter += kOptBlock / 2 * kRandomStep;
       at.next();
     }
     e.store(d.m_exp + block, d.v_exp + block, count, lane);
@@ -207,10 +208,16 @@ struct Step {
   }
 };
 
+// Blocks from `block` on whose pairs' indices have the same high word.
+__device__ __forceinline__ uint32_t run_length(uint32_t block) {
+  constexpr uint32_t kBlocks = (1ull << 33) / kOptBlock;
+  return kBlocks - block % kBlocks;
+}
+
 template <int Weight, bool Bf16Grad, bool Eight, bool Random>
-__global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight)) step_kernel(const __grid_constant__ StepParams p) {
+__global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16Grad)) step_kernel(const __grid_constant__ StepParams p) {
   using S = Step<Weight, Bf16Grad, Eight, Random>;
-  const uint32_t per_warp = Eight ? p.work.unit_blocks / kOptWarps : 1;
+  const uint32_t per_warp = Eight ? p.per_warp : 1;
   const int lane = threadIdx.x % 32;
   uint32_t b = (blockIdx.x * kOptWarps + threadIdx.x / 32) * per_warp;
   const uint32_t end = min(b + per_warp, p.work.n_blocks);
@@ -229,7 +236,7 @@ __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight)) step_kernel(
     if (block < whole) {
       RandomKey key = {0, 0};
       if (Random) key = random_key(p.key, d.tensor);
-      const uint32_t count = Eight ? min(end - b, whole - block) : 1;
+      const uint32_t count = Eight ? min(min(end - b, whole - block), run_length(block)) : 1;
       S::whole(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
       b += count;
     } else {
@@ -263,7 +270,7 @@ auto for_class(const StepClass& c, bool random, F&& f) {
 }  // namespace
 
 cudaError_t launch_step(const StepClass& c, const StepParams& p, cudaStream_t s) {
-  return for_class(c, p.random != 0, [&](auto kernel) { return launch_chained(kernel, p.work.n_units, 32 * kOptWarps, 0, s, p); });
+  return for_class(c, p.random != 0, [&](auto kernel) { return launch_chained(kernel, static_cast<int>(p.work.n_starts), 32 * kOptWarps, 0, s, p); });
 }
 
 }  // namespace frk
