@@ -43,27 +43,30 @@ static_assert(sizeof(OptDesc) == 96, "OptDesc layout");
 struct OptWork {
   const OptDesc* tensors;
   const uint32_t* start;
-  uint32_t n_blocks, n_starts;
+  uint32_t n_tensors, n_blocks, n_starts;
 };
 
-constexpr int kOptWarps = 8;  // per CTA, in every kernel here
+constexpr int kOptWarps = 8;  // per CTA of the step and the conversion
 constexpr uint32_t kSms = 152;  // of a GB300
 
 // ---- the norm
 
 // A launch's sums are added in an order that segments and CTAs decide, so both
-// follow from the sizes alone, not from the GPU: at most 4 CTAs per SM, about
-// four segments for each, of 2 to 16 blocks per warp.  CTA c of g takes the
-// segments c, c + g, ..., its warps a segment's blocks in turn.  (One range of
-// blocks per CTA: an 8B rank's 2 GB 287 us, so 276.)
-constexpr uint32_t kClipSegment = 16 * kOptWarps;
-constexpr uint32_t kClipCtas = 4 * kSms;
+// follow from the sizes alone, not from the GPU: segments of 1 to 16 blocks per
+// warp, one CTA per SM at most; CTA c of g takes the segments c, c + g, ..., its
+// warps a segment's blocks in turn.  (One CTA of 32 warps, not four of 8: each
+// that ends costs the last one's count; the norm of 1 million elements 4.6 us,
+// 8.6 with four.  One range of blocks per CTA: an 8B rank's 2 GB 287 us, so 276.)
+constexpr int kClipWarps = 32;
+constexpr uint32_t kClipCtas = kSms;
+constexpr uint32_t kClipMost = 16;  // blocks per warp
 inline uint32_t clip_segment(uint64_t n_blocks) {
-  const uint64_t per_warp = n_blocks / (4 * kClipCtas * kOptWarps);
-  return static_cast<uint32_t>(per_warp < 2 ? 2 : per_warp < 16 ? per_warp : 16) * kOptWarps;
+  const uint64_t per_warp = (n_blocks + kClipCtas * kClipWarps - 1) / (kClipCtas * kClipWarps);
+  return static_cast<uint32_t>(per_warp < 1 ? 1 : per_warp < kClipMost ? per_warp : kClipMost) * kClipWarps;
 }
-struct ClipPartial {  // of one CTA
-  double sumsq;
+struct ClipPartial {  // a sum of squares, of a lane, a warp or a CTA: hi + lo + exact
+  float hi, lo;       // of what was added in fp32
+  double exact;       // of what was added in fp64
   uint64_t nonfinite;
 };
 struct ClipParams {
@@ -71,8 +74,7 @@ struct ClipParams {
   uint32_t segment;        // blocks
   ClipPartial* partials;  // one per CTA
   uint32_t* done;  // CTAs that have written theirs; zero before a launch and after it
-  double grad_scale;
-  float max_norm;
+  float grad_scale, max_norm;
   fr_clip* out;
 };
 cudaError_t launch_clip(const ClipParams& p, cudaStream_t s);

@@ -22,7 +22,7 @@ struct WorkList {
   std::vector<OptDesc> tensors;
   std::vector<uint32_t> start;
   uint64_t n_blocks = 0;
-  uint32_t n_starts = 0;
+  uint32_t n_tensors = 0, n_starts = 0;
   OptDesc* d_tensors = nullptr;
   uint32_t* d_start = nullptr;
 
@@ -30,6 +30,7 @@ struct WorkList {
     d.first = static_cast<uint32_t>(n_blocks);
     n_blocks += d.n_blocks;
     tensors.push_back(d);
+    ++n_tensors;
   }
   // For CTAs whose first blocks are first(0) <= first(1) <= ...
   template <class F>
@@ -49,7 +50,7 @@ struct WorkList {
     mem.table(&d_tensors, tensors);
     mem.table(&d_start, start);
   }
-  OptWork work() const { return {d_tensors, d_start, static_cast<uint32_t>(n_blocks), n_starts}; }
+  OptWork work() const { return {d_tensors, d_start, n_tensors, static_cast<uint32_t>(n_blocks), n_starts}; }
 };
 
 }  // namespace

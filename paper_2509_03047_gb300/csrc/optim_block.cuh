@@ -12,10 +12,17 @@
 
 namespace frk {
 
-// The tensor of block b of a launch, from one that is not after it.
+// The tensor of block b of a launch (b the same in the whole warp), from one, t,
+// that is not after it.  The lanes look at 32 tensors at a time: of many small
+// ones, one after the other cost 0.3 us each.
 __device__ __forceinline__ uint32_t tensor_of(const OptWork& w, uint32_t t, uint32_t b) {
-  while (b - w.tensors[t].first >= w.tensors[t].n_blocks) ++t;
-  return t;
+  if (b - w.tensors[t].first < w.tensors[t].n_blocks) return t;
+  const uint32_t lane = threadIdx.x % 32;
+  for (++t;; t += 32) {
+    const bool after = t + lane >= w.n_tensors || w.tensors[t + lane].first > b;
+    const uint32_t m = __ballot_sync(0xFFFFFFFFu, after);
+    if (m) return t + __ffs(m) - 2;  // the one before the first that starts after b
+  }
 }
 
 // ---- vectors

@@ -13,8 +13,6 @@
 // Which lane has which element does not depend on the address (the order of the
 // sums must not): off the 16-byte boundary a lane loads the granules around its
 // elements and shifts them out.
-#include <cmath>
-
 #include "kernels.h"
 #include "optim_block.cuh"
 
@@ -22,18 +20,12 @@ namespace frk {
 
 namespace {
 
-static_assert(kClipSegment / kOptWarps * kOptLane / 2 <= 64, "squares in one fp32 sum");
+static_assert(kClipMost * kOptLane / 2 <= 64, "squares in one fp32 sum");
 
 template <bool Bf16>
 __device__ __forceinline__ float element(const void* p, uint64_t i) {
   return Bf16 ? __uint_as_float(static_cast<uint32_t>(static_cast<const uint16_t*>(p)[i]) << 16) : static_cast<const float*>(p)[i];
 }
-
-struct LaneSums {
-  float hi = 0.0f, lo = 0.0f;  // of sums in fp32
-  double exact = 0.0;          // of sums in fp64
-  uint32_t nonfinite = 0;
-};
 
 // (hi, lo) += (h, l), error-free in hi (Knuth's TwoSum), to 2^-44 in all.
 __device__ __forceinline__ void add_to_pair(float& hi, float& lo, float h, float l) {
@@ -89,9 +81,9 @@ __device__ __forceinline__ void add_words(const uint32_t (&w)[Bf16 ? 4 : 8], Pai
   }
 }
 
-// The warp's blocks [block, stop) of one tensor, every kOptWarps-th.
+// The warp's blocks [block, stop) of one tensor, every kClipWarps-th.
 template <bool Bf16, bool Shifted>
-__device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_t block, uint32_t stop, int lane, LaneSums& s) {
+__device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_t block, uint32_t stop, int lane, ClipPartial& s) {
   constexpr int kAhead = (Bf16 ? 8 : 4) / (Shifted ? 2 : 1);  // blocks loaded at a time
   constexpr int kBytes = Bf16 ? 2 : 4;
   Pair sum = pair(0.0f);
@@ -100,10 +92,10 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
   const uint64_t base = reinterpret_cast<uint64_t>(grad) - shift + lane * kOptLane * kBytes;
   const uint32_t whole = static_cast<uint32_t>(min(n / kOptBlock, static_cast<uint64_t>(stop)));
   uint32_t b = block;
-  for (; b + (kAhead - 1) * kOptWarps < whole; b += kAhead * kOptWarps) {
+  for (; b + (kAhead - 1) * kClipWarps < whole; b += kAhead * kClipWarps) {
     Granules<Bf16, Shifted> r[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) r[k].load(base + static_cast<uint64_t>(b + k * kOptWarps) * kOptBlock * kBytes);
+    for (int k = 0; k < kAhead; ++k) r[k].load(base + static_cast<uint64_t>(b + k * kClipWarps) * kOptBlock * kBytes);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       uint32_t w[Bf16 ? 4 : 8];
@@ -111,7 +103,7 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
       add_words<Bf16>(w, sum, any);
     }
   }
-  for (; b < stop; b += kOptWarps) {
+  for (; b < stop; b += kClipWarps) {
     const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
     if (b < whole) {
       Granules<Bf16, Shifted> r;
@@ -131,10 +123,10 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
     }
   }
   const float t = __fadd_rn(sum.x, sum.y);
-  // A square below 2^-126 is off by 2^-150 at most: nothing beside 2^-90.  (Of
-  // sums below 2^96 the pair does not overflow: a lane has fewer than 2^31.)
-  if (!(t < 0x1p96f) || (t < 0x1p-90f && any != 0)) {
-    for (b = block; b < stop; b += kOptWarps) {
+  // A square below 2^-126 is off by 2^-150 at most: nothing beside 2^-90.  (Sums
+  // below 2^80 do not overflow the pairs: a plan has fewer than 2^40 elements.)
+  if (!(t < 0x1p80f) || (t < 0x1p-90f && any != 0)) {
+    for (b = block; b < stop; b += kClipWarps) {
       const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
       for (int j = 0; j < kOptLane && at + j < n; ++j) {
         const float x = element<Bf16>(grad, at + j);
@@ -150,103 +142,106 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
   add_to_pair(s.hi, s.lo, sum.y, 0.0f);
 }
 
-// A warp's sum, in lane 0; the fp64 pipe is narrow, so as float pairs where no lane has a sum in fp64.
-__device__ __forceinline__ double warp_sum(const LaneSums& s) {
-  if (__any_sync(0xFFFFFFFFu, s.exact != 0.0)) {
-    double d = static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact;
-#pragma unroll
-    for (int k = 16; k > 0; k /= 2) d += __shfl_down_sync(0xFFFFFFFFu, d, k);
-    return d;
-  }
-  float hi = s.hi, lo = s.lo;
+// The sum over a warp, in lane 0.  The fp64 pipe is narrow (a conversion and an
+// addition in each of an SM's warps take 0.7 us): it is left out where no lane
+// has a sum in fp64.
+__device__ __forceinline__ void warp_sum(ClipPartial& s) {
 #pragma unroll
   for (int k = 16; k > 0; k /= 2) {
-    const float h = __shfl_down_sync(0xFFFFFFFFu, hi, k), l = __shfl_down_sync(0xFFFFFFFFu, lo, k);
-    add_to_pair(hi, lo, h, l);
+    const float h = __shfl_down_sync(0xFFFFFFFFu, s.hi, k), l = __shfl_down_sync(0xFFFFFFFFu, s.lo, k);
+    add_to_pair(s.hi, s.lo, h, l);
   }
-  return static_cast<double>(hi) + static_cast<double>(lo);
-}
-
-__device__ __forceinline__ uint64_t warp_count(uint64_t n) {
+  if (!__any_sync(0xFFFFFFFFu, s.exact != 0.0 || s.nonfinite != 0)) return;
 #pragma unroll
-  for (int k = 16; k > 0; k /= 2) n += __shfl_down_sync(0xFFFFFFFFu, n, k);
-  return n;
-}
-
-// sqrt(x) to 2^-44: one step of Newton's from fp32's, of x over a power of four.
-__device__ __forceinline__ double square_root(double x) {
-  if (x == 0.0) return 0.0;
-  const int k = (ilogb(x) & ~1);
-  const double s = scalbn(x, -k), y = static_cast<double>(rsqrtf(static_cast<float>(s))), r = s * y;
-  return scalbn(r + 0.5 * y * fma(-r, r, s), k / 2);
-}
-
-__global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_constant__ ClipParams p) {
-  __shared__ ClipPartial warps[kOptWarps];
-  uint32_t t = 0;
-  if (p.work.n_blocks) {  // (the plan's tables: nothing writes them)
-    t = p.work.start[blockIdx.x];
-    asm volatile("prefetch.global.L1 [%0];" ::"l"(p.work.tensors + t));
+  for (int k = 16; k > 0; k /= 2) {
+    s.exact += __shfl_down_sync(0xFFFFFFFFu, s.exact, k);
+    s.nonfinite += __shfl_down_sync(0xFFFFFFFFu, s.nonfinite, k);
   }
-  wait_for_kernel_before();
+}
+
+// The square root of a sum, in fp32 as long as the sum is: a step of Newton's
+// from an approximation, its residual exact (0.6 us less than in fp64).
+__device__ __forceinline__ float root(const ClipPartial& s) {
+  if (s.exact != 0.0) return static_cast<float>(sqrt(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact));
+  if (s.hi == 0.0f) return 0.0f;
+  const float y = rsqrtf(s.hi), r = __fmul_rn(s.hi, y), rr = __fmul_rn(r, r);
+  const float e = __fadd_rn(__fsub_rn(__fsub_rn(s.hi, rr), __fmaf_rn(r, r, -rr)), s.lo);
+  return __fmaf_rn(__fmul_rn(0.5f, y), e, r);
+}
+
+// What the norm needs of a tensor.
+struct Tensor {
+  const void* grad;
+  uint64_t n;
+  uint32_t first, n_blocks, bf16;
+};
+__device__ __forceinline__ Tensor tensor(const ClipParams& p, uint32_t t) {
+  const OptDesc& d = p.work.tensors[t];
+  return {d.grad, d.n, d.first, d.n_blocks, d.bf16_grad};
+}
+
+__global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(const __grid_constant__ ClipParams p) {
+  __shared__ ClipPartial warps[kClipWarps];
   const int lane = threadIdx.x % 32;
   const uint32_t warp = threadIdx.x / 32;
-  LaneSums s;
+  uint32_t t = 0;
+  Tensor d = {};
+  if (p.work.n_blocks) d = tensor(p, t = p.work.start[blockIdx.x]);  // (the plan's tables: nothing writes them)
+  wait_for_kernel_before();
+  ClipPartial s = {0.0f, 0.0f, 0.0, 0};
   for (uint32_t k = blockIdx.x; k < p.work.n_starts; k += gridDim.x) {
     const uint32_t end = min((k + 1) * p.segment, p.work.n_blocks);
-    if (k != blockIdx.x) t = p.work.start[k];
+    if (k != blockIdx.x && p.work.start[k] != t) d = tensor(p, t = p.work.start[k]);
     for (uint32_t b = k * p.segment + warp; b < end;) {
-      t = tensor_of(p.work, t, b);
-      const OptDesc& d = p.work.tensors[t];
+      if (b - d.first >= d.n_blocks) d = tensor(p, t = tensor_of(p.work, t, b));
       const uint32_t from = b - d.first, to = min(end - d.first, d.n_blocks);
       const bool shifted = reinterpret_cast<uint64_t>(d.grad) % 16 != 0;
-      if (d.bf16_grad)
+      if (d.bf16)
         shifted ? add_blocks<true, true>(d.grad, d.n, from, to, lane, s) : add_blocks<true, false>(d.grad, d.n, from, to, lane, s);
       else
         shifted ? add_blocks<false, true>(d.grad, d.n, from, to, lane, s) : add_blocks<false, false>(d.grad, d.n, from, to, lane, s);
-      b += (to - from + kOptWarps - 1) / kOptWarps * kOptWarps;
+      b += (to - from + kClipWarps - 1) / kClipWarps * kClipWarps;
     }
   }
-  const double sum_of_warp = warp_sum(s);
-  const uint32_t count_of_warp = __reduce_add_sync(0xFFFFFFFFu, s.nonfinite);  // (a warp has fewer than 2^32 elements)
-  if (lane == 0) warps[warp] = {sum_of_warp, count_of_warp};
+  warp_sum(s);
+  if (lane == 0) warps[warp] = s;
   __syncthreads();
   if (warp != 0) return;
-  ClipPartial mine = {0.0, 0};
-  if (lane < kOptWarps) mine = warps[lane];
-  static_assert(kOptWarps == 8, "three halvings");
-#pragma unroll
-  for (int k = kOptWarps / 2; k > 0; k /= 2) {
-    mine.sumsq += __shfl_down_sync(0xFFFFFFFFu, mine.sumsq, k);
-    mine.nonfinite += __shfl_down_sync(0xFFFFFFFFu, mine.nonfinite, k);
-  }
+  if (lane < kClipWarps) s = warps[lane];
+  else s = {0.0f, 0.0f, 0.0, 0};
+  warp_sum(s);
   uint32_t before = 0;
   if (lane == 0) {
-    p.partials[blockIdx.x] = mine;
+    p.partials[blockIdx.x] = s;
     // releases the partial sum, and acquires the others' for the last; wraps to zero with it
     asm volatile("atom.inc.acq_rel.gpu.global.u32 %0, [%1], %2;" : "=r"(before) : "l"(p.done), "r"(gridDim.x - 1) : "memory");
   }
   if (__shfl_sync(0xFFFFFFFFu, before, 0) != gridDim.x - 1) return;
   __syncwarp();
-  double sum = 0.0;
-  uint64_t count = 0;
-  constexpr int kMost = (kClipCtas + 31) / 32;
+  s = {0.0f, 0.0f, 0.0, 0};
+  constexpr int kEach = (kClipCtas + 31) / 32;
+  ClipPartial q[kEach];
 #pragma unroll
-  for (int k = 0; k < kMost; ++k) {
+  for (int k = 0; k < kEach; ++k) {
     const uint32_t i = k * 32 + lane;
+    q[k] = {0.0f, 0.0f, 0.0, 0};
     if (i < gridDim.x) {
-      sum += __ldcg(&p.partials[i].sumsq);
-      count += __ldcg(&p.partials[i].nonfinite);
+      const ClipPartial* at = p.partials + i;
+      q[k] = {__ldcg(&at->hi), __ldcg(&at->lo), __ldcg(&at->exact), __ldcg(&at->nonfinite)};
     }
   }
 #pragma unroll
-  for (int k = 16; k > 0; k /= 2) sum += __shfl_down_sync(0xFFFFFFFFu, sum, k);
-  count = warp_count(count);
+  for (int k = 0; k < kEach; ++k) {
+    add_to_pair(s.hi, s.lo, q[k].hi, q[k].lo);
+    if (q[k].exact != 0.0) s.exact += q[k].exact;
+    s.nonfinite += q[k].nonfinite;
+  }
+  warp_sum(s);
   if (lane == 0) {
     fr_clip r;
-    r.norm = static_cast<float>(p.grad_scale * square_root(sum));
-    r.scale = count ? 0.0f : r.norm > p.max_norm ? __fmul_rn(static_cast<float>(p.grad_scale), __fdiv_rn(p.max_norm, r.norm)) : static_cast<float>(p.grad_scale);
-    r.nonfinite = count;
+    r.norm = __fmul_rn(p.grad_scale, root(s));
+    r.scale = s.nonfinite ? 0.0f : r.norm > p.max_norm ? __fmul_rn(p.grad_scale, __fdiv_rn(p.max_norm, r.norm)) : p.grad_scale;
+    r.nonfinite = s.nonfinite;
     *p.out = r;
   }
 }
@@ -255,7 +250,7 @@ __global__ void __launch_bounds__(32 * kOptWarps, 4) clip_kernel(const __grid_co
 
 cudaError_t launch_clip(const ClipParams& p, cudaStream_t s) {
   const uint32_t n_ctas = p.work.n_starts < 1 ? 1 : p.work.n_starts < kClipCtas ? p.work.n_starts : kClipCtas;
-  return launch_chained(clip_kernel, static_cast<int>(n_ctas), 32 * kOptWarps, 0, s, p);
+  return launch_chained(clip_kernel, static_cast<int>(n_ctas), 32 * kClipWarps, 0, s, p);
 }
 
 }  // namespace frk
