@@ -60,9 +60,10 @@ constexpr uint32_t kSms = 152;  // of a GB300
 constexpr int kClipWarps = 32;
 constexpr uint32_t kClipCtas = kSms;
 constexpr uint32_t kClipMost = 16;  // blocks per warp
-inline uint32_t clip_segment(uint64_t n_blocks) {
-  const uint64_t per_warp = (n_blocks + kClipCtas * kClipWarps - 1) / (kClipCtas * kClipWarps);
-  return static_cast<uint32_t>(per_warp < 1 ? 1 : per_warp < kClipMost ? per_warp : kClipMost) * kClipWarps;
+inline uint32_t clip_segment(uint64_t n_blocks) {  // so that every CTA has the same number
+  constexpr uint64_t kRound = static_cast<uint64_t>(kClipCtas) * kClipWarps;
+  const uint64_t rounds = (n_blocks + kRound * kClipMost - 1) / (kRound * kClipMost);
+  return rounds ? static_cast<uint32_t>((n_blocks + kRound * rounds - 1) / (kRound * rounds)) * kClipWarps : kClipWarps;
 }
 struct ClipPartial {  // a sum of squares, of a lane, a warp or a CTA: hi + lo + exact
   float hi, lo;       // of what was added in fp32

@@ -45,6 +45,10 @@ struct Granules {
 #pragma unroll
     for (int k = 0; k < kLoaded; ++k) g[k] = load_16(reinterpret_cast<const uint4*>(at) + k);
   }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int k = 0; k < kLoaded; ++k) g[k] = make_uint4(0, 0, 0, 0);
+  }
   // shift: bytes from there to the first element
   __device__ __forceinline__ void words(uint32_t shift, uint32_t (&w)[kWords]) const {
     uint32_t a[4 * kLoaded];
@@ -81,7 +85,7 @@ __device__ __forceinline__ void add_words(const uint32_t (&w)[Bf16 ? 4 : 8], Pai
   }
 }
 
-// The warp's blocks [block, stop) of one tensor, every kClipWarps-th.
+// The warp's blocks [block, stop) of one tensor.
 template <bool Bf16, bool Shifted>
 __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_t block, uint32_t stop, int lane, ClipPartial& s) {
   constexpr int kAhead = (Bf16 ? 8 : 4) / (Shifted ? 2 : 1);  // blocks loaded at a time
@@ -92,10 +96,15 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
   const uint64_t base = reinterpret_cast<uint64_t>(grad) - shift + lane * kOptLane * kBytes;
   const uint32_t whole = static_cast<uint32_t>(min(n / kOptBlock, static_cast<uint64_t>(stop)));
   uint32_t b = block;
-  for (; b + (kAhead - 1) * kClipWarps < whole; b += kAhead * kClipWarps) {
+  for (; b < whole; b += kAhead) {
     Granules<Bf16, Shifted> r[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) r[k].load(base + static_cast<uint64_t>(b + k * kClipWarps) * kOptBlock * kBytes);
+    for (int k = 0; k < kAhead; ++k) {
+      if (b + k < whole)
+        r[k].load(base + static_cast<uint64_t>(b + k) * kOptBlock * kBytes);
+      else
+        r[k].clear();
+    }
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       uint32_t w[Bf16 ? 4 : 8];
@@ -103,30 +112,24 @@ __device__ __forceinline__ void add_blocks(const void* grad, uint64_t n, uint32_
       add_words<Bf16>(w, sum, any);
     }
   }
-  for (; b < stop; b += kClipWarps) {
-    const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
-    if (b < whole) {
-      Granules<Bf16, Shifted> r;
-      uint32_t w[Bf16 ? 4 : 8];
-      r.load(base + static_cast<uint64_t>(b) * kOptBlock * kBytes);
-      r.words(shift, w);
-      add_words<Bf16>(w, sum, any);
-    } else {
+  // the tensor's last block, where it is not whole and this warp's
+  const uint32_t last = static_cast<uint32_t>(n / kOptBlock);
+  if (last < stop && n % kOptBlock && last >= block) {
+    const uint64_t at = static_cast<uint64_t>(last) * kOptBlock + lane * kOptLane;
 #pragma unroll
-      for (int j = 0; j < kOptLane; j += 2) {
-        Pair x;
-        x.x = at + j < n ? element<Bf16>(grad, at + j) : 0.0f;
-        x.y = at + j + 1 < n ? element<Bf16>(grad, at + j + 1) : 0.0f;
-        sum = fma2(x, x, sum);
-        any |= __float_as_uint(x.x) | __float_as_uint(x.y);
-      }
+    for (int j = 0; j < kOptLane; j += 2) {
+      Pair x;
+      x.x = at + j < n ? element<Bf16>(grad, at + j) : 0.0f;
+      x.y = at + j + 1 < n ? element<Bf16>(grad, at + j + 1) : 0.0f;
+      sum = fma2(x, x, sum);
+      any |= __float_as_uint(x.x) | __float_as_uint(x.y);
     }
   }
   const float t = __fadd_rn(sum.x, sum.y);
   // A square below 2^-126 is off by 2^-150 at most: nothing beside 2^-90.  (Sums
   // below 2^80 do not overflow the pairs: a plan has fewer than 2^40 elements.)
   if (!(t < 0x1p80f) || (t < 0x1p-90f && any != 0)) {
-    for (b = block; b < stop; b += kClipWarps) {
+    for (b = block; b < stop; ++b) {
       const uint64_t at = static_cast<uint64_t>(b) * kOptBlock + lane * kOptLane;
       for (int j = 0; j < kOptLane && at + j < n; ++j) {
         const float x = element<Bf16>(grad, at + j);
@@ -183,16 +186,17 @@ __device__ __forceinline__ Tensor tensor(const ClipParams& p, uint32_t t) {
 __global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kClipWarps];
   const int lane = threadIdx.x % 32;
-  const uint32_t warp = threadIdx.x / 32;
+  const uint32_t warp = threadIdx.x / 32, per_warp = p.segment / kClipWarps;
   uint32_t t = 0;
   Tensor d = {};
   if (p.work.n_blocks) d = tensor(p, t = p.work.start[blockIdx.x]);  // (the plan's tables: nothing writes them)
   wait_for_kernel_before();
   ClipPartial s = {0.0f, 0.0f, 0.0, 0};
   for (uint32_t k = blockIdx.x; k < p.work.n_starts; k += gridDim.x) {
-    const uint32_t end = min((k + 1) * p.segment, p.work.n_blocks);
+    uint32_t b = k * p.segment + warp * per_warp;
+    const uint32_t end = min(b + per_warp, p.work.n_blocks);
     if (k != blockIdx.x && p.work.start[k] != t) d = tensor(p, t = p.work.start[k]);
-    for (uint32_t b = k * p.segment + warp; b < end;) {
+    while (b < end) {
       if (b - d.first >= d.n_blocks) d = tensor(p, t = tensor_of(p.work, t, b));
       const uint32_t from = b - d.first, to = min(end - d.first, d.n_blocks);
       const bool shifted = reinterpret_cast<uint64_t>(d.grad) % 16 != 0;
@@ -200,7 +204,7 @@ __global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(
         shifted ? add_blocks<true, true>(d.grad, d.n, from, to, lane, s) : add_blocks<true, false>(d.grad, d.n, from, to, lane, s);
       else
         shifted ? add_blocks<false, true>(d.grad, d.n, from, to, lane, s) : add_blocks<false, false>(d.grad, d.n, from, to, lane, s);
-      b += (to - from + kClipWarps - 1) / kClipWarps * kClipWarps;
+      b += to - from;
     }
   }
   warp_sum(s);

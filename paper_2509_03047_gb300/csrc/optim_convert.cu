@@ -77,38 +77,37 @@ __device__ __noinline__ void convert_any(const OptDesc* from, const OptDesc* to,
 
 template <bool ToEight, bool Random>
 __global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_constant__ ConvertParams p) {
-  constexpr int kBlocks = kConvertBlocks;
+  constexpr uint32_t kBlocks = kConvertBlocks;
   const int lane = threadIdx.x % 32;
-  uint32_t b = blockIdx.x * (kBlocks * kOptWarps) + threadIdx.x / 32;
-  if (b >= p.src.n_blocks) return;
+  uint32_t b = (blockIdx.x * kOptWarps + threadIdx.x / 32) * kBlocks;
+  const uint32_t end = min(b + kBlocks, p.src.n_blocks);
+  if (b >= end) return;
   uint32_t t = tensor_of(p.src, p.src.start[blockIdx.x], b);
   OptDesc s = p.src.tensors[t], d = p.dst.tensors[t];  // (the plans' tables: nothing writes them)
   wait_for_kernel_before();
-  RandomKey key = {0, 0};
-  if (Random) key = random_key(p.key, s.tensor);
-  if (s.aligned && d.aligned && b - s.first + (kBlocks - 1) * kOptWarps < s.n / kOptBlock) {
-    Raw<ToEight> r[kBlocks];
-#pragma unroll
-    for (int k = 0; k < kBlocks; ++k) r[k].load(s, b - s.first + k * kOptWarps, lane);
-#pragma unroll
-    for (int k = 0; k < kBlocks; ++k) convert_whole<ToEight, Random>(r[k], d, b - s.first + k * kOptWarps, key, lane);
-    return;
-  }
 #pragma unroll 1
-  for (int k = 0;;) {
-    const uint32_t block = b - s.first;
-    if (s.aligned && d.aligned && block < s.n / kOptBlock) {
+  for (;;) {
+    RandomKey key = {0, 0};
+    if (Random) key = random_key(p.key, s.tensor);
+    const uint32_t block = b - s.first, whole = s.aligned && d.aligned ? static_cast<uint32_t>(s.n / kOptBlock) : 0;
+    if (b + kBlocks == end && block + kBlocks <= whole) {
+      Raw<ToEight> r[kBlocks];
+#pragma unroll
+      for (uint32_t k = 0; k < kBlocks; ++k) r[k].load(s, block + k, lane);
+#pragma unroll
+      for (uint32_t k = 0; k < kBlocks; ++k) convert_whole<ToEight, Random>(r[k], d, block + k, key, lane);
+      return;
+    }
+    if (block < whole) {
       Raw<ToEight> r;
       r.load(s, block, lane);
       convert_whole<ToEight, Random>(r, d, block, key, lane);
     } else {
       convert_any<ToEight, Random>(p.src.tensors + t, p.dst.tensors + t, block, key, lane);
     }
-    b += kOptWarps;
-    if (++k == kBlocks || b >= p.src.n_blocks) return;
+    if (++b == end) return;
     t = tensor_of(p.src, t, b);
     s = p.src.tensors[t], d = p.dst.tensors[t];
-    if (Random) key = random_key(p.key, s.tensor);
   }
 }
 
