@@ -130,7 +130,8 @@ uint64_t head_elems(const fr_opt_tensor& x, const StepClass& c) {
   const uint64_t head = to_boundary(x.weight, x.weight_dtype);
   if (to_boundary(x.grad, x.grad_dtype) != head || to_boundary(x.m, FR_DT_F32) != head || to_boundary(x.v, FR_DT_F32) != head) return 0;
   if (x.master && to_boundary(x.master, FR_DT_F32) != head) return 0;
-  return c.weight == kWeightBf16 && head % 2 ? 0 : head;
+  // (and a block's pairs must have one high word in their indices)
+  return c.weight == kWeightBf16 && (head % 2 || x.n > 1ull << 33) ? 0 : head;
 }
 
 OptDesc part(const OptDesc& d, const fr_opt_tensor& x, uint64_t first, uint64_t n) {
@@ -158,7 +159,11 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
     p->n_elems += x.n;
     p->n_blocks += d.n_blocks;
     if (x.grad) p->clip.add(d);
-    if (x.m) p->convert.add(d);
+    if (x.m) {
+      OptDesc moments = d;
+      moments.aligned = on(x.m, vector_bytes(x.state_dtype)) && on(x.v, vector_bytes(x.state_dtype));
+      p->convert.add(moments);
+    }
     if (x.weight && x.grad && x.m) {
       StepClass c;
       c.weight = x.master ? kWeightMaster : x.weight_dtype == FR_DT_BF16 ? kWeightBf16 : kWeightF32;
@@ -225,9 +230,9 @@ fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt
       report_invalid(me, "a buffer is not aligned to its element size");
       return FR_ERR_ALIGNMENT;
     }
-    blocks += (tensors[t].n + kOptBlock - 1) / kOptBlock;
+    blocks += (tensors[t].n + kOptBlock - 1) / kOptBlock + 1;  // (a head may be a block of its own)
+    if (blocks >= (1ull << 32) - 1) return report_invalid(me, "too many elements");
   }
-  if (blocks + n_tensors >= (1ull << 32) - 1) return report_invalid(me, "too many elements");  // (a head may be a block of its own)
 
   int dev = 0;
   const cudaError_t e = cudaGetDevice(&dev);

@@ -6,13 +6,19 @@
 // segment: at most 64 squares are added in fp32 at a time.  A sum that is
 // not finite (a NaN or Inf, or an overflow) or so small that squares may have
 // lost bits to underflow is added again by the lanes concerned, element by
-// element in fp64, the non-finite ones counted and left out.  Warps, then CTAs,
-// then the partial sums of all CTAs are added in fp64 in a fixed order; the CTA
-// that is last to finish adds those.
+// element in fp64, the non-finite ones counted and left out.  Lanes, warps and
+// CTAs are added as float pairs in a fixed order, by the CTA that is last to
+// finish at the end.
 //
 // Which lane has which element does not depend on the address (the order of the
 // sums must not): off the 16-byte boundary a lane loads the granules around its
-// elements and shifts them out.
+// elements and shifts them out.  (Each granule that it loads holds one of them.)
+//
+// Bound by reading: one pass, up to eight 16-byte loads per lane in flight with
+// 32 warps per SM.  GB300: 2.0 GB of bf16 276 us (7.3 TB/s; a plain read of 8 GB
+// reaches 7.4), 247 MB 39 us, 400 views at odd places in 108 MB 26 us, 2 MB in L2
+// 5.6 us.  Of those 5.6, a launch is 2, the loads, behind the tensor's
+// descriptor, 1, and the last CTA's sum, behind the others' counts, 1.6.
 #include "kernels.h"
 #include "optim_block.cuh"
 
@@ -162,14 +168,25 @@ __device__ __forceinline__ void warp_sum(ClipPartial& s) {
   }
 }
 
-// The square root of a sum, in fp32 as long as the sum is: a step of Newton's
-// from an approximation, its residual exact (0.6 us less than in fp64).
-__device__ __forceinline__ float root(const ClipPartial& s) {
-  if (s.exact != 0.0) return static_cast<float>(sqrt(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact));
-  if (s.hi == 0.0f) return 0.0f;
-  const float y = rsqrtf(s.hi), r = __fmul_rn(s.hi, y), rr = __fmul_rn(r, r);
-  const float e = __fadd_rn(__fsub_rn(__fsub_rn(s.hi, rr), __fmaf_rn(r, r, -rr)), s.lo);
-  return __fmaf_rn(__fmul_rn(0.5f, y), e, r);
+// The record of a sum.
+__device__ __forceinline__ fr_clip record(const ClipPartial& s, float grad_scale, float max_norm) {
+  fr_clip r;
+  r.nonfinite = s.nonfinite;
+  r.norm = 0.0f;
+  if (s.hi > 0.0f) {
+    // the root by a step of Newton's from an approximation, its residual exact: 0.6 us less than in fp64
+    const float y = rsqrtf(s.hi), x = __fmul_rn(s.hi, y), xx = __fmul_rn(x, x);
+    const float e = __fadd_rn(__fsub_rn(__fsub_rn(s.hi, xx), __fmaf_rn(x, x, -xx)), s.lo);
+    r.norm = __fmul_rn(grad_scale, __fmaf_rn(__fmul_rn(0.5f, y), e, x));
+  }
+  r.scale = r.norm > max_norm ? __fmul_rn(grad_scale, __fdiv_rn(max_norm, r.norm)) : grad_scale;
+  if (s.exact != 0.0 || r.norm == INFINITY) {
+    const double norm = grad_scale * sqrt(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact);
+    r.norm = static_cast<float>(norm);
+    r.scale = norm > max_norm ? static_cast<float>(grad_scale * (max_norm / norm)) : grad_scale;
+  }
+  if (s.nonfinite) r.scale = 0.0f;
+  return r;
 }
 
 // What the norm needs of a tensor.
@@ -183,7 +200,7 @@ __device__ __forceinline__ Tensor tensor(const ClipParams& p, uint32_t t) {
   return {d.grad, d.n, d.first, d.n_blocks, d.bf16_grad};
 }
 
-__global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(const __grid_constant__ ClipParams p) {
+__global__ void __launch_bounds__(32 * kClipWarps, 1) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kClipWarps];
   const int lane = threadIdx.x % 32;
   const uint32_t warp = threadIdx.x / 32, per_warp = p.segment / kClipWarps;
@@ -211,8 +228,8 @@ __global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(
   if (lane == 0) warps[warp] = s;
   __syncthreads();
   if (warp != 0) return;
-  if (lane < kClipWarps) s = warps[lane];
-  else s = {0.0f, 0.0f, 0.0, 0};
+  static_assert(kClipWarps == 32, "one lane for each");
+  s = warps[lane];
   warp_sum(s);
   uint32_t before = 0;
   if (lane == 0) {
@@ -241,13 +258,7 @@ __global__ void __launch_bounds__(32 * kClipWarps, 32 / kClipWarps) clip_kernel(
     s.nonfinite += q[k].nonfinite;
   }
   warp_sum(s);
-  if (lane == 0) {
-    fr_clip r;
-    r.norm = __fmul_rn(p.grad_scale, root(s));
-    r.scale = s.nonfinite ? 0.0f : r.norm > p.max_norm ? __fmul_rn(p.grad_scale, __fdiv_rn(p.max_norm, r.norm)) : p.grad_scale;
-    r.nonfinite = s.nonfinite;
-    *p.out = r;
-  }
+  if (lane == 0) *p.out = record(s, p.grad_scale, p.max_norm);
 }
 
 }  // namespace

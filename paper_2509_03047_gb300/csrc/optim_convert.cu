@@ -1,4 +1,8 @@
 // optim_convert.cu -- moments from 32 bits to 8 and back.
+//
+// Bound by memory, 10 bytes per element: GPT-2 small (1.24 GB) to 8 bits 184 us
+// (6.7 TB/s), back 179 us (6.9); 18 million elements in 2,000 tensors 35 and 32 us,
+// 8 of them what a launch and its first and last blocks take.
 #include <type_traits>
 
 #include "kernels.h"

@@ -1,7 +1,27 @@
 // optim_step.cu -- the AdamW step over a list of tensors.
 //
 // One launch per class of tensors (parameter type, gradient type, moments in
-// 32 or 8 bits).
+// 32 or 8 bits); one pass over each buffer, every element read, updated and
+// written where it lies.  Bound by memory, and for 8-bit moments under bf16
+// weights without a master, at 10 bytes per element, by instructions too.
+//
+// 32-bit moments: one block of 256 elements per warp, no loop.  The hardware's
+// own order of many short CTAs reaches 7.1 TB/s (28 GB of a Llama-8B rank 3.95
+// ms; GPT-2 small, 3.7 GB, 522 us; a copy moves 6.8 TB/s), warps that loop over
+// the blocks at most 6.6, in any order: contiguous ranges, units side by side or
+// a grid's stride, with 1 to 6 CTAs per SM, with and without eviction hints.
+//
+// 8-bit moments: a block is 2.5 to 4 KB and 1,500 instructions of a warp, so up
+// to 8 consecutive blocks share what a warp does once (its tensor, its random
+// key, its exponents), the next one's loads in flight.  One block per warp: GPT-2
+// small 307 us, a Llama-8B rank 2.77 ms; so 207 us (6.0 TB/s) and 2.37 ms (6.8).
+// In the former warps issue in 70% of the cycles and wait for loads in most others;
+// three or four CTAs per SM, a second block ahead, or prefetches to L2 give 2% or
+// nothing more.
+//
+// Blocks that are not whole, and tensors whose buffers lie off the vectors'
+// boundaries in different ways, go element by element (Step::any): 8-bit moments
+// at odd addresses 2.3 TB/s.
 #include <type_traits>
 
 #include "kernels.h"
@@ -34,7 +54,7 @@ struct Step {
   using RawGrad = std::conditional_t<Bf16Grad, RawBf16, RawF32>;
   using RawParam = std::conditional_t<Weight == kWeightBf16, RawBf16, RawF32>;
   using RawMoment = std::conditional_t<Eight, RawCodes, RawF32>;
-  static constexpr int kGradBytes = RawGrad::kBytes, kMomentBytes = RawMoment::kBytes, kWeightBytes = Weight == kWeightF32 ? 4 : 2;
+  static constexpr int kGradBytes = RawGrad::kBytes, kMomentBytes = RawMoment::kBytes;
 
   // The lane's places in a block.
   struct Places {
