@@ -1,10 +1,10 @@
 // optim_block.cuh -- a warp's block of 256 elements: finding its tensor, loads,
 // stores, random bits, coding of 8-bit moments.
 //
-// A whole block whose buffers are aligned moves as vectors: lane l has the
-// elements 8 l ... 8 l + 7.  Any other block moves element by element, lane l
-// with the elements l, l + 32, ..., those past the tensor's end read as zero.
-// Both give the same bits.
+// Where a tensor's buffers are aligned a block moves as vectors: lane l has the
+// elements 8 l ... 8 l + 7.  Else (and a conversion's last block of a tensor)
+// it moves element by element, lane l with the elements l, l + 32, ...  What lies
+// past the tensor's end reads as zero.  Both give the same bits.
 #pragma once
 
 #include "optim.h"
@@ -33,16 +33,22 @@ __device__ __forceinline__ uint4 load_16(const void* p) {
   return r;
 }
 
-// A lane's eight elements as they lie in memory.  (32 bytes go by one
-// instruction: two of 16 bytes, each lane's beside one another, write at 4.7
-// TB/s where this does at 7.0.)
+// A lane's eight elements as they lie in memory.  `left` of them are in the
+// tensor: in its last block fewer than eight, or none, and these go one by one.
+// (32 bytes go by one instruction: two of 16 bytes, each lane's beside one
+// another, write at 4.7 TB/s where this does at 7.0.)
 struct RawF32 {
   static constexpr int kBytes = 4;
   uint32_t a[8];
-  __device__ __forceinline__ void load(const void* p) {
-    asm volatile("ld.global.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7])
-                 : "l"(p));
+  __device__ __forceinline__ void load(const void* p, int left) {
+    if (left >= kOptLane) {
+      asm volatile("ld.global.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                   : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7])
+                   : "l"(p));
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < kOptLane; ++j) a[j] = j < left ? static_cast<const uint32_t*>(p)[j] : 0u;
   }
   __device__ __forceinline__ void get(Pair (&x)[4]) const {
 #pragma unroll
@@ -51,27 +57,72 @@ struct RawF32 {
 };
 struct RawBf16 {
   static constexpr int kBytes = 2;
-  uint4 a;
-  __device__ __forceinline__ void load(const void* p) { a = load_16(p); }
-  __device__ __forceinline__ void get(Pair (&x)[4]) const {
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+  uint32_t a[4];
+  __device__ __forceinline__ void load(const void* p, int left) {
+    if (left >= kOptLane) {
+      const uint4 q = load_16(p);
+      a[0] = q.x, a[1] = q.y, a[2] = q.z, a[3] = q.w;
+      return;
+    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xFFFF0000u));
+    for (int j = 0; j < kOptLane; ++j) {
+      const uint32_t x = j < left ? static_cast<const uint16_t*>(p)[j] : 0u;
+      a[j / 2] = j & 1 ? a[j / 2] | x << 16 : x;
+    }
+  }
+  __device__ __forceinline__ void get(Pair (&x)[4]) const {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(a[j] << 16), __uint_as_float(a[j] & 0xFFFF0000u));
   }
 };
 struct RawCodes {
   static constexpr int kBytes = 1;
-  uint2 a;
-  __device__ __forceinline__ void load(const void* p) {
-    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(a.x), "=r"(a.y) : "l"(p));
+  uint32_t a[2];
+  __device__ __forceinline__ void load(const void* p, int left) {
+    if (left >= kOptLane) {
+      asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(a[0]), "=r"(a[1]) : "l"(p));
+      return;
+    }
+    a[0] = a[1] = 0;
+#pragma unroll
+    for (int j = 0; j < kOptLane; ++j)
+      if (j < left) a[j / 4] |= static_cast<uint32_t>(static_cast<const uint8_t*>(p)[j]) << 8 * (j & 3);
   }
 };
-__device__ __forceinline__ void store_f32(void* p, const Pair (&x)[4]) {
-  asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y),
-               "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y), "l"(p)
-               : "memory");
+__device__ __forceinline__ void store_f32(void* p, int left, const Pair (&x)[4]) {
+  if (left >= kOptLane) {
+    asm volatile("st.global.v8.f32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};" ::"f"(x[0].x), "f"(x[0].y), "f"(x[1].x), "f"(x[1].y),
+                 "f"(x[2].x), "f"(x[2].y), "f"(x[3].x), "f"(x[3].y), "l"(p)
+                 : "memory");
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j)
+    if (j < left) static_cast<float*>(p)[j] = j & 1 ? x[j / 2].y : x[j / 2].x;
 }
-__device__ __forceinline__ void store_bf16(void* p, const uint32_t (&w)[4]) { *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]); }
+__device__ __forceinline__ void store_bf16(void* p, int left, const uint32_t (&w)[4]) {
+  if (left >= kOptLane) {
+    *static_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j)
+    if (j < left) static_cast<uint16_t*>(p)[j] = static_cast<uint16_t>(j & 1 ? w[j / 2] >> 16 : w[j / 2]);
+}
+__device__ __forceinline__ void store_bytes(uint8_t* p, int left, const uint32_t (&w)[2]) {
+  if (left >= kOptLane) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j)
+    if (j < left) p[j] = static_cast<uint8_t>(w[j / 4] >> 8 * (j & 3));
+}
+// Of a lane's elements of a block of a tensor of n.
+__device__ __forceinline__ int elements_left(uint64_t n, uint32_t block, int lane) {
+  const uint64_t first = static_cast<uint64_t>(block) * kOptBlock;
+  return n - first >= kOptBlock ? kOptLane : min(max(static_cast<int>(n - first) - lane * kOptLane, 0), kOptLane);
+}
 
 // A lane's place in a block of a buffer.
 template <int Bytes>
@@ -148,7 +199,7 @@ __device__ __forceinline__ float min3(float a, float b, float c) {
 // Codes a whole block's moments and stores them at the lane's place; returns the
 // exponent.  u: the lane's random_pairs.
 template <bool Signed, bool Random>
-__device__ __forceinline__ uint32_t store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes) {
+__device__ __forceinline__ uint32_t store_codes(const Pair (&x)[4], const uint32_t (&u)[4], uint8_t* codes, int left) {
   const uint32_t e = block_exponent(block_top(x), Signed ? kSpanM : kSpanV);
   uint32_t h[4], w[2];
 #pragma unroll
@@ -163,7 +214,7 @@ __device__ __forceinline__ uint32_t store_codes(const Pair (&x)[4], const uint32
         if ((j & 1 ? x[j / 2].y : x[j / 2].x) == 0.0f) w[j / 4] &= ~(0xFFu << 8 * (j & 3));
   }
   if (e >= 255) w[0] = w[1] = 0;
-  *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
+  store_bytes(codes, left, w);
   return e;
 }
 

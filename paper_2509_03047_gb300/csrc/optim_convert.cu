@@ -22,8 +22,8 @@ struct Raw {
   std::conditional_t<ToEight, RawF32, RawCodes> m, v;
   uint32_t em, ev;
   __device__ __forceinline__ void load(const OptDesc& s, uint32_t block, int lane) {
-    m.load(lane_at<ToEight ? 4 : 1>(s.m, block, lane));
-    v.load(lane_at<ToEight ? 4 : 1>(s.v, block, lane));
+    m.load(lane_at<ToEight ? 4 : 1>(s.m, block, lane), kOptLane);
+    v.load(lane_at<ToEight ? 4 : 1>(s.v, block, lane), kOptLane);
     if (!ToEight) em = read_exponent(s.m_exp[block], kSpanM), ev = read_exponent(s.v_exp[block], kSpanV);
   }
 };
@@ -39,22 +39,22 @@ __device__ __forceinline__ void convert_whole(const Raw<ToEight>& r, const OptDe
     for (int j = 0; j < 4; ++j) v[j] = make_float2(not_negative(v[j].x), not_negative(v[j].y));
     uint32_t u[4];
     if (Random) random_pairs(key, random_counter(key, (first >> 1) + 4 * lane), u);
-    const uint32_t em = store_codes<true, Random>(m, u, lane_at<1>(d.m, block, lane));
-    const uint32_t ev = store_codes<false, Random>(v, u, lane_at<1>(d.v, block, lane));
+    const uint32_t em = store_codes<true, Random>(m, u, lane_at<1>(d.m, block, lane), kOptLane);
+    const uint32_t ev = store_codes<false, Random>(v, u, lane_at<1>(d.v, block, lane), kOptLane);
     if (lane == 0) d.m_exp[block] = stored_exponent(em), d.v_exp[block] = stored_exponent(ev);
   } else {
-    decode4<true>(r.m.a.x, r.em, m[0], m[1]);
-    decode4<true>(r.m.a.y, r.em, m[2], m[3]);
-    decode4<false>(r.v.a.x, r.ev, v[0], v[1]);
-    decode4<false>(r.v.a.y, r.ev, v[2], v[3]);
+    decode4<true>(r.m.a[0], r.em, m[0], m[1]);
+    decode4<true>(r.m.a[1], r.em, m[2], m[3]);
+    decode4<false>(r.v.a[0], r.ev, v[0], v[1]);
+    decode4<false>(r.v.a[1], r.ev, v[2], v[3]);
     const Pair nan = pair(__uint_as_float(0x7FC00000u));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (r.em == 255) m[j] = nan;
       if (r.ev == 255) v[j] = nan;
     }
-    store_f32(lane_at<4>(d.m, block, lane), m);
-    store_f32(lane_at<4>(d.v, block, lane), v);
+    store_f32(lane_at<4>(d.m, block, lane), kOptLane, m);
+    store_f32(lane_at<4>(d.v, block, lane), kOptLane, v);
   }
 }
 

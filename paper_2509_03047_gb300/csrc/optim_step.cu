@@ -19,9 +19,8 @@
 // three or four CTAs per SM, a second block ahead, or prefetches to L2 give 2% or
 // nothing more.
 //
-// Blocks that are not whole, and tensors whose buffers lie off the vectors'
-// boundaries in different ways, go element by element (Step::any): 8-bit moments
-// at odd addresses 2.3 TB/s.
+// Tensors whose buffers lie off the vectors' boundaries in different ways go
+// element by element (Step::any): 8-bit moments at odd addresses 2.3 TB/s.
 #include <type_traits>
 
 #include "kernels.h"
@@ -75,27 +74,27 @@ struct Step {
       v += kOptBlock * kMomentBytes;
     }
   };
-  // A whole block's loads, `ahead` blocks further.
+  // A block's loads, `ahead` blocks further.
   struct Raw {
     RawGrad g;
     RawParam p;
     RawMoment m, v;
-    __device__ __forceinline__ void load(const Places& at, int ahead) {
-      g.load(at.g + ahead * (kOptBlock * kGradBytes));
-      m.load(at.m + ahead * (kOptBlock * kMomentBytes));
-      v.load(at.v + ahead * (kOptBlock * kMomentBytes));
-      p.load(at.p + ahead * (kOptBlock * RawParam::kBytes));
+    __device__ __forceinline__ void load(const Places& at, int ahead, int left) {
+      g.load(at.g + ahead * (kOptBlock * kGradBytes), left);
+      m.load(at.m + ahead * (kOptBlock * kMomentBytes), left);
+      v.load(at.v + ahead * (kOptBlock * kMomentBytes), left);
+      p.load(at.p + ahead * (kOptBlock * RawParam::kBytes), left);
     }
   };
   // The rest of it; em and ev: its exponents, old and new.
-  static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, uint32_t counter, RandomKey key, const Raw& r, uint32_t& em,
-                                                uint32_t& ev) {
+  static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, int left, uint32_t counter, RandomKey key, const Raw& r,
+                                                uint32_t& em, uint32_t& ev) {
     Pair g[4], p[4], m[4], v[4];
     if constexpr (Eight) {
-      decode4<true>(r.m.a.x, em, m[0], m[1]);
-      decode4<true>(r.m.a.y, em, m[2], m[3]);
-      decode4<false>(r.v.a.x, ev, v[0], v[1]);
-      decode4<false>(r.v.a.y, ev, v[2], v[3]);
+      decode4<true>(r.m.a[0], em, m[0], m[1]);
+      decode4<true>(r.m.a[1], em, m[2], m[3]);
+      decode4<false>(r.v.a[0], ev, v[0], v[1]);
+      decode4<false>(r.v.a[1], ev, v[2], v[3]);
       if (em == 255 || ev == 255) {  // (rare) a block that has lost its moments
         const float nan = __uint_as_float(0x7FC00000u);
 #pragma unroll
@@ -121,46 +120,63 @@ struct Step {
       uint32_t w[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) w[j] = Random ? random_bf16x2(p[j], u[j]) : nearest_bf16x2(p[j]);
-      store_bf16(at.p, w);
+      store_bf16(at.p, left, w);
     } else {
-      store_f32(at.p, p);
+      store_f32(at.p, left, p);
       if (Weight == kWeightMaster) {
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = nearest_bf16x2(p[j]);
-        store_bf16(at.w, w);
+        store_bf16(at.w, left, w);
       }
     }
     if constexpr (Eight) {
-      em = store_codes<true, Random>(m, u, at.m);
-      ev = store_codes<false, Random>(v, u, at.v);
+      em = store_codes<true, Random>(m, u, at.m, left);
+      ev = store_codes<false, Random>(v, u, at.v, left);
     } else {
-      store_f32(at.m, m);
-      store_f32(at.v, v);
+      store_f32(at.m, left, m);
+      store_f32(at.v, left, v);
     }
   }
 
-  // `count` whole blocks one after the other, one loaded ahead.  Not unrolled:
-  // the code must stay in the instruction cache.
-  static __device__ __forceinline__ void whole(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
+  // One block of an aligned tensor, whole or its last.
+  static __device__ __forceinline__ void one(const Hyper& h, const OptDesc& d, uint32_t block, RandomKey key, int lane) {
+    const Places at(d, block, lane);
+    const int left = elements_left(d.n, block, lane);
+    const uint32_t counter = random_counter(key, (static_cast<uint64_t>(block) * kOptBlock + d.skipped) / 2 + 4 * lane);
+    Raw r;
+    r.load(at, 0, left);
+    Exponents e = {0, 0};
+    if (Eight) e.load(d.m_exp + block, d.v_exp + block, 1, lane);
+    uint32_t em = e.of_m(0), ev = e.of_v(0);
+    finish(h, at, left, counter, key, r, em, ev);
+    e = {em, ev};
+    if (Eight) e.store(d.m_exp + block, d.v_exp + block, 1, lane);
+  }
+  static __device__ __noinline__ void last(const StepParams& p, float scale, uint32_t t) {
+    const OptDesc d = p.work.tensors[t];
+    RandomKey key = {0, 0};
+    if (Random) key = random_key(p.key, d.tensor);
+    one(hyper(p, scale, d), d, d.n_blocks - 1, key, threadIdx.x % 32);
+  }
+
+  // `count` whole blocks of an aligned tensor one after the other, one loaded
+  // ahead.  Not unrolled: the code must stay in the instruction cache.
+  static __device__ __forceinline__ void run(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
     Places at(d, block, lane);
     // (a run does not pass a multiple of 2^32 pairs: see run_length)
-    uint32_t counter = random_counter(key, (static_cast<uint64_t>(block) * kOptBlock + d.skipped) / 2 + 4 * lane);
+    uint32_t counter = random_counter(key, static_cast<uint64_t>(block) * (kOptBlock / 2) + 4 * lane);
     Raw r;
-    r.load(at, 0);
-    uint32_t em = 0, ev = 0;
-    if (!Eight) {
-      finish(h, at, counter, key, r, em, ev);
-      return;
-    }
+    r.load(at, 0, kOptLane);
+    uint32_t em, ev;
     Exponents e;
     e.load(d.m_exp + block, d.v_exp + block, count, lane);
 #pragma unroll 1
     for (int k = 0;;) {
       Raw next;
-      if (k + 1 < count) next.load(at, 1);
+      if (k + 1 < count) next.load(at, 1, kOptLane);
       em = e.of_m(k), ev = e.of_v(k);
-      finish(h, at, counter, key, r, em, ev);
+      finish(h, at, kOptLane, counter, key, r, em, ev);
       e.set(k, lane, em, ev);
       if (++k == count) break;
       r = next;
@@ -252,17 +268,24 @@ __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16G
   }
 #pragma unroll 1
   for (;;) {
-    const uint32_t block = b - d.first, whole = d.aligned && !p.exact ? static_cast<uint32_t>(d.n / kOptBlock) : 0;
-    if (block < whole) {
+    const uint32_t block = b - d.first;
+    uint32_t count = 1;
+    if (d.aligned && !p.exact) {
       RandomKey key = {0, 0};
       if (Random) key = random_key(p.key, d.tensor);
-      const uint32_t count = Eight ? min(min(end - b, whole - block), run_length(block)) : 1;
-      S::whole(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
-      b += count;
+      const uint32_t whole = static_cast<uint32_t>(d.n / kOptBlock);
+      if (!Eight) {
+        S::one(hyper(p, scale, d), d, block, key, lane);
+      } else if (block < whole) {
+        count = min(min(end - b, whole - block), run_length(block));
+        S::run(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
+      } else {
+        S::last(p, scale, t);
+      }
     } else {
       S::any(p, scale, t, block);
-      ++b;
     }
+    b += count;
     if (b >= end) return;
     t = tensor_of(p.work, t, b);
     d = p.work.tensors[t];
