@@ -108,9 +108,9 @@ struct StepParams {
   uint32_t per_warp;           // consecutive blocks
   uint64_t key;                // of the random bits: mix64(mix64(seed) + step)
 };
-// CTAs of eight warps per SM, what the registers of a lane's elements allow: of
-// the 8-bit classes the one that loads least is as fast with 64 as with 80 (GPT-2
-// small 207 us with 4 CTAs, 211 with 3; with a master 326 and 299).
+// CTAs of eight warps per SM, what the registers of a lane's elements allow.  (Of
+// the 8-bit classes the one that loads least gains by a fourth: GPT-2 small 193 us,
+// 200 with three; with masters 299 with four, 290 with three.)
 constexpr int step_ctas(bool eight, int weight, bool bf16_grad) { return eight && !(weight == kWeightBf16 && bf16_grad) ? 3 : 4; }
 // Consecutive blocks per warp.
 inline uint32_t step_blocks(bool eight, uint64_t n_blocks) {

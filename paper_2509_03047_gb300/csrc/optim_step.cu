@@ -11,13 +11,13 @@
 // the blocks at most 6.6, in any order: contiguous ranges, units side by side or
 // a grid's stride, with 1 to 6 CTAs per SM, with and without eviction hints.
 //
-// 8-bit moments: a block is 2.5 to 4 KB and 1,500 instructions of a warp, so up
+// 8-bit moments: a block is 2.5 to 4 KB and 1,400 instructions of a warp, so up
 // to 8 consecutive blocks share what a warp does once (its tensor, its random
-// key, its exponents), the next one's loads in flight.  One block per warp: GPT-2
-// small 307 us, a Llama-8B rank 2.77 ms; so 207 us (6.0 TB/s) and 2.37 ms (6.8).
-// In the former warps issue in 70% of the cycles and wait for loads in most others;
-// three or four CTAs per SM, a second block ahead, or prefetches to L2 give 2% or
-// nothing more.
+// key, its exponents), and the next ones come to shared memory meanwhile, by
+// asynchronous copies that take no registers.  One block per warp: GPT-2 small in
+// bf16 307 us, a Llama-8B rank with masters 2.77 ms; runs with the next block in
+// registers 207 us and 2.38 ms; so 193 us (6.4 TB/s) and 2.31 ms (7.0).  At the
+// former's 10 bytes per element warps issue in three of four cycles.
 //
 // Tensors whose buffers lie off the vectors' boundaries in different ways go
 // element by element (Step::any): 8-bit moments at odd addresses 2.3 TB/s.
@@ -55,6 +55,8 @@ struct Step {
   using RawMoment = std::conditional_t<Eight, RawCodes, RawF32>;
   static constexpr int kGradBytes = RawGrad::kBytes, kMomentBytes = RawMoment::kBytes;
 
+  // Of a block in shared memory, and how many (a CTA's stay under 48 KiB).
+  static constexpr int kSlot = kOptBlock * (kGradBytes + RawParam::kBytes + 2 * kMomentBytes), kSlots = kSlot <= 1536 ? 3 : 2;
   // The lane's places in a block.
   struct Places {
     const uint8_t* g;
@@ -160,26 +162,50 @@ struct Step {
     one(hyper(p, scale, d), d, d.n_blocks - 1, key, threadIdx.x % 32);
   }
 
-  // `count` whole blocks of an aligned tensor one after the other, one loaded
-  // ahead.  Not unrolled: the code must stay in the instruction cache.
+  // `count` whole blocks of an aligned tensor one after the other, the next one or
+  // two on their way through shared memory.  Not unrolled: the code must stay in
+  // the instruction cache.
   static __device__ __forceinline__ void run(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
+    __shared__ __align__(16) uint8_t slots[Eight ? kOptWarps * kSlots * kSlot : 16];
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(slots)) + (threadIdx.x / 32) * (kSlots * kSlot);
     Places at(d, block, lane);
     // (a run does not pass a multiple of 2^32 pairs: see run_length)
     uint32_t counter = random_counter(key, static_cast<uint64_t>(block) * (kOptBlock / 2) + 4 * lane);
-    Raw r;
-    r.load(at, 0, kOptLane);
+    constexpr int kAtP = kOptBlock * kGradBytes, kAtM = kAtP + kOptBlock * RawParam::kBytes, kAtV = kAtM + kOptBlock * kMomentBytes;
+    auto fetch = [&](int ahead, int slot) {
+      const uint32_t to = mine + slot * kSlot;
+      RawGrad::fetch(to, at.g + ahead * (kOptBlock * kGradBytes), lane);
+      RawParam::fetch(to + kAtP, at.p + ahead * (kOptBlock * RawParam::kBytes), lane);
+      RawMoment::fetch(to + kAtM, at.m + ahead * (kOptBlock * kMomentBytes), lane);
+      RawMoment::fetch(to + kAtV, at.v + ahead * (kOptBlock * kMomentBytes), lane);
+    };
+#pragma unroll
+    for (int k = 0; k < kSlots - 1; ++k) {
+      if (k < count) fetch(k, k);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
     uint32_t em, ev;
     Exponents e;
     e.load(d.m_exp + block, d.v_exp + block, count, lane);
 #pragma unroll 1
-    for (int k = 0;;) {
-      Raw next;
-      if (k + 1 < count) next.load(at, 1, kOptLane);
+    for (int k = 0, slot = 0;;) {
+      // into the slot that the block before has left
+      if (k + kSlots - 1 < count) fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
+      asm volatile("cp.async.commit_group;" ::: "memory");  // (of nothing too: the wait counts groups)
+      asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
+      __syncwarp();  // what the other lanes fetched is there
+      Raw r;
+      const uint32_t from = mine + slot * kSlot;
+      r.g.take(from, lane);
+      r.p.take(from + kAtP, lane);
+      r.m.take(from + kAtM, lane);
+      r.v.take(from + kAtV, lane);
+      __syncwarp();  // and taken, before the next turn fetches into the slot
       em = e.of_m(k), ev = e.of_v(k);
       finish(h, at, kOptLane, counter, key, r, em, ev);
       e.set(k, lane, em, ev);
       if (++k == count) break;
-      r = next;
+      slot = slot == kSlots - 1 ? 0 : slot + 1;
       counter += kOptBlock / 2 * kRandomStep;
       at.next();
     }
