@@ -15,9 +15,10 @@
 // elements and shifts them out.  (Each granule that it loads holds one of them.)
 //
 // Bound by reading: one pass, up to eight 16-byte loads per lane in flight with
-// 32 warps per SM.  GB300: 2.0 GB of bf16 276 us (7.3 TB/s; a plain read of 8 GB
-// reaches 7.4), 247 MB 39 us, 400 views at odd places in 108 MB 26 us, 2 MB in L2
-// 5.6 us.  Of those 5.6, a launch is 2, the loads, behind the tensor's
+// 32 warps per SM.  GB300: 2.0 GB of bf16 278 us (7.2 TB/s; a plain read of 8 GB
+// reaches 7.4), 247 MB 38 us, 400 views at odd places in 108 MB 25 us (a tensor's
+// end inside a warp's blocks costs it two latencies), 2 MB of 51 tensors in L2 6.1
+// us, of one tensor 4.6.  Of these a launch is 2, the loads, behind the tensor's
 // descriptor, 1, and the last CTA's sum, behind the others' counts, 1.6.
 #include "kernels.h"
 #include "optim_block.cuh"
@@ -212,16 +213,19 @@ __global__ void __launch_bounds__(32 * kClipWarps, 1) clip_kernel(const __grid_c
   for (uint32_t k = blockIdx.x; k < p.work.n_starts; k += gridDim.x) {
     uint32_t b = k * p.segment + warp * per_warp;
     const uint32_t end = min(b + per_warp, p.work.n_blocks);
+    if (b >= end) break;
     if (k != blockIdx.x && p.work.start[k] != t) d = tensor(p, t = p.work.start[k]);
-    while (b < end) {
-      if (b - d.first >= d.n_blocks) d = tensor(p, t = tensor_of(p.work, t, b));
+    if (b - d.first >= d.n_blocks) d = tensor(p, t = tensor_of(p.work, t, b));
+    for (;;) {
       const uint32_t from = b - d.first, to = min(end - d.first, d.n_blocks);
+      b += to - from;
       const bool shifted = reinterpret_cast<uint64_t>(d.grad) % 16 != 0;
       if (d.bf16)
         shifted ? add_blocks<true, true>(d.grad, d.n, from, to, lane, s) : add_blocks<true, false>(d.grad, d.n, from, to, lane, s);
       else
         shifted ? add_blocks<false, true>(d.grad, d.n, from, to, lane, s) : add_blocks<false, false>(d.grad, d.n, from, to, lane, s);
-      b += to - from;
+      if (b >= end) break;
+      d = tensor(p, ++t);  // a warp's blocks are side by side: so are their tensors
     }
   }
   warp_sum(s);
