@@ -1,10 +1,11 @@
 // optim_api.cu -- the C ABI of the optimizer step (declared in
 // include/flashrec.h) and its planner: the tensors of each launch in one list,
-// with the tensor that each CTA's first block is in.
+// with the tensors that its CTAs or warps start in.
 #include <cuda_runtime.h>
 
 #include <algorithm>
 #include <cmath>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -22,7 +23,8 @@ struct WorkList {
   std::vector<OptDesc> tensors;
   std::vector<uint32_t> start;
   uint64_t n_blocks = 0;
-  uint32_t n_tensors = 0, n_starts = 0;
+  uint32_t n_tensors = 0, n_groups = 0, per_warp = 1;
+  bool start_of_warps = true;
   OptDesc* d_tensors = nullptr;
   uint32_t* d_start = nullptr;
 
@@ -32,25 +34,25 @@ struct WorkList {
     tensors.push_back(d);
     ++n_tensors;
   }
-  // For CTAs whose first blocks are first(0) <= first(1) <= ...
-  template <class F>
-  void cut(uint64_t ctas, F&& first) {
-    n_starts = static_cast<uint32_t>(ctas);
-    start.resize(n_starts);
+  // For CTAs of `warps` warps.
+  void cut(uint32_t blocks_per_warp, int warps) {
+    per_warp = blocks_per_warp;
+    const uint64_t per_group = static_cast<uint64_t>(per_warp) * warps, n_warps = (n_blocks + per_warp - 1) / per_warp;
+    n_groups = static_cast<uint32_t>((n_blocks + per_group - 1) / per_group);
+    start_of_warps = n_warps <= kMostWarpStarts;
+    const uint64_t step = start_of_warps ? per_warp : per_group;
+    start.resize(start_of_warps ? n_warps : n_groups);
     size_t t = 0;
-    for (uint32_t c = 0; c < n_starts; ++c) {
-      while (t + 1 < tensors.size() && tensors[t + 1].first <= first(c)) ++t;
-      start[c] = static_cast<uint32_t>(t);
+    for (size_t i = 0; i < start.size(); ++i) {
+      while (t + 1 < tensors.size() && tensors[t + 1].first <= i * step) ++t;
+      start[i] = static_cast<uint32_t>(t);
     }
-  }
-  void cut_every(uint64_t blocks) {
-    cut((n_blocks + blocks - 1) / blocks, [&](uint32_t c) { return c * blocks; });
   }
   void place(PlanMemory& mem) {
     mem.table(&d_tensors, tensors);
     mem.table(&d_start, start);
   }
-  OptWork work() const { return {d_tensors, d_start, n_tensors, static_cast<uint32_t>(n_blocks), n_starts}; }
+  OptWork work() const { return {d_tensors, d_start, n_tensors, static_cast<uint32_t>(n_blocks), n_groups, per_warp, start_of_warps}; }
 };
 
 }  // namespace
@@ -185,16 +187,16 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
     if (x.m) (x.state_dtype == FR_DT_BYTES ? p->eight : p->thirty_two) = true;
   }
   PlanMemory mem;
-  p->clip.cut_every(clip_segment(p->clip.n_blocks));
+  p->clip.cut(clip_blocks(p->clip.n_blocks), kClipWarps);
   p->clip.place(mem);
   if (p->moments) {
-    p->convert.cut_every(kConvertBlocks * kOptWarps);
+    p->convert.cut(kConvertBlocks, kOptWarps);
     p->convert.place(mem);
   }
   if (p->params)
     for (int c = 0; c < kStepClasses; ++c) {
       if (p->step[c].n_blocks == 0) continue;
-      p->step[c].cut_every(step_blocks(p->classes[c].eight, p->step[c].n_blocks) * kOptWarps);
+      p->step[c].cut(step_blocks(p->classes[c].eight, p->step[c].n_blocks), kOptWarps);
       p->step[c].place(mem);
     }
   mem.table(&p->d_done, std::vector<uint32_t>(1, 0));
@@ -231,7 +233,7 @@ fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt
       return FR_ERR_ALIGNMENT;
     }
     blocks += (tensors[t].n + kOptBlock - 1) / kOptBlock + 1;  // (a head may be a block of its own)
-    if (blocks >= (1ull << 32) - 1) return report_invalid(me, "too many elements");
+    if (blocks >= (1ull << 32) - 4096) return report_invalid(me, "too many elements");
   }
 
   int dev = 0;
@@ -244,7 +246,7 @@ fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt
   fr_status st;
   try {
     st = fill_opt(p, tensors, n_tensors);
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {  // std::bad_alloc, std::length_error
     st = report_invalid(me, "out of host memory");
   }
   if (st != FR_OK) {
@@ -285,7 +287,6 @@ fr_status fr_grad_clip(fr_opt p, float max_norm, float grad_scale, fr_clip* out_
   if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
   ClipParams cp;
   cp.work = p->clip.work();
-  cp.segment = clip_segment(p->clip.n_blocks);
   cp.partials = p->d_partials;
   cp.done = p->d_done;
   cp.grad_scale = grad_scale;
@@ -329,7 +330,6 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   for (int c = 0; c < kStepClasses; ++c) {
     if (p->step[c].n_blocks == 0) continue;
     sp.work = p->step[c].work();
-    sp.per_warp = step_blocks(p->classes[c].eight, p->step[c].n_blocks);
     const cudaError_t e = launch_step(p->classes[c], sp, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return report_cuda("step kernel launch", e);
   }

@@ -25,6 +25,11 @@ __device__ __forceinline__ uint32_t tensor_of(const OptWork& w, uint32_t t, uint
   }
 }
 
+// The tensor of a warp's first block, b.
+__device__ __forceinline__ uint32_t first_tensor(const OptWork& w, uint32_t group, uint32_t warp, int warps, uint32_t b) {
+  return w.start_of_warps ? w.start[group * warps + warp] : tensor_of(w, w.start[group], b);
+}
+
 // ---- vectors
 
 __device__ __forceinline__ uint4 load_16(const void* p) {

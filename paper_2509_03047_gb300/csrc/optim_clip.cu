@@ -204,18 +204,20 @@ __device__ __forceinline__ Tensor tensor(const ClipParams& p, uint32_t t) {
 __global__ void __launch_bounds__(32 * kClipWarps, 1) clip_kernel(const __grid_constant__ ClipParams p) {
   __shared__ ClipPartial warps[kClipWarps];
   const int lane = threadIdx.x % 32;
-  const uint32_t warp = threadIdx.x / 32, per_warp = p.segment / kClipWarps;
-  uint32_t t = 0;
+  const uint32_t warp = threadIdx.x / 32, per_warp = p.work.per_warp;
+  uint32_t t = 0, b = (blockIdx.x * kClipWarps + warp) * per_warp;
   Tensor d = {};
-  if (p.work.n_blocks) d = tensor(p, t = p.work.start[blockIdx.x]);  // (the plan's tables: nothing writes them)
+  if (b < p.work.n_blocks) d = tensor(p, t = first_tensor(p.work, blockIdx.x, warp, kClipWarps, b));  // (the plan's tables: nothing writes them)
   wait_for_kernel_before();
   ClipPartial s = {0.0f, 0.0f, 0.0, 0};
-  for (uint32_t k = blockIdx.x; k < p.work.n_starts; k += gridDim.x) {
-    uint32_t b = k * p.segment + warp * per_warp;
+  for (uint32_t k = blockIdx.x; k < p.work.n_groups; k += gridDim.x) {
+    b = (k * kClipWarps + warp) * per_warp;
     const uint32_t end = min(b + per_warp, p.work.n_blocks);
     if (b >= end) break;
-    if (k != blockIdx.x && p.work.start[k] != t) d = tensor(p, t = p.work.start[k]);
-    if (b - d.first >= d.n_blocks) d = tensor(p, t = tensor_of(p.work, t, b));
+    if (k != blockIdx.x) {
+      const uint32_t now = first_tensor(p.work, k, warp, kClipWarps, b);
+      if (now != t) d = tensor(p, t = now);
+    }
     for (;;) {
       const uint32_t from = b - d.first, to = min(end - d.first, d.n_blocks);
       b += to - from;
@@ -268,7 +270,7 @@ __global__ void __launch_bounds__(32 * kClipWarps, 1) clip_kernel(const __grid_c
 }  // namespace
 
 cudaError_t launch_clip(const ClipParams& p, cudaStream_t s) {
-  const uint32_t n_ctas = p.work.n_starts < 1 ? 1 : p.work.n_starts < kClipCtas ? p.work.n_starts : kClipCtas;
+  const uint32_t n_ctas = p.work.n_groups < 1 ? 1 : p.work.n_groups < kClipCtas ? p.work.n_groups : kClipCtas;
   return launch_chained(clip_kernel, static_cast<int>(n_ctas), 32 * kClipWarps, 0, s, p);
 }
 

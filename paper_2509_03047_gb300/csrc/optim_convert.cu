@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_co
   uint32_t b = (blockIdx.x * kOptWarps + threadIdx.x / 32) * kBlocks;
   const uint32_t end = min(b + kBlocks, p.src.n_blocks);
   if (b >= end) return;
-  uint32_t t = tensor_of(p.src, p.src.start[blockIdx.x], b);
+  uint32_t t = first_tensor(p.src, blockIdx.x, threadIdx.x / 32, kOptWarps, b);
   OptDesc s = p.src.tensors[t], d = p.dst.tensors[t];  // (the plans' tables: nothing writes them)
   wait_for_kernel_before();
 #pragma unroll 1
@@ -118,10 +118,10 @@ __global__ void __launch_bounds__(32 * kOptWarps) convert_kernel(const __grid_co
 }  // namespace
 
 cudaError_t launch_convert(const ConvertParams& p, cudaStream_t s) {
-  const int n_starts = static_cast<int>(p.src.n_starts);
-  if (!p.to_eight) return launch_chained(convert_kernel<false, false>, n_starts, 32 * kOptWarps, 0, s, p);
-  if (p.random) return launch_chained(convert_kernel<true, true>, n_starts, 32 * kOptWarps, 0, s, p);
-  return launch_chained(convert_kernel<true, false>, n_starts, 32 * kOptWarps, 0, s, p);
+  const int n_ctas = static_cast<int>(p.src.n_groups);
+  if (!p.to_eight) return launch_chained(convert_kernel<false, false>, n_ctas, 32 * kOptWarps, 0, s, p);
+  if (p.random) return launch_chained(convert_kernel<true, true>, n_ctas, 32 * kOptWarps, 0, s, p);
+  return launch_chained(convert_kernel<true, false>, n_ctas, 32 * kOptWarps, 0, s, p);
 }
 
 }  // namespace frk

@@ -279,12 +279,12 @@ __device__ __forceinline__ uint32_t run_length(uint32_t block) {
 template <int Weight, bool Bf16Grad, bool Eight, bool Random>
 __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16Grad)) step_kernel(const __grid_constant__ StepParams p) {
   using S = Step<Weight, Bf16Grad, Eight, Random>;
-  const uint32_t per_warp = Eight ? p.per_warp : 1;
+  const uint32_t per_warp = Eight ? p.work.per_warp : 1, warp = threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
-  uint32_t b = (blockIdx.x * kOptWarps + threadIdx.x / 32) * per_warp;
+  uint32_t b = (blockIdx.x * kOptWarps + warp) * per_warp;
   const uint32_t end = min(b + per_warp, p.work.n_blocks);
   if (b >= end) return;
-  uint32_t t = tensor_of(p.work, p.work.start[blockIdx.x], b);
+  uint32_t t = first_tensor(p.work, blockIdx.x, warp, kOptWarps, b);
   OptDesc d = p.work.tensors[t];  // (the plan's tables: nothing writes them)
   wait_for_kernel_before();
   float scale = 1.0f;
@@ -339,7 +339,7 @@ auto for_class(const StepClass& c, bool random, F&& f) {
 }  // namespace
 
 cudaError_t launch_step(const StepClass& c, const StepParams& p, cudaStream_t s) {
-  return for_class(c, p.random != 0, [&](auto kernel) { return launch_chained(kernel, static_cast<int>(p.work.n_starts), 32 * kOptWarps, 0, s, p); });
+  return for_class(c, p.random != 0, [&](auto kernel) { return launch_chained(kernel, static_cast<int>(p.work.n_groups), 32 * kOptWarps, 0, s, p); });
 }
 
 }  // namespace frk

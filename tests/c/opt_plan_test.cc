@@ -36,6 +36,14 @@ uint32_t find(const OptWork& w, uint32_t t, uint32_t b) {
   return t;
 }
 
+// The tensor that a warp starts its blocks from b on with, as first_tensor finds it.
+uint32_t first(const OptWork& w, uint32_t group, uint32_t warp, int warps, uint32_t b) {
+  if (!w.start_of_warps) return find(w, w.start[group], b);
+  const uint32_t t = w.start[group * warps + warp];
+  CHECK(find(w, t, b) == t);
+  return t;
+}
+
 using Seen = std::map<uint32_t, std::vector<uint8_t>>;  // per tensor of the plan, how often each element came up
 
 void see(Seen& seen, const std::vector<fr_opt_tensor>& list, const OptDesc& d, uint32_t block, bool vectors) {
@@ -67,12 +75,14 @@ void all_seen(const Seen& seen, const std::vector<fr_opt_tensor>& list, const st
 }
 
 void walk_step(Seen& seen, const std::vector<fr_opt_tensor>& list, const StepClass& c, const StepParams& p) {
-  const uint32_t per_warp = c.eight ? p.per_warp : 1;
-  for (uint32_t cta = 0; cta < p.work.n_starts; ++cta)
+  const uint32_t per_warp = c.eight ? p.work.per_warp : 1;
+  CHECK(c.eight || p.work.per_warp == 1);
+  for (uint32_t cta = 0; cta < p.work.n_groups; ++cta)
     for (uint32_t warp = 0; warp < kOptWarps; ++warp) {
       uint32_t b = (cta * kOptWarps + warp) * per_warp;
       const uint32_t end = std::min(b + per_warp, p.work.n_blocks);
-      for (uint32_t t = p.work.start[cta]; b < end; ++b) {
+      if (b >= end) continue;
+      for (uint32_t t = first(p.work, cta, warp, kOptWarps, b); b < end; ++b) {
         t = find(p.work, t, b);
         const OptDesc& d = p.work.tensors[t];
         const bool vectors = d.aligned && b - d.first < d.n / kOptBlock;
@@ -80,33 +90,37 @@ void walk_step(Seen& seen, const std::vector<fr_opt_tensor>& list, const StepCla
         see(seen, list, d, b - d.first, vectors);
       }
     }
-  CHECK(static_cast<uint64_t>(p.work.n_starts) * kOptWarps * per_warp >= p.work.n_blocks);
+  CHECK(static_cast<uint64_t>(p.work.n_groups) * kOptWarps * per_warp >= p.work.n_blocks);
 }
 
 void walk_clip(Seen& seen, const std::vector<fr_opt_tensor>& list, const ClipParams& p) {
-  const uint32_t n_ctas = std::max(1u, std::min(p.work.n_starts, kClipCtas)), per_warp = p.segment / kClipWarps;
-  CHECK(p.segment % kClipWarps == 0 && per_warp >= 1 && per_warp <= kClipMost);
+  const uint32_t n_ctas = std::max(1u, std::min(p.work.n_groups, kClipCtas)), per_warp = p.work.per_warp;
+  CHECK(per_warp >= 1 && per_warp <= kClipMost);
   CHECK(*p.done == 0);
   for (uint32_t cta = 0; cta < n_ctas; ++cta) {
     p.partials[cta] = {};  // (there is one for each)
-    for (uint32_t k = cta; k < p.work.n_starts; k += n_ctas)
+    for (uint32_t k = cta; k < p.work.n_groups; k += n_ctas)
       for (uint32_t warp = 0; warp < kClipWarps; ++warp) {
-        const uint32_t first = k * p.segment + warp * per_warp, end = std::min(first + per_warp, p.work.n_blocks);
-        uint32_t t = p.work.start[k];
-        for (uint32_t b = first; b < end; ++b) {
-          t = find(p.work, t, b);
-          see(seen, list, p.work.tensors[t], b - p.work.tensors[t].first, false);
+        uint32_t b = (k * kClipWarps + warp) * per_warp;
+        const uint32_t end = std::min(b + per_warp, p.work.n_blocks);
+        if (b >= end) continue;
+        for (uint32_t t = first(p.work, k, warp, kClipWarps, b);; ++t) {  // on to the next tensor, without a search
+          const OptDesc& d = p.work.tensors[t];
+          CHECK(t < p.work.n_tensors && b >= d.first && b - d.first < d.n_blocks);
+          for (; b < std::min(end, d.first + d.n_blocks); ++b) see(seen, list, d, b - d.first, false);
+          if (b >= end) break;
         }
       }
   }
 }
 
 void walk_convert(Seen& seen, const std::vector<fr_opt_tensor>& list, const ConvertParams& p, bool src) {
-  for (uint32_t cta = 0; cta < p.src.n_starts; ++cta)
+  for (uint32_t cta = 0; cta < p.src.n_groups; ++cta)
     for (uint32_t warp = 0; warp < kOptWarps; ++warp) {
       uint32_t b = (cta * kOptWarps + warp) * kConvertBlocks;
       const uint32_t end = std::min(b + kConvertBlocks, p.src.n_blocks);
-      for (uint32_t t = p.src.start[cta]; b < end; ++b) {
+      if (b >= end) continue;
+      for (uint32_t t = first(p.src, cta, warp, kOptWarps, b); b < end; ++b) {
         t = find(p.src, t, b);
         const OptDesc &s = p.src.tensors[t], &d = p.dst.tensors[t];
         CHECK(s.first == d.first && s.n == d.n && s.tensor == d.tensor);
@@ -218,10 +232,41 @@ int main() {
     fr_opt_destroy(pb);
   }
 
+  // a list whose tables go by CTA: 2^18 blocks of one tensor and more, small ones around it
+  for (uint32_t dtype : {FR_DT_F32, FR_DT_BYTES}) {
+    std::vector<fr_opt_tensor> list;
+    std::set<uint32_t> whole;
+    uint64_t at = 1ull << 30;
+    for (uint64_t n : {5ull, 300ull, (1ull << 27) + 77, 9ull, 70000ull, 1ull}) {
+      fr_opt_tensor x = {};
+      x.n = n;
+      x.weight_dtype = x.grad_dtype = FR_DT_BF16;
+      x.state_dtype = dtype;
+      x.lr_scale = x.decay_scale = 1.0f;
+      auto place = [&](uint64_t bytes) { void* q = reinterpret_cast<void*>(at); at += (bytes + 1023) / 512 * 512; return q; };
+      x.weight = place(2 * n), x.grad = place(2 * n), x.m = place(4 * n), x.v = place(4 * n);
+      if (dtype == FR_DT_BYTES) x.m_exp = static_cast<uint8_t*>(place(n / 256 + 1)), x.v_exp = static_cast<uint8_t*>(place(n / 256 + 1));
+      whole.insert(static_cast<uint32_t>(list.size()));
+      list.push_back(x);
+    }
+    fr_opt p = make(list);
+    fr_adamw h = {1e-3, 0.9, 0.95, 1e-8, 0.1, 3, 7, FR_ROUND_RANDOM, 0};
+    fr_clip record;
+    steps.clear(), clips.clear();
+    CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_OK && steps.size() == 1 && fr_grad_clip(p, 1.0f, 1.0f, &record, nullptr) == FR_OK);
+    CHECK(steps[0].second.work.start_of_warps == (dtype == FR_DT_BYTES) && clips[0].work.start_of_warps);
+    Seen seen;
+    walk_step(seen, list, steps[0].first, steps[0].second);
+    all_seen(seen, list, whole);
+    seen.clear();
+    walk_clip(seen, list, clips[0]);
+    all_seen(seen, list, whole);
+    fr_opt_destroy(p);
+  }
+
   // sizes near the limits: what follows from them stays in 32 bits
   for (uint64_t n : {1ull, 4863ull, 4864ull, 4865ull, 77824ull, 77825ull, 3921936ull, 1ull << 31, (1ull << 32) - 2}) {
-    const uint32_t s = clip_segment(n);
-    CHECK(s % kClipWarps == 0 && s >= static_cast<uint32_t>(kClipWarps) && s <= kClipMost * kClipWarps);
+    CHECK(clip_blocks(n) >= 1 && clip_blocks(n) <= kClipMost);
     CHECK(step_blocks(false, n) == 1 && step_blocks(true, n) >= 1 && step_blocks(true, n) <= 8);
   }
 
