@@ -488,7 +488,7 @@ const char* fr_status_str(fr_status s) {
 
 const char* fr_last_error(void) { return g_err; }
 
-int fr_version(void) { return 10100; }
+int fr_version(void) { return 10200; }
 
 fr_status fr_plan_create_batched(const fr_tensor* tensors, uint64_t n_tensors, uint64_t chunk_bytes,
                                  uint32_t n_batches, fr_plan* out) {
