@@ -418,8 +418,9 @@ typedef struct fr_opt_s* fr_opt;
 
 /* Plan the step over `n_tensors` tensors (host array, copied; a tensor of 0
  * elements is allowed).  As with fr_plan_create, the plan is bound to the
- * current device and to the tensors' addresses, it allocates here and nowhere
- * else, and one stream at a time may use it.
+ * current device and to the tensors' addresses (gradients keep theirs from step
+ * to step: in PyTorch, zero_grad(set_to_none=False)), it allocates here and
+ * nowhere else, and one stream at a time may use it.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT, FR_ERR_CUDA. */
 fr_status fr_opt_create(const fr_opt_tensor* tensors, uint64_t n_tensors, fr_opt* out);
 
@@ -447,7 +448,7 @@ typedef struct {
 fr_status fr_grad_clip(fr_opt plan, float max_norm, float grad_scale, fr_clip* out_dev, void* stream);
 
 /* One step's numbers.  0 <= beta1, beta2 < 1, eps > 0, lr and weight_decay
- * >= 0, all finite; step counts from 1 (a skipped step does not count). */
+ * >= 0, all finite in fp32; step counts from 1 (a skipped step does not count). */
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay;
   uint64_t step;
@@ -461,7 +462,9 @@ typedef struct {
  *   p <- p - lr lr_scale ((m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
  *                         + weight_decay decay_scale p)
  * m and v each by separately rounded products and sums (so 8-bit codes are
- * the same bits wherever they are computed); p uses them before they are coded.
+ * the same bits wherever they are computed); p uses them before they are coded,
+ * with a square root and a reciprocal good to 2^-23 (correctly rounded ones
+ * where eps is so small that subnormal second moments count).
  * `clip_dev`: the record of fr_grad_clip, read on the device: its scale, and
  * if its nonfinite is not 0 the step leaves every byte as it is.  NULL: scale 1.
  * In a CUDA graph the numbers in `hyper` are those of the capture.

@@ -301,12 +301,12 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   const char* const me = "fr_adamw_step";
   if (p == nullptr || h == nullptr) return report_invalid(me, "plan or hyper is null");
   if (!p->params) return report_invalid(me, "a tensor of the plan has no weight, gradient or moments");
-  if (!(h->lr >= 0.0) || !std::isfinite(h->lr)) return report_invalid(me, "lr must be finite and not negative");
-  if (!(h->weight_decay >= 0.0) || !std::isfinite(h->weight_decay))
+  if (!(h->lr >= 0.0) || !std::isfinite(static_cast<float>(h->lr))) return report_invalid(me, "lr must be finite and not negative");
+  if (!(h->weight_decay >= 0.0) || !std::isfinite(static_cast<float>(h->weight_decay)))
     return report_invalid(me, "weight_decay must be finite and not negative");
   if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0))
     return report_invalid(me, "betas must be in [0, 1)");
-  if (!(static_cast<float>(h->eps) > 0.0f) || !std::isfinite(h->eps)) return report_invalid(me, "eps must be positive and finite");
+  if (!(static_cast<float>(h->eps) > 0.0f) || !std::isfinite(static_cast<float>(h->eps))) return report_invalid(me, "eps must be positive and finite");
   if (h->step == 0) return report_invalid(me, "step counts from 1");
   if (h->rounding > FR_ROUND_RANDOM) return report_invalid(me, "unknown rounding");
   if (h->reserved != 0) return report_invalid(me, "reserved must be 0");

@@ -286,6 +286,14 @@ int main() {
   steps.clear();
   h = good, h.beta2 = 1.0;
   CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
+  for (double bad : {1e300, -1.0, HUGE_VAL, NAN}) {
+    h = good, h.lr = bad;
+    CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
+    h = good, h.weight_decay = bad;
+    CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
+    h = good, h.eps = bad;
+    CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
+  }
   h = good, h.step = 0;
   CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
   CHECK(fr_adamw_step(p, &good, reinterpret_cast<fr_clip*>(4), nullptr) == FR_ERR_INVALID_ARG);
