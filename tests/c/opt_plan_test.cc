@@ -286,7 +286,7 @@ int main() {
   steps.clear();
   h = good, h.beta2 = 1.0;
   CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
-  for (double bad : {1e300, -1.0, HUGE_VAL, NAN}) {
+  for (double bad : {1e300, -1.0, HUGE_VAL, static_cast<double>(NAN)}) {
     h = good, h.lr = bad;
     CHECK(fr_adamw_step(p, &h, nullptr, nullptr) == FR_ERR_INVALID_ARG);
     h = good, h.weight_decay = bad;
