@@ -8,6 +8,7 @@ fallback of any kind.
 from __future__ import annotations
 
 import array
+import contextlib
 import ctypes
 import os
 from typing import List, Optional, Sequence
@@ -146,6 +147,15 @@ def _stream(stream) -> int:
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
+
+
+def _allocating_on(stream, device: torch.device):
+    """A context in which a tensor that a call on `stream` writes is allocated and filled in that stream's order."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return torch.cuda.stream(stream)
 
 
 def fr_dtype_of(t: torch.Tensor) -> int:
@@ -612,7 +622,9 @@ class OptPlan:
     def clip(self, max_norm: float = float("inf"), grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
              stream=None) -> torch.Tensor:
         """fr_grad_clip: returns the record, for step()."""
-        out = self.new_clip() if out is None else out
+        if out is None:
+            with _allocating_on(stream, self.device):
+                out = self.new_clip()
         fr_grad_clip(self.handle, max_norm, grad_scale, out, stream)
         return out
 

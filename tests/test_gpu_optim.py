@@ -349,6 +349,21 @@ def test_calls_back_to_back_and_from_a_graph_equal_calls_with_waits(bits):
         assert all(torch.equal(x, y) for x, y in zip(values, results[0][1]))
 
 
+@pytest.mark.parametrize("as_handle", [False, True])
+def test_a_record_made_for_another_stream_is_not_filled_later(as_handle):
+    """The current stream is busy while a norm runs on another one, which has a record of its own: whatever fills that must
+    not wait for the current stream's work and come after the norm."""
+    _, plan = _plan(_state(33, [5000, 300], "master", "f32", 32), 0)
+    want = plan.clip(0.5, 1.0)
+    torch.cuda.synchronize()
+    s, busy = torch.cuda.Stream(), torch.empty(1 << 30, dtype=torch.uint8, device="cuda")
+    for _ in range(100):  # 15 ms and more
+        busy.fill_(1)
+    got = plan.clip(0.5, 1.0, stream=s.cuda_stream if as_handle else s)
+    torch.cuda.synchronize()
+    assert torch.equal(got.view(torch.uint8), want.view(torch.uint8)) and float(fr.clip_view(want)[0]) > 0
+
+
 def test_offsets_past_32_bits():
     """A bf16 tensor of 2^33 + 777 elements with 8-bit moments (52 GB): its last blocks, where a pair's index passes 2^32,
     against the definition, and the norm of gradients that are zero but there."""
