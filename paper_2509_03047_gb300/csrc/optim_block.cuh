@@ -4,8 +4,12 @@
 // Where a tensor's buffers are aligned a block moves as vectors: lane l has the
 // elements 8 l ... 8 l + 7.  Else (and a conversion's last block of a tensor)
 // it moves element by element, lane l with the elements l, l + 32, ...  What lies
-// past the tensor's end reads as zero.  Both give the same bits.
+// past the tensor's end reads as zero.  Both give the same bits.  (The 8-bit
+// step brings whole blocks from any place to the vectors' order: fetch_odd,
+// take_odd, copy_out.)
 #pragma once
+
+#include <type_traits>
 
 #include "optim.h"
 #include "optim_math.cuh"
@@ -44,17 +48,32 @@ __device__ __forceinline__ void copy_16(uint32_t to, const void* from) {
 __device__ __forceinline__ void copy_8(uint32_t to, const void* from) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void copy_4(uint32_t to, const void* from) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t shared_4(uint32_t at) {
+  uint32_t q;
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q) : "r"(at));
+  return q;
+}
 __device__ __forceinline__ uint4 shared_16(uint32_t at) {
   uint4 q;
   asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at));
   return q;
 }
 
+// Bytes of the word before an address in it.
+__device__ __forceinline__ uint32_t odd_bytes(const void* p) { return static_cast<uint32_t>(reinterpret_cast<uint64_t>(p)) & 3; }
+
 // A lane's eight elements as they lie in memory, p: its place in the block.
 // load() brings them to registers; `left` of them are in the tensor, in its last
 // block fewer than eight, or none, and these go one by one.  fetch() starts the
 // whole block's way to shared memory, each copy of the warp 512 or 256
 // consecutive bytes, from where take() has them.
+// fetch_odd() and take_odd(): the same at any alignment.  A block off the boundary
+// that fetch() needs goes by the 4-byte words that hold its elements (of the first
+// and last one the neighbours' bytes too, which are dropped); if it starts inside
+// a word there is one more than it fills, which goes to `extra`.
 // (32 bytes go by one instruction: two of 16 bytes, each lane's beside one
 // another, write at 4.7 TB/s where this does at 7.0.)
 struct RawF32 {
@@ -69,6 +88,13 @@ struct RawF32 {
     const uint4 x = shared_16(from + 32 * lane), y = shared_16(from + 32 * lane + 16);
     a[0] = x.x, a[1] = x.y, a[2] = x.z, a[3] = x.w, a[4] = y.x, a[5] = y.y, a[6] = y.z, a[7] = y.w;
   }
+  static __device__ __forceinline__ void fetch_odd(uint32_t to, uint32_t, const void* p, int lane) {
+    if (reinterpret_cast<uint64_t>(p) % 16 == 0) return fetch(to, p, lane);
+    const uint8_t* q = static_cast<const uint8_t*>(p) - 28 * lane;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) copy_4(to + 128 * j + 4 * lane, q + 128 * j);
+  }
+  __device__ __forceinline__ void take_odd(uint32_t from, uint32_t, const void*, int lane) { take(from, lane); }
   __device__ __forceinline__ void load(const void* p, int left) {
     if (left >= kOptLane) {
       asm volatile("ld.global.L1::no_allocate.v8.u32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -91,6 +117,20 @@ struct RawBf16 {
   __device__ __forceinline__ void take(uint32_t from, int lane) {
     const uint4 q = shared_16(from + 16 * lane);
     a[0] = q.x, a[1] = q.y, a[2] = q.z, a[3] = q.w;
+  }
+  static __device__ __forceinline__ void fetch_odd(uint32_t to, uint32_t extra, const void* p, int lane) {
+    if (reinterpret_cast<uint64_t>(p) % 16 == 0) return fetch(to, p, lane);
+    const uint32_t shift = odd_bytes(p);
+    const uint8_t* q = static_cast<const uint8_t*>(p) - shift - 12 * lane;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) copy_4(to + 128 * j + 4 * lane, q + 128 * j);
+    if (shift && lane == 0) copy_4(extra, q + 512);
+  }
+  __device__ __forceinline__ void take_odd(uint32_t from, uint32_t extra, const void* p, int lane) {
+    take(from, lane);
+    const uint32_t shift = 8 * odd_bytes(p), more = shared_4(lane < 31 ? from + 16 * lane + 16 : extra);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __funnelshift_r(a[i], i < 3 ? a[i + 1] : more, shift);
   }
   __device__ __forceinline__ void load(const void* p, int left) {
     if (left >= kOptLane) {
@@ -115,6 +155,20 @@ struct RawCodes {
   static __device__ __forceinline__ void fetch(uint32_t to, const void* p, int lane) { copy_8(to + 8 * lane, p); }
   __device__ __forceinline__ void take(uint32_t from, int lane) {
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a[0]), "=r"(a[1]) : "r"(from + 8 * lane));
+  }
+  static __device__ __forceinline__ void fetch_odd(uint32_t to, uint32_t extra, const void* p, int lane) {
+    if (reinterpret_cast<uint64_t>(p) % 8 == 0) return fetch(to, p, lane);
+    const uint32_t shift = odd_bytes(p);
+    const uint8_t* q = static_cast<const uint8_t*>(p) - shift - 4 * lane;
+    copy_4(to + 4 * lane, q);
+    copy_4(to + 128 + 4 * lane, q + 128);
+    if (shift && lane == 0) copy_4(extra, q + 256);
+  }
+  __device__ __forceinline__ void take_odd(uint32_t from, uint32_t extra, const void* p, int lane) {
+    take(from, lane);
+    const uint32_t shift = 8 * odd_bytes(p), more = shared_4(lane < 31 ? from + 8 * lane + 8 : extra);
+    a[0] = __funnelshift_r(a[0], a[1], shift);
+    a[1] = __funnelshift_r(a[1], more, shift);
   }
   __device__ __forceinline__ void load(const void* p, int left) {
     if (left >= kOptLane) {
@@ -155,6 +209,28 @@ __device__ __forceinline__ void store_bytes(uint8_t* p, int left, const uint32_t
 #pragma unroll
   for (int j = 0; j < kOptLane; ++j)
     if (j < left) p[j] = static_cast<uint8_t>(w[j / 4] >> 8 * (j & 3));
+}
+// A whole block from shared memory, as the lanes have put it there at their
+// places: by vectors where it starts on their boundary, else element by element,
+// in each store of the warp 32 consecutive ones.  (By 4-byte words shifted
+// together, the first and the last by bytes: 2% slower.)
+template <class T>
+__device__ __forceinline__ void copy_out(void* block, const uint8_t* staged, int lane) {
+  using V = std::conditional_t<sizeof(T) == 1, uint2, uint4>;
+  constexpr int kVectors = kOptLane * sizeof(T) / sizeof(V);
+  if (reinterpret_cast<uint64_t>(block) % sizeof(V) == 0) {
+    V x[kVectors];
+#pragma unroll
+    for (int j = 0; j < kVectors; ++j) x[j] = reinterpret_cast<const V*>(staged)[32 * j + lane];
+#pragma unroll
+    for (int j = 0; j < kVectors; ++j) static_cast<V*>(block)[32 * j + lane] = x[j];
+    return;
+  }
+  T x[kOptLane];
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j) x[j] = reinterpret_cast<const T*>(staged)[32 * j + lane];
+#pragma unroll
+  for (int j = 0; j < kOptLane; ++j) static_cast<T*>(block)[32 * j + lane] = x[j];
 }
 // Of a lane's elements of a block of a tensor of n.
 __device__ __forceinline__ int elements_left(uint64_t n, uint32_t block, int lane) {

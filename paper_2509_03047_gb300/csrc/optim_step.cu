@@ -1,7 +1,7 @@
 // optim_step.cu -- the AdamW step over a list of tensors.
 //
 // One launch per class of tensors (parameter type, gradient type, moments in
-// 32 or 8 bits); one pass over each buffer, every element read, updated and
+// 32 bits, in 8, or in 8 off the vectors' boundaries); one pass over each buffer, every element read, updated and
 // written where it lies.  Bound by memory, and for 8-bit moments under bf16
 // weights without a master, at 10 bytes per element, by instructions too.
 //
@@ -19,8 +19,13 @@
 // registers 207 us and 2.38 ms; so 193 us (6.4 TB/s) and 2.31 ms (7.0).  At the
 // former's 10 bytes per element warps issue in three of four cycles.
 //
-// Tensors whose buffers lie off the vectors' boundaries in different ways go
-// element by element (Step::any): 8-bit moments at odd addresses 2.3 TB/s.
+// Tensors whose buffers lie off the vectors' boundaries in different ways: with
+// 32-bit moments element by element (Step::any), 5.1 to 5.5 TB/s.  With 8-bit ones
+// whole blocks come and go through shared memory, each buffer by vectors where it
+// can; 134 million elements in bf16 280 us with only the gradient off, 350 with
+// all (aligned 203, element by element 820), with masters 327 and 451 (313, 860).
+// Without the choice for each buffer 301 and 316, with masters 407 and 439: flat
+// groups of gradients beside states of their own are the more usual.
 #include <type_traits>
 
 #include "kernels.h"
@@ -48,15 +53,17 @@ __device__ __forceinline__ Hyper hyper(const StepParams& p, float scale, const O
   return {p.numbers, scale, __fmul_rn(p.lr, d.lr_scale), __fmul_rn(p.decay, d.decay_scale)};
 }
 
-template <int Weight, bool Bf16Grad, bool Eight, bool Random>
+template <int Weight, bool Bf16Grad, bool Eight, bool Odd, bool Random>
 struct Step {
   using RawGrad = std::conditional_t<Bf16Grad, RawBf16, RawF32>;
   using RawParam = std::conditional_t<Weight == kWeightBf16, RawBf16, RawF32>;
   using RawMoment = std::conditional_t<Eight, RawCodes, RawF32>;
   static constexpr int kGradBytes = RawGrad::kBytes, kMomentBytes = RawMoment::kBytes;
 
-  // Of a block in shared memory, and how many (a CTA's stay under 48 KiB).
-  static constexpr int kSlot = kOptBlock * (kGradBytes + RawParam::kBytes + 2 * kMomentBytes), kSlots = kSlot <= 1536 ? 3 : 2;
+  // Of a block in shared memory (Odd: and the four buffers' extra words, see
+  // fetch_odd), and how many (a CTA's stay under 48 KiB).
+  static constexpr int kSlot = kOptBlock * (kGradBytes + RawParam::kBytes + 2 * kMomentBytes), kSlotSize = kSlot + (Odd ? 16 : 0),
+                       kSlots = kSlot <= 1536 ? 3 : 2;
   // The lane's places in a block.
   struct Places {
     const uint8_t* g;
@@ -88,7 +95,8 @@ struct Step {
       p.load(at.p + ahead * (kOptBlock * RawParam::kBytes), left);
     }
   };
-  // The rest of it; em and ev: its exponents, old and new.
+  // The rest of it; em and ev: its exponents, old and new.  Odd: stores go to the
+  // lane's places in shared memory, `at` points there.
   static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, int left, uint32_t counter, RandomKey key, const Raw& r,
                                                 uint32_t& em, uint32_t& ev) {
     Pair g[4], p[4], m[4], v[4];
@@ -124,7 +132,12 @@ struct Step {
       for (int j = 0; j < 4; ++j) w[j] = Random ? random_bf16x2(p[j], u[j]) : nearest_bf16x2(p[j]);
       store_bf16(at.p, left, w);
     } else {
-      store_f32(at.p, left, p);
+      if constexpr (Odd) {
+        reinterpret_cast<float4*>(at.p)[0] = make_float4(p[0].x, p[0].y, p[1].x, p[1].y);
+        reinterpret_cast<float4*>(at.p)[1] = make_float4(p[2].x, p[2].y, p[3].x, p[3].y);
+      } else {
+        store_f32(at.p, left, p);
+      }
       if (Weight == kWeightMaster) {
         uint32_t w[4];
 #pragma unroll
@@ -162,22 +175,29 @@ struct Step {
     one(hyper(p, scale, d), d, d.n_blocks - 1, key, threadIdx.x % 32);
   }
 
-  // `count` whole blocks of an aligned tensor one after the other, the next one or
-  // two on their way through shared memory.  Not unrolled: the code must stay in
-  // the instruction cache.
+  // `count` whole blocks of a tensor one after the other, the next one or two on
+  // their way through shared memory.  Not unrolled: the code must stay in the
+  // instruction cache.  Odd: off the vectors' boundaries; results leave by way of
+  // the slot that their block came to.
   static __device__ __forceinline__ void run(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
-    __shared__ __align__(16) uint8_t slots[Eight ? kOptWarps * kSlots * kSlot : 16];
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(slots)) + (threadIdx.x / 32) * (kSlots * kSlot);
+    __shared__ __align__(16) uint8_t slots[Eight ? kOptWarps * kSlots * kSlotSize : 16];
+    uint8_t* const my_slots = slots + (threadIdx.x / 32) * (kSlots * kSlotSize);
+    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(my_slots));
     Places at(d, block, lane);
     // (a run does not pass a multiple of 2^32 pairs: see run_length)
     uint32_t counter = random_counter(key, static_cast<uint64_t>(block) * (kOptBlock / 2) + 4 * lane);
     constexpr int kAtP = kOptBlock * kGradBytes, kAtM = kAtP + kOptBlock * RawParam::kBytes, kAtV = kAtM + kOptBlock * kMomentBytes;
     auto fetch = [&](int ahead, int slot) {
-      const uint32_t to = mine + slot * kSlot;
-      RawGrad::fetch(to, at.g + ahead * (kOptBlock * kGradBytes), lane);
-      RawParam::fetch(to + kAtP, at.p + ahead * (kOptBlock * RawParam::kBytes), lane);
-      RawMoment::fetch(to + kAtM, at.m + ahead * (kOptBlock * kMomentBytes), lane);
-      RawMoment::fetch(to + kAtV, at.v + ahead * (kOptBlock * kMomentBytes), lane);
+      const uint32_t to = mine + slot * kSlotSize;
+      auto one = [&](auto raw, int offset, int extra, const uint8_t* p) {
+        using R = decltype(raw);
+        p += ahead * (kOptBlock * R::kBytes);
+        Odd ? R::fetch_odd(to + offset, to + kSlot + extra, p, lane) : R::fetch(to + offset, p, lane);
+      };
+      one(RawGrad(), 0, 0, at.g);
+      one(RawParam(), kAtP, 4, at.p);
+      one(RawMoment(), kAtM, 8, at.m);
+      one(RawMoment(), kAtV, 12, at.v);
     };
 #pragma unroll
     for (int k = 0; k < kSlots - 1; ++k) {
@@ -195,14 +215,35 @@ struct Step {
       asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 1) : "memory");
       __syncwarp();  // what the other lanes fetched is there
       Raw r;
-      const uint32_t from = mine + slot * kSlot;
-      r.g.take(from, lane);
-      r.p.take(from + kAtP, lane);
-      r.m.take(from + kAtM, lane);
-      r.v.take(from + kAtV, lane);
+      const uint32_t from = mine + slot * kSlotSize;
+      auto take = [&](auto& raw, int offset, int extra, const uint8_t* p) {
+        Odd ? raw.take_odd(from + offset, from + kSlot + extra, p, lane) : raw.take(from + offset, lane);
+      };
+      take(r.g, 0, 0, at.g);
+      take(r.p, kAtP, 4, at.p);
+      take(r.m, kAtM, 8, at.m);
+      take(r.v, kAtV, 12, at.v);
       __syncwarp();  // and taken, before the next turn fetches into the slot
       em = e.of_m(k), ev = e.of_v(k);
-      finish(h, at, kOptLane, counter, key, r, em, ev);
+      if constexpr (Odd) {
+        constexpr int kP = 0, kW = kOptBlock * RawParam::kBytes, kM = kW + (Weight == kWeightMaster ? kOptBlock * 2 : 0), kV = kM + kOptBlock;
+        static_assert(kV + kOptBlock <= kSlot, "a block's results in its slot");
+        uint8_t* const out = my_slots + slot * kSlotSize;
+        Places to = at;
+        to.p = out + kP + lane * kOptLane * RawParam::kBytes;
+        to.w = out + kW + lane * kOptLane * 2;
+        to.m = out + kM + lane * kOptLane;
+        to.v = out + kV + lane * kOptLane;
+        finish(h, to, kOptLane, counter, key, r, em, ev);
+        __syncwarp();
+        copy_out<std::conditional_t<Weight == kWeightBf16, uint16_t, float>>(at.p - lane * kOptLane * RawParam::kBytes, out + kP, lane);
+        if (Weight == kWeightMaster) copy_out<uint16_t>(at.w - lane * kOptLane * 2, out + kW, lane);
+        copy_out<uint8_t>(at.m - lane * kOptLane, out + kM, lane);
+        copy_out<uint8_t>(at.v - lane * kOptLane, out + kV, lane);
+        __syncwarp();  // as above
+      } else {
+        finish(h, at, kOptLane, counter, key, r, em, ev);
+      }
       e.set(k, lane, em, ev);
       if (++k == count) break;
       slot = slot == kSlots - 1 ? 0 : slot + 1;
@@ -212,7 +253,8 @@ struct Step {
     e.store(d.m_exp + block, d.v_exp + block, count, lane);
   }
 
-  // Any block of tensor t, element by element.
+  // Any block of tensor t, element by element: with 8-bit moments a tensor's last,
+  // where its buffers are not aligned, and all for an eps that is too small.
   static __device__ __noinline__ void any(const StepParams& p, float scale, uint32_t t, uint32_t block) {
     const OptDesc d = p.work.tensors[t];
     const int lane = threadIdx.x % 32;
@@ -276,9 +318,9 @@ __device__ __forceinline__ uint32_t run_length(uint32_t block) {
   return kBlocks - block % kBlocks;
 }
 
-template <int Weight, bool Bf16Grad, bool Eight, bool Random>
+template <int Weight, bool Bf16Grad, bool Eight, bool Odd, bool Random>
 __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16Grad)) step_kernel(const __grid_constant__ StepParams p) {
-  using S = Step<Weight, Bf16Grad, Eight, Random>;
+  using S = Step<Weight, Bf16Grad, Eight, Odd, Random>;
   const uint32_t per_warp = Eight ? p.work.per_warp : 1, warp = threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
   uint32_t b = (blockIdx.x * kOptWarps + warp) * per_warp;
@@ -296,16 +338,16 @@ __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16G
   for (;;) {
     const uint32_t block = b - d.first;
     uint32_t count = 1;
-    if (d.aligned && !p.exact) {
+    const uint32_t whole = static_cast<uint32_t>(d.n / kOptBlock);
+    if (Odd ? !p.exact && block < whole : d.aligned && !p.exact) {
       RandomKey key = {0, 0};
       if (Random) key = random_key(p.key, d.tensor);
-      const uint32_t whole = static_cast<uint32_t>(d.n / kOptBlock);
       if (!Eight) {
         S::one(hyper(p, scale, d), d, block, key, lane);
       } else if (block < whole) {
         count = min(min(end - b, whole - block), run_length(block));
         S::run(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
-      } else {
+      } else if (!Odd) {
         S::last(p, scale, t);
       }
     } else {
@@ -320,17 +362,21 @@ __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16G
 
 template <class F>
 auto for_class(const StepClass& c, bool random, F&& f) {
-  auto with = [&](auto weight, auto grad, auto eight) {
+  auto with = [&](auto weight, auto grad, auto eight, auto odd) {
     // random rounding concerns codes, and bf16 weights without a master
-    if constexpr (decltype(eight)::value || decltype(weight)::value == kWeightBf16)
-      if (random) return f(step_kernel<decltype(weight)::value, decltype(grad)::value, decltype(eight)::value, true>);
-    return f(step_kernel<decltype(weight)::value, decltype(grad)::value, decltype(eight)::value, false>);
+    constexpr int kWeight = decltype(weight)::value;
+    constexpr bool kGrad = decltype(grad)::value, kEight = decltype(eight)::value, kOdd = decltype(odd)::value;
+    if constexpr (kEight || kWeight == kWeightBf16)
+      if (random) return f(step_kernel<kWeight, kGrad, kEight, kOdd, true>);
+    return f(step_kernel<kWeight, kGrad, kEight, kOdd, false>);
   };
-  auto with_types = [&](auto weight) {
-    if (c.bf16_grad)
-      return c.eight ? with(weight, std::true_type(), std::true_type()) : with(weight, std::true_type(), std::false_type());
-    return c.eight ? with(weight, std::false_type(), std::true_type()) : with(weight, std::false_type(), std::false_type());
+  const std::true_type yes;
+  const std::false_type no;
+  auto with_moments = [&](auto weight, auto grad) {
+    if (!c.eight) return with(weight, grad, no, no);
+    return c.odd ? with(weight, grad, yes, yes) : with(weight, grad, yes, no);
   };
+  auto with_types = [&](auto weight) { return c.bf16_grad ? with_moments(weight, yes) : with_moments(weight, no); };
   if (c.weight == kWeightMaster) return with_types(std::integral_constant<int, kWeightMaster>());
   if (c.weight == kWeightBf16) return with_types(std::integral_constant<int, kWeightBf16>());
   return with_types(std::integral_constant<int, kWeightF32>());

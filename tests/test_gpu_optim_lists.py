@@ -99,6 +99,28 @@ def test_buffers_that_start_at_different_places(param, bits):
     _check_step(host, {k: x.get() for k, x in b.items()}, h, scale, bits == 8)
 
 
+@pytest.mark.parametrize("rounding", [0, 1])
+@pytest.mark.parametrize("param,grad", [("master", "f32"), ("master", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
+def test_runs_of_blocks_have_the_same_bits_at_every_place(param, grad, rounding):
+    """As test_runs_of_blocks, three steps, every buffer or only some of them off the vectors' boundaries, by all numbers of
+    bytes that a word has: each byte is the one that aligned buffers get, and none outside the tensors changes."""
+    sizes = [2_000_003, 255, 256, 1_500_001, 77, 300_000, 512 * 256]
+    host = _state(10, sizes, param, grad, 8)
+    results = []
+    for shifts in ({}, {"grad": 1}, {"m": 2, "v": 5, "weight": 3}, {"weight": 1, "grad": 3, "masters": 2, "m": 1, "v": 3}):
+        b = {k: Buffers(v, shifts.get(k, 0)) for k, v in host.items()}
+        names = {"weight": "weights", "grad": "grads"}
+        plan = fr.OptPlan(**{names.get(k, k): x.tensors for k, x in b.items()})
+        assert plan.n_blocks > 2 * 7296
+        for t in range(1, 4):
+            plan.step(_hyper(ref.Numbers(seed=3, step=t), rounding), _record(0.375))
+        results.append({k: x.get() for k, x in b.items()})
+    for other in results[1:]:
+        for k, arrays in results[0].items():
+            for x, y in zip(arrays, other[k]):
+                assert x.tobytes() == y.tobytes(), k
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 def test_a_tiny_eps_keeps_the_formula_where_second_moments_are_subnormal(bits):
     """Gradients of 2^-66 to 2^-70 with eps = 1e-30: squares from 2^-132 to 2^-140, exact in fp32's subnormal numbers, as is the
