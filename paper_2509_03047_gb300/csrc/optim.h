@@ -84,16 +84,17 @@ cudaError_t launch_clip(const ClipParams& p, cudaStream_t s);
 
 // ---- the step
 
-// Tensors of one launch have one type of everything.  Those of 8-bit moments
-// whose buffers are not all aligned have launches of their own: in one kernel with
-// the others they cost these up to 1% (10,000 tensors of 1 to 28,000 elements 3%).
+// Tensors of one launch have one type of everything.  Those that are odd (not all
+// buffers on the vectors' boundaries, and a whole block) have launches of their
+// own: in one kernel with the others they cost these up to 1% with 8-bit moments
+// (10,000 tensors of 1 to 28,000 elements 3%).
 enum : int { kWeightF32 = 0, kWeightBf16 = 1, kWeightMaster = 2 };  // the parameter: fp32 weight, bf16 weight, master
 struct StepClass {
   int weight;
   bool bf16_grad, eight, odd;
-  int index() const { return (weight * 2 + bf16_grad) * 3 + eight + odd; }
+  int index() const { return ((weight * 2 + bf16_grad) * 2 + eight) * 2 + odd; }
 };
-constexpr int kStepClasses = 3 * 2 * 3;
+constexpr int kStepClasses = 3 * 2 * 2 * 2;
 
 using Pair = float2;
 
@@ -113,8 +114,9 @@ struct StepParams {
 };
 // CTAs of eight warps per SM, what the registers of a lane's elements allow.  (Of
 // the 8-bit classes the one that loads least gains by a fourth: GPT-2 small 193 us,
-// 200 with three; with masters 299 with four, 290 with three.)
-constexpr int step_ctas(bool eight, int weight, bool bf16_grad) { return eight && !(weight == kWeightBf16 && bf16_grad) ? 3 : 4; }
+// 200 with three; with masters 299 with four, 290 with three.  Odd ones with every
+// buffer off: 345 with four, 332 with three.)
+constexpr int step_ctas(bool eight, int weight, bool bf16_grad, bool odd) { return eight && (odd || !(weight == kWeightBf16 && bf16_grad)) ? 3 : 4; }
 // Consecutive blocks per warp.
 inline uint32_t step_blocks(bool eight, uint64_t n_blocks) {
   if (!eight) return 1;

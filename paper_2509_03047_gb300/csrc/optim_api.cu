@@ -171,9 +171,9 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
       c.weight = x.master ? kWeightMaster : x.weight_dtype == FR_DT_BF16 ? kWeightBf16 : kWeightF32;
       c.bf16_grad = x.grad_dtype == FR_DT_BF16;
       c.eight = x.state_dtype == FR_DT_BYTES;
-      c.odd = c.eight && !d.aligned;
-      p->classes[c.index()] = c;
       const uint64_t head = head_elems(x, c);
+      c.odd = !d.aligned && head == 0 && x.n >= kOptBlock;
+      p->classes[c.index()] = c;
       if (head > 0 && head < x.n) {
         p->step[c.index()].add(part(d, x, 0, head));
         p->step[c.index()].add(part(d, x, head, x.n - head));

@@ -4,9 +4,9 @@
 // Where a tensor's buffers are aligned a block moves as vectors: lane l has the
 // elements 8 l ... 8 l + 7.  Else (and a conversion's last block of a tensor)
 // it moves element by element, lane l with the elements l, l + 32, ...  What lies
-// past the tensor's end reads as zero.  Both give the same bits.  (The 8-bit
-// step brings whole blocks from any place to the vectors' order: fetch_odd,
-// take_odd, copy_out.)
+// past the tensor's end reads as zero.  Both give the same bits.  (The step
+// brings whole blocks from any place to the vectors' order: fetch_odd, take_odd,
+// copy_out.)
 #pragma once
 
 #include <type_traits>

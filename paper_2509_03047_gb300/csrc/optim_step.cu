@@ -1,7 +1,7 @@
 // optim_step.cu -- the AdamW step over a list of tensors.
 //
 // One launch per class of tensors (parameter type, gradient type, moments in
-// 32 bits, in 8, or in 8 off the vectors' boundaries); one pass over each buffer, every element read, updated and
+// 32 or 8 bits, on the vectors' boundaries or off them); one pass over each buffer, every element read, updated and
 // written where it lies.  Bound by memory, and for 8-bit moments under bf16
 // weights without a master, at 10 bytes per element, by instructions too.
 //
@@ -19,13 +19,14 @@
 // registers 207 us and 2.38 ms; so 193 us (6.4 TB/s) and 2.31 ms (7.0).  At the
 // former's 10 bytes per element warps issue in three of four cycles.
 //
-// Tensors whose buffers lie off the vectors' boundaries in different ways: with
-// 32-bit moments element by element (Step::any), 5.1 to 5.5 TB/s.  With 8-bit ones
-// whole blocks come and go through shared memory, each buffer by vectors where it
-// can; 134 million elements in bf16 280 us with only the gradient off, 350 with
-// all (aligned 203, element by element 820), with masters 327 and 451 (313, 860).
-// Without the choice for each buffer 301 and 316, with masters 407 and 439: flat
-// groups of gradients beside states of their own are the more usual.
+// Tensors whose buffers lie off the vectors' boundaries in different ways: whole
+// blocks come and go through shared memory, each buffer by vectors where it can.
+// 134 million elements (aligned; only the gradient off; every buffer off; and one
+// buffer off, by Step::any): bf16 with 32-bit moments 419, 456, 532 and 568 us,
+// with 8-bit ones 203, 278, 332 and 817; with masters 533, 560, 657 and 679, and
+// 313, 326, 449 and 861.  (8-bit without the choice for each buffer 301 and 316,
+// with masters 407 and 439: flat groups of gradients beside states of their own
+// are the more usual.)
 #include <type_traits>
 
 #include "kernels.h"
@@ -63,7 +64,7 @@ struct Step {
   // Of a block in shared memory (Odd: and the four buffers' extra words, see
   // fetch_odd), and how many (a CTA's stay under 48 KiB).
   static constexpr int kSlot = kOptBlock * (kGradBytes + RawParam::kBytes + 2 * kMomentBytes), kSlotSize = kSlot + (Odd ? 16 : 0),
-                       kSlots = kSlot <= 1536 ? 3 : 2;
+                       kSlots = !Eight ? 1 : kSlot <= 1536 ? 3 : 2;
   // The lane's places in a block.
   struct Places {
     const uint8_t* g;
@@ -95,6 +96,14 @@ struct Step {
       p.load(at.p + ahead * (kOptBlock * RawParam::kBytes), left);
     }
   };
+  static __device__ __forceinline__ void put_f32(uint8_t* at, int left, const Pair (&x)[4]) {
+    if constexpr (Odd) {
+      reinterpret_cast<float4*>(at)[0] = make_float4(x[0].x, x[0].y, x[1].x, x[1].y);
+      reinterpret_cast<float4*>(at)[1] = make_float4(x[2].x, x[2].y, x[3].x, x[3].y);
+    } else {
+      store_f32(at, left, x);
+    }
+  }
   // The rest of it; em and ev: its exponents, old and new.  Odd: stores go to the
   // lane's places in shared memory, `at` points there.
   static __device__ __forceinline__ void finish(const Hyper& h, const Places& at, int left, uint32_t counter, RandomKey key, const Raw& r,
@@ -132,12 +141,7 @@ struct Step {
       for (int j = 0; j < 4; ++j) w[j] = Random ? random_bf16x2(p[j], u[j]) : nearest_bf16x2(p[j]);
       store_bf16(at.p, left, w);
     } else {
-      if constexpr (Odd) {
-        reinterpret_cast<float4*>(at.p)[0] = make_float4(p[0].x, p[0].y, p[1].x, p[1].y);
-        reinterpret_cast<float4*>(at.p)[1] = make_float4(p[2].x, p[2].y, p[3].x, p[3].y);
-      } else {
-        store_f32(at.p, left, p);
-      }
+      put_f32(at.p, left, p);
       if (Weight == kWeightMaster) {
         uint32_t w[4];
 #pragma unroll
@@ -149,8 +153,8 @@ struct Step {
       em = store_codes<true, Random>(m, u, at.m, left);
       ev = store_codes<false, Random>(v, u, at.v, left);
     } else {
-      store_f32(at.m, left, m);
-      store_f32(at.v, left, v);
+      put_f32(at.m, left, m);
+      put_f32(at.v, left, v);
     }
   }
 
@@ -180,7 +184,7 @@ struct Step {
   // instruction cache.  Odd: off the vectors' boundaries; results leave by way of
   // the slot that their block came to.
   static __device__ __forceinline__ void run(const Hyper& h, const OptDesc& d, uint32_t block, int count, RandomKey key, int lane) {
-    __shared__ __align__(16) uint8_t slots[Eight ? kOptWarps * kSlots * kSlotSize : 16];
+    __shared__ __align__(16) uint8_t slots[kOptWarps * kSlots * kSlotSize];
     uint8_t* const my_slots = slots + (threadIdx.x / 32) * (kSlots * kSlotSize);
     const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(my_slots));
     Places at(d, block, lane);
@@ -205,8 +209,8 @@ struct Step {
       asm volatile("cp.async.commit_group;" ::: "memory");
     }
     uint32_t em, ev;
-    Exponents e;
-    e.load(d.m_exp + block, d.v_exp + block, count, lane);
+    Exponents e = {0, 0};
+    if (Eight) e.load(d.m_exp + block, d.v_exp + block, count, lane);
 #pragma unroll 1
     for (int k = 0, slot = 0;;) {
       // into the slot that the block before has left
@@ -226,20 +230,21 @@ struct Step {
       __syncwarp();  // and taken, before the next turn fetches into the slot
       em = e.of_m(k), ev = e.of_v(k);
       if constexpr (Odd) {
-        constexpr int kP = 0, kW = kOptBlock * RawParam::kBytes, kM = kW + (Weight == kWeightMaster ? kOptBlock * 2 : 0), kV = kM + kOptBlock;
-        static_assert(kV + kOptBlock <= kSlot, "a block's results in its slot");
+        constexpr int kP = 0, kW = kOptBlock * RawParam::kBytes, kM = kW + (Weight == kWeightMaster ? kOptBlock * 2 : 0), kV = kM + kOptBlock * kMomentBytes;
+        static_assert(kV + kOptBlock * kMomentBytes <= kSlot, "a block's results in its slot");
         uint8_t* const out = my_slots + slot * kSlotSize;
         Places to = at;
         to.p = out + kP + lane * kOptLane * RawParam::kBytes;
         to.w = out + kW + lane * kOptLane * 2;
-        to.m = out + kM + lane * kOptLane;
-        to.v = out + kV + lane * kOptLane;
+        to.m = out + kM + lane * kOptLane * kMomentBytes;
+        to.v = out + kV + lane * kOptLane * kMomentBytes;
         finish(h, to, kOptLane, counter, key, r, em, ev);
         __syncwarp();
         copy_out<std::conditional_t<Weight == kWeightBf16, uint16_t, float>>(at.p - lane * kOptLane * RawParam::kBytes, out + kP, lane);
         if (Weight == kWeightMaster) copy_out<uint16_t>(at.w - lane * kOptLane * 2, out + kW, lane);
-        copy_out<uint8_t>(at.m - lane * kOptLane, out + kM, lane);
-        copy_out<uint8_t>(at.v - lane * kOptLane, out + kV, lane);
+        using Moment = std::conditional_t<Eight, uint8_t, float>;
+        copy_out<Moment>(at.m - lane * kOptLane * kMomentBytes, out + kM, lane);
+        copy_out<Moment>(at.v - lane * kOptLane * kMomentBytes, out + kV, lane);
         __syncwarp();  // as above
       } else {
         finish(h, at, kOptLane, counter, key, r, em, ev);
@@ -250,11 +255,11 @@ struct Step {
       counter += kOptBlock / 2 * kRandomStep;
       at.next();
     }
-    e.store(d.m_exp + block, d.v_exp + block, count, lane);
+    if (Eight) e.store(d.m_exp + block, d.v_exp + block, count, lane);
   }
 
-  // Any block of tensor t, element by element: with 8-bit moments a tensor's last,
-  // where its buffers are not aligned, and all for an eps that is too small.
+  // Any block of tensor t, element by element: a tensor's last one, or a head of
+  // less than a block, off the vectors' boundaries; all for an eps that is too small.
   static __device__ __noinline__ void any(const StepParams& p, float scale, uint32_t t, uint32_t block) {
     const OptDesc d = p.work.tensors[t];
     const int lane = threadIdx.x % 32;
@@ -319,7 +324,7 @@ __device__ __forceinline__ uint32_t run_length(uint32_t block) {
 }
 
 template <int Weight, bool Bf16Grad, bool Eight, bool Odd, bool Random>
-__global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16Grad)) step_kernel(const __grid_constant__ StepParams p) {
+__global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16Grad, Odd)) step_kernel(const __grid_constant__ StepParams p) {
   using S = Step<Weight, Bf16Grad, Eight, Odd, Random>;
   const uint32_t per_warp = Eight ? p.work.per_warp : 1, warp = threadIdx.x / 32;
   const int lane = threadIdx.x % 32;
@@ -342,10 +347,10 @@ __global__ void __launch_bounds__(32 * kOptWarps, step_ctas(Eight, Weight, Bf16G
     if (Odd ? !p.exact && block < whole : d.aligned && !p.exact) {
       RandomKey key = {0, 0};
       if (Random) key = random_key(p.key, d.tensor);
-      if (!Eight) {
+      if constexpr (!Eight && !Odd) {
         S::one(hyper(p, scale, d), d, block, key, lane);
       } else if (block < whole) {
-        count = min(min(end - b, whole - block), run_length(block));
+        if (Eight) count = min(min(end - b, whole - block), run_length(block));
         S::run(hyper(p, scale, d), d, block, static_cast<int>(count), key, lane);
       } else if (!Odd) {
         S::last(p, scale, t);
@@ -373,8 +378,8 @@ auto for_class(const StepClass& c, bool random, F&& f) {
   const std::true_type yes;
   const std::false_type no;
   auto with_moments = [&](auto weight, auto grad) {
-    if (!c.eight) return with(weight, grad, no, no);
-    return c.odd ? with(weight, grad, yes, yes) : with(weight, grad, yes, no);
+    if (c.odd) return c.eight ? with(weight, grad, yes, yes) : with(weight, grad, no, yes);
+    return c.eight ? with(weight, grad, yes, no) : with(weight, grad, no, no);
   };
   auto with_types = [&](auto weight) { return c.bf16_grad ? with_moments(weight, yes) : with_moments(weight, no); };
   if (c.weight == kWeightMaster) return with_types(std::integral_constant<int, kWeightMaster>());

@@ -100,12 +100,13 @@ def test_buffers_that_start_at_different_places(param, bits):
 
 
 @pytest.mark.parametrize("rounding", [0, 1])
+@pytest.mark.parametrize("bits", [8, 32])
 @pytest.mark.parametrize("param,grad", [("master", "f32"), ("master", "bf16"), ("bf16", "bf16"), ("f32", "f32")])
-def test_runs_of_blocks_have_the_same_bits_at_every_place(param, grad, rounding):
+def test_runs_of_blocks_have_the_same_bits_at_every_place(param, grad, bits, rounding):
     """As test_runs_of_blocks, three steps, every buffer or only some of them off the vectors' boundaries, by all numbers of
     bytes that a word has: each byte is the one that aligned buffers get, and none outside the tensors changes."""
     sizes = [2_000_003, 255, 256, 1_500_001, 77, 300_000, 512 * 256]
-    host = _state(10, sizes, param, grad, 8)
+    host = _state(10, sizes, param, grad, bits)
     results = []
     for shifts in ({}, {"grad": 1}, {"m": 2, "v": 5, "weight": 3}, {"weight": 1, "grad": 3, "masters": 2, "m": 1, "v": 3}):
         b = {k: Buffers(v, shifts.get(k, 0)) for k, v in host.items()}
