@@ -154,7 +154,8 @@ def _allocating_on(stream, device: torch.device):
     if stream is None:
         return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(stream), device=device)
+        # 0 and 1 are the legacy default stream's handles; torch makes a stream of its own of a 0, and takes no 1
+        stream = torch.cuda.default_stream(device) if int(stream) in (0, 1) else torch.cuda.ExternalStream(int(stream), device=device)
     return torch.cuda.stream(stream)
 
 

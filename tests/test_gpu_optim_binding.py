@@ -1,0 +1,28 @@
+"""The binding of the optimizer step: streams by handle."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+fr = pytest.importorskip("paper_2509_03047_gb300.flashrec")
+
+
+@pytest.mark.parametrize("handle", [0, 1])
+def test_a_record_for_the_default_stream_by_handle_is_made_in_its_order(handle):
+    """0 and 1 both name the legacy default stream, which is torch's default stream; a call with the handle gives the record
+    that one without it gives, also from inside another stream's context."""
+    device = torch.device("cuda", torch.cuda.current_device())
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with fr._allocating_on(handle, device):
+            assert torch.cuda.current_stream() == torch.cuda.default_stream()
+        assert torch.cuda.current_stream() == side
+    plan = fr.OptPlan(grads=[torch.linspace(-1, 1, 70001, device="cuda")])
+    want = plan.clip(0.5, 0.25)
+    torch.cuda.synchronize()
+    got = plan.clip(0.5, 0.25, stream=handle)
+    with torch.cuda.stream(side):
+        aside = plan.clip(0.5, 0.25, stream=handle)
+    torch.cuda.synchronize()
+    assert float(fr.clip_view(want)[0]) > 0
+    assert torch.equal(got, want) and torch.equal(aside, want)
