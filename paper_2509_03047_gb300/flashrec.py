@@ -600,7 +600,8 @@ class OptPlan:
                  decay_scale=None):
         lists = [weights, grads, m, v, masters, m_exp, v_exp]
         self.buffers = [None if x is None else list(x) for x in lists]  # the plan holds their addresses
-        first = next((t for x in self.buffers if x for t in x if t is not None), None)
+        # (a tensor without elements may lie anywhere)
+        first = next((t for x in self.buffers if x for t in x if t is not None and t.is_cuda), None)
         self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
         self.handle = None
         self.handle = fr_opt_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale)

@@ -1,4 +1,4 @@
-"""The binding of the optimizer step: streams by handle."""
+"""The binding of the optimizer step: streams by handle, the device of a list."""
 import pytest
 import torch
 
@@ -26,3 +26,13 @@ def test_a_record_for_the_default_stream_by_handle_is_made_in_its_order(handle):
     torch.cuda.synchronize()
     assert float(fr.clip_view(want)[0]) > 0
     assert torch.equal(got, want) and torch.equal(aside, want)
+
+
+@pytest.mark.parametrize("sizes", [(5,), (5, 0), ()])
+def test_a_list_that_starts_with_an_empty_host_tensor_has_its_records_on_the_gpu(sizes):
+    grads = [torch.empty(0)] + [torch.full((n,), 2.0, device="cuda") for n in sizes]
+    plan = fr.OptPlan(grads=grads)
+    record = plan.clip()
+    assert plan.device.type == record.device.type == "cuda"
+    norm, scale, bad = (x.item() for x in fr.clip_view(record))
+    assert abs(norm - 2.0 * sum(sizes) ** 0.5) <= 1e-6 and scale == 1.0 and bad == 0
