@@ -382,6 +382,7 @@ def _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scal
     count = len(given[0])
     sizes = [None] * count
     columns, codes = [], {}
+    device = None  # of every tensor that has elements
     for name, tensors, allowed, per in lists:
         if tensors is None:
             columns.append([0] * count)
@@ -396,8 +397,12 @@ def _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scal
                 code.append(0)
                 continue
             n = t.numel()
-            if n and not t.is_cuda:
-                raise ValueError("%s[%d] is not on a CUDA device" % (name, i))
+            if n and t.get_device() != device:
+                if not t.is_cuda:
+                    raise ValueError("%s[%d] is not on a CUDA device" % (name, i))
+                if device is not None:
+                    raise ValueError("%s[%d] is on CUDA device %d, the tensors before it on %d" % (name, i, t.get_device(), device))
+                device = t.get_device()
             if not t.is_contiguous():
                 raise ValueError("%s[%d] is not contiguous" % (name, i))
             c = allowed.get(t.dtype)
@@ -416,6 +421,8 @@ def _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scal
         codes[name] = code
     if any(a != b for a, b in zip(codes["m"], codes["v"])):
         raise ValueError("m and v differ in type")
+    if device is not None and device != torch.cuda.current_device():  # the one that the plan is bound to
+        raise ValueError("the tensors are on CUDA device %d, the current one is %d" % (device, torch.cuda.current_device()))
 
     def factors(x):
         x = array.array("f", [1.0] * count if x is None else x)
@@ -435,8 +442,9 @@ def _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scal
 
 def fr_opt_create(weights=None, grads=None, m=None, v=None, masters=None, m_exp=None, v_exp=None, lr_scale=None,
                   decay_scale=None):
-    """Plan over lists of contiguous CUDA tensors (a list, or an entry, may be None; factors default to 1).  Moments
-    are fp32, or uint8 codes with one uint8 exponent per FR_OPT_BLOCK elements.  Returns the opaque handle (int)."""
+    """Plan over lists of contiguous CUDA tensors on the current device (a list, or an entry, may be None; factors default
+    to 1).  Moments are fp32, or uint8 codes with one uint8 exponent per FR_OPT_BLOCK elements.  Returns the opaque handle
+    (int)."""
     arr, count = _opt_array(weights, grads, m, v, masters, m_exp, v_exp, lr_scale, decay_scale)
     h = ctypes.c_void_p()
     _check(lib.fr_opt_create(arr, count, ctypes.byref(h)), "fr_opt_create")
@@ -601,7 +609,7 @@ class OptPlan:
         lists = [weights, grads, m, v, masters, m_exp, v_exp]
         self.buffers = [None if x is None else list(x) for x in lists]  # the plan holds their addresses
         # (a tensor without elements may lie anywhere)
-        first = next((t for x in self.buffers if x for t in x if t is not None and t.is_cuda), None)
+        first = next((t for x in self.buffers if x for t in x if t is not None and t.numel()), None)
         self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
         self.handle = None
         self.handle = fr_opt_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale)
@@ -621,16 +629,23 @@ class OptPlan:
     def new_clip(self) -> torch.Tensor:
         return torch.zeros(CLIP_BYTES, dtype=torch.uint8, device=self.device)
 
+    def _here(self, record: torch.Tensor) -> None:
+        if record.device != self.device:
+            raise ValueError("the clip record is on %s, the plan on %s" % (record.device, self.device))
+
     def clip(self, max_norm: float = float("inf"), grad_scale: float = 1.0, out: Optional[torch.Tensor] = None,
              stream=None) -> torch.Tensor:
         """fr_grad_clip: returns the record, for step()."""
         if out is None:
             with _allocating_on(stream, self.device):
                 out = self.new_clip()
+        self._here(out)
         fr_grad_clip(self.handle, max_norm, grad_scale, out, stream)
         return out
 
     def step(self, hyper: fr_adamw, clip: Optional[torch.Tensor] = None, stream=None) -> None:
+        if clip is not None:
+            self._here(clip)
         fr_adamw_step(self.handle, hyper, clip, stream)
 
     def convert_to(self, dst: "OptPlan", rounding: int = FR_ROUND_NEAREST, seed: int = 0, stream=None) -> None:
