@@ -449,7 +449,8 @@ typedef struct {
 fr_status fr_grad_clip(fr_opt plan, float max_norm, float grad_scale, fr_clip* out_dev, void* stream);
 
 /* One step's numbers.  0 <= beta1, beta2 < 1, eps > 0, lr and weight_decay
- * >= 0, all finite in fp32; step counts from 1 (a skipped step does not count). */
+ * >= 0, all finite in fp32, and so their products with the tensors' factors;
+ * step counts from 1 (a skipped step does not count). */
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay;
   uint64_t step;

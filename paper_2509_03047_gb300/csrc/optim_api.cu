@@ -64,6 +64,7 @@ struct fr_opt_s {
   std::vector<uint64_t> sizes;  // of every tensor
   bool grads = true, params = true, moments = true;  // every tensor with elements has them
   bool eight = false, thirty_two = false;            // some tensor's moments have 8, 32 bits
+  float most_lr = 0.0f, most_decay = 0.0f;           // the largest |lr_scale| and |decay_scale| of a step's tensors
   WorkList clip, convert;
   WorkList step[kStepClasses];
   StepClass classes[kStepClasses];
@@ -171,6 +172,8 @@ fr_status fill_opt(fr_opt p, const fr_opt_tensor* tensors, uint64_t n_tensors) {
       c.weight = x.master ? kWeightMaster : x.weight_dtype == FR_DT_BF16 ? kWeightBf16 : kWeightF32;
       c.bf16_grad = x.grad_dtype == FR_DT_BF16;
       c.eight = x.state_dtype == FR_DT_BYTES;
+      p->most_lr = std::max(p->most_lr, std::fabs(x.lr_scale));
+      p->most_decay = std::max(p->most_decay, std::fabs(x.decay_scale));
       const uint64_t head = head_elems(x, c);
       c.odd = !d.aligned && head == 0 && x.n >= kOptBlock;
       p->classes[c.index()] = c;
@@ -308,6 +311,9 @@ fr_status fr_adamw_step(fr_opt p, const fr_adamw* h, const fr_clip* clip_dev, vo
   if (!(h->beta1 >= 0.0 && h->beta1 < 1.0) || !(h->beta2 >= 0.0 && h->beta2 < 1.0))
     return report_invalid(me, "betas must be in [0, 1)");
   if (!(static_cast<float>(h->eps) > 0.0f) || !std::isfinite(static_cast<float>(h->eps))) return report_invalid(me, "eps must be positive and finite");
+  if (!std::isfinite(static_cast<float>(h->lr) * p->most_lr)) return report_invalid(me, "lr times a tensor's lr_scale must be finite in fp32");
+  if (!std::isfinite(static_cast<float>(h->weight_decay) * p->most_decay))
+    return report_invalid(me, "weight_decay times a tensor's decay_scale must be finite in fp32");
   if (h->step == 0) return report_invalid(me, "step counts from 1");
   if (h->rounding > FR_ROUND_RANDOM) return report_invalid(me, "unknown rounding");
   if (h->reserved != 0) return report_invalid(me, "reserved must be 0");
