@@ -180,8 +180,10 @@ __device__ __forceinline__ fr_clip record(const ClipPartial& s, float grad_scale
     const float e = __fadd_rn(__fsub_rn(__fsub_rn(s.hi, xx), __fmaf_rn(x, x, -xx)), s.lo);
     r.norm = __fmul_rn(grad_scale, __fmaf_rn(__fmul_rn(0.5f, y), e, x));
   }
-  r.scale = r.norm > max_norm ? __fmul_rn(grad_scale, __fdiv_rn(max_norm, r.norm)) : grad_scale;
-  if (s.exact != 0.0 || r.norm == INFINITY) {
+  const float part = r.norm > max_norm ? __fdiv_rn(max_norm, r.norm) : 1.0f;
+  r.scale = __fmul_rn(grad_scale, part);
+  // in fp64 too where fp32 holds the norm or the quotient, and with it perhaps the factor, with fewer bits
+  if (s.exact != 0.0 || r.norm == INFINITY || (s.hi > 0.0f && r.norm < 0x1p-126f) || part < 0x1p-126f) {
     const double norm = grad_scale * sqrt(static_cast<double>(s.hi) + static_cast<double>(s.lo) + s.exact);
     r.norm = static_cast<float>(norm);
     r.scale = norm > max_norm ? static_cast<float>(grad_scale * (max_norm / norm)) : grad_scale;
