@@ -83,7 +83,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         path = os.path.join(CSRC, src)
         obj = os.path.join(OUT_DIR, src.replace(".cu", ".o"))
         if force or _stale(obj, [path] + headers):
-            cmd = [exe] + ARCH + NVCC_FLAGS + os.environ.get("FR_EXTRA", "").split() + ["-c", path, "-o", obj]
+            cmd = [exe] + ARCH + NVCC_FLAGS + ["-c", path, "-o", obj]
             r = subprocess.run(cmd, capture_output=True, text=True)
             with open(obj + ".log", "w") as f:
                 f.write(" ".join(cmd) + "\n" + r.stdout + r.stderr)
