@@ -44,6 +44,9 @@ def _stale(target: str, deps) -> bool:
 # diff kernels); host-only planning and API code is not among them.
 KERNEL_FILES = ["sweep_fp.cu", "sweep_pack.cu", "sweep_unpack.cu", "sweep_unpack_fp.cu", "finalize.cu", "gf2.cuh",
                 "layout.h", "kernels.h", "sweep_impl.cuh"]
+# The same of the optimizer step.
+OPTIM_KERNEL_FILES = ["optim_clip.cu", "optim_step.cu", "optim_convert.cu", "optim_block.cuh", "optim_math.cuh", "optim.h",
+                      "kernels.h"]
 
 
 def _code_only(text: str) -> str:
@@ -57,21 +60,31 @@ def _code_only(text: str) -> str:
     return "\n".join(line.rstrip() for line in text.splitlines() if line.strip())
 
 
-def source_digest(kernels_only: bool = False) -> str:
-    """Hash of the sources' code (comments left out) and the compile flags:
-    identifies what a profile measured.  With `kernels_only`, of the
-    device-kernel files alone."""
+def _digest(names, paths=()):
     import hashlib
 
     h = hashlib.sha256(" ".join(a for a in ARCH + NVCC_FLAGS if not os.path.isabs(a)).encode())
-    names = KERNEL_FILES if kernels_only else SOURCES + HEADERS
     for name in sorted(names):
         with open(os.path.join(CSRC, name), encoding="utf-8") as f:
             h.update(name.encode() + b"\0" + _code_only(f.read()).encode())
-    if not kernels_only:
-        with open(os.path.join(ROOT, "include", "flashrec.h"), encoding="utf-8") as f:
+    for path in paths:
+        with open(path, encoding="utf-8") as f:
             h.update(_code_only(f.read()).encode())
     return h.hexdigest()[:16]
+
+
+def source_digest(kernels_only: bool = False) -> str:
+    """Hash of the sources' code (comments left out) and the compile flags:
+    identifies what a profile measured.  With `kernels_only`, of the sweeps'
+    device-kernel files alone."""
+    if kernels_only:
+        return _digest(KERNEL_FILES)
+    return _digest(SOURCES + HEADERS, [os.path.join(ROOT, "include", "flashrec.h")])
+
+
+def optim_digest() -> str:
+    """The same of the optimizer step's device-kernel files."""
+    return _digest(OPTIM_KERNEL_FILES)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
