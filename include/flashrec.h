@@ -388,12 +388,19 @@ fr_status fr_fingerprint_static(const fr_tensor* tensors, uint64_t n_tensors, ui
  * E = 255, and all its elements read as NaN.
  *
  * Rounding to fewer bits: FR_ROUND_NEAREST (ties to even) or FR_ROUND_RANDOM,
- * up with the probability that makes the mean exact: with beta2 = 0.999 a
- * second moment changes by less than half a step of its code per update, so
- * that to nearest it would stand still.  The random bits come from a counter:
- * a function of seed, step, the tensor's index in the plan and the element's
- * index, so replicas draw the same.  FR_ROUND_RANDOM also rounds a bf16
- * weight without a master. */
+ * from code 1 on up with the probability that makes the mean exact (to 2^-16 of
+ * a code's step): with beta2 = 0.999 a second moment changes by less than half
+ * a step of its code per update, so that to nearest it would stand still.  Below
+ * code 1 neither rounding keeps means.  An m between the base's value, 2^(E -
+ * 142) or about 2^-15 of the block's largest, and code 1 becomes code 1 with the
+ * probability that lies between the two, else 0; one below the base's value
+ * always 0: elements whose gradients stay there have no momentum meanwhile,
+ * they move by (1 - beta1) of what the formula gives.  A v below code 1, 1.125
+ * 2^(E - 158), is raised to it, which makes such elements'
+ * updates smaller.  The random bits come from a counter: a function of seed,
+ * step, the tensor's index in the plan and the element's index, so replicas
+ * draw the same.  FR_ROUND_RANDOM also rounds a bf16 weight without a master,
+ * its mean exact everywhere. */
 #define FR_OPT_BLOCK 256
 
 typedef enum { FR_ROUND_NEAREST = 0, FR_ROUND_RANDOM = 1 } fr_rounding;
