@@ -384,8 +384,12 @@ fr_status fr_fingerprint_static(const fr_tensor* tensors, uint64_t n_tensors, ui
  * below the block's top.  c = 0 is zero.  Coding adds to the pattern of |x|
  * what the rounding gives below bit 20 and cuts there; what falls below code 1
  * becomes 0 in m, and code 1 in v if it is not zero (a second moment rounded
- * to zero would make the next step explode).  A block with an Inf or NaN gets
- * E = 255, and all its elements read as NaN.
+ * to zero would make the next step explode).  A block with an Inf, a NaN or a
+ * value whose pattern is above 0x7F700000 (1.875 2^127) gets E = 255, and all its
+ * elements read as NaN.  So a finite gradient too large to square (|h| above
+ * 1.8e19) costs its block: at the next step its FR_OPT_BLOCK parameters are NaN,
+ * where with 32-bit moments that element alone stands still.  fr_clip's count of
+ * non-finite gradients does not see it; a max_norm below 1e19 keeps it away.
  *
  * Rounding to fewer bits: FR_ROUND_NEAREST (ties to even) or FR_ROUND_RANDOM,
  * from code 1 on up with the probability that makes the mean exact (to 2^-16 of
