@@ -453,9 +453,12 @@ typedef struct {
  * factor by which fr_adamw_step multiplies each gradient.  `grad_scale` (finite,
  * > 0) undoes a loss scale or a gradient accumulation; `max_norm` > 0,
  * INFINITY for no clipping.  Sums of squares neither overflow nor underflow.
+ * A norm above fp32's range is INFINITY in the record, its factor is right.
  * Reads the gradients once.  With the parameters spread over several ranks or
- * plans, add their norms' squares and their counts and write the record by a
- * kernel of your own.  `out_dev`: 8-byte aligned.
+ * plans, add their norms' squares, in fp64 (a square need not fit fp32 where the
+ * norm does), and their counts, and write the record by a kernel of your own;
+ * each rank's record does not say more than its norm, so an INFINITY among them
+ * cannot be joined.  `out_dev`: 8-byte aligned.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
 fr_status fr_grad_clip(fr_opt plan, float max_norm, float grad_scale, fr_clip* out_dev, void* stream);
 

@@ -35,3 +35,17 @@ def test_the_factor_keeps_its_precision_at_the_ends_of_fp32(value, n, grad_scale
     assert got_bad == bad == 0
     assert abs(got_norm - norm) <= 33 * ref.U * norm + 2.0 ** -150
     assert abs(got_scale - scale) <= 34 * ref.U * scale + 2.0 ** -150
+
+
+@pytest.mark.parametrize("size", [1e-30, 1.0, 1e25, 1e36])
+def test_records_of_several_plans_joined_in_64_bits_are_the_whole_list_s(size):
+    """Squares of norms, added in fp64 as the header says, against one plan over all tensors: 33 u for each."""
+    r = np.random.default_rng(6)
+    gs = [(r.normal(size=n) * size).astype(np.float32) for n in (5000, 70001, 3)]
+    tensors = [torch.from_numpy(g).cuda() for g in gs]
+    parts = [fr.clip_view(fr.OptPlan(grads=[t]).clip(grad_scale=0.5)) for t in tensors]
+    norm = torch.cat([p[0] for p in parts]).double().square().sum().sqrt().item()
+    whole, factor, bad = (x.item() for x in fr.clip_view(fr.OptPlan(grads=tensors).clip(size, 0.5)))
+    want, want_factor, _ = ref.norm64(gs, float(np.float32(size)), 0.5)
+    assert abs(norm - want) <= 34 * ref.U * want and abs(whole - want) <= 33 * ref.U * want
+    assert abs(0.5 * np.float32(size) / norm - factor) <= 70 * ref.U * factor and bad == sum(p[2].item() for p in parts) == 0
