@@ -53,9 +53,12 @@ __device__ __forceinline__ float decode_v(uint32_t code, uint32_t e) {
 //
 // A counter-based generator: two rounds of multiplication and shift over the
 // index of a pair of elements, keyed by 64 bits per tensor, then one product
-// for each number that is taken.  The factors are the golden ratio's and, from
-// L'Ecuyer, "Tables of linear congruential generators of different sizes and
-// good lattice structure" (1999) and its successors, multipliers modulo 2^32.
+// for each number that is taken.  The factors are, from L'Ecuyer, "Tables of
+// linear congruential generators of different sizes and good lattice structure"
+// (1999) and its successors, multipliers modulo 2^32; the golden ratio's in 64
+// bits; and two odd 32-bit numbers of many scattered bits for a counter's low
+// and high word, of which nothing is asked but that (the first a prime near the
+// golden ratio's; the tests measure what comes out).
 struct RandomKey {
   uint32_t lo, hi;
 };

@@ -84,16 +84,16 @@ struct Step {
       v += kOptBlock * kMomentBytes;
     }
   };
-  // A block's loads, `ahead` blocks further.
+  // A block's loads.
   struct Raw {
     RawGrad g;
     RawParam p;
     RawMoment m, v;
-    __device__ __forceinline__ void load(const Places& at, int ahead, int left) {
-      g.load(at.g + ahead * (kOptBlock * kGradBytes), left);
-      m.load(at.m + ahead * (kOptBlock * kMomentBytes), left);
-      v.load(at.v + ahead * (kOptBlock * kMomentBytes), left);
-      p.load(at.p + ahead * (kOptBlock * RawParam::kBytes), left);
+    __device__ __forceinline__ void load(const Places& at, int left) {
+      g.load(at.g, left);
+      m.load(at.m, left);
+      v.load(at.v, left);
+      p.load(at.p, left);
     }
   };
   static __device__ __forceinline__ void put_f32(uint8_t* at, int left, const Pair (&x)[4]) {
@@ -164,7 +164,7 @@ struct Step {
     const int left = elements_left(d.n, block, lane);
     const uint32_t counter = random_counter(key, (static_cast<uint64_t>(block) * kOptBlock + d.skipped) / 2 + 4 * lane);
     Raw r;
-    r.load(at, 0, left);
+    r.load(at, left);
     Exponents e = {0, 0};
     if (Eight) e.load(d.m_exp + block, d.v_exp + block, 1, lane);
     uint32_t em = e.of_m(0), ev = e.of_v(0);
