@@ -6,27 +6,35 @@
 // weights without a master, at 10 bytes per element, by instructions too.
 //
 // 32-bit moments: one block of 256 elements per warp, no loop.  The hardware's
-// own order of many short CTAs reaches 7.1 TB/s (28 GB of a Llama-8B rank 3.95
-// ms; GPT-2 small, 3.7 GB, 522 us; a copy moves 6.8 TB/s), warps that loop over
+// own order of many short CTAs reaches 7.1 TB/s (28 GB of a Llama-8B rank 3.97
+// ms; GPT-2 small, 3.7 GB, 522 us; 0.77 GB in 10,000 tensors of 1 to 28,183
+// elements 114 us, 6.7 TB/s; a copy moves 6.8 TB/s), warps that loop over
 // the blocks at most 6.6, in any order: contiguous ranges, units side by side or
 // a grid's stride, with 1 to 6 CTAs per SM, with and without eviction hints.
 //
-// 8-bit moments: a block is 2.5 to 4 KB and 1,400 instructions of a warp, so up
+// 8-bit moments: a block is 2.5 to 4 KB and 380 instructions of a warp, so up
 // to 8 consecutive blocks share what a warp does once (its tensor, its random
 // key, its exponents), and the next ones come to shared memory meanwhile, by
 // asynchronous copies that take no registers.  One block per warp: GPT-2 small in
 // bf16 307 us, a Llama-8B rank with masters 2.77 ms; runs with the next block in
-// registers 207 us and 2.38 ms; so 193 us (6.4 TB/s) and 2.31 ms (7.0).  At the
-// former's 10 bytes per element warps issue in three of four cycles.
+// registers 207 us and 2.38 ms; so 190 us (6.5 TB/s) and 2.31 ms (7.0).  At the
+// former's 10 bytes per element warps issue in four of five cycles.  Lists of
+// many small tensors wait for latencies, a tensor's last block, out of line,
+// above all: 10,000 with masters, of 1 to 28,183 elements 91 us (4.8 TB/s), of 1
+// to 2,000, 42 MB, 19.5 us (2.2).
 //
 // Tensors whose buffers lie off the vectors' boundaries in different ways: whole
 // blocks come and go through shared memory, each buffer by vectors where it can.
-// 134 million elements (aligned; only the gradient off; every buffer off; and one
-// buffer off, by Step::any): bf16 with 32-bit moments 419, 456, 532 and 568 us,
-// with 8-bit ones 203, 278, 332 and 817; with masters 533, 560, 657 and 679, and
-// 313, 326, 449 and 861.  (8-bit without the choice for each buffer 301 and 316,
-// with masters 407 and 439: flat groups of gradients beside states of their own
-// are the more usual.)
+// 134 million elements (aligned; only the gradient off; every buffer, each in its
+// own way; and the gradient alone element by element, by Step::any): bf16 with
+// 32-bit moments 421, 460, 537 and 568 us, with 8-bit ones 203, 278, 342 and 818;
+// with masters 535, 564, 663 and 679, and 313, 327, 459 and 861.  (8-bit without
+// the choice for each buffer 301 and 316, with masters 407 and 439: flat groups
+// of gradients beside states of their own are the more usual.)
+//
+// An eps too small for the approximations (optim_math.cuh) takes Step::any for
+// every block: GPT-2 small with masters 674 us (522), in bf16 with 8-bit moments
+// 808 (190); a Llama-8B rank 5.39 ms (3.97), with 8-bit moments 7.10 (2.31).
 #include <type_traits>
 
 #include "kernels.h"
