@@ -1,0 +1,112 @@
+// muon.h -- the orthogonalised update's plan tables and kernel launchers
+// (internal to libflashrec).
+//
+// An iterate X of a matrix is held in blocks of 128 rows and 64 columns, 16 KiB
+// each, block row after block row; sides are filled up with zeros to multiples of
+// 128.  A block's row is 128 bytes, its eight 16-byte chunks permuted by the row
+// (chunk c of row r lies at c ^ (r % 8)): the layout that the tensor cores read
+// from shared memory, with the row as the contraction's index or the column, so a
+// block goes there by plain bulk copies and serves X X^T, X^T X, and products from
+// either side without a transposition.  The square matrices of the smaller side,
+// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike.
+//
+// Scales: X 2^14, S 2^13, P 2^11, so that fp16 holds what the bounds on the
+// polynomials (flashrec.h) allow: |X| <= 2, |S| <= 4, |P| <= 16 in the spectral
+// norm, which no element exceeds; and elements down to 2^-28, 2^-27, 2^-25 of 1 are
+// normal numbers.
+#pragma once
+
+#include <cstdint>
+#include <vector>
+
+#include <cuda_runtime.h>
+
+#include "../../include/flashrec.h"
+
+namespace frk {
+
+constexpr int kBlockRows = 128, kBlockCols = 64, kBlockBytes = kBlockRows * kBlockCols * 2;
+constexpr float kScaleX = 0x1p14f, kScaleS = 0x1p13f, kScaleP = 0x1p11f;
+constexpr double kMostX = 2.0, kMostP = 15.0;
+
+struct MuonDesc {        // one matrix that has elements
+  void* weight;
+  const void* grad;
+  float* master;
+  float* momentum;
+  void* update;
+  uint64_t rows, cols;
+  uint64_t x[2];         // bytes in the workspace: the iterate's first halves, old and new
+  uint64_t low;          // its second halves
+  uint64_t s, p;
+  uint32_t row_blocks, col_blocks;  // of 128 rows, of 64 columns (an even number)
+  uint32_t side_blocks;  // of 128, of the smaller side
+  uint32_t tall;         // more rows than columns: S = X^T X, X <- X P
+  uint32_t first_unit, n_units;     // of the norm
+  uint32_t first_block;  // of all blocks of the plan's iterates
+  uint32_t tensor;       // index in the plan
+  uint32_t bf16_weight, bf16_grad, bf16_update;
+  float lr_scale, decay_scale, update_scale;
+};
+
+// ---- elements: momentum and norm, X from G, the weights' update
+
+constexpr int kUnit = 4096;       // elements of the norm that a CTA adds up
+constexpr int kElementThreads = 256;
+
+struct MuonPartial {  // a unit's sum of squares: sum * 4^exponent
+  float sum;
+  int exponent;
+};
+struct MuonNorm {     // a matrix's: X = (G * to_one) * factor, in X's scale
+  float to_one, factor;
+  uint32_t done;      // units that have been added; zero before a launch and after it
+  uint32_t reserved;
+};
+
+struct MuonParams {
+  const MuonDesc* tensors;
+  const uint32_t* units;   // matrix of each unit
+  const uint32_t* blocks;  // matrix of each block
+  uint32_t n_units, n_blocks;
+  MuonPartial* partials;
+  MuonNorm* norms;
+  uint8_t* work;
+  const fr_clip* clip;     // may be null
+  float beta, beta_rest;   // beta, 1 - beta
+  float lr, decay;
+  uint32_t momentum;       // 0: G is the gradient
+  uint32_t nesterov;
+  uint32_t random;
+  uint64_t key;            // as in StepParams
+  uint32_t last;           // which of x[] holds the last iterate
+};
+cudaError_t launch_muon_norm(const MuonParams& p, cudaStream_t s);
+cudaError_t launch_muon_iterate(const MuonParams& p, cudaStream_t s);   // X, from G and the norm
+cudaError_t launch_muon_apply(const MuonParams& p, cudaStream_t s);     // the step's weights
+cudaError_t launch_muon_update(const MuonParams& p, cudaStream_t s);    // fr_orthogonalize's output
+
+// ---- products
+
+enum : int { kGram = 0, kPoly = 1, kNext = 2 };  // S, P, the next X
+constexpr int kPhases = 3;
+
+struct MuonTile {
+  uint32_t tensor;
+  uint16_t row, col;  // of tiles, of the product
+};
+// The tiles of each phase's products.
+void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile> (&tiles)[kPhases]);
+struct MuonProduct {
+  const MuonDesc* tensors;
+  const MuonTile* tiles;
+  uint32_t n_tiles;
+  uint8_t* work;
+  const fr_clip* clip;
+  float a, b, c;
+  uint32_t from;  // which of x[] is the old iterate
+};
+constexpr int kTile = 64;
+cudaError_t launch_muon_product(int phase, const MuonProduct& p, cudaStream_t s);
+
+}  // namespace frk

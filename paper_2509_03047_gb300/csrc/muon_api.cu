@@ -1,0 +1,334 @@
+// muon_api.cu -- the C ABI of the orthogonalised update (declared in
+// include/flashrec.h) and its planner: places of the iterates and of their
+// squares in the plan's memory, units of the norm, blocks, tiles of the products.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <exception>
+#include <new>
+#include <vector>
+
+#include "../../include/flashrec.h"
+#include "host.h"
+#include "kernels.h"
+#include "muon.h"
+#include "optim.h"
+
+using namespace frk;
+
+struct fr_muon_plan_s {
+  int device = 0;
+  void* d_memory = nullptr;
+  uint64_t n_tensors = 0, n_elems = 0, device_bytes = 0;
+  bool params = true, updates = true;       // every matrix with elements has what the step, fr_orthogonalize needs
+  float most_lr = 0.0f, most_decay = 0.0f;  // the largest |lr_scale| and |decay_scale|
+  uint32_t n_units = 0, n_blocks = 0;
+  uint32_t n_tiles[kPhases] = {};
+  MuonDesc* d_tensors = nullptr;
+  uint32_t* d_units = nullptr;
+  uint32_t* d_blocks = nullptr;
+  MuonTile* d_tiles[kPhases] = {};
+  MuonPartial* d_partials = nullptr;
+  MuonNorm* d_norms = nullptr;
+  uint8_t* d_work = nullptr;
+};
+
+namespace {
+
+constexpr uint64_t kMostSide = FR_MUON_MOST_SIDE;
+constexpr uint64_t kMostElems = 1ull << 40;
+
+bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
+uint64_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
+bool is_float(uint32_t dtype) { return dtype == FR_DT_BF16 || dtype == FR_DT_F32; }
+
+const char* check(const fr_muon_tensor& x, bool& misaligned) {
+  misaligned = false;
+  if (x.flags != 0 || x.reserved != 0) return "tensor flags and reserved must be 0";
+  if (x.rows > kMostSide || x.cols > kMostSide) return "a matrix has too many rows or columns";
+  if (!std::isfinite(x.lr_scale) || !std::isfinite(x.decay_scale) || !std::isfinite(x.update_scale)) return "a matrix's factors must be finite";
+  if (x.weight && !is_float(x.weight_dtype)) return "weights are bf16 or fp32";
+  if (x.grad && !is_float(x.grad_dtype)) return "gradients are bf16 or fp32";
+  if (x.update && !is_float(x.update_dtype)) return "updates are bf16 or fp32";
+  if (x.master && (x.weight == nullptr || x.weight_dtype != FR_DT_BF16)) return "a master belongs to a bf16 weight";
+  misaligned = (x.weight && !on(x.weight, type_bytes(x.weight_dtype))) || (x.grad && !on(x.grad, type_bytes(x.grad_dtype))) ||
+               (x.update && !on(x.update, type_bytes(x.update_dtype))) || !on(x.master, 4) || !on(x.momentum, 4);
+  return nullptr;
+}
+
+uint32_t pieces(uint64_t n, uint64_t of) { return static_cast<uint32_t>((n + of - 1) / of); }
+
+// A matrix's descriptor but for its places in the workspace.
+MuonDesc describe(const fr_muon_tensor& x, uint64_t index) {
+  MuonDesc d = {};
+  d.weight = x.weight;
+  d.grad = x.grad;
+  d.master = x.master;
+  d.momentum = x.momentum;
+  d.update = x.update;
+  d.rows = x.rows;
+  d.cols = x.cols;
+  d.row_blocks = pieces(x.rows, kBlockRows);
+  d.col_blocks = 2 * pieces(x.cols, 2 * kBlockCols);
+  d.tall = x.rows > x.cols;
+  d.side_blocks = d.tall ? d.col_blocks / 2 : d.row_blocks;
+  d.n_units = pieces(x.rows * x.cols, kUnit);
+  d.tensor = static_cast<uint32_t>(index);
+  d.bf16_weight = x.weight && x.weight_dtype == FR_DT_BF16;
+  d.bf16_grad = x.grad && x.grad_dtype == FR_DT_BF16;
+  d.bf16_update = x.update && x.update_dtype == FR_DT_BF16;
+  d.lr_scale = x.lr_scale;
+  d.decay_scale = x.decay_scale;
+  d.update_scale = x.update_scale;
+  return d;
+}
+
+uint64_t square_blocks(const MuonDesc& d) { return 2ull * d.side_blocks * d.side_blocks; }
+
+fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_tensors) {
+  std::vector<MuonDesc> descs;
+  std::vector<uint32_t> units, blocks;
+  std::vector<MuonTile> tiles[kPhases];
+  uint64_t bytes = 0;
+  auto take = [&](uint64_t n_blocks) {
+    const uint64_t at = bytes;
+    bytes += n_blocks * kBlockBytes;
+    return at;
+  };
+  p->n_tensors = n_tensors;
+  for (uint64_t t = 0; t < n_tensors; ++t) {
+    const fr_muon_tensor& x = tensors[t];
+    if (x.rows == 0 || x.cols == 0) continue;
+    p->n_elems += x.rows * x.cols;
+    p->params &= x.weight && x.grad && x.momentum;
+    p->updates &= x.grad && x.update;
+    p->most_lr = std::max(p->most_lr, std::fabs(x.lr_scale));
+    p->most_decay = std::max(p->most_decay, std::fabs(x.decay_scale));
+    MuonDesc d = describe(x, t);
+    const uint64_t n = static_cast<uint64_t>(d.row_blocks) * d.col_blocks;
+    d.x[0] = take(n);
+    d.x[1] = take(n);
+    d.low = take(n);
+    d.s = take(square_blocks(d));
+    d.p = take(square_blocks(d));
+    d.first_unit = static_cast<uint32_t>(units.size());
+    d.first_block = static_cast<uint32_t>(blocks.size());
+    const uint32_t me = static_cast<uint32_t>(descs.size());
+    units.insert(units.end(), d.n_units, me);
+    blocks.insert(blocks.end(), n, me);
+    descs.push_back(d);
+  }
+  plan_tiles(descs, tiles);
+  PlanMemory mem;
+  mem.table(&p->d_tensors, descs);
+  mem.table(&p->d_units, units);
+  mem.table(&p->d_blocks, blocks);
+  for (int k = 0; k < kPhases; ++k) {
+    mem.table(&p->d_tiles[k], tiles[k]);
+    p->n_tiles[k] = static_cast<uint32_t>(tiles[k].size());
+  }
+  mem.table(&p->d_norms, std::vector<MuonNorm>(descs.size(), MuonNorm{}));
+  mem.scratch(&p->d_partials, units.size());
+  // (to the bulk copies' boundary from PlanMemory's)
+  mem.scratch(&p->d_work, bytes);
+  p->n_units = static_cast<uint32_t>(units.size());
+  p->n_blocks = static_cast<uint32_t>(blocks.size());
+  p->device_bytes = bytes;
+  const cudaError_t e = mem.commit(&p->d_memory);
+  return e == cudaSuccess ? FR_OK : report_cuda("plan device tables", e);
+}
+
+// Largest |f| on [0, top] of an odd or even polynomial given by its values and the places where its derivative in s^2 vanishes.
+template <class F>
+double most(F f, double top, double q2, double q1, double q0) {
+  double r = std::max(std::fabs(f(0.0)), std::fabs(f(top)));
+  auto at = [&](double u) {  // a root u = s^2
+    if (u > 0.0 && u < top * top) r = std::max(r, std::fabs(f(std::sqrt(u))));
+  };
+  if (q2 == 0.0) {
+    if (q1 != 0.0) at(-q0 / q1);
+  } else {
+    const double disc = q1 * q1 - 4.0 * q2 * q0;
+    if (disc >= 0.0) {
+      at((-q1 + std::sqrt(disc)) / (2.0 * q2));
+      at((-q1 - std::sqrt(disc)) / (2.0 * q2));
+    }
+  }
+  return r;
+}
+
+const char* check_iterations(const fr_muon& h) {
+  if (h.iterations < 1 || h.iterations > FR_MUON_MOST) return "iterations must be 1 to FR_MUON_MOST";
+  double top = 1.0;
+  for (uint32_t i = 0; i < h.iterations; ++i) {
+    const double a = h.coef[i][0], b = h.coef[i][1], c = h.coef[i][2];
+    if (!std::isfinite(a) || !std::isfinite(b) || !std::isfinite(c)) return "coefficients must be finite";
+    auto p = [&](double s) { return a + s * s * (b + c * s * s); };
+    auto next = [&](double s) { return s * p(s); };
+    // (a hair more than the bound, for the roundings of X)
+    const double reach = top * 1.01;
+    // (one by one: a bound on P's parts keeps fp16 from overflow in b S and c S^2 alike)
+    if (!(most(p, reach, 0.0, 2.0 * c, b) <= kMostP)) return "a polynomial exceeds 15 on the singular values that it meets";
+    top = most(next, reach, 5.0 * c, 3.0 * b, a);
+    if (!(top <= kMostX)) return "an iteration takes a singular value above 2";
+  }
+  return nullptr;
+}
+
+// X through all iterations, in the plan's workspace.
+fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t s) {
+  cudaError_t e = launch_muon_norm(mp, s);
+  if (e == cudaSuccess) e = launch_muon_iterate(mp, s);
+  if (e != cudaSuccess) return report_cuda("element kernel launch", e);
+  MuonProduct q = {};
+  q.tensors = p->d_tensors;
+  q.work = p->d_work;
+  q.clip = mp.clip;
+  for (uint32_t i = 0; i < h.iterations; ++i) {
+    q.a = static_cast<float>(h.coef[i][0]);
+    q.b = static_cast<float>(h.coef[i][1]);
+    q.c = static_cast<float>(h.coef[i][2]);
+    q.from = i % 2;
+    for (int phase = 0; phase < kPhases; ++phase) {
+      q.tiles = p->d_tiles[phase];
+      q.n_tiles = p->n_tiles[phase];
+      e = launch_muon_product(phase, q, s);
+      if (e != cudaSuccess) return report_cuda("product kernel launch", e);
+    }
+  }
+  mp.last = h.iterations % 2;
+  return FR_OK;
+}
+
+MuonParams params(fr_muon_plan p) {
+  MuonParams mp = {};
+  mp.tensors = p->d_tensors;
+  mp.units = p->d_units;
+  mp.blocks = p->d_blocks;
+  mp.n_units = p->n_units;
+  mp.n_blocks = p->n_blocks;
+  mp.partials = p->d_partials;
+  mp.norms = p->d_norms;
+  mp.work = p->d_work;
+  return mp;
+}
+
+}  // namespace
+
+extern "C" {
+
+fr_status fr_muon_create(const fr_muon_tensor* tensors, uint64_t n_tensors, fr_muon_plan* out) {
+  CallRange nvtx("fr_muon_create");
+  const char* const me = "fr_muon_create";
+  if (out == nullptr) return report_invalid(me, "out is null");
+  *out = nullptr;
+  if (n_tensors > 0 && tensors == nullptr) return report_invalid(me, "tensors is null");
+  if (n_tensors >= (1ull << 32)) return report_invalid(me, "too many tensors");
+  uint64_t filled = 0;  // elements with the sides filled up
+  for (uint64_t t = 0; t < n_tensors; ++t) {
+    bool misaligned;
+    if (const char* what = check(tensors[t], misaligned)) return report_invalid(me, what);
+    if (misaligned) {
+      report_invalid(me, "a buffer is not aligned to its element size");
+      return FR_ERR_ALIGNMENT;
+    }
+    if (tensors[t].rows == 0 || tensors[t].cols == 0) continue;
+    const MuonDesc d = describe(tensors[t], t);
+    filled += 1ull * d.row_blocks * d.col_blocks * kBlockRows * kBlockCols + square_blocks(d) * kBlockRows * kBlockCols;
+    if (filled >= kMostElems) return report_invalid(me, "too many elements");
+  }
+
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return report_cuda("cudaGetDevice", e);
+
+  fr_muon_plan p = new (std::nothrow) fr_muon_plan_s;
+  if (p == nullptr) return report_invalid(me, "out of host memory");
+  p->device = dev;
+  fr_status st;
+  try {
+    st = fill_muon(p, tensors, n_tensors);
+  } catch (const std::exception&) {  // std::bad_alloc, std::length_error
+    st = report_invalid(me, "out of host memory");
+  }
+  if (st != FR_OK) {
+    cudaFree(p->d_memory);
+    delete p;
+    return st;
+  }
+  *out = p;
+  return FR_OK;
+}
+
+fr_status fr_muon_info(fr_muon_plan p, uint64_t* n_tensors, uint64_t* n_elems, uint64_t* device_bytes) {
+  if (p == nullptr) return report_invalid("fr_muon_info", "plan is null");
+  if (n_tensors) *n_tensors = p->n_tensors;
+  if (n_elems) *n_elems = p->n_elems;
+  if (device_bytes) *device_bytes = p->device_bytes;
+  return FR_OK;
+}
+
+void fr_muon_destroy(fr_muon_plan p) {
+  CallRange nvtx("fr_muon_destroy");
+  if (p == nullptr) return;
+  DeviceGuard g(p->device);
+  cudaDeviceSynchronize();
+  cudaFree(p->d_memory);
+  delete p;
+}
+
+fr_status fr_muon_step(fr_muon_plan p, const fr_muon* h, const fr_clip* clip_dev, void* stream) {
+  CallRange nvtx("fr_muon_step");
+  const char* const me = "fr_muon_step";
+  if (p == nullptr || h == nullptr) return report_invalid(me, "plan or hyper is null");
+  if (!p->params) return report_invalid(me, "a matrix of the plan has no weight, gradient or momentum");
+  if (!(h->lr >= 0.0) || !std::isfinite(static_cast<float>(h->lr))) return report_invalid(me, "lr must be finite and not negative");
+  if (!(h->weight_decay >= 0.0) || !std::isfinite(static_cast<float>(h->weight_decay)))
+    return report_invalid(me, "weight_decay must be finite and not negative");
+  if (!(h->beta >= 0.0 && h->beta < 1.0)) return report_invalid(me, "beta must be in [0, 1)");
+  if (!std::isfinite(static_cast<float>(h->lr) * p->most_lr)) return report_invalid(me, "lr times a matrix's lr_scale must be finite in fp32");
+  if (!std::isfinite(static_cast<float>(h->weight_decay) * p->most_decay))
+    return report_invalid(me, "weight_decay times a matrix's decay_scale must be finite in fp32");
+  if (h->nesterov > 1) return report_invalid(me, "nesterov must be 0 or 1");
+  if (h->step == 0) return report_invalid(me, "step counts from 1");
+  if (h->rounding > FR_ROUND_RANDOM) return report_invalid(me, "unknown rounding");
+  if (h->reserved != 0) return report_invalid(me, "reserved must be 0");
+  if (const char* what = check_iterations(*h)) return report_invalid(me, what);
+  if (clip_dev != nullptr && !on(clip_dev, 8)) return report_invalid(me, "clip_dev is not 8-byte aligned");
+  if (p->n_blocks == 0) return FR_OK;
+  DeviceGuard g(p->device);
+  if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
+  MuonParams mp = params(p);
+  mp.clip = clip_dev;
+  mp.beta = static_cast<float>(h->beta);
+  mp.beta_rest = static_cast<float>(1.0 - h->beta);
+  mp.lr = static_cast<float>(h->lr);
+  mp.decay = static_cast<float>(h->weight_decay);
+  mp.momentum = 1;
+  mp.nesterov = h->nesterov;
+  mp.random = h->rounding == FR_ROUND_RANDOM;
+  mp.key = mix64(mix64(h->seed) + h->step);
+  const fr_status st = iterate(p, *h, mp, static_cast<cudaStream_t>(stream));
+  if (st != FR_OK) return st;
+  const cudaError_t e = launch_muon_apply(mp, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FR_OK : report_cuda("weight kernel launch", e);
+}
+
+fr_status fr_orthogonalize(fr_muon_plan p, const fr_muon* h, void* stream) {
+  CallRange nvtx("fr_orthogonalize");
+  const char* const me = "fr_orthogonalize";
+  if (p == nullptr || h == nullptr) return report_invalid(me, "plan or hyper is null");
+  if (!p->updates) return report_invalid(me, "a matrix of the plan has no gradient or update");
+  if (const char* what = check_iterations(*h)) return report_invalid(me, what);
+  if (p->n_blocks == 0) return FR_OK;
+  DeviceGuard g(p->device);
+  if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
+  MuonParams mp = params(p);
+  const fr_status st = iterate(p, *h, mp, static_cast<cudaStream_t>(stream));
+  if (st != FR_OK) return st;
+  const cudaError_t e = launch_muon_update(mp, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? FR_OK : report_cuda("update kernel launch", e);
+}
+
+}  // extern "C"

@@ -31,6 +31,7 @@ FR_DT_BYTES, FR_DT_BF16, FR_DT_F32 = 0, 1, 2
 FP_ENTRY_BYTES = 16
 FR_OPT_BLOCK = 256
 FR_ROUND_NEAREST, FR_ROUND_RANDOM = 0, 1
+FR_MUON_MOST, FR_MUON_MOST_SIDE = 10, 1 << 20
 CLIP_BYTES = 16
 
 _TORCH_TO_FR = {torch.bfloat16: FR_DT_BF16, torch.float32: FR_DT_F32, torch.uint8: FR_DT_BYTES,
@@ -60,6 +61,22 @@ class fr_adamw(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
                 ("weight_decay", ctypes.c_double), ("step", ctypes.c_uint64), ("seed", ctypes.c_uint64),
                 ("rounding", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class fr_muon_tensor(ctypes.Structure):
+    _fields_ = [("weight", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+                ("momentum", ctypes.c_void_p), ("update", ctypes.c_void_p), ("rows", ctypes.c_uint64),
+                ("cols", ctypes.c_uint64), ("weight_dtype", ctypes.c_uint32), ("grad_dtype", ctypes.c_uint32),
+                ("update_dtype", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("lr_scale", ctypes.c_float),
+                ("decay_scale", ctypes.c_float), ("update_scale", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
+class fr_muon(ctypes.Structure):
+    """One step's numbers (see muon()); a training loop keeps one and counts `step` up."""
+    _fields_ = [("lr", ctypes.c_double), ("beta", ctypes.c_double), ("weight_decay", ctypes.c_double),
+                ("coef", ctypes.c_double * 3 * FR_MUON_MOST), ("step", ctypes.c_uint64), ("seed", ctypes.c_uint64),
+                ("iterations", ctypes.c_uint32), ("nesterov", ctypes.c_uint32), ("rounding", ctypes.c_uint32),
+                ("reserved", ctypes.c_uint32)]
 
 
 class FlashrecError(RuntimeError):
@@ -106,6 +123,12 @@ def _load() -> ctypes.CDLL:
     L.fr_grad_clip.argtypes = [vp, ctypes.c_float, ctypes.c_float, vp, vp]
     L.fr_adamw_step.argtypes = [vp, ctypes.POINTER(fr_adamw), vp, vp]
     L.fr_opt_convert.argtypes = [vp, vp, u32, u64, vp]
+    L.fr_muon_create.argtypes = [ctypes.POINTER(fr_muon_tensor), u64, ctypes.POINTER(vp)]
+    L.fr_muon_info.argtypes = [vp, u64p, u64p, u64p]
+    L.fr_muon_destroy.argtypes = [vp]
+    L.fr_muon_destroy.restype = None
+    L.fr_muon_step.argtypes = [vp, ctypes.POINTER(fr_muon), vp, vp]
+    L.fr_orthogonalize.argtypes = [vp, ctypes.POINTER(fr_muon), vp]
     L.fr_status_str.argtypes = [ctypes.c_int]
     L.fr_status_str.restype = ctypes.c_char_p
     L.fr_last_error.argtypes = []
@@ -116,7 +139,7 @@ def _load() -> ctypes.CDLL:
                  "fr_plan_create_batched", "fr_plan_batch", "fr_pack_batch", "fr_unpack_verify_batch",
                  "fr_unpack_collect", "fr_resend", "fr_restore", "fr_shard_pieces", "fr_pack_fp", "fr_unpack_verify_fp",
                  "fr_restore_fp", "fr_resend_fp", "fr_restore_multi", "fr_opt_create", "fr_opt_info", "fr_grad_clip",
-                 "fr_adamw_step", "fr_opt_convert"]:
+                 "fr_adamw_step", "fr_opt_convert", "fr_muon_create", "fr_muon_info", "fr_muon_step", "fr_orthogonalize"]:
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -483,6 +506,105 @@ def fr_opt_convert(src, dst, rounding: int = FR_ROUND_NEAREST, seed: int = 0, st
     _check(lib.fr_opt_convert(src, dst, rounding, seed, _stream(stream)), "fr_opt_convert")
 
 
+# ---------------------------------------------------------------- orthogonalised updates
+
+MUON_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
+
+
+def muon(lr: float = 0.0, beta: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+         coefficients=MUON_COEFFICIENTS, step: int = 1, seed: int = 0, rounding: int = FR_ROUND_NEAREST) -> fr_muon:
+    """The numbers of a step: one (a, b, c) per iteration."""
+    if not 1 <= len(coefficients) <= FR_MUON_MOST:
+        raise ValueError("1 to %d iterations, not %d" % (FR_MUON_MOST, len(coefficients)))
+    h = fr_muon(lr, beta, weight_decay, step=step, seed=seed, iterations=len(coefficients), nesterov=bool(nesterov), rounding=rounding)
+    for i, abc in enumerate(coefficients):
+        h.coef[i][:] = abc
+    return h
+
+
+def _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale):
+    """(fr_muon_tensor array, its length)"""
+    lists = [("weights", "weight", weights, _FLOATS), ("grads", "grad", grads, _FLOATS), ("masters", "master", masters, _F32),
+             ("momenta", "momentum", momenta, _F32), ("updates", "update", updates, _FLOATS)]
+    given = [x for _, _, x, _ in lists if x is not None]
+    if not given:
+        raise ValueError("a plan needs weights, gradients or momenta")
+    count = len(given[0])
+    arr = (fr_muon_tensor * max(count, 1))()
+    shapes = [None] * count
+    device = None  # of every matrix that has elements
+    for name, field, tensors, allowed in lists:
+        if tensors is None:
+            continue
+        if len(tensors) != count:
+            raise ValueError("%s holds %d matrices, not %d" % (name, len(tensors), count))
+        typed = field in ("weight", "grad", "update")
+        for i, t in enumerate(tensors):
+            if t is None:
+                continue
+            if t.dim() != 2:
+                raise ValueError("%s[%d] has %d dimensions, a matrix has two" % (name, i, t.dim()))
+            if t.numel() and t.get_device() != device:
+                if not t.is_cuda:
+                    raise ValueError("%s[%d] is not on a CUDA device" % (name, i))
+                if device is not None:
+                    raise ValueError("%s[%d] is on CUDA device %d, the matrices before it on %d" % (name, i, t.get_device(), device))
+                device = t.get_device()
+            if not t.is_contiguous():
+                raise ValueError("%s[%d] is not contiguous" % (name, i))
+            code = allowed.get(t.dtype)
+            if code is None:
+                raise ValueError("%s[%d]: unsupported dtype %s" % (name, i, t.dtype))
+            if shapes[i] is None:
+                shapes[i] = t.shape
+                arr[i].rows, arr[i].cols = t.shape
+            elif shapes[i] != t.shape:
+                raise ValueError("%s[%d] is %d x %d, not %d x %d" % (name, i, *t.shape, *shapes[i]))
+            if t.numel():
+                setattr(arr[i], field, t.data_ptr())
+            if typed:
+                setattr(arr[i], field + "_dtype", code)
+    if device is not None and device != torch.cuda.current_device():  # the one that the plan is bound to
+        raise ValueError("the matrices are on CUDA device %d, the current one is %d" % (device, torch.cuda.current_device()))
+    for field, x in (("lr_scale", lr_scale), ("decay_scale", decay_scale), ("update_scale", update_scale)):
+        x = [1.0] * count if x is None else list(x)
+        if len(x) != count:
+            raise ValueError("%d factors for %d matrices" % (len(x), count))
+        for i, v in enumerate(x):
+            setattr(arr[i], field, v)
+    return arr, count
+
+
+def fr_muon_create(weights=None, grads=None, momenta=None, masters=None, updates=None, lr_scale=None, decay_scale=None,
+                   update_scale=None):
+    """Plan over lists of contiguous two-dimensional CUDA tensors on the current device (a list, or an entry, may be None;
+    factors default to 1).  Momenta and masters are fp32, the others bf16 or fp32.  Returns the opaque handle (int)."""
+    arr, count = _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale)
+    h = ctypes.c_void_p()
+    _check(lib.fr_muon_create(arr, count, ctypes.byref(h)), "fr_muon_create")
+    return h.value
+
+
+def fr_muon_info(plan):
+    """(matrices, elements, bytes of device memory)"""
+    t, n, b = ctypes.c_uint64(), ctypes.c_uint64(), ctypes.c_uint64()
+    _check(lib.fr_muon_info(plan, ctypes.byref(t), ctypes.byref(n), ctypes.byref(b)), "fr_muon_info")
+    return t.value, n.value, b.value
+
+
+def fr_muon_destroy(plan) -> None:
+    if plan:
+        lib.fr_muon_destroy(plan)
+
+
+def fr_muon_step(plan, hyper: fr_muon, clip: Optional[torch.Tensor] = None, stream=None) -> None:
+    _check(lib.fr_muon_step(plan, hyper, None if clip is None else _record(clip), _stream(stream)), "fr_muon_step")
+
+
+def fr_orthogonalize(plan, hyper: fr_muon, stream=None) -> None:
+    _check(lib.fr_orthogonalize(plan, hyper, _stream(stream)), "fr_orthogonalize")
+
+
 # ---------------------------------------------------------------- convenience
 
 def fr_shard_pieces(n_elems: int, elem_bytes: int, n_dst: int, rank: int, n_src: int):
@@ -650,3 +772,38 @@ class OptPlan:
 
     def convert_to(self, dst: "OptPlan", rounding: int = FR_ROUND_NEAREST, seed: int = 0, stream=None) -> None:
         fr_opt_convert(self.handle, dst.handle, rounding, seed, stream)
+
+
+class MuonPlan:
+    """A plan of the orthogonalised update over lists of two-dimensional CUDA tensors (arguments as fr_muon_create).  The
+    clip record comes from an OptPlan over all gradients."""
+
+    def __init__(self, weights=None, grads=None, momenta=None, masters=None, updates=None, lr_scale=None, decay_scale=None,
+                 update_scale=None):
+        lists = [weights, grads, momenta, masters, updates]
+        self.buffers = [None if x is None else list(x) for x in lists]  # the plan holds their addresses
+        first = next((t for x in self.buffers if x for t in x if t is not None and t.numel()), None)
+        self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
+        self.handle = None
+        self.handle = fr_muon_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale, update_scale=update_scale)
+        self.n_tensors, self.n_elems, self.device_bytes = fr_muon_info(self.handle)
+
+    def close(self) -> None:
+        if self.handle:
+            fr_muon_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, hyper: fr_muon, clip: Optional[torch.Tensor] = None, stream=None) -> None:
+        if clip is not None and clip.device != self.device:
+            raise ValueError("the clip record is on %s, the plan on %s" % (clip.device, self.device))
+        fr_muon_step(self.handle, hyper, clip, stream)
+
+    def orthogonalize(self, hyper: Optional[fr_muon] = None, stream=None) -> None:
+        """Writes the plan's updates from its gradients."""
+        fr_orthogonalize(self.handle, muon() if hyper is None else hyper, stream)
