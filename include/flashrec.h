@@ -21,6 +21,8 @@
  *   fr_opt_convert    moments from 32 bits to 8 and back
  *   fr_muon_step      momentum, its orthogonalised form and the update of matrices
  *   fr_orthogonalize  the orthogonalised form alone
+ *   fr_embed_lookup   rows of an embedding table for a batch of tokens
+ *   fr_embed_grad     the table's gradient from the rows' gradients
  *
  * All device work runs in hand-written CUDA kernels for sm_103a.  There is no
  * CPU fallback: without a usable GPU every call returns FR_ERR_CUDA.
@@ -585,6 +587,49 @@ fr_status fr_muon_step(fr_muon_plan plan, const fr_muon* hyper, const fr_clip* c
  * iterations and coefficients count.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
 fr_status fr_orthogonalize(fr_muon_plan plan, const fr_muon* hyper, void* stream);
+
+/* ---------------------------------------------------------------- embeddings */
+
+/* A rank's part of a model's embedding: the rows [first, first + rows) of a table of
+ * `dim` columns, row after row.  fr_embed_lookup takes a batch's rows from it,
+ * fr_embed_grad makes the gradient that fr_grad_clip and fr_adamw_step read.  As
+ * with these, every result is a function of the values and the arguments alone: a
+ * token's gradients are added in an order that the batch decides, not the order in which
+ * blocks run, so replicas stay bit-identical.
+ *
+ * Tokens are signed integers of 4 or 8 bytes.  Those outside the slice (another
+ * rank's, or negative ones, as padding is marked) look up zeros, +0, and add nothing to
+ * the gradient; so ranks that split the vocabulary add up their lookups. */
+typedef struct fr_embed_s* fr_embed;
+
+/* Plan for batches of up to `max_tokens` tokens, bound to the current device; it
+ * allocates here and nowhere else, and one stream at a time may use it for
+ * fr_embed_grad (fr_embed_lookup uses no memory of it).  Device memory: 8 to 16
+ * bytes per token, a byte per row, and workspace of up to 30 MB.
+ * rows, max_tokens < 2^31, dim <= 2^20, first <= 2^62; rows * dim and max_tokens *
+ * dim <= 2^40.  Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
+fr_status fr_embed_create(uint64_t rows, uint64_t dim, uint64_t max_tokens, uint64_t first, fr_embed* out);
+
+/* A plan's numbers and bytes of device memory (host; any may be NULL). */
+fr_status fr_embed_info(fr_embed plan, uint64_t* rows, uint64_t* dim, uint64_t* max_tokens, uint64_t* device_bytes);
+
+/* Free the plan and its device memory (synchronizes the device first). */
+void fr_embed_destroy(fr_embed plan);
+
+/* out[i] = scale * table[tokens[i] - first], `n` rows of dim elements, multiplied in
+ * fp32 and rounded once, to nearest even; zeros where the token is outside.  Types
+ * are FR_DT_BF16 or FR_DT_F32; `scale` is finite.
+ * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT (any buffer off its element size), FR_ERR_CUDA. */
+fr_status fr_embed_lookup(fr_embed plan, const void* table, uint32_t table_dtype, const void* tokens, uint32_t token_bytes,
+                          uint64_t n, float scale, void* out, uint32_t out_dtype, void* stream);
+
+/* grad[r] = scale * (the sum of out[i] over the tokens i of row first + r), all
+ * `rows` rows, or with `accumulate` 1 added to what is there, where rows that no
+ * token meets are not touched.  Sums are in fp32, parts of at most n / 12,000 (or n *
+ * dim / 3 million, or 8) tokens one after the other, rounded once at the end.  `out` is read only.
+ * Errors: as fr_embed_lookup. */
+fr_status fr_embed_grad(fr_embed plan, const void* out, uint32_t out_dtype, const void* tokens, uint32_t token_bytes,
+                        uint64_t n, float scale, void* grad, uint32_t grad_dtype, uint32_t accumulate, void* stream);
 
 /* ---------------------------------------------------------------- status */
 

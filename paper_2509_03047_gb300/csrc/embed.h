@@ -1,0 +1,114 @@
+// embed.h -- the embedding's plan and kernel launchers (internal to libflashrec).
+#pragma once
+
+#include <cstdint>
+
+#include <cuda_runtime.h>
+
+#include "../../include/flashrec.h"
+#include "optim.h"
+
+namespace frk {
+
+// A batch's tokens: 4 or 8 bytes each.  Row of the slice, or rows and above.
+struct Tokens {
+  const void* at;
+  uint64_t n;
+  uint64_t first, rows;
+  uint32_t wide;
+#ifdef __CUDACC__
+  __device__ __forceinline__ uint64_t row(uint64_t i) const {
+    const int64_t t = wide ? static_cast<const int64_t*>(at)[i] : static_cast<const int32_t*>(at)[i];
+    return static_cast<uint64_t>(t) - first;
+  }
+#endif
+};
+
+// ---- lookup
+
+struct LookupParams {
+  Tokens tokens;
+  const void* table;
+  void* out;
+  uint64_t dim;
+  float scale;
+  uint32_t bf16_table, bf16_out;
+};
+cudaError_t launch_lookup(const LookupParams& p, cudaStream_t s);
+
+// Elements that move together, so that a vector of `a` and one of `b` start on the boundaries of their loads and stores.
+inline int vector_elems(uint64_t dim, const void* a, uint32_t a_bytes, const void* b, uint32_t b_bytes) {
+  for (int v = 8; v > 1; v /= 2) {
+    auto on = [&](const void* p, uint32_t bytes) { return reinterpret_cast<uintptr_t>(p) % (v * bytes < 16 ? v * bytes : 16) == 0; };
+    if (dim % v == 0 && on(a, a_bytes) && on(b, b_bytes)) return v;
+  }
+  return 1;
+}
+
+// ---- the batch's tokens of the slice, sorted by row, in their order within a row
+
+struct Met {  // a token of the batch
+  uint32_t row, at;
+};
+constexpr int kSortThreads = 1024, kSortEach = 4, kSortTile = kSortThreads * kSortEach;
+constexpr uint32_t kSortCtas = 128;
+constexpr uint64_t kSortShare = 2 * kSortTile;  // tokens per CTA, at least
+constexpr int kMostDigit = 11;                  // bits of a pass
+
+struct SortPlan {
+  int passes, bits;  // bits of a pass
+  uint32_t bins() const { return 1u << bits; }
+};
+inline SortPlan sort_plan(uint64_t rows) {
+  int bits = 1;
+  while (bits < 31 && (1ull << bits) < rows) ++bits;
+  const int passes = (bits + kMostDigit - 1) / kMostDigit;
+  return {passes, (bits + passes - 1) / passes};
+}
+struct SortParams {
+  Tokens tokens;
+  Met* sorted[2];   // the passes' results in turn
+  uint32_t* counts; // per CTA and bin
+  uint32_t* found;  // tokens of the slice
+  uint32_t* n_long; // set to zero
+  uint8_t* met;     // per row: set to 1 where a token meets it, or null
+  uint64_t share;   // tokens per CTA
+  uint32_t ctas;
+  int bits;
+  int pass;
+};
+cudaError_t configure_sort();
+// All passes; the result is sorted[last].
+cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStream_t s);
+
+// ---- the gradient
+
+// The sorted tokens are cut into ranges of equal length, one for a warp per 32 vectors of columns.
+constexpr uint32_t kSumWarps = 8;
+constexpr uint32_t kRangeWarps = kSms * 80;  // ranges times column tiles, about
+constexpr uint32_t kLeastRange = 8;
+inline uint32_t column_tiles(uint64_t dim, int v) { return static_cast<uint32_t>((dim + 32 * v - 1) / (32 * v)); }
+inline uint32_t ranges_of(uint64_t n, uint32_t tiles) {
+  const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = (kRangeWarps + tiles - 1) / tiles;
+  return static_cast<uint32_t>(most < fill ? most : fill);
+}
+struct SumParams {
+  const Met* sorted;
+  const uint32_t* found;
+  uint32_t* n_long;  // rows in several ranges' parts
+  uint32_t* longs;   // the range where each starts
+  float* parts;      // two rows per range
+  uint8_t* met;      // null: accumulating
+  const void* out;
+  void* grad;
+  uint64_t dim, rows;
+  float scale;
+  uint32_t ranges, tiles;
+  uint32_t sum_ctas, zero_ctas;
+  uint32_t rows_per_zero_cta;
+  uint32_t bf16_out, bf16_grad;
+  int v;
+};
+cudaError_t launch_sum(const SumParams& p, cudaStream_t s);
+
+}  // namespace frk

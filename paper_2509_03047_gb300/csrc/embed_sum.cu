@@ -1,0 +1,235 @@
+// embed_sum.cu -- the table's gradient: per row the sum of its tokens' gradients.
+//
+// The tokens, sorted by row, are cut into ranges of equal length whatever the rows
+// are, so that a token that is a third of the batch costs no more than others: a
+// warp takes a range, and 32 vectors of columns of it.  It adds row by row in
+// fp32, in the tokens' order, and writes a row at its last token.  A range's
+// border inside a row moves to the row's start if the row has no more tokens than a
+// range.  A longer row's parts, one per range, go to the workspace; another launch
+// adds them, in the ranges' order.  Ranges follow from the batch alone, so a
+// repeated call gives the same bits.
+#include <cuda_runtime.h>
+
+#include "embed.h"
+#include "embed_vector.cuh"
+#include "kernels.h"
+
+namespace frk {
+
+namespace {
+
+constexpr uint32_t kAll = 0xFFFFFFFFu;
+constexpr int kThreads = kSumWarps * 32;
+
+__device__ __forceinline__ uint32_t span_of(uint32_t found, uint32_t ranges) {
+  const uint32_t share = (found + ranges - 1) / ranges;
+  return share < kLeastRange ? kLeastRange : share;
+}
+
+// The first place in [lo, hi) whose row is `row` or above, or hi; 32 places are looked at together.
+__device__ __forceinline__ uint32_t first_at_least(const Met* sorted, uint32_t lo, uint32_t hi, uint32_t row, uint32_t lane) {
+  while (lo < hi) {
+    const uint32_t step = (hi - lo + 31) / 32, i = lo + lane * step;
+    const uint32_t below = __popc(__ballot_sync(kAll, i < hi && sorted[i].row < row));
+    if (below == 0) return lo;
+    hi = min(hi, lo + below * step);
+    lo += (below - 1) * step + 1;
+  }
+  return lo;
+}
+
+// Where the range that would start at b does, and whether that is inside a long row.
+struct Border {
+  uint32_t at;
+  bool inside;
+};
+__device__ __forceinline__ Border border(const Met* sorted, uint32_t found, uint32_t span, uint64_t b, uint32_t lane) {
+  if (b == 0) return {0, false};
+  if (b >= found) return {found, false};
+  const uint32_t at = static_cast<uint32_t>(b), row = sorted[at].row;
+  if (sorted[at - 1].row != row) return {at, false};
+  const uint32_t start = first_at_least(sorted, at > span ? at - span : 0, at, row, lane);
+  // (a start a whole span before, or the row beyond, is a long row)
+  const uint32_t end = first_at_least(sorted, at, static_cast<uint32_t>(min(b + span, static_cast<uint64_t>(found))), row + 1, lane);
+  return end - start > span || at - start >= span ? Border{at, true} : Border{start, false};
+}
+
+template <int V>
+__device__ __forceinline__ void add(float (&sum)[V], const float (&x)[V]) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = __fadd_rn(sum[j], x[j]);
+}
+
+// scale * sum, and what is there already, rounded once.
+template <int V, bool Bf16, bool Add>
+__device__ __forceinline__ void finish(void* grad, uint64_t element, float scale, const float (&sum)[V], const Raw<V, Bf16>& old) {
+  float x[V];
+  if (Add) {
+    old.get(x);
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = __fmaf_rn(scale, sum[j], x[j]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = __fmul_rn(scale, sum[j]);
+  }
+  Raw<V, Bf16> w;
+  w.set(x);
+  w.store(grad, element);
+}
+
+// The rows that no token meets: zeros.
+template <int V, bool Bf16>
+__device__ __forceinline__ void clear_rows(const SumParams& p, uint32_t cta) {
+  const uint64_t begin = static_cast<uint64_t>(cta) * p.rows_per_zero_cta, end = min(begin + p.rows_per_zero_cta, p.rows);
+  const uint64_t across = p.dim / V;
+  Raw<V, Bf16> zero;
+  zero.clear();
+  for (uint64_t r = begin; r < end; ++r) {
+    if (p.met[r]) continue;
+    for (uint64_t c = threadIdx.x; c < across; c += kThreads) zero.store(p.grad, r * p.dim + c * V);
+  }
+  __syncthreads();
+  for (uint64_t r = begin + threadIdx.x; r < end; r += kThreads) p.met[r] = 0;  // for the next call
+}
+
+template <int V, bool Bf16Out, bool Bf16Grad, bool Add>
+__global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ SumParams p) {
+  constexpr int kAhead = Add ? 4 : 8;  // tokens whose vectors are on their way together
+  wait_for_kernel_before();
+  if (blockIdx.x >= p.sum_ctas) {
+    if (!Add) clear_rows<V, Bf16Grad>(p, blockIdx.x - p.sum_ctas);
+    return;
+  }
+  const uint32_t lane = threadIdx.x % 32, warp = blockIdx.x * kSumWarps + threadIdx.x / 32;
+  const uint32_t g = warp / p.tiles, found = *p.found, span = span_of(found, p.ranges);
+  const uint64_t b = static_cast<uint64_t>(g) * span;
+  if (g >= p.ranges || b >= found) return;
+  const Border from = border(p.sorted, found, span, b, lane), to = border(p.sorted, found, span, b + span, lane);
+  const uint64_t column = (static_cast<uint64_t>(warp % p.tiles) * 32 + lane) * V;
+  const bool mine = column < p.dim;
+  bool head = from.inside;  // the row at hand started in a range before
+  float sum[V] = {};
+  for (uint32_t i = from.at; i < to.at; i += 32) {
+    const uint32_t here = min(to.at - i, 32u);
+    const Met m = lane < here ? p.sorted[i + lane] : Met{kAll, 0};
+    const uint32_t after = i + lane + 1 < found ? p.sorted[i + lane + 1].row : kAll;
+    const uint32_t ends = __ballot_sync(kAll, lane < here && m.row != after);
+    for (uint32_t k = 0; k < here; k += kAhead) {
+      Raw<V, Bf16Out> in[kAhead];
+      Raw<V, Bf16Grad> old[Add ? kAhead : 1];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const uint64_t at = __shfl_sync(kAll, m.at, k + u);
+        if (k + u < here && mine) in[u].load(p.out, at * p.dim + column);
+        if (Add) {
+          const uint64_t row = __shfl_sync(kAll, m.row, k + u);
+          if (k + u < here && mine && ends >> (k + u) & 1) old[u].load(p.grad, row * p.dim + column);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const uint64_t row = __shfl_sync(kAll, m.row, k + u);
+        if (k + u >= here) break;
+        float x[V];
+        in[u].get(x);
+        add(sum, x);
+        if (!(ends >> (k + u) & 1)) continue;
+        if (mine) {
+          if (head) {
+            Raw<V, false> w;
+            w.set(sum);
+            w.store(p.parts, 2ull * g * p.dim + column);
+          } else {
+            finish<V, Bf16Grad, Add>(p.grad, row * p.dim + column, p.scale, sum, old[Add ? u : 0]);
+          }
+        }
+        head = false;
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] = 0.0f;
+      }
+    }
+  }
+  if (!to.inside) return;
+  if (mine) {
+    Raw<V, false> w;
+    w.set(sum);
+    w.store(p.parts, (2ull * g + !head) * p.dim + column);
+  }
+  if (!head && warp % p.tiles == 0 && lane == 0) p.longs[atomicAdd(p.n_long, 1u)] = g;
+}
+
+// A long row's parts: the second of the range where it starts, the first of the ranges after it that start inside it.  (The list's order
+// is any; each row has its place.)
+template <int V, bool Bf16Grad, bool Add>
+__global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ SumParams p) {
+  __shared__ float sums[kSumWarps][32 * V + 1];
+  wait_for_kernel_before();
+  const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint32_t found = *p.found, span = span_of(found, p.ranges);
+  const uint64_t items = static_cast<uint64_t>(*p.n_long) * p.tiles;
+  for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint32_t g = p.longs[item / p.tiles];
+    const uint32_t row = p.sorted[static_cast<uint64_t>(g + 1) * span].row;
+    uint32_t more = 0;  // parts after the first one
+    for (;;) {
+      const uint64_t at = static_cast<uint64_t>(g + 1 + more + threadIdx.x) * span;
+      const uint32_t n = __syncthreads_count(at < found && p.sorted[at < found ? at : 0].row == row);
+      more += n;
+      if (n < kThreads) break;
+    }
+    const uint64_t column = (item % p.tiles * 32 + lane) * V;
+    const bool mine = column < p.dim;
+    float sum[V] = {};
+    if (mine) {
+#pragma unroll 4
+      for (uint32_t k = warp; k <= more; k += kSumWarps) {
+        Raw<V, false> w;
+        w.load(p.parts, (2ull * (g + k) + (k == 0)) * p.dim + column);
+        float x[V];
+        w.get(x);
+        add(sum, x);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j) sums[warp][lane * V + j] = sum[j];
+    __syncthreads();
+    if (warp == 0 && mine) {
+      for (int w = 1; w < static_cast<int>(kSumWarps); ++w)
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] = __fadd_rn(sum[j], sums[w][lane * V + j]);
+      Raw<V, Bf16Grad> old;
+      if (Add) old.load(p.grad, row * p.dim + column);
+      finish<V, Bf16Grad, Add>(p.grad, row * p.dim + column, p.scale, sum, old);
+    }
+    __syncthreads();
+  }
+}
+
+template <int V, bool Bf16Out, bool Bf16Grad, bool Add>
+cudaError_t launch(const SumParams& p, cudaStream_t s) {
+  cudaError_t e = launch_chained(sum_kernel<V, Bf16Out, Bf16Grad, Add>, static_cast<int>(p.sum_ctas + p.zero_ctas), kThreads, 0, s, p);
+  if (e == cudaSuccess) e = launch_chained(join_kernel<V, Bf16Grad, Add>, static_cast<int>(kSms * 4), kThreads, 0, s, p);
+  return e;
+}
+template <int V, bool Bf16Out>
+cudaError_t launch_typed(const SumParams& p, cudaStream_t s) {
+  if (p.met == nullptr) return p.bf16_grad ? launch<V, Bf16Out, true, true>(p, s) : launch<V, Bf16Out, false, true>(p, s);
+  return p.bf16_grad ? launch<V, Bf16Out, true, false>(p, s) : launch<V, Bf16Out, false, false>(p, s);
+}
+template <int V>
+cudaError_t launch_wide(const SumParams& p, cudaStream_t s) {
+  return p.bf16_out ? launch_typed<V, true>(p, s) : launch_typed<V, false>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_sum(const SumParams& p, cudaStream_t s) {
+  switch (p.v) {
+    case 8: return launch_wide<8>(p, s);
+    case 4: return launch_wide<4>(p, s);
+    case 2: return launch_wide<2>(p, s);
+    default: return launch_wide<1>(p, s);
+  }
+}
+
+}  // namespace frk

@@ -61,6 +61,7 @@ class PlanMemory {
     places_.push_back({reinterpret_cast<void**>(at), scratch_, true});
     scratch_ = align_up(scratch_ + count * sizeof(T), kAlign);
   }
+  uint64_t scratch_bytes() const { return scratch_; }
   // Allocates, copies the tables and sets every pointer.  The wait is for the
   // copy's last part: one from pageable memory may return while that is still
   // on its way, on the legacy stream, and a call on a non-blocking stream is

@@ -129,6 +129,12 @@ def _load() -> ctypes.CDLL:
     L.fr_muon_destroy.restype = None
     L.fr_muon_step.argtypes = [vp, ctypes.POINTER(fr_muon), vp, vp]
     L.fr_orthogonalize.argtypes = [vp, ctypes.POINTER(fr_muon), vp]
+    L.fr_embed_create.argtypes = [u64, u64, u64, u64, ctypes.POINTER(vp)]
+    L.fr_embed_info.argtypes = [vp, u64p, u64p, u64p, u64p]
+    L.fr_embed_destroy.argtypes = [vp]
+    L.fr_embed_destroy.restype = None
+    L.fr_embed_lookup.argtypes = [vp, vp, u32, vp, u32, u64, ctypes.c_float, vp, u32, vp]
+    L.fr_embed_grad.argtypes = [vp, vp, u32, vp, u32, u64, ctypes.c_float, vp, u32, u32, vp]
     L.fr_status_str.argtypes = [ctypes.c_int]
     L.fr_status_str.restype = ctypes.c_char_p
     L.fr_last_error.argtypes = []
@@ -139,7 +145,8 @@ def _load() -> ctypes.CDLL:
                  "fr_plan_create_batched", "fr_plan_batch", "fr_pack_batch", "fr_unpack_verify_batch",
                  "fr_unpack_collect", "fr_resend", "fr_restore", "fr_shard_pieces", "fr_pack_fp", "fr_unpack_verify_fp",
                  "fr_restore_fp", "fr_resend_fp", "fr_restore_multi", "fr_opt_create", "fr_opt_info", "fr_grad_clip",
-                 "fr_adamw_step", "fr_opt_convert", "fr_muon_create", "fr_muon_info", "fr_muon_step", "fr_orthogonalize"]:
+                 "fr_adamw_step", "fr_opt_convert", "fr_muon_create", "fr_muon_info", "fr_muon_step", "fr_orthogonalize",
+                 "fr_embed_create", "fr_embed_info", "fr_embed_lookup", "fr_embed_grad"]:
         getattr(L, name).restype = ctypes.c_int
     return L
 
@@ -605,6 +612,61 @@ def fr_orthogonalize(plan, hyper: fr_muon, stream=None) -> None:
     _check(lib.fr_orthogonalize(plan, hyper, _stream(stream)), "fr_orthogonalize")
 
 
+# ---------------------------------------------------------------- embeddings
+
+_TOKENS = {torch.int32: 4, torch.int64: 8}
+
+
+def _buffer(name: str, t: torch.Tensor, allowed):
+    """(address, code of the type) of a contiguous CUDA tensor"""
+    if t.numel() and not t.is_cuda:
+        raise ValueError("%s is not on a CUDA device" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s is not contiguous" % name)
+    code = allowed.get(t.dtype)
+    if code is None:
+        raise ValueError("%s: unsupported dtype %s" % (name, t.dtype))
+    return (t.data_ptr() if t.numel() else None), code
+
+
+def fr_embed_create(rows: int, dim: int, max_tokens: int, first: int = 0):
+    """Plan of an embedding's slice [first, first + rows) on the current device.  Returns the opaque handle (int)."""
+    if min(rows, dim, max_tokens, first) < 0:
+        raise ValueError("rows, dim, max_tokens and first are not negative")
+    h = ctypes.c_void_p()
+    _check(lib.fr_embed_create(rows, dim, max_tokens, first, ctypes.byref(h)), "fr_embed_create")
+    return h.value
+
+
+def fr_embed_info(plan):
+    """(rows, dim, max_tokens, bytes of device memory)"""
+    x = [ctypes.c_uint64() for _ in range(4)]
+    _check(lib.fr_embed_info(plan, *(ctypes.byref(v) for v in x)), "fr_embed_info")
+    return tuple(v.value for v in x)
+
+
+def fr_embed_destroy(plan) -> None:
+    if plan:
+        lib.fr_embed_destroy(plan)
+
+
+def fr_embed_lookup(plan, table: torch.Tensor, tokens: torch.Tensor, scale: float, out: torch.Tensor, stream=None) -> None:
+    """`out`: as many rows as `tokens` (int32 or int64) has elements."""
+    w, wt = _buffer("table", table, _FLOATS)
+    t, tb = _buffer("tokens", tokens, _TOKENS)
+    o, ot = _buffer("out", out, _FLOATS)
+    _check(lib.fr_embed_lookup(plan, w, wt, t, tb, tokens.numel(), scale, o, ot, _stream(stream)), "fr_embed_lookup")
+
+
+def fr_embed_grad(plan, out: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                  stream=None) -> None:
+    """The table's gradient `grad` from the rows' gradients `out`."""
+    o, ot = _buffer("out", out, _FLOATS)
+    t, tb = _buffer("tokens", tokens, _TOKENS)
+    g, gt = _buffer("grad", grad, _FLOATS)
+    _check(lib.fr_embed_grad(plan, o, ot, t, tb, tokens.numel(), scale, g, gt, int(bool(accumulate)), _stream(stream)), "fr_embed_grad")
+
+
 # ---------------------------------------------------------------- convenience
 
 def fr_shard_pieces(n_elems: int, elem_bytes: int, n_dst: int, rank: int, n_src: int):
@@ -807,3 +869,58 @@ class MuonPlan:
     def orthogonalize(self, hyper: Optional[fr_muon] = None, stream=None) -> None:
         """Writes the plan's updates from its gradients."""
         fr_orthogonalize(self.handle, muon() if hyper is None else hyper, stream)
+
+
+class EmbedPlan:
+    """A plan of an embedding's slice on the current device (arguments as fr_embed_create)."""
+
+    def __init__(self, rows: int, dim: int, max_tokens: int, first: int = 0):
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.handle = None
+        self.handle = fr_embed_create(rows, dim, max_tokens, first)
+        self.rows, self.dim, self.max_tokens, self.device_bytes = fr_embed_info(self.handle)
+        self.first = first
+
+    def close(self) -> None:
+        if self.handle:
+            fr_embed_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _here(self, name: str, t: torch.Tensor, shape) -> None:
+        if t.numel() and t.device != self.device:
+            raise ValueError("%s is on %s, the plan on %s" % (name, t.device, self.device))
+        if shape is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError("%s has the shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+
+    def lookup(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+        """scale * table[tokens - first], of the shape of `tokens` and dim; by default in the table's type."""
+        self._here("table", table, (self.rows, self.dim))
+        self._here("tokens", tokens, None)
+        if out is None:
+            with _allocating_on(stream, self.device):
+                out = torch.empty(*tokens.shape, self.dim, dtype=table.dtype, device=self.device)
+        self._here("out", out, (*tokens.shape, self.dim))
+        fr_embed_lookup(self.handle, table, tokens, scale, out, stream)
+        return out
+
+    def grad(self, out: torch.Tensor, tokens: torch.Tensor, grad: Optional[torch.Tensor] = None, scale: float = 1.0,
+             accumulate: bool = False, stream=None) -> torch.Tensor:
+        """The table's gradient from the gradient `out` of what lookup() gave, in `grad` (by default a new one, in fp32), or
+        added to what is there."""
+        self._here("out", out, (*tokens.shape, self.dim))
+        self._here("tokens", tokens, None)
+        if grad is None:
+            if accumulate:
+                raise ValueError("accumulate needs a gradient to add to")
+            with _allocating_on(stream, self.device):
+                grad = torch.empty(self.rows, self.dim, dtype=torch.float32, device=self.device)
+        self._here("grad", grad, (self.rows, self.dim))
+        fr_embed_grad(self.handle, out, tokens, grad, scale, accumulate, stream)
+        return grad
