@@ -588,6 +588,11 @@ fr_status fr_muon_step(fr_muon_plan plan, const fr_muon* hyper, const fr_clip* c
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
 fr_status fr_orthogonalize(fr_muon_plan plan, const fr_muon* hyper, void* stream);
 
+/* Synchronize `stream`, then return and clear the condition that the plan's kernels
+ * recorded: FR_ERR_DEVICE_TIMEOUT, a wait inside a kernel given up after seconds (weights
+ * and updates are left as they were, then and until this call), else FR_OK. */
+fr_status fr_muon_sync_status(fr_muon_plan plan, void* stream);
+
 /* ---------------------------------------------------------------- embeddings */
 
 /* A rank's part of a model's embedding: the rows [first, first + rows) of a table of

@@ -21,8 +21,8 @@ SOURCES = ["sweep_fp.cu", "sweep_pack.cu", "sweep_unpack.cu", "sweep_unpack_fp.c
            "muon_api.cu", "muon_elements.cu", "muon_product.cu", "embed_api.cu", "embed_lookup.cu",
            "embed_sort.cu", "embed_sum.cu"]
 HEADERS = ["gf2.cuh", "layout.h", "kernels.h", "sweep_impl.cuh", "warp_share.h", "seg_walk.h", "host.h", "optim.h",
-           "optim_math.cuh", "optim_block.cuh", "muon.h", "muon_block.cuh", "embed.h",
-           "embed_vector.cuh"]
+           "optim_math.cuh", "optim_block.cuh", "muon.h", "muon_block.cuh", "muon_tiles.h",
+           "tensor_core.cuh", "embed.h", "embed_vector.cuh"]
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr",

@@ -17,8 +17,8 @@
 #pragma once
 
 #include <cstdint>
-#include <vector>
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/flashrec.h"
@@ -73,6 +73,7 @@ struct MuonParams {
   MuonNorm* norms;
   uint8_t* work;
   const fr_clip* clip;     // may be null
+  const uint32_t* status;  // not zero: a product gave up, nothing is written
   float beta, beta_rest;   // beta, 1 - beta
   float lr, decay;
   uint32_t momentum;       // 0: G is the gradient
@@ -91,22 +92,25 @@ cudaError_t launch_muon_update(const MuonParams& p, cudaStream_t s);    // fr_or
 enum : int { kGram = 0, kPoly = 1, kNext = 2 };  // S, P, the next X
 constexpr int kPhases = 3;
 
-struct MuonTile {
+struct MuonTile {       // by a pair of CTAs
   uint32_t tensor;
-  uint16_t row, col;  // of tiles, of the product
+  uint16_t row, col;    // of blocks of 128, even numbers
+  uint32_t wide;        // 256 columns, else 128
 };
-// The tiles of each phase's products.
-void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile> (&tiles)[kPhases]);
 struct MuonProduct {
   const MuonDesc* tensors;
   const MuonTile* tiles;
   uint32_t n_tiles;
   uint8_t* work;
   const fr_clip* clip;
+  uint32_t* status;  // set to 1 by a kernel that gave up a wait
   float a, b, c;
   uint32_t from;  // which of x[] is the old iterate
 };
-constexpr int kTile = 64;
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, cudaStream_t s);
+// Per device, before the first launch: opt the kernels in to their shared-memory size.
+cudaError_t configure_muon_product();
+// map: the workspace as rows of 128 bytes, kMapRows of which a copy takes.
+constexpr uint32_t kMapRows = 64;
+cudaError_t launch_muon_product(int phase, const MuonProduct& p, const CUtensorMap& map, cudaStream_t s);
 
 }  // namespace frk

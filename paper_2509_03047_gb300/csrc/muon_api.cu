@@ -13,6 +13,7 @@
 #include "host.h"
 #include "kernels.h"
 #include "muon.h"
+#include "muon_tiles.h"
 #include "optim.h"
 
 using namespace frk;
@@ -32,12 +33,14 @@ struct fr_muon_plan_s {
   MuonPartial* d_partials = nullptr;
   MuonNorm* d_norms = nullptr;
   uint8_t* d_work = nullptr;
+  uint32_t* d_status = nullptr;
+  CUtensorMap map;
 };
 
 namespace {
 
 constexpr uint64_t kMostSide = FR_MUON_MOST_SIDE;
-constexpr uint64_t kMostElems = 1ull << 40;
+constexpr uint64_t kMostElems = 1ull << 35;  // filled up: the workspace's rows of 128 bytes have 31-bit indices
 
 bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 uint64_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
@@ -86,6 +89,21 @@ MuonDesc describe(const fr_muon_tensor& x, uint64_t index) {
 
 uint64_t square_blocks(const MuonDesc& d) { return 2ull * d.side_blocks * d.side_blocks; }
 
+// The workspace as rows of 128 bytes.
+cudaError_t make_map(CUtensorMap* map, void* at, uint64_t bytes) {
+  void* entry = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
+  if (e != cudaSuccess) return e;
+  if (found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  const cuuint64_t sizes[2] = {64, bytes / 128}, strides[1] = {128};
+  const cuuint32_t box[2] = {64, kMapRows}, steps[2] = {1, 1};
+  const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(entry)(
+      map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, at, sizes, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_tensors) {
   std::vector<MuonDesc> descs;
   std::vector<uint32_t> units, blocks;
@@ -130,13 +148,17 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   }
   mem.table(&p->d_norms, std::vector<MuonNorm>(descs.size(), MuonNorm{}));
   mem.scratch(&p->d_partials, units.size());
-  // (to the bulk copies' boundary from PlanMemory's)
+  mem.table(&p->d_status, std::vector<uint32_t>(1, 0));
   mem.scratch(&p->d_work, bytes);
   p->n_units = static_cast<uint32_t>(units.size());
   p->n_blocks = static_cast<uint32_t>(blocks.size());
   p->device_bytes = bytes;
-  const cudaError_t e = mem.commit(&p->d_memory);
-  return e == cudaSuccess ? FR_OK : report_cuda("plan device tables", e);
+  cudaError_t e = mem.commit(&p->d_memory);
+  if (e != cudaSuccess) return report_cuda("plan device tables", e);
+  if (bytes == 0) return FR_OK;
+  e = configure_muon_product();
+  if (e == cudaSuccess) e = make_map(&p->map, p->d_work, bytes);
+  return e == cudaSuccess ? FR_OK : report_cuda("tensor map of the workspace", e);
 }
 
 // Largest |f| on [0, top] of an odd or even polynomial given by its values and the places where its derivative in s^2 vanishes.
@@ -185,6 +207,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   q.tensors = p->d_tensors;
   q.work = p->d_work;
   q.clip = mp.clip;
+  q.status = p->d_status;
   for (uint32_t i = 0; i < h.iterations; ++i) {
     q.a = static_cast<float>(h.coef[i][0]);
     q.b = static_cast<float>(h.coef[i][1]);
@@ -193,7 +216,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
     for (int phase = 0; phase < kPhases; ++phase) {
       q.tiles = p->d_tiles[phase];
       q.n_tiles = p->n_tiles[phase];
-      e = launch_muon_product(phase, q, s);
+      e = launch_muon_product(phase, q, p->map, s);
       if (e != cudaSuccess) return report_cuda("product kernel launch", e);
     }
   }
@@ -211,6 +234,7 @@ MuonParams params(fr_muon_plan p) {
   mp.partials = p->d_partials;
   mp.norms = p->d_norms;
   mp.work = p->d_work;
+  mp.status = p->d_status;
   return mp;
 }
 
@@ -313,6 +337,24 @@ fr_status fr_muon_step(fr_muon_plan p, const fr_muon* h, const fr_clip* clip_dev
   if (st != FR_OK) return st;
   const cudaError_t e = launch_muon_apply(mp, static_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? FR_OK : report_cuda("weight kernel launch", e);
+}
+
+fr_status fr_muon_sync_status(fr_muon_plan p, void* stream) {
+  CallRange nvtx("fr_muon_sync_status");
+  if (p == nullptr) return report_invalid("fr_muon_sync_status", "plan is null");
+  if (p->n_blocks == 0) return FR_OK;
+  DeviceGuard g(p->device);
+  if (!g.ok) return report_cuda("select plan device", cudaGetLastError());
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  uint32_t status = 0;
+  cudaError_t e = cudaMemcpyAsync(&status, p->d_status, sizeof status, cudaMemcpyDeviceToHost, s);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+  if (e == cudaSuccess && status != 0) {
+    e = cudaMemsetAsync(p->d_status, 0, sizeof status, s);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(s);
+    if (e == cudaSuccess) return FR_ERR_DEVICE_TIMEOUT;
+  }
+  return e == cudaSuccess ? FR_OK : report_cuda("read the plan's status", e);
 }
 
 fr_status fr_orthogonalize(fr_muon_plan p, const fr_muon* h, void* stream) {

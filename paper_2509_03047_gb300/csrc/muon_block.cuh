@@ -1,5 +1,5 @@
 // muon_block.cuh -- an iterate's blocks: places of chunks of eight elements,
-// halves of a number, what a product's sum becomes.
+// halves of a number.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -43,39 +43,6 @@ __device__ __forceinline__ void floats(const uint4& w, float (&x)[8]) {
 }
 __device__ __forceinline__ uint4 halves(const float (&x)[8]) {
   return make_uint4(half2_bits(x[0], x[1]), half2_bits(x[2], x[3]), half2_bits(x[4], x[5]), half2_bits(x[6], x[7]));
-}
-
-// What eight sums of a product, of row r and the columns 8 c ..., become.
-//   S = X X^T            sums in X's scale twice
-//   P = a I + b S + c S^2
-//   X = P X1 + a X2      X1, X2 the halves of the old X; a I in P has the first one's part
-template <int kPhase>
-__device__ __forceinline__ void finish_chunk(const MuonProduct& p, const MuonDesc& d, uint32_t r, uint32_t c, float (&v)[8]) {
-  if (kPhase == kGram) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= kScaleS / (kScaleX * kScaleX);
-    *reinterpret_cast<uint4*>(p.work + d.s + chunk_at(2 * d.side_blocks, r, c)) = halves(v);
-  } else if (kPhase == kPoly) {
-    const uint64_t at = chunk_at(2 * d.side_blocks, r, c);
-    float s[8];
-    floats(*reinterpret_cast<const uint4*>(p.work + d.s + at), s);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float own = r == 8 * c + j ? p.a * kScaleP : 0.0f;
-      v[j] = own + s[j] * (p.b * (kScaleP / kScaleS)) + v[j] * (p.c * (kScaleP / (kScaleS * kScaleS)));
-    }
-    *reinterpret_cast<uint4*>(p.work + d.p + at) = halves(v);
-  } else {
-    const uint64_t at = chunk_at(d.col_blocks, r, c);
-    float x[8];
-    floats(*reinterpret_cast<const uint4*>(p.work + d.low + at), x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = v[j] * (1.0f / kScaleP) + p.a * x[j];
-    uint4 hi, lo;
-    split(v, hi, lo);
-    *reinterpret_cast<uint4*>(p.work + d.x[p.from ^ 1] + at) = hi;
-    *reinterpret_cast<uint4*>(p.work + d.low + at) = lo;
-  }
 }
 
 }  // namespace frk

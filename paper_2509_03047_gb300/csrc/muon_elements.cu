@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kElementThreads) apply_kernel(const __grid_con
   const uint32_t t = p.blocks[blockIdx.x];
   const MuonDesc& d = p.tensors[t];
   wait_for_kernel_before();
-  if (skipped(p)) return;
+  if (skipped(p) || *p.status != 0) return;
   const Chunks at(d, blockIdx.x);
   const float lr = __fmul_rn(p.lr, d.lr_scale), decay = __fmul_rn(p.decay, d.decay_scale);
   const RandomKey key = random_key(p.key, d.tensor);
@@ -268,6 +268,7 @@ __global__ void __launch_bounds__(kElementThreads) update_kernel(const __grid_co
   const uint32_t t = p.blocks[blockIdx.x];
   const MuonDesc& d = p.tensors[t];
   wait_for_kernel_before();
+  if (*p.status != 0) return;
   const Chunks at(d, blockIdx.x);
 #pragma unroll
   for (int k = 0; k < kChunks; ++k) {

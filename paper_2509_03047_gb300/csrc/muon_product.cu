@@ -1,82 +1,334 @@
 // muon_product.cu -- the products of the orthogonalised update, all matrices of a
 // list in one launch.
-#include <cuda_runtime.h>
+//
+// D[i][j] = sum over k of A(i, k) B(j, k), tiles of 256 x 256 by pairs of CTAs, one
+// pair per two SMs, each taking every n-th tile of the list.  A warp brings the
+// factors' blocks, 64 of the contraction at a time; a thread multiplies; eight warps
+// turn the sums into fp16 blocks, while the next tile's products fill the other half
+// of tensor memory.  The blocks lie in memory as the tensor cores read them, by rows
+// or by columns, so X X^T, X^T X and products from either side need no
+// transposition, and results leave as they come, by bulk copies.  Of the symmetric
+// products the tiles on and below the diagonal are computed, and those below written
+// a second time, transposed.
+#include <algorithm>
 
 #include "kernels.h"
 #include "muon_block.cuh"
+#include "optim.h"
+#include "tensor_core.cuh"
 
 namespace frk {
 
 namespace {
 
-// A product's factors as D[i][j] = sum over k of A(i, k) B(j, k): each a matrix of the workspace, read by its rows or by its columns.
+constexpr int kStages = 5;
+constexpr int kFactorBytes = 16384;  // 128 rows or columns of a factor, 64 of the contraction
+constexpr int kHalf = 8192;
+constexpr int kStageBytes = 2 * kFactorBytes;
+constexpr int kGroups = 2;           // of four warps, one of 64 columns each
+constexpr int kThreads = 64 + kGroups * 128;
+constexpr int kStaging = 2 * kBlockBytes;  // per group
+constexpr int kTensorColumns = 512;
+constexpr size_t kShared = 1024 + kStages * kStageBytes + kGroups * kStaging;
+
+struct Control {
+  uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2], in[kGroups];
+  uint32_t tensor;
+  uint32_t gave_up;
+};
+
+// A factor's blocks: a matrix of the workspace, by its rows or by its columns.
 struct Factor {
-  const uint8_t* at;
+  uint64_t at;
   uint32_t col_blocks;
   bool by_columns;
-  __device__ __forceinline__ float get(uint32_t i, uint32_t k) const {
-    const uint32_t r = by_columns ? k : i, c = by_columns ? i : k;
-    return __half2float(*reinterpret_cast<const __half*>(at + chunk_at(col_blocks, r, c / 8) + c % 8 * 2));
+  // Row, in units of 128 bytes, of the workspace where half `h` (of 64 rows or columns) of block b of the operand begins, step k of the contraction.
+  __device__ __forceinline__ int32_t row(uint32_t b, uint32_t h, uint32_t k) const {
+    const uint64_t block = by_columns ? static_cast<uint64_t>(k / 2) * col_blocks + 2 * b + h : static_cast<uint64_t>(b) * col_blocks + k;
+    return static_cast<int32_t>((at + block * kBlockBytes) / 128 + 64 * (by_columns ? k % 2 : h));
   }
 };
 
 template <int kPhase>
-__global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ MuonProduct p) {
-  __shared__ float a[16][kTile + 1], b[16][kTile + 1];
-  wait_for_kernel_before();
-  if (p.clip != nullptr && p.clip->nonfinite != 0) return;
-  const MuonTile t = p.tiles[blockIdx.x];
-  const MuonDesc& d = p.tensors[t.tensor];
-  const Factor x = {p.work + d.x[p.from], d.col_blocks, (kPhase == kGram) == (d.tall != 0)};
-  Factor f = x, g = x;
-  if (kPhase == kPoly) f = g = {p.work + d.s, 2 * d.side_blocks, false};
-  if (kPhase == kNext) {
-    const Factor q = {p.work + d.p, 2 * d.side_blocks, false};
-    f = d.tall ? Factor{x.at, x.col_blocks, false} : q;
-    g = d.tall ? q : Factor{x.at, x.col_blocks, true};
-  }
-  const uint32_t depth = kPhase == kGram ? (d.tall ? d.row_blocks * kBlockRows : d.col_blocks * kBlockCols) : d.side_blocks * 128;
-  const uint32_t i0 = t.row * kTile, j0 = t.col * kTile;
-  const int row = threadIdx.x / 8, col = threadIdx.x % 8;  // two rows, 32 apart, of eight columns
-  float sum[2][8] = {};
-  for (uint32_t k0 = 0; k0 < depth; k0 += 16) {
-    for (int q = threadIdx.x; q < 16 * kTile; q += 256) {
-      const int k = q % 16, i = q / 16;
-      a[k][i] = f.get(i0 + i, k0 + k);
-      b[k][i] = g.get(j0 + i, k0 + k);
+struct Operands {
+  Factor a, b;
+  uint32_t depth;     // steps of 64
+  uint32_t a_blocks;  // rows of the product, in blocks of 128
+  __device__ __forceinline__ Operands(const MuonProduct& p, const MuonDesc& d) {
+    const uint64_t x = d.x[p.from];
+    const uint32_t side = d.side_blocks;
+    if (kPhase == kGram) {
+      a = b = {x, d.col_blocks, d.tall != 0};
+      depth = d.tall ? 2 * d.row_blocks : d.col_blocks;
+      a_blocks = side;
+    } else if (kPhase == kPoly) {
+      a = b = {d.s, 2 * side, false};
+      depth = 2 * side;
+      a_blocks = side;
+    } else {
+      const Factor q = {d.p, 2 * side, false};
+      a = d.tall ? Factor{x, d.col_blocks, false} : q;
+      b = d.tall ? q : Factor{x, d.col_blocks, true};
+      depth = 2 * side;
+      a_blocks = d.row_blocks;
     }
-    __syncthreads();
+  }
+};
+
+// Where a stage and its phase stand.
+struct Ring {
+  uint32_t stage = 0, phase = 0;
+  __device__ __forceinline__ void next() {
+    if (++stage == kStages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  }
+};
+
+__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
+
+// The same, and whether `ok` is true of every thread: nobody leaves a group alone.
+__device__ __forceinline__ bool group_agrees(int group, bool ok) {
+  uint32_t all;
+  asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %2, 0;\n\tbarrier.cta.red.and.pred b, %1, 128, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
+               : "=r"(all)
+               : "r"(group + 1), "r"(static_cast<uint32_t>(ok))
+               : "memory");
+  return all != 0;
+}
+
+template <int kPhase>
+__device__ __forceinline__ void bring(const MuonProduct& p, const CUtensorMap& map, uint32_t ring_at, Control& c, uint32_t rank) {
+  Ring r;
+  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2) {
+    const MuonTile tile = p.tiles[t];
+    const Operands<kPhase> o(p, p.tensors[tile.tensor]);
+    // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
+    const uint32_t a = min(tile.row + rank, o.a_blocks - 1);
+    const uint32_t bytes = 2 * kFactorBytes + (tile.wide ? 2 * kFactorBytes : kFactorBytes);
+    for (uint32_t k = 0; k < o.depth; ++k) {
+      const uint32_t full = shared_address(&c.full[r.stage]), to = ring_at + r.stage * kStageBytes;
+      if (!wait_phase(shared_address(&c.empty[r.stage]), r.phase ^ 1, &c.gave_up)) return let_copies_land();
+      if (rank == 0) expect_bytes(full, bytes);
+      load_rows(to, &map, o.a.row(a, 0, k), full);
+      load_rows(to + kHalf, &map, o.a.row(a, 1, k), full);
+      if (tile.wide) {
+        load_rows(to + kFactorBytes, &map, o.b.row(tile.col + rank, 0, k), full);
+        load_rows(to + kFactorBytes + kHalf, &map, o.b.row(tile.col + rank, 1, k), full);
+      } else {
+        load_rows(to + kFactorBytes, &map, o.b.row(tile.col, rank, k), full);
+      }
+      r.next();
+    }
+  }
+}
+
+template <int kPhase>
+__device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ring_at, Control& c) {
+  Ring r;
+  uint32_t n = 0;
+  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2, ++n) {
+    const MuonTile tile = p.tiles[t];
+    const Operands<kPhase> o(p, p.tensors[tile.tensor]);
+    const uint32_t half = n % 2, kind = product_kind(o.a.by_columns, o.b.by_columns, tile.wide ? 256 : 128);
+    const uint32_t a_step = o.a.by_columns ? 2048 >> 4 : 32 >> 4, b_step = o.b.by_columns ? 2048 >> 4 : 32 >> 4;
+    if (!wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up)) return let_copies_land();
+    tensor_fence_after();
+    const uint32_t sums = c.tensor + half * 256;
+    for (uint32_t k = 0; k < o.depth; ++k) {
+      if (!wait_phase(shared_address(&c.full[r.stage]), r.phase, &c.gave_up)) return let_copies_land();
+      tensor_fence_after();
+      const uint32_t at = ring_at + r.stage * kStageBytes;
+      const uint64_t a = factor(at, o.a.by_columns, kHalf), b = factor(at + kFactorBytes, o.b.by_columns, kHalf);
 #pragma unroll
-    for (int k = 0; k < 16; ++k)
+      for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + j * b_step, kind, k + j > 0);
+      arrive_after_products(shared_address(&c.empty[r.stage]));
+      r.next();
+    }
+    arrive_after_products(shared_address(&c.sums_full[half]));
+  }
+}
+
+// What sums of a product, the thread's row and 64 columns of it, become, in shared memory:
+//   S = X X^T             sums in X's scale twice
+//   P = a I + b S + c S^2
+//   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part
+// `one`: block of S or P, or of second halves (the old ones are there); `two`: the transposed block, or the first halves.
+template <int kPhase>
+__device__ __forceinline__ void finish_row(const MuonProduct& p, uint32_t row, uint32_t diagonal, float (&v)[64], uint8_t* one, uint8_t* two, bool transpose) {
+#pragma unroll
+  for (uint32_t c = 0; c < 8; ++c) {
+    float x[8], y[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = v[8 * c + j];
+    const uint32_t at = row * 128 + ((c ^ (row % 8)) * 16);
+    uint4* const q = reinterpret_cast<uint4*>(one + at);
+    if (kPhase == kGram) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= kScaleS / (kScaleX * kScaleX);
+      *q = halves(x);
+    } else if (kPhase == kPoly) {
+      floats(*q, y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        sum[0][j] += a[k][row] * b[k][col * 8 + j];
-        sum[1][j] += a[k][row + 32] * b[k][col * 8 + j];
+        const float own = diagonal == 8 * c + j ? p.a * kScaleP : 0.0f;
+        x[j] = own + y[j] * (p.b * (kScaleP / kScaleS)) + x[j] * (p.c * (kScaleP / (kScaleS * kScaleS)));
       }
-    __syncthreads();
+      *q = halves(x);
+    } else {
+      floats(*q, y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = x[j] * (1.0f / kScaleP) + p.a * y[j];
+      uint4 hi, lo;
+      split(x, hi, lo);
+      *q = lo;
+      *reinterpret_cast<uint4*>(two + at) = hi;
+    }
+    if (kPhase != kNext && transpose) {
+      // (neighbouring threads write neighbouring columns: no bank is met twice)
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j)
+        *reinterpret_cast<__half*>(two + row / 64 * kHalf + (8 * c + j) * 128 + (((row % 64 / 8) ^ j) * 16) + row % 8 * 2) = __float2half_rn(x[j]);
+    }
   }
-  finish_chunk<kPhase>(p, d, i0 + row, j0 / 8 + col, sum[0]);
-  finish_chunk<kPhase>(p, d, i0 + row + 32, j0 / 8 + col, sum[1]);
+}
+
+template <int kPhase>
+__device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* staging, Control& c, uint32_t rank) {
+  const int group = (threadIdx.x - 64) / 128;
+  const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + threadIdx.x % 32;  // a warp reads the quarter of its index
+  const bool one_thread = threadIdx.x % 128 == 64;  // of the group
+  uint8_t *const one = staging + group * kStaging, *const two = one + kBlockBytes;
+  const uint32_t one_at = shared_address(one), two_at = shared_address(two), in = shared_address(&c.in[group]);
+  uint32_t n = 0, phase = 0;
+  bool ok = true;
+  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2, ++n) {
+    const MuonTile tile = p.tiles[t];
+    const MuonDesc& d = p.tensors[tile.tensor];
+    const uint32_t half = n % 2, parts = tile.wide ? 4 : 2;
+    const uint32_t block_row = tile.row + rank, across = kPhase == kNext ? d.col_blocks : 2 * d.side_blocks;
+    const bool mine = block_row < (kPhase == kNext ? d.row_blocks : d.side_blocks);
+    const bool transpose = kPhase != kNext && tile.row != tile.col;
+    for (uint32_t q = group; q < parts; q += kGroups) {
+      const uint64_t at = (static_cast<uint64_t>(block_row) * across + 2 * tile.col + q) * kBlockBytes;
+      if (mine && one_thread) {
+        wait_stores_read();  // of the blocks before
+        if (kPhase != kGram) {
+          expect_bytes(in, kBlockBytes);
+          load_bytes(one_at, p.work + (kPhase == kPoly ? d.s : d.low) + at, kBlockBytes, in);
+        }
+      }
+      if (q == static_cast<uint32_t>(group)) {
+        ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up);
+        tensor_fence_after();
+      }
+      __syncwarp();
+      float v[64];
+      const uint32_t from = c.tensor + (quarter * 32 << 16) + half * 256 + q * 64;
+      tensor_load(from, v);
+      tensor_load(from + 32, v + 32);
+      tensor_load_wait();
+      if (q + kGroups >= parts) tensor_fence_before();
+      if (mine) {
+        if (kPhase != kGram) {
+          ok = wait_phase(in, phase, &c.gave_up) && ok;
+          phase ^= 1;
+        } else {
+          group_sync(group);
+        }
+        // (the diagonal's column of this row among the block's)
+        finish_row<kPhase>(p, row, block_row * kBlockRows + row - (2 * tile.col + q) * kBlockCols, v, one, two, transpose);
+        before_copies();
+      }
+      __syncwarp();
+      if (!group_agrees(group, ok)) return let_copies_land();
+      if (one_thread) {
+        if (q + kGroups >= parts) arrive_in_first(shared_address(&c.sums_empty[half]));
+        if (mine) {
+          if (kPhase == kNext) {
+            store_bytes(p.work + d.low + at, one_at, kBlockBytes);
+            store_bytes(p.work + d.x[p.from ^ 1] + at, two_at, kBlockBytes);
+          } else {
+            uint8_t* const to = p.work + (kPhase == kGram ? d.s : d.p);
+            store_bytes(to + at, one_at, kBlockBytes);
+            if (transpose) {
+              uint8_t* const other = to + (static_cast<uint64_t>(tile.col + q / 2) * across + 2 * block_row) * kBlockBytes + q % 2 * kHalf;
+              store_bytes(other, two_at, kHalf);
+              store_bytes(other + kBlockBytes, two_at + kHalf, kHalf);
+            }
+          }
+          end_stores();
+        }
+      }
+    }
+  }
+  if (one_thread) wait_stores();
+}
+
+template <int kPhase>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+    product_kernel(const __grid_constant__ MuonProduct p, const __grid_constant__ CUtensorMap map) {
+  extern __shared__ uint8_t raw[];
+  __shared__ Control c;
+  const uint32_t ring_at = (shared_address(raw) + 1023) & ~1023u;
+  uint8_t* const staging = raw + (ring_at - shared_address(raw)) + kStages * kStageBytes;
+  const uint32_t rank = rank_in_pair(), warp = threadIdx.x / 32;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      barrier_init(shared_address(&c.full[i]), 1);
+      barrier_init(shared_address(&c.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      barrier_init(shared_address(&c.sums_full[i]), 1);
+      barrier_init(shared_address(&c.sums_empty[i]), 2 * kGroups);
+    }
+    for (int i = 0; i < kGroups; ++i) barrier_init(shared_address(&c.in[i]), 1);
+    c.gave_up = 0;
+    barrier_init_done();
+  }
+  if (warp == 1) tensor_alloc(shared_address(&c.tensor), kTensorColumns);
+  tensor_fence_before();
+  __syncthreads();
+  pair_sync();
+  tensor_fence_after();
+  wait_for_kernel_before();
+  if (p.clip == nullptr || p.clip->nonfinite == 0) {
+    if (warp == 0) {
+      if (threadIdx.x == 0) bring<kPhase>(p, map, ring_at, c, rank);
+    } else if (warp == 1) {
+      if (rank == 0 && threadIdx.x == 32) multiply_tiles<kPhase>(p, ring_at, c);
+    } else {
+      finish_tiles<kPhase>(p, staging, c, rank);
+    }
+  }
+  // Neither CTA frees or leaves while the other's products or arrivals may still reach it.
+  __syncwarp();
+  tensor_fence_before();
+  __syncthreads();
+  if (threadIdx.x == 0 && c.gave_up) *p.status = 1;
+  pair_sync();
+  tensor_fence_after();
+  if (warp == 1) tensor_free(c.tensor, kTensorColumns);
+}
+
+template <class K>
+cudaError_t configure(K* kernel) {
+  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
 }
 
 }  // namespace
 
-void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile> (&tiles)[kPhases]) {
-  for (uint32_t t = 0; t < descs.size(); ++t) {
-    const MuonDesc& d = descs[t];
-    auto all = [&](int phase, uint32_t rows, uint32_t cols) {
-      for (uint32_t r = 0; r < rows / kTile; ++r)
-        for (uint32_t c = 0; c < cols / kTile; ++c) tiles[phase].push_back({t, static_cast<uint16_t>(r), static_cast<uint16_t>(c)});
-    };
-    all(kGram, d.side_blocks * 128, d.side_blocks * 128);
-    all(kPoly, d.side_blocks * 128, d.side_blocks * 128);
-    all(kNext, d.row_blocks * kBlockRows, d.col_blocks * kBlockCols);
-  }
+cudaError_t configure_muon_product() {
+  cudaError_t e = configure(product_kernel<kGram>);
+  if (e == cudaSuccess) e = configure(product_kernel<kPoly>);
+  if (e == cudaSuccess) e = configure(product_kernel<kNext>);
+  return e;
 }
 
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, cudaStream_t s) {
+cudaError_t launch_muon_product(int phase, const MuonProduct& p, const CUtensorMap& map, cudaStream_t s) {
   auto* const kernel = phase == kGram ? product_kernel<kGram> : phase == kPoly ? product_kernel<kPoly> : product_kernel<kNext>;
-  return launch_chained(kernel, static_cast<int>(p.n_tiles), 256, 0, s, p);
+  return launch_chained(kernel, static_cast<int>(std::min(2 * p.n_tiles, kSms)), kThreads, kShared, s, p, map);
 }
 
 }  // namespace frk

@@ -128,6 +128,7 @@ def _load() -> ctypes.CDLL:
     L.fr_muon_destroy.argtypes = [vp]
     L.fr_muon_destroy.restype = None
     L.fr_muon_step.argtypes = [vp, ctypes.POINTER(fr_muon), vp, vp]
+    L.fr_muon_sync_status.argtypes = [vp, vp]
     L.fr_orthogonalize.argtypes = [vp, ctypes.POINTER(fr_muon), vp]
     L.fr_embed_create.argtypes = [u64, u64, u64, u64, ctypes.POINTER(vp)]
     L.fr_embed_info.argtypes = [vp, u64p, u64p, u64p, u64p]
@@ -145,7 +146,7 @@ def _load() -> ctypes.CDLL:
                  "fr_plan_create_batched", "fr_plan_batch", "fr_pack_batch", "fr_unpack_verify_batch",
                  "fr_unpack_collect", "fr_resend", "fr_restore", "fr_shard_pieces", "fr_pack_fp", "fr_unpack_verify_fp",
                  "fr_restore_fp", "fr_resend_fp", "fr_restore_multi", "fr_opt_create", "fr_opt_info", "fr_grad_clip",
-                 "fr_adamw_step", "fr_opt_convert", "fr_muon_create", "fr_muon_info", "fr_muon_step", "fr_orthogonalize",
+                 "fr_adamw_step", "fr_opt_convert", "fr_muon_create", "fr_muon_info", "fr_muon_step", "fr_muon_sync_status", "fr_orthogonalize",
                  "fr_embed_create", "fr_embed_info", "fr_embed_lookup", "fr_embed_grad"]:
         getattr(L, name).restype = ctypes.c_int
     return L
@@ -608,6 +609,10 @@ def fr_muon_step(plan, hyper: fr_muon, clip: Optional[torch.Tensor] = None, stre
     _check(lib.fr_muon_step(plan, hyper, None if clip is None else _record(clip), _stream(stream)), "fr_muon_step")
 
 
+def fr_muon_sync_status(plan, stream=None) -> int:
+    return lib.fr_muon_sync_status(plan, _stream(stream))
+
+
 def fr_orthogonalize(plan, hyper: fr_muon, stream=None) -> None:
     _check(lib.fr_orthogonalize(plan, hyper, _stream(stream)), "fr_orthogonalize")
 
@@ -865,6 +870,9 @@ class MuonPlan:
         if clip is not None and clip.device != self.device:
             raise ValueError("the clip record is on %s, the plan on %s" % (clip.device, self.device))
         fr_muon_step(self.handle, hyper, clip, stream)
+
+    def sync_status(self, stream=None) -> int:
+        return fr_muon_sync_status(self.handle, stream)
 
     def orthogonalize(self, hyper: Optional[fr_muon] = None, stream=None) -> None:
         """Writes the plan's updates from its gradients."""
