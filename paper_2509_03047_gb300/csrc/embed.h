@@ -51,9 +51,10 @@ struct Met {  // a token of the batch
   uint32_t row, at;
 };
 constexpr int kSortThreads = 1024, kSortEach = 4, kSortTile = kSortThreads * kSortEach;
-constexpr uint32_t kSortCtas = 128;
-constexpr uint64_t kSortShare = 2 * kSortTile;  // tokens per CTA, at least
-constexpr int kMostDigit = 11;                  // bits of a pass
+constexpr uint32_t kSortCluster = 16;  // CTAs that sort a batch of up to a tile for each in one launch
+constexpr uint64_t kClusterTokens = static_cast<uint64_t>(kSortCluster) * kSortTile;
+constexpr uint32_t kSortCtas = 128;    // of a larger batch's launches
+constexpr int kMostDigit = 11;         // bits of a pass
 
 struct SortPlan {
   int passes, bits;  // bits of a pass
@@ -74,6 +75,7 @@ struct SortParams {
   uint8_t* met;     // per row: set to 1 where a token meets it, or null
   uint64_t share;   // tokens per CTA
   uint32_t ctas;
+  int each;         // tokens per thread and tile
   int bits;
   int pass;
 };
@@ -83,11 +85,22 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
 
 // ---- the gradient
 
-// The sorted tokens are cut into ranges of equal length, one for a warp per 32 vectors of columns.
+// Vectors of a token's row that a lane has, 32 vectors apart.
+constexpr int lane_vectors(int v) { return v >= 8 ? 1 : v == 4 ? 2 : 4; }
+// The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns.
 constexpr uint32_t kSumWarps = 8;
-constexpr uint32_t kRangeWarps = kSms * 80;  // ranges times column tiles, about
-constexpr uint32_t kLeastRange = 8;
-inline uint32_t column_tiles(uint64_t dim, int v) { return static_cast<uint32_t>((dim + 32 * v - 1) / (32 * v)); }
+#ifndef FR_RANGE_WARPS
+#define FR_RANGE_WARPS 80
+#endif
+#ifndef FR_LEAST_RANGE
+#define FR_LEAST_RANGE 16
+#endif
+constexpr uint32_t kRangeWarps = kSms * FR_RANGE_WARPS;  // ranges times column tiles, about
+constexpr uint32_t kLeastRange = FR_LEAST_RANGE;
+inline uint32_t column_tiles(uint64_t dim, int v) {
+  const uint64_t width = 32 * v * lane_vectors(v);
+  return static_cast<uint32_t>((dim + width - 1) / width);
+}
 inline uint32_t ranges_of(uint64_t n, uint32_t tiles) {
   const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = (kRangeWarps + tiles - 1) / tiles;
   return static_cast<uint32_t>(most < fill ? most : fill);

@@ -45,8 +45,8 @@ fr_status fill_embed(fr_embed p) {
   }
   elems = 2 * p->ranges * p->dim;
   mem.scratch(&p->d_sorted[0], n);
-  if (n > kSortTile && p->sort.passes > 1) mem.scratch(&p->d_sorted[1], n);
-  if (n > kSortTile) mem.scratch(&p->d_counts, static_cast<uint64_t>(kSortCtas) * p->sort.bins());
+  if (p->sort.passes > 1) mem.scratch(&p->d_sorted[1], n);
+  if (n > kClusterTokens) mem.scratch(&p->d_counts, static_cast<uint64_t>(kSortCtas) * p->sort.bins());
   mem.scratch(&p->d_longs, p->ranges);
   mem.scratch(&p->d_parts, elems);
   mem.scratch(&p->d_numbers, 2);

@@ -6,6 +6,10 @@
 // CTAs before it, and a token's among its CTA's by warps in turn: a warp's tokens
 // of one digit are found by a vote, those of the warps before by a table of counts
 // per warp and digit.  Nothing depends on the order in which anything runs.
+//
+// A batch of up to 65,536 tokens is sorted in one launch, by a cluster of CTAs that
+// read each other's counts from shared memory; a larger one by two launches per pass.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include "embed.h"
@@ -50,24 +54,24 @@ __device__ __forceinline__ uint32_t scan(uint32_t* x, uint32_t n, uint32_t* warp
 
 struct Shared {
   uint32_t* base;    // per digit: where the CTA's next token of it goes
-  uint16_t* before;  // per warp and digit
+  uint32_t* totals;  // per digit: of the tile
   uint32_t* warps;
+  uint16_t* before;  // per warp and digit
   __device__ Shared(uint8_t* at, uint32_t bins)
-      : base(reinterpret_cast<uint32_t*>(at)), before(reinterpret_cast<uint16_t*>(at + bins * 4)),
-        warps(reinterpret_cast<uint32_t*>(at + bins * (4 + kWarps * 2))) {}
+      : base(reinterpret_cast<uint32_t*>(at)), totals(base + bins), warps(totals + bins), before(reinterpret_cast<uint16_t*>(warps + kWarps)) {}
 };
-size_t shared_bytes(uint32_t bins) { return bins * (4 + kWarps * 2) + kWarps * 4; }
+size_t shared_bytes(uint32_t bins) { return bins * (8 + kWarps * 2) + kWarps * 4; }
 
-// Each token's place among the tile's of its digit, and the tile's counts per warp, then sums over the warps before in their place; totals
-// per digit by `add(digit, total)`.  digit >= bins: no token.  A warp's tokens are consecutive, the lanes' in turn.
-template <class Add>
-__device__ __forceinline__ void rank_tile(const Shared& sh, uint32_t bins, const uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach], Add add) {
+// Each token's place among the tile's of its digit, and the tile's counts per warp, then sums over the warps before in their place, and totals.
+// digit >= bins: no token.  A warp's tokens are consecutive, the lanes' in turn.
+__device__ __forceinline__ void rank_tile(const Shared& sh, uint32_t bins, int each, const uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach]) {
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   uint16_t* mine = sh.before + warp * bins;
-  for (uint32_t i = lane; i < bins; i += 32) mine[i] = 0;
+  for (uint32_t i = lane; i < bins / 2; i += 32) reinterpret_cast<uint32_t*>(mine)[i] = 0;
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < kSortEach; ++k) {
+    if (k >= each) break;
     const uint32_t same = __match_any_sync(kAll, digit[k]);
     const uint32_t earlier = digit[k] < bins ? mine[digit[k]] : 0;
     rank[k] = earlier + __popc(same & ((1u << lane) - 1));
@@ -78,28 +82,52 @@ __device__ __forceinline__ void rank_tile(const Shared& sh, uint32_t bins, const
   __syncthreads();
   for (uint32_t i = threadIdx.x; i < bins; i += kSortThreads) {
     uint32_t sum = 0;
-#pragma unroll 8
-    for (int w = 0; w < kWarps; ++w) {
-      const uint32_t n = sh.before[w * bins + i];
-      sh.before[w * bins + i] = static_cast<uint16_t>(sum);
-      sum += n;
+    for (int w = 0; w < kWarps; w += 8) {
+      uint32_t n[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) n[j] = sh.before[(w + j) * bins + i];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sh.before[(w + j) * bins + i] = static_cast<uint16_t>(sum);
+        sum += n[j];
+      }
     }
-    add(i, sum);
+    sh.totals[i] = sum;
   }
   __syncthreads();
 }
 
-// The token of place i in a tile as a thread has it: warps take 32 * kSortEach consecutive ones.
-__device__ __forceinline__ uint32_t tile_index(int k) { return (threadIdx.x / 32 * kSortEach + k) * 32 + threadIdx.x % 32; }
+// The place in a tile of a thread's token k: warps take 32 * each consecutive ones.
+__device__ __forceinline__ uint32_t tile_index(int each, int k) { return (threadIdx.x / 32 * each + k) * 32 + threadIdx.x % 32; }
 
 template <bool First>
-__device__ __forceinline__ Met get(const SortParams& p, uint64_t i) {
-  if (!First) return p.sorted[(p.pass + 1) % 2][i];
+__device__ __forceinline__ Met get(const SortParams& p, int pass, uint64_t i) {
+  if (!First) return p.sorted[(pass + 1) % 2][i];
   const uint64_t row = p.tokens.row(i);
   return {row < p.tokens.rows ? static_cast<uint32_t>(row) : kAll, static_cast<uint32_t>(i)};
 }
 __device__ __forceinline__ uint32_t digit_of(const SortParams& p, int pass, uint32_t row) {
   return row == kAll ? kAll : row >> (pass * p.bits) & ((1u << p.bits) - 1);
+}
+
+// Tokens [begin, end) of a tile, their digits and ranks.
+template <bool First>
+__device__ __forceinline__ void take_tile(const SortParams& p, const Shared& sh, uint32_t bins, int pass, uint64_t begin, uint64_t end, Met (&m)[kSortEach],
+                                          uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach]) {
+#pragma unroll
+  for (int k = 0; k < kSortEach; ++k) {
+    const uint64_t i = begin + tile_index(p.each, k);
+    m[k] = k < p.each && i < end ? get<First>(p, pass, i) : Met{kAll, 0};
+    digit[k] = digit_of(p, pass, m[k].row);
+    if (First && p.met != nullptr && m[k].row != kAll) p.met[m[k].row] = 1;
+  }
+  rank_tile(sh, bins, p.each, digit, rank);
+}
+__device__ __forceinline__ void put_tile(const SortParams& p, const Shared& sh, uint32_t bins, int pass, const Met (&m)[kSortEach],
+                                         const uint32_t (&digit)[kSortEach], const uint32_t (&rank)[kSortEach]) {
+#pragma unroll
+  for (int k = 0; k < kSortEach; ++k)
+    if (digit[k] != kAll) p.sorted[pass % 2][sh.base[digit[k]] + sh.before[threadIdx.x / 32 * bins + digit[k]] + rank[k]] = m[k];
 }
 
 template <bool First>
@@ -110,11 +138,19 @@ __global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_consta
   wait_for_kernel_before();
   __syncthreads();
   const uint64_t n = First ? p.tokens.n : *p.found, begin = blockIdx.x * p.share, end = min(begin + p.share, n);
-  for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
-    const Met m = get<First>(p, i);
-    if (m.row == kAll) continue;
-    atomicAdd(counts + digit_of(p, p.pass, m.row), 1u);
-    if (First && p.met != nullptr) p.met[m.row] = 1;
+  for (uint64_t at = begin; at < end; at += kSortTile) {
+    uint32_t digit[kSortEach];
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+      const uint64_t i = at + k * kSortThreads + threadIdx.x;
+      digit[k] = digit_of(p, p.pass, i < end ? get<First>(p, p.pass, i).row : kAll);
+    }
+    // (one addition for a warp's tokens of one digit: a third of a batch may be the same)
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+      const uint32_t same = __match_any_sync(kAll, digit[k]);
+      if (digit[k] != kAll && threadIdx.x % 32 == 31 - __clz(same)) atomicAdd(counts + digit[k], static_cast<uint32_t>(__popc(same)));
+    }
   }
   if (First && blockIdx.x == 0 && threadIdx.x == 0) *p.n_long = 0;
   __syncthreads();
@@ -151,64 +187,78 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   const uint64_t n = First ? p.tokens.n : *p.found, begin = blockIdx.x * p.share, end = min(begin + p.share, n);
   for (uint64_t at = begin; at < end; at += kSortTile) {
     Met m[kSortEach];
-    uint32_t digit[kSortEach], rank[kSortEach], place[kSortEach];
-#pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-      const uint64_t i = at + tile_index(k);
-      m[k] = i < end ? get<First>(p, i) : Met{kAll, 0};
-      digit[k] = digit_of(p, p.pass, m[k].row);
-    }
-    uint32_t totals[2] = {0, 0};
-    rank_tile(sh, bins, digit, rank, [&](uint32_t i, uint32_t total) { totals[i >= kSortThreads] = total; });
-#pragma unroll
-    for (int k = 0; k < kSortEach; ++k)
-      place[k] = digit[k] != kAll ? sh.base[digit[k]] + sh.before[threadIdx.x / 32 * bins + digit[k]] + rank[k] : 0;
+    uint32_t digit[kSortEach], rank[kSortEach];
+    take_tile<First>(p, sh, bins, p.pass, at, end, m, digit, rank);
+    put_tile(p, sh, bins, p.pass, m, digit, rank);
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (threadIdx.x + j * kSortThreads < bins) sh.base[threadIdx.x + j * kSortThreads] += totals[j];
-#pragma unroll
-    for (int k = 0; k < kSortEach; ++k)
-      if (digit[k] != kAll) p.sorted[p.pass % 2][place[k]] = m[k];
-    // (rank_tile's barriers come between these sums and their next use)
+    for (uint32_t i = threadIdx.x; i < bins; i += kSortThreads) sh.base[i] += sh.totals[i];
+    // (the next tile's barriers come between these sums and their use)
   }
 }
 
-// A batch of one tile: all passes in one CTA.
-__global__ void __launch_bounds__(kSortThreads) small_kernel(const __grid_constant__ SortParams p, int passes) {
+// All passes of a batch of a tile per CTA of the cluster.
+__global__ void __launch_bounds__(kSortThreads) cluster_kernel(const __grid_constant__ SortParams p, int passes) {
   extern __shared__ __align__(16) uint8_t raw[];
-  const uint32_t bins = 1u << p.bits;
-  Met* const tile = reinterpret_cast<Met*>(raw);
-  const Shared sh(raw + kSortTile * sizeof(Met), bins);
+  namespace cg = cooperative_groups;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const uint32_t bins = 1u << p.bits, me = cluster.block_rank();
+  const Shared sh(raw, bins);
   wait_for_kernel_before();
-  uint32_t n = static_cast<uint32_t>(p.tokens.n);
+  uint64_t n = p.tokens.n;
   for (int pass = 0; pass < passes; ++pass) {
     Met m[kSortEach];
     uint32_t digit[kSortEach], rank[kSortEach];
+    const uint64_t begin = me * p.share, end = min(begin + p.share, n);
+    if (pass == 0)
+      take_tile<true>(p, sh, bins, pass, begin, end, m, digit, rank);
+    else
+      take_tile<false>(p, sh, bins, pass, begin, end, m, digit, rank);
+    cluster.sync();
+    uint32_t before[2] = {0, 0};
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-      const uint32_t i = tile_index(k);
-      m[k] = i < n ? (pass == 0 ? get<true>(p, i) : tile[i]) : Met{kAll, 0};
-      digit[k] = digit_of(p, pass, m[k].row);
-      if (pass == 0 && p.met != nullptr && m[k].row != kAll) p.met[m[k].row] = 1;
-    }
-    rank_tile(sh, bins, digit, rank, [&](uint32_t i, uint32_t total) { sh.base[i] = total; });
-    n = scan(sh.base, bins, sh.warps);
-#pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-      if (digit[k] == kAll) continue;
-      const uint32_t to = sh.base[digit[k]] + sh.before[threadIdx.x / 32 * bins + digit[k]] + rank[k];
-      if (pass + 1 < passes)
-        tile[to] = m[k];
-      else
-        p.sorted[0][to] = m[k];
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t i = threadIdx.x + j * kSortThreads;
+      if (i >= bins) break;
+      uint32_t total = 0;
+#pragma unroll 16
+      for (uint32_t c = 0; c < p.ctas; ++c) {
+        if (c == me) before[j] = total;
+        total += *cluster.map_shared_rank(sh.totals + i, c);
+      }
+      sh.base[i] = total;
     }
     __syncthreads();
+    n = scan(sh.base, bins, sh.warps);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      if (threadIdx.x + j * kSortThreads < bins) sh.base[threadIdx.x + j * kSortThreads] += before[j];
+    __syncthreads();
+    put_tile(p, sh, bins, pass, m, digit, rank);
+    // the tokens for the next pass; and no CTA changes or leaves counts that others read
+    cluster.sync();
   }
-  if (threadIdx.x == 0) {
-    *p.found = n;
+  if (me == 0 && threadIdx.x == 0) {
+    *p.found = static_cast<uint32_t>(n);
     *p.n_long = 0;
   }
+}
+
+cudaError_t launch_cluster(const SortParams& p, int passes, size_t shared, cudaStream_t s) {
+  cudaLaunchAttribute a[2] = {};
+  a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  a[0].val.programmaticStreamSerializationAllowed = 1;
+  a[1].id = cudaLaunchAttributeClusterDimension;
+  a[1].val.clusterDim.x = p.ctas;
+  a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(p.ctas);
+  c.blockDim = dim3(kSortThreads);
+  c.dynamicSmemBytes = shared;
+  c.stream = s;
+  c.attrs = a;
+  c.numAttrs = 2;
+  cudaLaunchKernelEx(&c, cluster_kernel, p, passes);
+  return cudaGetLastError();
 }
 
 }  // namespace
@@ -217,27 +267,31 @@ cudaError_t configure_sort() {
   const int big = static_cast<int>(shared_bytes(1u << kMostDigit));
   cudaError_t e = cudaFuncSetAttribute(place_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, big);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(place_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, big);
-  if (e == cudaSuccess)
-    e = cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, big + kSortTile * static_cast<int>(sizeof(Met)));
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(cluster_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, big);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(cluster_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
   return e;
 }
 
 cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStream_t s) {
   p.bits = plan.bits;
-  if (p.tokens.n <= kSortTile) {
-    *last = 0;
-    return launch_chained(small_kernel, 1, kSortThreads, shared_bytes(plan.bins()) + kSortTile * sizeof(Met), s, p, plan.passes);
+  *last = (plan.passes - 1) % 2;
+  const uint64_t n = p.tokens.n;
+  if (n <= kClusterTokens) {
+    p.ctas = 1;
+    while (p.ctas < kSortCluster && p.ctas * static_cast<uint64_t>(kSortThreads) < n) p.ctas *= 2;
+    p.each = n == 0 ? 1 : static_cast<int>((n + p.ctas * kSortThreads - 1) / (p.ctas * kSortThreads));
+    p.share = static_cast<uint64_t>(p.each) * kSortThreads;
+    return launch_cluster(p, plan.passes, shared_bytes(plan.bins()), s);
   }
-  p.share = (p.tokens.n + kSortCtas - 1) / kSortCtas;
-  p.share = p.share < kSortShare ? kSortShare : (p.share + kSortTile - 1) / kSortTile * kSortTile;
-  p.ctas = static_cast<uint32_t>((p.tokens.n + p.share - 1) / p.share);
+  p.each = kSortEach;
+  p.share = ((n + kSortCtas - 1) / kSortCtas + kSortTile - 1) / kSortTile * kSortTile;
+  p.ctas = static_cast<uint32_t>((n + p.share - 1) / p.share);
   for (p.pass = 0; p.pass < plan.passes; ++p.pass) {
     cudaError_t e = launch_chained(p.pass == 0 ? count_kernel<true> : count_kernel<false>, static_cast<int>(p.ctas), kSortThreads, 0, s, p);
     if (e == cudaSuccess)
       e = launch_chained(p.pass == 0 ? place_kernel<true> : place_kernel<false>, static_cast<int>(p.ctas), kSortThreads, shared_bytes(plan.bins()), s, p);
     if (e != cudaSuccess) return e;
   }
-  *last = (plan.passes - 1) % 2;
   return cudaSuccess;
 }
 

@@ -46,12 +46,17 @@ struct Border {
 __device__ __forceinline__ Border border(const Met* sorted, uint32_t found, uint32_t span, uint64_t b, uint32_t lane) {
   if (b == 0) return {0, false};
   if (b >= found) return {found, false};
-  const uint32_t at = static_cast<uint32_t>(b), row = sorted[at].row;
-  if (sorted[at - 1].row != row) return {at, false};
-  const uint32_t start = first_at_least(sorted, at > span ? at - span : 0, at, row, lane);
-  // (a start a whole span before, or the row beyond, is a long row)
-  const uint32_t end = first_at_least(sorted, at, static_cast<uint32_t>(min(b + span, static_cast<uint64_t>(found))), row + 1, lane);
-  return end - start > span || at - start >= span ? Border{at, true} : Border{start, false};
+  const uint32_t at = static_cast<uint32_t>(b);
+  // the 32 tokens on either side, by one latency
+  const uint32_t left = at >= lane + 1 ? sorted[at - 1 - lane].row : kAll, right = at + lane < found ? sorted[at + lane].row : kAll;
+  const uint32_t row = __shfl_sync(kAll, right, 0);
+  const uint32_t other_left = ~__ballot_sync(kAll, left == row), other_right = ~__ballot_sync(kAll, right == row);
+  uint32_t before = other_left ? __ffs(other_left) - 1 : 32, after = other_right ? __ffs(other_right) - 1 : 32;
+  if (before == 0) return {at, false};
+  if (span > 32 && before == 32) before = at - first_at_least(sorted, at > span ? at - span : 0, at, row, lane);
+  if (span > 32 && after == 32) after = first_at_least(sorted, at, static_cast<uint32_t>(min(b + span, static_cast<uint64_t>(found))), row + 1, lane) - at;
+  // (a count cut off at a span, or at 32 of a span of up to 32, is of a long row)
+  return before + after > span ? Border{at, true} : Border{at - before, false};
 }
 
 template <int V>
@@ -77,6 +82,13 @@ __device__ __forceinline__ void finish(void* grad, uint64_t element, float scale
   w.store(grad, element);
 }
 
+template <int V>
+__device__ __forceinline__ void put_part(const SumParams& p, uint64_t part, uint64_t column, const float (&sum)[V]) {
+  Raw<V, false> w;
+  w.set(sum);
+  w.store(p.parts, part * p.dim + column);
+}
+
 // The rows that no token meets: zeros.
 template <int V, bool Bf16>
 __device__ __forceinline__ void clear_rows(const SumParams& p, uint32_t cta) {
@@ -92,9 +104,16 @@ __device__ __forceinline__ void clear_rows(const SumParams& p, uint32_t cta) {
   for (uint64_t r = begin + threadIdx.x; r < end; r += kThreads) p.met[r] = 0;  // for the next call
 }
 
+// Tokens whose vectors are on their way together: what 48 registers hold of them and, where they are added to, of the rows.
+constexpr int tokens_ahead(int elems, bool bf16_out, bool bf16_grad, bool add) {
+  const int words = (elems * (bf16_out ? 2 : 4) + (add ? elems * (bf16_grad ? 2 : 4) : 0) + 3) / 4;
+  return 48 / words >= 8 ? 8 : 48 / words >= 4 ? 4 : 2;
+}
+
 template <int V, bool Bf16Out, bool Bf16Grad, bool Add>
-__global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ SumParams p) {
-  constexpr int kAhead = Add ? 4 : 8;  // tokens whose vectors are on their way together
+__global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant__ SumParams p) {
+  constexpr int kVectors = lane_vectors(V);
+  constexpr int kAhead = tokens_ahead(V * kVectors, Bf16Out, Bf16Grad, Add);
   wait_for_kernel_before();
   if (blockIdx.x >= p.sum_ctas) {
     if (!Add) clear_rows<V, Bf16Grad>(p, blockIdx.x - p.sum_ctas);
@@ -105,56 +124,62 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ S
   const uint64_t b = static_cast<uint64_t>(g) * span;
   if (g >= p.ranges || b >= found) return;
   const Border from = border(p.sorted, found, span, b, lane), to = border(p.sorted, found, span, b + span, lane);
-  const uint64_t column = (static_cast<uint64_t>(warp % p.tiles) * 32 + lane) * V;
-  const bool mine = column < p.dim;
+  const uint64_t first = static_cast<uint64_t>(warp % p.tiles) * (32 * V * kVectors) + lane * V;
+  auto column = [&](int c) { return first + c * (32 * V); };
+  auto mine = [&](int c) { return column(c) < p.dim; };
   bool head = from.inside;  // the row at hand started in a range before
-  float sum[V] = {};
+  float sum[kVectors][V] = {};
   for (uint32_t i = from.at; i < to.at; i += 32) {
     const uint32_t here = min(to.at - i, 32u);
     const Met m = lane < here ? p.sorted[i + lane] : Met{kAll, 0};
     const uint32_t after = i + lane + 1 < found ? p.sorted[i + lane + 1].row : kAll;
     const uint32_t ends = __ballot_sync(kAll, lane < here && m.row != after);
     for (uint32_t k = 0; k < here; k += kAhead) {
-      Raw<V, Bf16Out> in[kAhead];
-      Raw<V, Bf16Grad> old[Add ? kAhead : 1];
+      Raw<V, Bf16Out> in[kAhead][kVectors];
+      Raw<V, Bf16Grad> old[Add ? kAhead : 1][kVectors];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const uint64_t at = __shfl_sync(kAll, m.at, k + u);
-        if (k + u < here && mine) in[u].load(p.out, at * p.dim + column);
-        if (Add) {
-          const uint64_t row = __shfl_sync(kAll, m.row, k + u);
-          if (k + u < here && mine && ends >> (k + u) & 1) old[u].load(p.grad, row * p.dim + column);
-        }
+        const uint64_t at = static_cast<uint64_t>(__shfl_sync(kAll, m.at, k + u)) * p.dim;
+        const uint64_t row = Add ? static_cast<uint64_t>(__shfl_sync(kAll, m.row, k + u)) * p.dim : 0;
+        if (k + u >= here) continue;
+#pragma unroll
+        for (int c = 0; c < kVectors; ++c)
+          if (mine(c)) in[u][c].load(p.out, at + column(c));
+        if (!Add || !(ends >> (k + u) & 1)) continue;
+#pragma unroll
+        for (int c = 0; c < kVectors; ++c)
+          if (mine(c)) old[u][c].load(p.grad, row + column(c));
       }
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const uint64_t row = __shfl_sync(kAll, m.row, k + u);
         if (k + u >= here) break;
-        float x[V];
-        in[u].get(x);
-        add(sum, x);
+#pragma unroll
+        for (int c = 0; c < kVectors; ++c) {
+          float x[V];
+          in[u][c].get(x);
+          add(sum[c], x);
+        }
         if (!(ends >> (k + u) & 1)) continue;
-        if (mine) {
-          if (head) {
-            Raw<V, false> w;
-            w.set(sum);
-            w.store(p.parts, 2ull * g * p.dim + column);
-          } else {
-            finish<V, Bf16Grad, Add>(p.grad, row * p.dim + column, p.scale, sum, old[Add ? u : 0]);
+        const uint64_t row = static_cast<uint64_t>(__shfl_sync(kAll, m.row, k + u)) * p.dim;
+#pragma unroll
+        for (int c = 0; c < kVectors; ++c) {
+          if (mine(c)) {
+            if (head)
+              put_part<V>(p, 2ull * g, column(c), sum[c]);
+            else
+              finish<V, Bf16Grad, Add>(p.grad, row + column(c), p.scale, sum[c], old[Add ? u : 0][c]);
           }
+#pragma unroll
+          for (int j = 0; j < V; ++j) sum[c][j] = 0.0f;
         }
         head = false;
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] = 0.0f;
       }
     }
   }
   if (!to.inside) return;
-  if (mine) {
-    Raw<V, false> w;
-    w.set(sum);
-    w.store(p.parts, (2ull * g + !head) * p.dim + column);
-  }
+#pragma unroll
+  for (int c = 0; c < kVectors; ++c)
+    if (mine(c)) put_part<V>(p, 2ull * g + !head, column(c), sum[c]);
   if (!head && warp % p.tiles == 0 && lane == 0) p.longs[atomicAdd(p.n_long, 1u)] = g;
 }
 
@@ -166,9 +191,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
   wait_for_kernel_before();
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t found = *p.found, span = span_of(found, p.ranges);
-  const uint64_t items = static_cast<uint64_t>(*p.n_long) * p.tiles;
+  const uint32_t tiles = static_cast<uint32_t>((p.dim + 32 * V - 1) / (32 * V));
+  const uint64_t items = static_cast<uint64_t>(*p.n_long) * tiles;
   for (uint64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const uint32_t g = p.longs[item / p.tiles];
+    const uint32_t g = p.longs[item / tiles];
     const uint32_t row = p.sorted[static_cast<uint64_t>(g + 1) * span].row;
     uint32_t more = 0;  // parts after the first one
     for (;;) {
@@ -177,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const __grid_constant__ 
       more += n;
       if (n < kThreads) break;
     }
-    const uint64_t column = (item % p.tiles * 32 + lane) * V;
+    const uint64_t column = (item % tiles * 32 + lane) * V;
     const bool mine = column < p.dim;
     float sum[V] = {};
     if (mine) {
