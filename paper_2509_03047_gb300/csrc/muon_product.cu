@@ -42,10 +42,14 @@ struct Factor {
   uint64_t at;
   uint32_t col_blocks;
   bool by_columns;
-  // Row, in units of 128 bytes, of the workspace where half `h` (of 64 rows or columns) of block b of the operand begins, step k of the contraction.
-  __device__ __forceinline__ int32_t row(uint32_t b, uint32_t h, uint32_t k) const {
-    const uint64_t block = by_columns ? static_cast<uint64_t>(k / 2) * col_blocks + 2 * b + h : static_cast<uint64_t>(b) * col_blocks + k;
-    return static_cast<int32_t>((at + block * kBlockBytes) / 128 + 64 * (by_columns ? k % 2 : h));
+  // Row, in units of 128 bytes, of the workspace where block b of the operand begins; its second 64 rows or columns begin second() after.
+  __device__ __forceinline__ int32_t row(uint32_t b) const {
+    return static_cast<int32_t>(at / 128 + (by_columns ? 2ull * b : static_cast<uint64_t>(b) * col_blocks) * kBlockRows);
+  }
+  __device__ __forceinline__ int32_t second() const { return by_columns ? kBlockRows : kMapRows; }
+  // From step k of the contraction to the next one, for even and odd k.
+  __device__ __forceinline__ int32_t step(uint32_t odd) const {
+    return !by_columns ? kBlockRows : odd ? static_cast<int32_t>(col_blocks * kBlockRows - kMapRows) : static_cast<int32_t>(kMapRows);
   }
 };
 
@@ -101,24 +105,25 @@ __device__ __forceinline__ bool group_agrees(int group, bool ok) {
 template <int kPhase>
 __device__ __forceinline__ void bring(const MuonProduct& p, const CUtensorMap& map, uint32_t ring_at, Control& c, uint32_t rank) {
   Ring r;
+  const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]);
   for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2) {
     const MuonTile tile = p.tiles[t];
     const Operands<kPhase> o(p, p.tensors[tile.tensor]);
     // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
-    const uint32_t a = min(tile.row + rank, o.a_blocks - 1);
+    int32_t a = o.a.row(min(tile.row + rank, o.a_blocks - 1)), b = tile.wide ? o.b.row(tile.col + rank) : o.b.row(tile.col) + rank * o.b.second();
+    const int32_t a_second = o.a.second(), b_second = o.b.second(), a_even = o.a.step(0), a_odd = o.a.step(1), b_even = o.b.step(0), b_odd = o.b.step(1);
     const uint32_t bytes = 2 * kFactorBytes + (tile.wide ? 2 * kFactorBytes : kFactorBytes);
+    // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < o.depth; ++k) {
-      const uint32_t full = shared_address(&c.full[r.stage]), to = ring_at + r.stage * kStageBytes;
-      if (!wait_phase(shared_address(&c.empty[r.stage]), r.phase ^ 1, &c.gave_up)) return let_copies_land();
+      const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
+      if (!wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up)) return let_copies_land();
       if (rank == 0) expect_bytes(full, bytes);
-      load_rows(to, &map, o.a.row(a, 0, k), full);
-      load_rows(to + kHalf, &map, o.a.row(a, 1, k), full);
-      if (tile.wide) {
-        load_rows(to + kFactorBytes, &map, o.b.row(tile.col + rank, 0, k), full);
-        load_rows(to + kFactorBytes + kHalf, &map, o.b.row(tile.col + rank, 1, k), full);
-      } else {
-        load_rows(to + kFactorBytes, &map, o.b.row(tile.col, rank, k), full);
-      }
+      load_rows(to, &map, a, full);
+      load_rows(to + kHalf, &map, a + a_second, full);
+      load_rows(to + kFactorBytes, &map, b, full);
+      if (tile.wide) load_rows(to + kFactorBytes + kHalf, &map, b + b_second, full);
+      a += k % 2 ? a_odd : a_even;
+      b += k % 2 ? b_odd : b_even;
       r.next();
     }
   }
@@ -127,6 +132,7 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const CUtensorMap& m
 template <int kPhase>
 __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ring_at, Control& c) {
   Ring r;
+  const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]), tensor = c.tensor;
   uint32_t n = 0;
   for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2, ++n) {
     const MuonTile tile = p.tiles[t];
@@ -135,15 +141,15 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
     const uint32_t a_step = o.a.by_columns ? 2048 >> 4 : 32 >> 4, b_step = o.b.by_columns ? 2048 >> 4 : 32 >> 4;
     if (!wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up)) return let_copies_land();
     tensor_fence_after();
-    const uint32_t sums = c.tensor + half * 256;
+    const uint32_t sums = tensor + half * 256;
+    const uint64_t a0 = factor(ring_at, o.a.by_columns, kHalf), b0 = factor(ring_at + kFactorBytes, o.b.by_columns, kHalf);
     for (uint32_t k = 0; k < o.depth; ++k) {
-      if (!wait_phase(shared_address(&c.full[r.stage]), r.phase, &c.gave_up)) return let_copies_land();
+      if (!wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up)) return let_copies_land();
       tensor_fence_after();
-      const uint32_t at = ring_at + r.stage * kStageBytes;
-      const uint64_t a = factor(at, o.a.by_columns, kHalf), b = factor(at + kFactorBytes, o.b.by_columns, kHalf);
+      const uint64_t a = a0 + r.stage * (kStageBytes >> 4), b = b0 + r.stage * (kStageBytes >> 4);
 #pragma unroll
       for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + j * b_step, kind, k + j > 0);
-      arrive_after_products(shared_address(&c.empty[r.stage]));
+      arrive_after_products(empty0 + r.stage * 8);
       r.next();
     }
     arrive_after_products(shared_address(&c.sums_full[half]));
