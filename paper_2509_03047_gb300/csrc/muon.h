@@ -109,8 +109,10 @@ struct MuonProduct {
 };
 // Per device, before the first launch: opt the kernels in to their shared-memory size.
 cudaError_t configure_muon_product();
-// map: the workspace as rows of 128 bytes, kMapRows of which a copy takes.
-constexpr uint32_t kMapRows = 64;
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, const CUtensorMap& map, cudaStream_t s);
+// The workspace as blocks of two halves of 64 rows of 128 bytes.  A copy takes a block, the same half of two neighbouring blocks, or a half.
+struct MuonMaps {
+  CUtensorMap rows, columns, half;
+};
+cudaError_t launch_muon_product(int phase, const MuonProduct& p, const MuonMaps& maps, cudaStream_t s);
 
 }  // namespace frk

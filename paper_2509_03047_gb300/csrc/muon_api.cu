@@ -34,13 +34,13 @@ struct fr_muon_plan_s {
   MuonNorm* d_norms = nullptr;
   uint8_t* d_work = nullptr;
   uint32_t* d_status = nullptr;
-  CUtensorMap map;
+  MuonMaps maps;
 };
 
 namespace {
 
 constexpr uint64_t kMostSide = FR_MUON_MOST_SIDE;
-constexpr uint64_t kMostElems = 1ull << 35;  // filled up: the workspace's rows of 128 bytes have 31-bit indices
+constexpr uint64_t kMostElems = 1ull << 35;  // filled up; copies' indices of blocks have 31 bits
 
 bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes == 0; }
 uint64_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
@@ -89,19 +89,21 @@ MuonDesc describe(const fr_muon_tensor& x, uint64_t index) {
 
 uint64_t square_blocks(const MuonDesc& d) { return 2ull * d.side_blocks * d.side_blocks; }
 
-// The workspace as rows of 128 bytes.
-cudaError_t make_map(CUtensorMap* map, void* at, uint64_t bytes) {
+cudaError_t make_maps(MuonMaps* maps, void* at, uint64_t bytes) {
   void* entry = nullptr;
   cudaDriverEntryPointQueryResult found;
   const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
   if (e != cudaSuccess) return e;
   if (found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
-  const cuuint64_t sizes[2] = {64, bytes / 128}, strides[1] = {128};
-  const cuuint32_t box[2] = {64, kMapRows}, steps[2] = {1, 1};
-  const CUresult r = reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(entry)(
-      map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, at, sizes, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
-      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+  const cuuint64_t sizes[4] = {kBlockCols, kBlockRows / 2, 2, bytes / kBlockBytes}, strides[3] = {128, kBlockBytes / 2, kBlockBytes};
+  const cuuint32_t steps[4] = {1, 1, 1, 1};
+  auto make = [&](CUtensorMap* map, cuuint32_t halves, cuuint32_t blocks) {
+    const cuuint32_t box[4] = {kBlockCols, kBlockRows / 2, halves, blocks};
+    return reinterpret_cast<decltype(&cuTensorMapEncodeTiled)>(entry)(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, at, sizes, strides, box, steps,
+                                                                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+  };
+  return make(&maps->rows, 2, 1) && make(&maps->columns, 1, 2) && make(&maps->half, 1, 1) ? cudaSuccess : cudaErrorInvalidValue;
 }
 
 fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_tensors) {
@@ -157,8 +159,8 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   if (bytes == 0) return FR_OK;
   e = configure_muon_product();
-  if (e == cudaSuccess) e = make_map(&p->map, p->d_work, bytes);
-  return e == cudaSuccess ? FR_OK : report_cuda("tensor map of the workspace", e);
+  if (e == cudaSuccess) e = make_maps(&p->maps, p->d_work, bytes);
+  return e == cudaSuccess ? FR_OK : report_cuda("tensor maps of the workspace", e);
 }
 
 // Largest |f| on [0, top] of an odd or even polynomial given by its values and the places where its derivative in s^2 vanishes.
@@ -216,7 +218,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
     for (int phase = 0; phase < kPhases; ++phase) {
       q.tiles = p->d_tiles[phase];
       q.n_tiles = p->n_tiles[phase];
-      e = launch_muon_product(phase, q, p->map, s);
+      e = launch_muon_product(phase, q, p->maps, s);
       if (e != cudaSuccess) return report_cuda("product kernel launch", e);
     }
   }

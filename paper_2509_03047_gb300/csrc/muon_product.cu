@@ -21,11 +21,15 @@ namespace frk {
 
 namespace {
 
-constexpr int kStages = 5;
+#ifndef FR_STAGES
+#define FR_STAGES 5
+#define FR_GROUPS 2
+#endif
+constexpr int kStages = FR_STAGES;
 constexpr int kFactorBytes = 16384;  // 128 rows or columns of a factor, 64 of the contraction
 constexpr int kHalf = 8192;
 constexpr int kStageBytes = 2 * kFactorBytes;
-constexpr int kGroups = 2;           // of four warps, one of 64 columns each
+constexpr int kGroups = FR_GROUPS;           // of four warps, one of 64 columns each
 constexpr int kThreads = 64 + kGroups * 128;
 constexpr int kStaging = 2 * kBlockBytes;  // per group
 constexpr int kTensorColumns = 512;
@@ -42,14 +46,19 @@ struct Factor {
   uint64_t at;
   uint32_t col_blocks;
   bool by_columns;
-  // Row, in units of 128 bytes, of the workspace where block b of the operand begins; its second 64 rows or columns begin second() after.
-  __device__ __forceinline__ int32_t row(uint32_t b) const {
-    return static_cast<int32_t>(at / 128 + (by_columns ? 2ull * b : static_cast<uint64_t>(b) * col_blocks) * kBlockRows);
+  // The workspace's block where block b of the operand begins.
+  __device__ __forceinline__ int32_t block(uint32_t b) const {
+    return static_cast<int32_t>(at / kBlockBytes + (by_columns ? 2ull * b : static_cast<uint64_t>(b) * col_blocks));
   }
-  __device__ __forceinline__ int32_t second() const { return by_columns ? kBlockRows : kMapRows; }
-  // From step k of the contraction to the next one, for even and odd k.
-  __device__ __forceinline__ int32_t step(uint32_t odd) const {
-    return !by_columns ? kBlockRows : odd ? static_cast<int32_t>(col_blocks * kBlockRows - kMapRows) : static_cast<int32_t>(kMapRows);
+};
+// Its place in the contraction, which goes from block to block of a row, or from half to half of a column's blocks.
+struct Place {
+  int32_t block, half, next, flip;
+  __device__ __forceinline__ Place(const Factor& f, int32_t block, int32_t half)
+      : block(block), half(half), next(f.by_columns ? static_cast<int32_t>(f.col_blocks) : 1), flip(f.by_columns) {}
+  __device__ __forceinline__ void advance() {
+    block += half & flip || !flip ? next : 0;
+    half ^= flip;
   }
 };
 
@@ -103,27 +112,38 @@ __device__ __forceinline__ bool group_agrees(int group, bool ok) {
 }
 
 template <int kPhase>
-__device__ __forceinline__ void bring(const MuonProduct& p, const CUtensorMap& map, uint32_t ring_at, Control& c, uint32_t rank) {
+__device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps, uint32_t ring_at, Control& c, uint32_t rank) {
   Ring r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]);
   for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2) {
     const MuonTile tile = p.tiles[t];
     const Operands<kPhase> o(p, p.tensors[tile.tensor]);
     // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
-    int32_t a = o.a.row(min(tile.row + rank, o.a_blocks - 1)), b = tile.wide ? o.b.row(tile.col + rank) : o.b.row(tile.col) + rank * o.b.second();
-    const int32_t a_second = o.a.second(), b_second = o.b.second(), a_even = o.a.step(0), a_odd = o.a.step(1), b_even = o.b.step(0), b_odd = o.b.step(1);
+    Place a(o.a, o.a.block(min(tile.row + rank, o.a_blocks - 1)), 0);
+    // (a narrow tile's CTAs have 64 rows or columns each)
+    Place b(o.b, tile.wide ? o.b.block(tile.col + rank) : o.b.block(tile.col) + (o.b.by_columns ? rank : 0), tile.wide || o.b.by_columns ? 0 : rank);
+    const CUtensorMap *const a_map = o.a.by_columns ? &maps.columns : &maps.rows,
+                      *const b_map = !tile.wide ? &maps.half : o.b.by_columns ? &maps.columns : &maps.rows;
     const uint32_t bytes = 2 * kFactorBytes + (tile.wide ? 2 * kFactorBytes : kFactorBytes);
+#ifdef FR_PREFETCH
+    Place pa = a, pb = b;
+    uint32_t ahead = 0;
+#endif
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < o.depth; ++k) {
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
+#ifdef FR_PREFETCH
+      while (ahead < o.depth && ahead < k + FR_PREFETCH) {
+        if (ahead >= k + kStages) { prefetch_blocks(a_map, pa.half, pa.block); prefetch_blocks(b_map, pb.half, pb.block); }
+        pa.advance(); pb.advance(); ++ahead;
+      }
+#endif
       if (!wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up)) return let_copies_land();
       if (rank == 0) expect_bytes(full, bytes);
-      load_rows(to, &map, a, full);
-      load_rows(to + kHalf, &map, a + a_second, full);
-      load_rows(to + kFactorBytes, &map, b, full);
-      if (tile.wide) load_rows(to + kFactorBytes + kHalf, &map, b + b_second, full);
-      a += k % 2 ? a_odd : a_even;
-      b += k % 2 ? b_odd : b_even;
+      load_blocks(to, a_map, a.half, a.block, full);
+      load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
+      a.advance();
+      b.advance();
       r.next();
     }
   }
@@ -274,7 +294,7 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
 
 template <int kPhase>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-    product_kernel(const __grid_constant__ MuonProduct p, const __grid_constant__ CUtensorMap map) {
+    product_kernel(const __grid_constant__ MuonProduct p, const __grid_constant__ MuonMaps maps) {
   extern __shared__ uint8_t raw[];
   __shared__ Control c;
   const uint32_t ring_at = (shared_address(raw) + 1023) & ~1023u;
@@ -301,7 +321,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   wait_for_kernel_before();
   if (p.clip == nullptr || p.clip->nonfinite == 0) {
     if (warp == 0) {
-      if (threadIdx.x == 0) bring<kPhase>(p, map, ring_at, c, rank);
+      if (threadIdx.x == 0) bring<kPhase>(p, maps, ring_at, c, rank);
     } else if (warp == 1) {
       if (rank == 0 && threadIdx.x == 32) multiply_tiles<kPhase>(p, ring_at, c);
     } else {
@@ -332,9 +352,9 @@ cudaError_t configure_muon_product() {
   return e;
 }
 
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, const CUtensorMap& map, cudaStream_t s) {
+cudaError_t launch_muon_product(int phase, const MuonProduct& p, const MuonMaps& maps, cudaStream_t s) {
   auto* const kernel = phase == kGram ? product_kernel<kGram> : phase == kPoly ? product_kernel<kPoly> : product_kernel<kNext>;
-  return launch_chained(kernel, static_cast<int>(std::min(2 * p.n_tiles, kSms)), kThreads, kShared, s, p, map);
+  return launch_chained(kernel, static_cast<int>(std::min(2 * p.n_tiles, kSms)), kThreads, kShared, s, p, maps);
 }
 
 }  // namespace frk

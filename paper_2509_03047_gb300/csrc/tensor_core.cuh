@@ -70,11 +70,14 @@ __device__ __forceinline__ void let_copies_land() {
 
 // ---- copies
 
-// `rows` of a map whose rows are 128 bytes; the bytes count at the pair's first CTA.
-__device__ __forceinline__ void load_rows(uint32_t to, const CUtensorMap* map, int32_t row, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
-               "l"(map), "r"(0), "r"(row), "r"(in_first(bar))
+// A box of a map of blocks in halves of 64 rows of 128 bytes; the bytes count at the pair's first CTA.
+__device__ __forceinline__ void load_blocks(uint32_t to, const CUtensorMap* map, int32_t half, int32_t block, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %2, %3, %4}], [%5];" ::"r"(to),
+               "l"(map), "r"(0), "r"(half), "r"(block), "r"(in_first(bar))
                : "memory");
+}
+__device__ __forceinline__ void prefetch_blocks(const CUtensorMap* map, int32_t half, int32_t block) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %1, %2, %3}];" ::"l"(map), "r"(0), "r"(half), "r"(block) : "memory");
 }
 __device__ __forceinline__ void load_bytes(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
