@@ -8,7 +8,8 @@
 // from shared memory, with the row as the contraction's index or the column, so a
 // block goes there by plain bulk copies and serves X X^T, X^T X, and products from
 // either side without a transposition.  The square matrices of the smaller side,
-// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike.
+// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike.  A plan's workspace
+// has all matrices' x[0], then all x[1], all second halves, all P, all S, in the same order.
 //
 // Scales: X 2^14, S 2^13, P 2^11, so that fp16 holds what the bounds on the
 // polynomials (flashrec.h) allow: |X| <= 2, |S| <= 4, |P| <= 16 in the spectral
@@ -92,20 +93,31 @@ cudaError_t launch_muon_update(const MuonParams& p, cudaStream_t s);    // fr_or
 enum : int { kGram = 0, kPoly = 1, kNext = 2 };  // S, P, the next X
 constexpr int kPhases = 3;
 
-struct MuonTile {       // by a pair of CTAs
-  uint32_t tensor;
-  uint16_t row, col;    // of blocks of 128, even numbers
-  uint32_t wide;        // 256 columns, else 128
+// D[i][j] = sum over k of A(i, k) B(j, k): a tile of it, 256 x 256 or 256 x 128, by a pair of CTAs.  All that a CTA needs of it in one record, so
+// that the next tile's is there when its turn comes.  Numbers of blocks: of x[0]'s place where a factor or the result is an iterate.
+struct __attribute__((aligned(16))) MuonTile {
+  uint32_t a[2], b[2];      // first block of each CTA's part of the factors
+  uint32_t a_next, b_next;  // from a block to the next one of the contraction
+  uint32_t depth;           // steps of 64 of the contraction
+  uint32_t flags;
+  uint32_t out;             // block of the result's first row and column
+  uint32_t across;          // the result's blocks per block of rows
+  uint16_t row, col;        // of the tile, in blocks of 128
+  uint32_t other;           // the transposed result's block (kTransposed)
 };
+static_assert(sizeof(MuonTile) == 48, "three loads of 16 bytes");
+// kNarrow: 128 columns.  kAColumns, kBColumns: a factor is read by its columns, else its rows.  kSecond: there are rows for the second CTA.
+enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kTransposed = 16, kAIterate = 32, kBIterate = 64 };
 struct MuonProduct {
-  const MuonDesc* tensors;
   const MuonTile* tiles;
   uint32_t n_tiles;
   uint8_t* work;
   const fr_clip* clip;
-  uint32_t* status;  // set to 1 by a kernel that gave up a wait
+  uint32_t* status;        // set to 1 by a kernel that gave up a wait
   float a, b, c;
-  uint32_t from;  // which of x[] is the old iterate
+  uint32_t from, to;       // blocks from x[0] to the old iterate and the new one
+  uint32_t low;            // blocks from x[0] to the second halves
+  uint32_t square;         // blocks from P to S
 };
 // Per device, before the first launch: opt the kernels in to their shared-memory size.
 cudaError_t configure_muon_product();

@@ -24,6 +24,7 @@ struct fr_muon_plan_s {
   uint64_t n_tensors = 0, n_elems = 0, device_bytes = 0;
   bool params = true, updates = true;       // every matrix with elements has what the step, fr_orthogonalize needs
   float most_lr = 0.0f, most_decay = 0.0f;  // the largest |lr_scale| and |decay_scale|
+  uint64_t x_blocks = 0, p_blocks = 0;      // of all iterates, all squares
   uint32_t n_units = 0, n_blocks = 0;
   uint32_t n_tiles[kPhases] = {};
   MuonDesc* d_tensors = nullptr;
@@ -110,12 +111,6 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   std::vector<MuonDesc> descs;
   std::vector<uint32_t> units, blocks;
   std::vector<MuonTile> tiles[kPhases];
-  uint64_t bytes = 0;
-  auto take = [&](uint64_t n_blocks) {
-    const uint64_t at = bytes;
-    bytes += n_blocks * kBlockBytes;
-    return at;
-  };
   p->n_tensors = n_tensors;
   for (uint64_t t = 0; t < n_tensors; ++t) {
     const fr_muon_tensor& x = tensors[t];
@@ -127,17 +122,23 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     p->most_decay = std::max(p->most_decay, std::fabs(x.decay_scale));
     MuonDesc d = describe(x, t);
     const uint64_t n = static_cast<uint64_t>(d.row_blocks) * d.col_blocks;
-    d.x[0] = take(n);
-    d.x[1] = take(n);
-    d.low = take(n);
-    d.s = take(square_blocks(d));
-    d.p = take(square_blocks(d));
+    d.x[0] = p->x_blocks * kBlockBytes;
+    d.p = p->p_blocks * kBlockBytes;
+    p->x_blocks += n;
+    p->p_blocks += square_blocks(d);
     d.first_unit = static_cast<uint32_t>(units.size());
     d.first_block = static_cast<uint32_t>(blocks.size());
     const uint32_t me = static_cast<uint32_t>(descs.size());
     units.insert(units.end(), d.n_units, me);
     blocks.insert(blocks.end(), n, me);
     descs.push_back(d);
+  }
+  const uint64_t x_bytes = p->x_blocks * kBlockBytes, p_bytes = p->p_blocks * kBlockBytes, bytes = 3 * x_bytes + 2 * p_bytes;
+  for (MuonDesc& d : descs) {
+    d.x[1] = d.x[0] + x_bytes;
+    d.low = d.x[1] + x_bytes;
+    d.p += 3 * x_bytes;
+    d.s = d.p + p_bytes;
   }
   plan_tiles(descs, tiles);
   PlanMemory mem;
@@ -206,7 +207,8 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   if (e == cudaSuccess) e = launch_muon_iterate(mp, s);
   if (e != cudaSuccess) return report_cuda("element kernel launch", e);
   MuonProduct q = {};
-  q.tensors = p->d_tensors;
+  q.low = static_cast<uint32_t>(2 * p->x_blocks);
+  q.square = static_cast<uint32_t>(p->p_blocks);
   q.work = p->d_work;
   q.clip = mp.clip;
   q.status = p->d_status;
@@ -214,7 +216,8 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
     q.a = static_cast<float>(h.coef[i][0]);
     q.b = static_cast<float>(h.coef[i][1]);
     q.c = static_cast<float>(h.coef[i][2]);
-    q.from = i % 2;
+    q.from = i % 2 ? static_cast<uint32_t>(p->x_blocks) : 0;
+    q.to = i % 2 ? 0 : static_cast<uint32_t>(p->x_blocks);
     for (int phase = 0; phase < kPhases; ++phase) {
       q.tiles = p->d_tiles[phase];
       q.n_tiles = p->n_tiles[phase];

@@ -21,15 +21,11 @@ namespace frk {
 
 namespace {
 
-#ifndef FR_STAGES
-#define FR_STAGES 5
-#define FR_GROUPS 2
-#endif
-constexpr int kStages = FR_STAGES;
+constexpr int kStages = 5;
 constexpr int kFactorBytes = 16384;  // 128 rows or columns of a factor, 64 of the contraction
 constexpr int kHalf = 8192;
 constexpr int kStageBytes = 2 * kFactorBytes;
-constexpr int kGroups = FR_GROUPS;           // of four warps, one of 64 columns each
+constexpr int kGroups = 2;           // of four warps, one of 64 columns each
 constexpr int kThreads = 64 + kGroups * 128;
 constexpr int kStaging = 2 * kBlockBytes;  // per group
 constexpr int kTensorColumns = 512;
@@ -41,50 +37,29 @@ struct Control {
   uint32_t gave_up;
 };
 
-// A factor's blocks: a matrix of the workspace, by its rows or by its columns.
-struct Factor {
-  uint64_t at;
-  uint32_t col_blocks;
-  bool by_columns;
-  // The workspace's block where block b of the operand begins.
-  __device__ __forceinline__ int32_t block(uint32_t b) const {
-    return static_cast<int32_t>(at / kBlockBytes + (by_columns ? 2ull * b : static_cast<uint64_t>(b) * col_blocks));
-  }
-};
-// Its place in the contraction, which goes from block to block of a row, or from half to half of a column's blocks.
+// A factor's place in the contraction, which goes from block to block of a row, or from half to half of a column's blocks.
 struct Place {
   int32_t block, half, next, flip;
-  __device__ __forceinline__ Place(const Factor& f, int32_t block, int32_t half)
-      : block(block), half(half), next(f.by_columns ? static_cast<int32_t>(f.col_blocks) : 1), flip(f.by_columns) {}
   __device__ __forceinline__ void advance() {
     block += half & flip || !flip ? next : 0;
     half ^= flip;
   }
 };
 
-template <int kPhase>
-struct Operands {
-  Factor a, b;
-  uint32_t depth;     // steps of 64
-  uint32_t a_blocks;  // rows of the product, in blocks of 128
-  __device__ __forceinline__ Operands(const MuonProduct& p, const MuonDesc& d) {
-    const uint64_t x = d.x[p.from];
-    const uint32_t side = d.side_blocks;
-    if (kPhase == kGram) {
-      a = b = {x, d.col_blocks, d.tall != 0};
-      depth = d.tall ? 2 * d.row_blocks : d.col_blocks;
-      a_blocks = side;
-    } else if (kPhase == kPoly) {
-      a = b = {d.s, 2 * side, false};
-      depth = 2 * side;
-      a_blocks = side;
-    } else {
-      const Factor q = {d.p, 2 * side, false};
-      a = d.tall ? Factor{x, d.col_blocks, false} : q;
-      b = d.tall ? q : Factor{x, d.col_blocks, true};
-      depth = 2 * side;
-      a_blocks = d.row_blocks;
-    }
+// This pair's tiles in turn, each record read a tile ahead.
+struct Tiles {
+  const MuonProduct& p;
+  uint32_t at;
+  MuonTile now, next;
+  __device__ __forceinline__ explicit Tiles(const MuonProduct& p) : p(p), at(blockIdx.x / 2) {
+    if (at < p.n_tiles) next = p.tiles[at];
+  }
+  __device__ __forceinline__ bool take() {
+    if (at >= p.n_tiles) return false;
+    now = next;
+    at += gridDim.x / 2;
+    if (at < p.n_tiles) next = p.tiles[at];
+    return true;
   }
 };
 
@@ -111,33 +86,20 @@ __device__ __forceinline__ bool group_agrees(int group, bool ok) {
   return all != 0;
 }
 
-template <int kPhase>
 __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps, uint32_t ring_at, Control& c, uint32_t rank) {
   Ring r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]);
-  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2) {
-    const MuonTile tile = p.tiles[t];
-    const Operands<kPhase> o(p, p.tensors[tile.tensor]);
-    // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
-    Place a(o.a, o.a.block(min(tile.row + rank, o.a_blocks - 1)), 0);
-    // (a narrow tile's CTAs have 64 rows or columns each)
-    Place b(o.b, tile.wide ? o.b.block(tile.col + rank) : o.b.block(tile.col) + (o.b.by_columns ? rank : 0), tile.wide || o.b.by_columns ? 0 : rank);
-    const CUtensorMap *const a_map = o.a.by_columns ? &maps.columns : &maps.rows,
-                      *const b_map = !tile.wide ? &maps.half : o.b.by_columns ? &maps.columns : &maps.rows;
-    const uint32_t bytes = 2 * kFactorBytes + (tile.wide ? 2 * kFactorBytes : kFactorBytes);
-#ifdef FR_PREFETCH
-    Place pa = a, pb = b;
-    uint32_t ahead = 0;
-#endif
+  for (Tiles tiles(p); tiles.take();) {
+    const MuonTile& t = tiles.now;
+    const bool narrow = t.flags & kNarrow, a_columns = t.flags & kAColumns, b_columns = t.flags & kBColumns;
+    Place a = {static_cast<int32_t>((rank ? t.a[1] : t.a[0]) + (t.flags & kAIterate ? p.from : 0)), 0, static_cast<int32_t>(t.a_next), a_columns};
+    Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? p.from : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
+               static_cast<int32_t>(t.b_next), b_columns};
+    const CUtensorMap *const a_map = a_columns ? &maps.columns : &maps.rows, *const b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
+    const uint32_t bytes = 2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
-    for (uint32_t k = 0; k < o.depth; ++k) {
+    for (uint32_t k = 0; k < t.depth; ++k) {
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
-#ifdef FR_PREFETCH
-      while (ahead < o.depth && ahead < k + FR_PREFETCH) {
-        if (ahead >= k + kStages) { prefetch_blocks(a_map, pa.half, pa.block); prefetch_blocks(b_map, pb.half, pb.block); }
-        pa.advance(); pb.advance(); ++ahead;
-      }
-#endif
       if (!wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up)) return let_copies_land();
       if (rank == 0) expect_bytes(full, bytes);
       load_blocks(to, a_map, a.half, a.block, full);
@@ -149,21 +111,20 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
   }
 }
 
-template <int kPhase>
 __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ring_at, Control& c) {
   Ring r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]), tensor = c.tensor;
   uint32_t n = 0;
-  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2, ++n) {
-    const MuonTile tile = p.tiles[t];
-    const Operands<kPhase> o(p, p.tensors[tile.tensor]);
-    const uint32_t half = n % 2, kind = product_kind(o.a.by_columns, o.b.by_columns, tile.wide ? 256 : 128);
-    const uint32_t a_step = o.a.by_columns ? 2048 >> 4 : 32 >> 4, b_step = o.b.by_columns ? 2048 >> 4 : 32 >> 4;
+  for (Tiles tiles(p); tiles.take(); ++n) {
+    const MuonTile& t = tiles.now;
+    const bool a_columns = t.flags & kAColumns, b_columns = t.flags & kBColumns;
+    const uint32_t half = n % 2, kind = product_kind(a_columns, b_columns, t.flags & kNarrow ? 128 : 256), depth = t.depth;
+    const uint32_t a_step = a_columns ? 2048 >> 4 : 32 >> 4, b_step = b_columns ? 2048 >> 4 : 32 >> 4;
+    const uint64_t a0 = factor(ring_at, a_columns, kHalf), b0 = factor(ring_at + kFactorBytes, b_columns, kHalf);
     if (!wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up)) return let_copies_land();
     tensor_fence_after();
     const uint32_t sums = tensor + half * 256;
-    const uint64_t a0 = factor(ring_at, o.a.by_columns, kHalf), b0 = factor(ring_at + kFactorBytes, o.b.by_columns, kHalf);
-    for (uint32_t k = 0; k < o.depth; ++k) {
+    for (uint32_t k = 0; k < depth; ++k) {
       if (!wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up)) return let_copies_land();
       tensor_fence_after();
       const uint64_t a = a0 + r.stage * (kStageBytes >> 4), b = b0 + r.stage * (kStageBytes >> 4);
@@ -227,22 +188,20 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
   const bool one_thread = threadIdx.x % 128 == 64;  // of the group
   uint8_t *const one = staging + group * kStaging, *const two = one + kBlockBytes;
   const uint32_t one_at = shared_address(one), two_at = shared_address(two), in = shared_address(&c.in[group]);
+  const uint64_t low = static_cast<uint64_t>(p.low) * kBlockBytes, square = static_cast<uint64_t>(p.square) * kBlockBytes;
   uint32_t n = 0, phase = 0;
   bool ok = true;
-  for (uint32_t t = blockIdx.x / 2; t < p.n_tiles; t += gridDim.x / 2, ++n) {
-    const MuonTile tile = p.tiles[t];
-    const MuonDesc& d = p.tensors[tile.tensor];
-    const uint32_t half = n % 2, parts = tile.wide ? 4 : 2;
-    const uint32_t block_row = tile.row + rank, across = kPhase == kNext ? d.col_blocks : 2 * d.side_blocks;
-    const bool mine = block_row < (kPhase == kNext ? d.row_blocks : d.side_blocks);
-    const bool transpose = kPhase != kNext && tile.row != tile.col;
+  for (Tiles tiles(p); tiles.take(); ++n) {
+    const MuonTile& t = tiles.now;
+    const uint32_t half = n % 2, parts = t.flags & kNarrow ? 2 : 4;
+    const bool mine = rank == 0 || t.flags & kSecond, transpose = kPhase != kNext && t.flags & kTransposed;
     for (uint32_t q = group; q < parts; q += kGroups) {
-      const uint64_t at = (static_cast<uint64_t>(block_row) * across + 2 * tile.col + q) * kBlockBytes;
+      uint8_t* const at = p.work + (static_cast<uint64_t>(t.out) + rank * t.across + q) * kBlockBytes;
       if (mine && one_thread) {
         wait_stores_read();  // of the blocks before
         if (kPhase != kGram) {
           expect_bytes(in, kBlockBytes);
-          load_bytes(one_at, p.work + (kPhase == kPoly ? d.s : d.low) + at, kBlockBytes, in);
+          load_bytes(one_at, at + (kPhase == kPoly ? square : low), kBlockBytes, in);
         }
       }
       if (q == static_cast<uint32_t>(group)) {
@@ -264,7 +223,7 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
           group_sync(group);
         }
         // (the diagonal's column of this row among the block's)
-        finish_row<kPhase>(p, row, block_row * kBlockRows + row - (2 * tile.col + q) * kBlockCols, v, one, two, transpose);
+        finish_row<kPhase>(p, row, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, one, two, transpose);
         before_copies();
       }
       __syncwarp();
@@ -273,13 +232,12 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
         if (q + kGroups >= parts) arrive_in_first(shared_address(&c.sums_empty[half]));
         if (mine) {
           if (kPhase == kNext) {
-            store_bytes(p.work + d.low + at, one_at, kBlockBytes);
-            store_bytes(p.work + d.x[p.from ^ 1] + at, two_at, kBlockBytes);
+            store_bytes(at + low, one_at, kBlockBytes);
+            store_bytes(at + static_cast<uint64_t>(p.to) * kBlockBytes, two_at, kBlockBytes);
           } else {
-            uint8_t* const to = p.work + (kPhase == kGram ? d.s : d.p);
-            store_bytes(to + at, one_at, kBlockBytes);
+            store_bytes(at, one_at, kBlockBytes);
             if (transpose) {
-              uint8_t* const other = to + (static_cast<uint64_t>(tile.col + q / 2) * across + 2 * block_row) * kBlockBytes + q % 2 * kHalf;
+              uint8_t* const other = p.work + (static_cast<uint64_t>(t.other) + q / 2 * t.across + 2 * rank) * kBlockBytes + q % 2 * kHalf;
               store_bytes(other, two_at, kHalf);
               store_bytes(other + kBlockBytes, two_at + kHalf, kHalf);
             }
@@ -321,9 +279,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   wait_for_kernel_before();
   if (p.clip == nullptr || p.clip->nonfinite == 0) {
     if (warp == 0) {
-      if (threadIdx.x == 0) bring<kPhase>(p, maps, ring_at, c, rank);
+      if (threadIdx.x == 0) bring(p, maps, ring_at, c, rank);
     } else if (warp == 1) {
-      if (rank == 0 && threadIdx.x == 32) multiply_tiles<kPhase>(p, ring_at, c);
+      if (rank == 0 && threadIdx.x == 32) multiply_tiles(p, ring_at, c);
     } else {
       finish_tiles<kPhase>(p, staging, c, rank);
     }

@@ -9,29 +9,78 @@
 
 namespace frk {
 
+// A factor of a product: a matrix of the workspace by its rows or by its columns.
+struct Factor {
+  uint32_t block, col_blocks;
+  bool by_columns, iterate;
+  uint32_t first(uint32_t b) const { return block + (by_columns ? 2 * b : b * col_blocks); }
+};
+
+// A phase's product for a matrix.
+struct ProductOf {
+  Factor a, b;
+  uint32_t depth;
+  uint32_t out, rows, cols;  // rows and columns in blocks of 128
+
+  ProductOf(int phase, const MuonDesc& d) {
+    const uint32_t x = static_cast<uint32_t>(d.x[0] / kBlockBytes), s = static_cast<uint32_t>(d.s / kBlockBytes), p = static_cast<uint32_t>(d.p / kBlockBytes);
+    const uint32_t side = d.side_blocks;
+    if (phase == kGram) {
+      a = b = {x, d.col_blocks, d.tall != 0, true};
+      depth = d.tall ? 2 * d.row_blocks : d.col_blocks;
+    } else if (phase == kPoly) {
+      a = b = {s, 2 * side, false, false};
+      depth = 2 * side;
+    } else {
+      const Factor q = {p, 2 * side, false, false};
+      a = d.tall ? Factor{x, d.col_blocks, false, true} : q;
+      b = d.tall ? q : Factor{x, d.col_blocks, true, true};
+      depth = 2 * side;
+    }
+    out = phase == kGram ? s : phase == kPoly ? p : x;
+    rows = phase == kNext ? d.row_blocks : side;
+    cols = phase == kNext ? d.col_blocks / 2 : side;
+  }
+  MuonTile tile(int phase, uint32_t r, uint32_t c) const {
+    MuonTile t = {};
+    const bool narrow = c + 1 == cols, second = r + 1 < rows;
+    t.a[0] = a.first(r);
+    // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
+    t.a[1] = a.first(second ? r + 1 : r);
+    t.b[0] = b.first(c);
+    // (a narrow tile's CTAs have 64 rows or columns each, of rows the halves of a block)
+    t.b[1] = !narrow ? b.first(c + 1) : b.first(c) + (b.by_columns ? 1 : 0);
+    t.a_next = a.by_columns ? a.col_blocks : 1;
+    t.b_next = b.by_columns ? b.col_blocks : 1;
+    t.depth = depth;
+    const bool transposed = phase != kNext && r != c;
+    t.flags = (narrow ? kNarrow : 0) | (a.by_columns ? kAColumns : 0) | (b.by_columns ? kBColumns : 0) | (second ? kSecond : 0) |
+              (transposed ? kTransposed : 0) | (a.iterate ? kAIterate : 0) | (b.iterate ? kBIterate : 0);
+    t.across = 2 * cols;
+    t.out = out + r * t.across + 2 * c;
+    t.other = out + c * t.across + 2 * r;
+    t.row = static_cast<uint16_t>(r);
+    t.col = static_cast<uint16_t>(c);
+    return t;
+  }
+};
+
 // The tiles of each phase's products, those with the longest contraction first, so that the last to be started are short.
 inline void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile> (&tiles)[kPhases]) {
   for (int phase = 0; phase < kPhases; ++phase) {
+    std::vector<ProductOf> all;
+    for (const MuonDesc& d : descs) all.emplace_back(phase, d);
     std::vector<uint32_t> order(descs.size());
     std::iota(order.begin(), order.end(), 0u);
-    auto depth = [&](uint32_t t) {
-      const MuonDesc& d = descs[t];
-      return phase == kGram ? (d.tall ? d.row_blocks : d.col_blocks / 2) : d.side_blocks;
-    };
-    std::stable_sort(order.begin(), order.end(), [&](uint32_t a, uint32_t b) { return depth(a) > depth(b); });
+    std::stable_sort(order.begin(), order.end(), [&](uint32_t x, uint32_t y) { return all[x].depth > all[y].depth; });
     for (uint32_t t : order) {
-      const MuonDesc& d = descs[t];
-      const uint32_t rows = phase == kNext ? d.row_blocks : d.side_blocks, cols = phase == kNext ? d.col_blocks / 2 : d.side_blocks;
-      // (tiles that share the long side's blocks one after the other)
-      auto add = [&](uint32_t r, uint32_t c) {
-        if (phase == kNext || c <= r) tiles[phase].push_back({t, static_cast<uint16_t>(r), static_cast<uint16_t>(c), c + 1 < cols});
-      };
-      if (phase == kNext && !d.tall) {
-        for (uint32_t c = 0; c < cols; c += 2)
-          for (uint32_t r = 0; r < rows; r += 2) add(r, c);
+      const ProductOf& q = all[t];
+      if (phase == kNext && !descs[t].tall) {  // (tiles that share the long side's blocks one after the other)
+        for (uint32_t c = 0; c < q.cols; c += 2)
+          for (uint32_t r = 0; r < q.rows; r += 2) tiles[phase].push_back(q.tile(phase, r, c));
       } else {
-        for (uint32_t r = 0; r < rows; r += 2)
-          for (uint32_t c = 0; c < cols; c += 2) add(r, c);
+        for (uint32_t r = 0; r < q.rows; r += 2)
+          for (uint32_t c = 0; c < (phase == kNext ? q.cols : r + 1); c += 2) tiles[phase].push_back(q.tile(phase, r, c));
       }
     }
   }

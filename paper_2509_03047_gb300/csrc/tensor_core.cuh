@@ -76,9 +76,6 @@ __device__ __forceinline__ void load_blocks(uint32_t to, const CUtensorMap* map,
                "l"(map), "r"(0), "r"(half), "r"(block), "r"(in_first(bar))
                : "memory");
 }
-__device__ __forceinline__ void prefetch_blocks(const CUtensorMap* map, int32_t half, int32_t block) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global [%0, {%1, %1, %2, %3}];" ::"l"(map), "r"(0), "r"(half), "r"(block) : "memory");
-}
 __device__ __forceinline__ void load_bytes(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
                : "memory");
