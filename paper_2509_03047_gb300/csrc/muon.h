@@ -82,6 +82,8 @@ struct MuonParams {
   uint32_t random;
   uint64_t key;            // as in StepParams
   uint32_t last;           // which of x[] holds the last iterate
+  uint32_t low;            // 1: the first iterate has second halves
+  uint32_t* done;          // the products' counters, set to zero
 };
 cudaError_t launch_muon_norm(const MuonParams& p, cudaStream_t s);
 cudaError_t launch_muon_iterate(const MuonParams& p, cudaStream_t s);   // X, from G and the norm
@@ -104,27 +106,39 @@ struct __attribute__((aligned(16))) MuonTile {
   uint32_t across;          // the result's blocks per block of rows
   uint16_t row, col;        // of the tile, in blocks of 128
   uint32_t other;           // the transposed result's block (kTransposed)
+  uint32_t phase;
+  uint32_t done;            // the counter of the matrix and phase
+  uint32_t needs;           // the counter of the phase that this one reads from,
+  uint32_t count;           // and what that adds to it in an iteration
 };
-static_assert(sizeof(MuonTile) == 48, "three loads of 16 bytes");
+static_assert(sizeof(MuonTile) == 64, "four loads of 16 bytes");
 // kNarrow: 128 columns.  kAColumns, kBColumns: a factor is read by its columns, else its rows.  kSecond: there are rows for the second CTA.
 enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kTransposed = 16, kAIterate = 32, kBIterate = 64 };
+constexpr uint32_t kSignals = 4;  // of a tile: two CTAs, two groups of warps
+
+// One launch takes a list through some iterations, or a phase of one: its tiles in order, iteration after iteration, each pair every n-th.  A tile waits until all
+// those that it reads from have counted; they come before it in that order, and all CTAs are resident, so every wait ends.
 struct MuonProduct {
   const MuonTile* tiles;
   uint32_t n_tiles;
+  uint32_t first, iterations;  // this launch's: [first, iterations)
   uint8_t* work;
   const fr_clip* clip;
-  uint32_t* status;        // set to 1 by a kernel that gave up a wait
-  float a, b, c;
-  uint32_t from, to;       // blocks from x[0] to the old iterate and the new one
-  uint32_t low;            // blocks from x[0] to the second halves
-  uint32_t square;         // blocks from P to S
+  uint32_t* status;         // set to 1 by a kernel that gave up a wait
+  uint32_t* done;           // counters, zero at the start
+  uint32_t x_blocks;        // of all iterates: from x[0] to x[1] and to the second halves
+  uint32_t p_blocks;        // from P to S
+  float coef[FR_MUON_MOST][3];
+  uint32_t low;             // bit i: the iterate before iteration i has second halves
 };
 // Per device, before the first launch: opt the kernels in to their shared-memory size.
 cudaError_t configure_muon_product();
+// How many pairs are resident together.
+cudaError_t muon_pairs(uint32_t* pairs);
 // The workspace as blocks of two halves of 64 rows of 128 bytes.  A copy takes a block, the same half of two neighbouring blocks, or a half.
 struct MuonMaps {
   CUtensorMap rows, columns, half;
 };
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, const MuonMaps& maps, cudaStream_t s);
+cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, bool waits, cudaStream_t s);
 
 }  // namespace frk

@@ -26,11 +26,13 @@ struct fr_muon_plan_s {
   float most_lr = 0.0f, most_decay = 0.0f;  // the largest |lr_scale| and |decay_scale|
   uint64_t x_blocks = 0, p_blocks = 0;      // of all iterates, all squares
   uint32_t n_units = 0, n_blocks = 0;
-  uint32_t n_tiles[kPhases] = {};
+  uint32_t ends[kPhases] = {};               // of each phase's tiles
+  uint32_t pairs = 0, most_tiles = 0;        // CTAs that are resident, two each; the most tiles of a phase
   MuonDesc* d_tensors = nullptr;
   uint32_t* d_units = nullptr;
   uint32_t* d_blocks = nullptr;
-  MuonTile* d_tiles[kPhases] = {};
+  MuonTile* d_tiles = nullptr;
+  uint32_t* d_done = nullptr;
   MuonPartial* d_partials = nullptr;
   MuonNorm* d_norms = nullptr;
   uint8_t* d_work = nullptr;
@@ -110,7 +112,7 @@ cudaError_t make_maps(MuonMaps* maps, void* at, uint64_t bytes) {
 fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_tensors) {
   std::vector<MuonDesc> descs;
   std::vector<uint32_t> units, blocks;
-  std::vector<MuonTile> tiles[kPhases];
+  std::vector<MuonTile> tiles;
   p->n_tensors = n_tensors;
   for (uint64_t t = 0; t < n_tensors; ++t) {
     const fr_muon_tensor& x = tensors[t];
@@ -140,15 +142,14 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     d.p += 3 * x_bytes;
     d.s = d.p + p_bytes;
   }
-  plan_tiles(descs, tiles);
+  plan_tiles(descs, tiles, p->ends);
+  for (int k = 0; k < kPhases; ++k) p->most_tiles = std::max(p->most_tiles, p->ends[k] - (k ? p->ends[k - 1] : 0));
   PlanMemory mem;
   mem.table(&p->d_tensors, descs);
   mem.table(&p->d_units, units);
   mem.table(&p->d_blocks, blocks);
-  for (int k = 0; k < kPhases; ++k) {
-    mem.table(&p->d_tiles[k], tiles[k]);
-    p->n_tiles[k] = static_cast<uint32_t>(tiles[k].size());
-  }
+  mem.table(&p->d_tiles, tiles);
+  mem.scratch(&p->d_done, descs.size() * kPhases);
   mem.table(&p->d_norms, std::vector<MuonNorm>(descs.size(), MuonNorm{}));
   mem.scratch(&p->d_partials, units.size());
   mem.table(&p->d_status, std::vector<uint32_t>(1, 0));
@@ -160,6 +161,7 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   if (bytes == 0) return FR_OK;
   e = configure_muon_product();
+  if (e == cudaSuccess) e = muon_pairs(&p->pairs);
   if (e == cudaSuccess) e = make_maps(&p->maps, p->d_work, bytes);
   return e == cudaSuccess ? FR_OK : report_cuda("tensor maps of the workspace", e);
 }
@@ -201,32 +203,50 @@ const char* check_iterations(const fr_muon& h) {
   return nullptr;
 }
 
+// Lists of up to this many tiles per pair in a phase go through all iterations in one launch.
+#ifndef FR_TOGETHER
+#define FR_TOGETHER 4
+#endif
+constexpr uint32_t kTogether = FR_TOGETHER;
+
 // X through all iterations, in the plan's workspace.
 fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t s) {
-  cudaError_t e = launch_muon_norm(mp, s);
-  if (e == cudaSuccess) e = launch_muon_iterate(mp, s);
-  if (e != cudaSuccess) return report_cuda("element kernel launch", e);
   MuonProduct q = {};
-  q.low = static_cast<uint32_t>(2 * p->x_blocks);
-  q.square = static_cast<uint32_t>(p->p_blocks);
   q.work = p->d_work;
   q.clip = mp.clip;
   q.status = p->d_status;
-  for (uint32_t i = 0; i < h.iterations; ++i) {
-    q.a = static_cast<float>(h.coef[i][0]);
-    q.b = static_cast<float>(h.coef[i][1]);
-    q.c = static_cast<float>(h.coef[i][2]);
-    q.from = i % 2 ? static_cast<uint32_t>(p->x_blocks) : 0;
-    q.to = i % 2 ? 0 : static_cast<uint32_t>(p->x_blocks);
-    for (int phase = 0; phase < kPhases; ++phase) {
-      q.tiles = p->d_tiles[phase];
-      q.n_tiles = p->n_tiles[phase];
-      e = launch_muon_product(phase, q, p->maps, s);
-      if (e != cudaSuccess) return report_cuda("product kernel launch", e);
+  q.done = p->d_done;
+  q.x_blocks = static_cast<uint32_t>(p->x_blocks);
+  q.p_blocks = static_cast<uint32_t>(p->p_blocks);
+  // An iterate keeps its second halves if the iterations after it raise small singular values, and a rounding among them, by more than 4.
+  double gain = 1.0;
+  for (uint32_t i = h.iterations; i-- > 0;) {
+    for (int j = 0; j < 3; ++j) q.coef[i][j] = static_cast<float>(h.coef[i][j]);
+    gain *= std::max(1.0, std::fabs(h.coef[i][0]));
+    q.low |= static_cast<uint32_t>(gain > 4.0) << i;
+  }
+  mp.low = q.low & 1;
+  mp.last = h.iterations % 2;
+  cudaError_t e = launch_muon_norm(mp, s);
+  if (e == cudaSuccess) e = launch_muon_iterate(mp, s);
+  if (e != cudaSuccess) return report_cuda("element kernel launch", e);
+  if (p->most_tiles <= kTogether * p->pairs) {
+    q.tiles = p->d_tiles;
+    q.n_tiles = p->ends[kPhases - 1];
+    q.iterations = h.iterations;
+    e = launch_muon_product(q, p->maps, std::min(p->pairs, p->most_tiles), true, s);
+    return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);
+  }
+  for (q.first = 0; q.first < h.iterations && e == cudaSuccess; ++q.first) {
+    q.iterations = q.first + 1;
+    for (int k = 0; k < kPhases && e == cudaSuccess; ++k) {
+      const uint32_t begin = k ? p->ends[k - 1] : 0;
+      q.tiles = p->d_tiles + begin;
+      q.n_tiles = p->ends[k] - begin;
+      e = launch_muon_product(q, p->maps, p->pairs, false, s);
     }
   }
-  mp.last = h.iterations % 2;
-  return FR_OK;
+  return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);
 }
 
 MuonParams params(fr_muon_plan p) {
@@ -240,6 +260,7 @@ MuonParams params(fr_muon_plan p) {
   mp.norms = p->d_norms;
   mp.work = p->d_work;
   mp.status = p->d_status;
+  mp.done = p->d_done;
   return mp;
 }
 

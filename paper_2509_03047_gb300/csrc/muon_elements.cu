@@ -191,6 +191,7 @@ __global__ void __launch_bounds__(kElementThreads) iterate_kernel(const __grid_c
   if (skipped(p)) return;
   const float scale = grad_scale(p), to_one = p.norms[t].to_one, factor = p.norms[t].factor;
   const Chunks at(d, blockIdx.x);
+  if (at.block == 0 && threadIdx.x < kPhases) p.done[t * kPhases + threadIdx.x] = 0;
 #pragma unroll
   for (int k = 0; k < kChunks; ++k) {
     const uint32_t r = at.row(k);
@@ -206,17 +207,15 @@ __global__ void __launch_bounds__(kElementThreads) iterate_kernel(const __grid_c
     split(x, hi, lo);
     const uint64_t to = chunk_at(d.col_blocks, r, at.chunk);
     *reinterpret_cast<uint4*>(p.work + d.x[0] + to) = hi;
-    *reinterpret_cast<uint4*>(p.work + d.low + to) = lo;
+    if (p.low) *reinterpret_cast<uint4*>(p.work + d.low + to) = lo;
   }
 }
 
+// (the last iterate has no second halves)
 __device__ __forceinline__ void last_iterate(const MuonParams& p, const MuonDesc& d, uint32_t r, uint32_t c, float (&o)[8]) {
-  const uint64_t at = chunk_at(d.col_blocks, r, c);
-  float lo[8];
-  floats(*reinterpret_cast<const uint4*>(p.work + d.x[p.last] + at), o);
-  floats(*reinterpret_cast<const uint4*>(p.work + d.low + at), lo);
+  floats(*reinterpret_cast<const uint4*>(p.work + d.x[p.last] + chunk_at(d.col_blocks, r, c)), o);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = (o[j] + lo[j]) * (1.0f / kScaleX);
+  for (int j = 0; j < 8; ++j) o[j] *= 1.0f / kScaleX;
 }
 
 // p - lr (update_scale O + decay p)

@@ -1,5 +1,5 @@
-// muon_product.cu -- the products of the orthogonalised update, all matrices of a
-// list in one launch.
+// muon_product.cu -- the products of the orthogonalised update, all iterations of all
+// matrices of a list in one launch.
 //
 // D[i][j] = sum over k of A(i, k) B(j, k), tiles of 256 x 256 by pairs of CTAs, one
 // pair per two SMs, each taking every n-th tile of the list.  A warp brings the
@@ -49,17 +49,29 @@ struct Place {
 // This pair's tiles in turn, each record read a tile ahead.
 struct Tiles {
   const MuonProduct& p;
-  uint32_t at;
+  uint32_t at, round, next_round;
   MuonTile now, next;
-  __device__ __forceinline__ explicit Tiles(const MuonProduct& p) : p(p), at(blockIdx.x / 2) {
-    if (at < p.n_tiles) next = p.tiles[at];
-  }
+  __device__ __forceinline__ explicit Tiles(const MuonProduct& p) : p(p), at(blockIdx.x / 2), next_round(p.first) { read(); }
   __device__ __forceinline__ bool take() {
-    if (at >= p.n_tiles) return false;
+    if (next_round >= p.iterations) return false;
     now = next;
+    round = next_round;
     at += gridDim.x / 2;
-    if (at < p.n_tiles) next = p.tiles[at];
+    read();
     return true;
+  }
+  // How often the counter that the tile needs must have been added to.
+  __device__ __forceinline__ uint32_t count() const { return now.count * (now.phase == kGram ? round : round + 1); }
+  // The place of the iterate before or after this round.
+  __device__ __forceinline__ uint32_t iterate(uint32_t after) const { return (round + after) % 2 ? p.x_blocks : 0; }
+
+ private:
+  __device__ __forceinline__ void read() {
+    while (at >= p.n_tiles && next_round < p.iterations) {
+      at -= p.n_tiles;
+      ++next_round;
+    }
+    if (next_round < p.iterations) next = p.tiles[at];
   }
 };
 
@@ -92,10 +104,11 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
   for (Tiles tiles(p); tiles.take();) {
     const MuonTile& t = tiles.now;
     const bool narrow = t.flags & kNarrow, a_columns = t.flags & kAColumns, b_columns = t.flags & kBColumns;
-    Place a = {static_cast<int32_t>((rank ? t.a[1] : t.a[0]) + (t.flags & kAIterate ? p.from : 0)), 0, static_cast<int32_t>(t.a_next), a_columns};
-    Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? p.from : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
+    Place a = {static_cast<int32_t>((rank ? t.a[1] : t.a[0]) + (t.flags & kAIterate ? tiles.iterate(0) : 0)), 0, static_cast<int32_t>(t.a_next), a_columns};
+    Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? tiles.iterate(0) : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
                static_cast<int32_t>(t.b_next), b_columns};
     const CUtensorMap *const a_map = a_columns ? &maps.columns : &maps.rows, *const b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
+    if (!wait_count(p.done + t.needs, tiles.count(), &c.gave_up)) return let_copies_land();
     const uint32_t bytes = 2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < t.depth; ++k) {
@@ -141,9 +154,10 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
 //   S = X X^T             sums in X's scale twice
 //   P = a I + b S + c S^2
 //   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part
-// `one`: block of S or P, or of second halves (the old ones are there); `two`: the transposed block, or the first halves.
+// `one`: block of S or P, or of second halves (what the result adds is there); `two`: the transposed block, or the first halves.
 template <int kPhase>
-__device__ __forceinline__ void finish_row(const MuonProduct& p, uint32_t row, uint32_t diagonal, float (&v)[64], uint8_t* one, uint8_t* two, bool transpose) {
+__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t row, uint32_t diagonal, float (&v)[64], uint8_t* one, uint8_t* two, bool transpose,
+                                           bool low_before, bool low_after) {
 #pragma unroll
   for (uint32_t c = 0; c < 8; ++c) {
     float x[8], y[8];
@@ -159,18 +173,23 @@ __device__ __forceinline__ void finish_row(const MuonProduct& p, uint32_t row, u
       floats(*q, y);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float own = diagonal == 8 * c + j ? p.a * kScaleP : 0.0f;
-        x[j] = own + y[j] * (p.b * (kScaleP / kScaleS)) + x[j] * (p.c * (kScaleP / (kScaleS * kScaleS)));
+        const float own = diagonal == 8 * c + j ? coef[0] * kScaleP : 0.0f;
+        x[j] = own + y[j] * (coef[1] * (kScaleP / kScaleS)) + x[j] * (coef[2] * (kScaleP / (kScaleS * kScaleS)));
       }
       *q = halves(x);
     } else {
-      floats(*q, y);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = x[j] * (1.0f / kScaleP) + p.a * y[j];
-      uint4 hi, lo;
-      split(x, hi, lo);
-      *q = lo;
-      *reinterpret_cast<uint4*>(two + at) = hi;
+      for (int j = 0; j < 8; ++j) x[j] *= 1.0f / kScaleP;
+      if (low_before) {
+        floats(*q, y);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] += coef[0] * y[j];
+      }
+      uint4* const r = reinterpret_cast<uint4*>(two + at);
+      if (low_after)
+        split(x, *r, *q);
+      else
+        *r = halves(x);
     }
     if (kPhase != kNext && transpose) {
       // (neighbouring threads write neighbouring columns: no bank is met twice)
@@ -181,31 +200,34 @@ __device__ __forceinline__ void finish_row(const MuonProduct& p, uint32_t row, u
   }
 }
 
-template <int kPhase>
 __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* staging, Control& c, uint32_t rank) {
   const int group = (threadIdx.x - 64) / 128;
   const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + threadIdx.x % 32;  // a warp reads the quarter of its index
   const bool one_thread = threadIdx.x % 128 == 64;  // of the group
   uint8_t *const one = staging + group * kStaging, *const two = one + kBlockBytes;
   const uint32_t one_at = shared_address(one), two_at = shared_address(two), in = shared_address(&c.in[group]);
-  const uint64_t low = static_cast<uint64_t>(p.low) * kBlockBytes, square = static_cast<uint64_t>(p.square) * kBlockBytes;
+  const uint64_t low = 2ull * p.x_blocks * kBlockBytes, square = static_cast<uint64_t>(p.p_blocks) * kBlockBytes;
   uint32_t n = 0, phase = 0;
   bool ok = true;
   for (Tiles tiles(p); tiles.take(); ++n) {
     const MuonTile& t = tiles.now;
     const uint32_t half = n % 2, parts = t.flags & kNarrow ? 2 : 4;
-    const bool mine = rank == 0 || t.flags & kSecond, transpose = kPhase != kNext && t.flags & kTransposed;
+    const bool mine = rank == 0 || t.flags & kSecond, transpose = t.flags & kTransposed;
+    const bool low_before = p.low >> tiles.round & 1, low_after = p.low >> (tiles.round + 1) & 1;
+    const bool adds = t.phase == kPoly || (t.phase == kNext && low_before);
+    const float coef[3] = {p.coef[tiles.round][0], p.coef[tiles.round][1], p.coef[tiles.round][2]};
+    if (one_thread && adds) ok = wait_count(p.done + t.needs, tiles.count(), &c.gave_up);
     for (uint32_t q = group; q < parts; q += kGroups) {
       uint8_t* const at = p.work + (static_cast<uint64_t>(t.out) + rank * t.across + q) * kBlockBytes;
       if (mine && one_thread) {
         wait_stores_read();  // of the blocks before
-        if (kPhase != kGram) {
+        if (adds) {
           expect_bytes(in, kBlockBytes);
-          load_bytes(one_at, at + (kPhase == kPoly ? square : low), kBlockBytes, in);
+          load_bytes(one_at, at + (t.phase == kPoly ? square : low), kBlockBytes, in);
         }
       }
       if (q == static_cast<uint32_t>(group)) {
-        ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up);
+        ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up) && ok;
         tensor_fence_after();
       }
       __syncwarp();
@@ -216,14 +238,20 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       tensor_load_wait();
       if (q + kGroups >= parts) tensor_fence_before();
       if (mine) {
-        if (kPhase != kGram) {
+        if (adds) {
           ok = wait_phase(in, phase, &c.gave_up) && ok;
           phase ^= 1;
         } else {
           group_sync(group);
         }
-        // (the diagonal's column of this row among the block's)
-        finish_row<kPhase>(p, row, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, one, two, transpose);
+        if (t.phase == kGram) {
+          finish_row<kGram>(coef, row, 0, v, one, two, transpose, false, false);
+        } else if (t.phase == kPoly) {
+          // (the diagonal's column of this row among the block's)
+          finish_row<kPoly>(coef, row, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, one, two, transpose, false, false);
+        } else {
+          finish_row<kNext>(coef, row, 0, v, one, two, false, low_before, low_after);
+        }
         before_copies();
       }
       __syncwarp();
@@ -231,9 +259,9 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       if (one_thread) {
         if (q + kGroups >= parts) arrive_in_first(shared_address(&c.sums_empty[half]));
         if (mine) {
-          if (kPhase == kNext) {
-            store_bytes(at + low, one_at, kBlockBytes);
-            store_bytes(at + static_cast<uint64_t>(p.to) * kBlockBytes, two_at, kBlockBytes);
+          if (t.phase == kNext) {
+            if (low_after) store_bytes(at + low, one_at, kBlockBytes);
+            store_bytes(at + static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes, two_at, kBlockBytes);
           } else {
             store_bytes(at, one_at, kBlockBytes);
             if (transpose) {
@@ -246,11 +274,13 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
         }
       }
     }
+    if (one_thread) {
+      wait_stores();
+      add_to_count(p.done + t.done);
+    }
   }
-  if (one_thread) wait_stores();
 }
 
-template <int kPhase>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ MuonProduct p, const __grid_constant__ MuonMaps maps) {
   extern __shared__ uint8_t raw[];
@@ -283,7 +313,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     } else if (warp == 1) {
       if (rank == 0 && threadIdx.x == 32) multiply_tiles(p, ring_at, c);
     } else {
-      finish_tiles<kPhase>(p, staging, c, rank);
+      finish_tiles(p, staging, c, rank);
     }
   }
   // Neither CTA frees or leaves while the other's products or arrivals may still reach it.
@@ -296,23 +326,41 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   if (warp == 1) tensor_free(c.tensor, kTensorColumns);
 }
 
-template <class K>
-cudaError_t configure(K* kernel) {
-  return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
+cudaLaunchConfig_t config(uint32_t pairs, cudaStream_t s, cudaLaunchAttribute (&attrs)[1]) {
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(2 * pairs);
+  c.blockDim = dim3(kThreads);
+  c.dynamicSmemBytes = kShared;
+  c.stream = s;
+  attrs[0].id = cudaLaunchAttributeCooperative;
+  attrs[0].val.cooperative = 1;
+  c.attrs = attrs;
+  c.numAttrs = 1;
+  return c;
 }
 
 }  // namespace
 
 cudaError_t configure_muon_product() {
-  cudaError_t e = configure(product_kernel<kGram>);
-  if (e == cudaSuccess) e = configure(product_kernel<kPoly>);
-  if (e == cudaSuccess) e = configure(product_kernel<kNext>);
-  return e;
+  return cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
 }
 
-cudaError_t launch_muon_product(int phase, const MuonProduct& p, const MuonMaps& maps, cudaStream_t s) {
-  auto* const kernel = phase == kGram ? product_kernel<kGram> : phase == kPoly ? product_kernel<kPoly> : product_kernel<kNext>;
-  return launch_chained(kernel, static_cast<int>(std::min(2 * p.n_tiles, kSms)), kThreads, kShared, s, p, maps);
+cudaError_t muon_pairs(uint32_t* pairs) {
+  cudaLaunchAttribute attrs[1] = {};
+  cudaLaunchConfig_t c = config(kSms / 2, nullptr, attrs);
+  c.numAttrs = 0;
+  int n = 0;
+  const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, product_kernel, &c);
+  *pairs = static_cast<uint32_t>(n);
+  return e != cudaSuccess ? e : n > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
+}
+
+cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, bool waits, cudaStream_t s) {
+  if (!waits) return launch_chained(product_kernel, static_cast<int>(2 * std::min(pairs, p.n_tiles)), kThreads, kShared, s, p, maps);
+  cudaLaunchAttribute attrs[1] = {};
+  const cudaLaunchConfig_t c = config(pairs, s, attrs);
+  cudaLaunchKernelEx(&c, product_kernel, p, maps);
+  return cudaGetLastError();
 }
 
 }  // namespace frk

@@ -41,8 +41,13 @@ struct ProductOf {
     rows = phase == kNext ? d.row_blocks : side;
     cols = phase == kNext ? d.col_blocks / 2 : side;
   }
+  uint32_t tiles(int phase) const {  // symmetric results: on and below the diagonal
+    const uint32_t r = (rows + 1) / 2, c = (cols + 1) / 2;
+    return phase == kNext ? r * c : r * (r + 1) / 2;
+  }
   MuonTile tile(int phase, uint32_t r, uint32_t c) const {
     MuonTile t = {};
+    t.phase = static_cast<uint32_t>(phase);
     const bool narrow = c + 1 == cols, second = r + 1 < rows;
     t.a[0] = a.first(r);
     // (beyond an odd number of blocks of rows: the last one again, its results are dropped)
@@ -65,24 +70,34 @@ struct ProductOf {
   }
 };
 
-// The tiles of each phase's products, those with the longest contraction first, so that the last to be started are short.
-inline void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile> (&tiles)[kPhases]) {
+// The tiles of an iteration: S of all matrices, then P, then X, in each those with the longest contraction first.  ends: where each phase's end.
+inline void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile>& tiles, uint32_t (&ends)[kPhases]) {
   for (int phase = 0; phase < kPhases; ++phase) {
     std::vector<ProductOf> all;
     for (const MuonDesc& d : descs) all.emplace_back(phase, d);
     std::vector<uint32_t> order(descs.size());
     std::iota(order.begin(), order.end(), 0u);
     std::stable_sort(order.begin(), order.end(), [&](uint32_t x, uint32_t y) { return all[x].depth > all[y].depth; });
-    for (uint32_t t : order) {
-      const ProductOf& q = all[t];
-      if (phase == kNext && !descs[t].tall) {  // (tiles that share the long side's blocks one after the other)
+    for (uint32_t m : order) {
+      const ProductOf& q = all[m];
+      const int from = (phase + kPhases - 1) % kPhases;
+      const uint32_t needs = m * kPhases + from, count = kSignals * ProductOf(from, descs[m]).tiles(from);
+      auto add = [&](uint32_t r, uint32_t c) {
+        MuonTile t = q.tile(phase, r, c);
+        t.done = m * kPhases + phase;
+        t.needs = needs;
+        t.count = count;
+        tiles.push_back(t);
+      };
+      if (phase == kNext && !descs[m].tall) {  // (tiles that share the long side's blocks one after the other)
         for (uint32_t c = 0; c < q.cols; c += 2)
-          for (uint32_t r = 0; r < q.rows; r += 2) tiles[phase].push_back(q.tile(phase, r, c));
+          for (uint32_t r = 0; r < q.rows; r += 2) add(r, c);
       } else {
         for (uint32_t r = 0; r < q.rows; r += 2)
-          for (uint32_t c = 0; c < (phase == kNext ? q.cols : r + 1); c += 2) tiles[phase].push_back(q.tile(phase, r, c));
+          for (uint32_t c = 0; c < (phase == kNext ? q.cols : r + 1); c += 2) add(r, c);
       }
     }
+    ends[phase] = static_cast<uint32_t>(tiles.size());
   }
 }
 

@@ -63,6 +63,25 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   }
   return true;
 }
+// Until a counter in memory has reached `count`; with it the writes before its additions are visible, to copies too.
+__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t count, volatile uint32_t* gave_up) {
+  const long long start = clock64();
+  for (;;) {
+    uint32_t now;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(counter) : "memory");
+    if (now >= count) break;
+    if (*gave_up || clock64() - start > (4ll << 30)) {
+      *gave_up = 1;
+      return false;
+    }
+  }
+  asm volatile("fence.proxy.async;" ::: "memory");
+  return true;
+}
+// After this thread's copies to memory have ended.
+__device__ __forceinline__ void add_to_count(uint32_t* counter) {
+  asm volatile("fence.proxy.async;\n\tred.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+}
 // The part of a role that has given up: its copies in flight land meanwhile.
 __device__ __forceinline__ void let_copies_land() {
   for (int i = 0; i < 20; ++i) __nanosleep(1000000);
