@@ -6,7 +6,7 @@
 // 128.  A block's row is 128 bytes, its eight 16-byte chunks permuted by the row
 // (chunk c of row r lies at c ^ (r % 8)): the layout that the tensor cores read
 // from shared memory, with the row as the contraction's index or the column, so a
-// block goes there by plain bulk copies and serves X X^T, X^T X, and products from
+// block goes there as it is and serves X X^T, X^T X, and products from
 // either side without a transposition.  The square matrices of the smaller side,
 // S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike.  A plan's workspace
 // has all matrices' x[0], then all x[1], all second halves, all P, all S, in the same order.
@@ -97,24 +97,29 @@ constexpr int kPhases = 3;
 
 // D[i][j] = sum over k of A(i, k) B(j, k): a tile of it, 256 x 256 or 256 x 128, by a pair of CTAs.  All that a CTA needs of it in one record, so
 // that the next tile's is there when its turn comes.  Numbers of blocks: of x[0]'s place where a factor or the result is an iterate.
+// Of S and P only the tiles on and below the diagonal exist: from a step on a factor's blocks are those on the diagonal's other side, read the
+// other way round.
 struct __attribute__((aligned(16))) MuonTile {
-  uint32_t a[2], b[2];      // first block of each CTA's part of the factors
-  uint32_t a_next, b_next;  // from a block to the next one of the contraction
-  uint32_t depth;           // steps of 64 of the contraction
+  uint32_t a[2], b[2];              // first block of each CTA's part of the factors,
+  uint32_t a_after[2], b_after[2];  // and the one at the step where the blocks change sides
+  uint32_t a_switch, b_switch;      // that step
+  uint32_t a_next, b_next;          // from a block to the next one of the contraction
+  uint32_t square;                  // and, by columns, in S and P
+  uint32_t depth;                   // steps of 64 of the contraction
   uint32_t flags;
-  uint32_t out;             // block of the result's first row and column
-  uint32_t across;          // the result's blocks per block of rows
-  uint16_t row, col;        // of the tile, in blocks of 128
-  uint32_t other;           // the transposed result's block (kTransposed)
   uint32_t phase;
-  uint32_t done;            // the counter of the matrix and phase
-  uint32_t needs;           // the counter of the phase that this one reads from,
-  uint32_t count;           // and what that adds to it in an iteration
+  uint32_t out;                     // block of the result's first row and column
+  uint32_t across;                  // the result's blocks per block of rows
+  uint16_t row, col;                // of the tile, in blocks of 128
+  uint32_t done;                    // the counter of the matrix and phase
+  uint32_t needs;                   // the counter of the phase that this one reads from,
+  uint32_t count;                   // and what that adds to it in an iteration
+  uint32_t reserved[2];
 };
-static_assert(sizeof(MuonTile) == 64, "four loads of 16 bytes");
+static_assert(sizeof(MuonTile) == 96, "six loads of 16 bytes");
 // kNarrow: 128 columns.  kAColumns, kBColumns: a factor is read by its columns, else its rows.  kSecond: there are rows for the second CTA.
-enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kTransposed = 16, kAIterate = 32, kBIterate = 64 };
-constexpr uint32_t kSignals = 4;  // of a tile: two CTAs, two groups of warps
+enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kAIterate = 16, kBIterate = 32 };
+constexpr uint32_t kSignals = 16;  // of a tile: two CTAs, eight warps
 
 // One launch takes a list through some iterations, or a phase of one: its tiles in order, iteration after iteration, each pair every n-th.  A tile waits until all
 // those that it reads from have counted; they come before it in that order, and all CTAs are resident, so every wait ends.
@@ -130,6 +135,7 @@ struct MuonProduct {
   uint32_t p_blocks;        // from P to S
   float coef[FR_MUON_MOST][3];
   uint32_t low;             // bit i: the iterate before iteration i has second halves
+  uint32_t waits;           // 1: tiles of several phases
 };
 // Per device, before the first launch: opt the kernels in to their shared-memory size.
 cudaError_t configure_muon_product();
@@ -139,6 +145,6 @@ cudaError_t muon_pairs(uint32_t* pairs);
 struct MuonMaps {
   CUtensorMap rows, columns, half;
 };
-cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, bool waits, cudaStream_t s);
+cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, cudaStream_t s);
 
 }  // namespace frk

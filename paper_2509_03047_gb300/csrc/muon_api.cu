@@ -234,7 +234,8 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
     q.tiles = p->d_tiles;
     q.n_tiles = p->ends[kPhases - 1];
     q.iterations = h.iterations;
-    e = launch_muon_product(q, p->maps, std::min(p->pairs, p->most_tiles), true, s);
+    q.waits = 1;
+    e = launch_muon_product(q, p->maps, std::min(p->pairs, p->most_tiles), s);
     return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);
   }
   for (q.first = 0; q.first < h.iterations && e == cudaSuccess; ++q.first) {
@@ -243,7 +244,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
       const uint32_t begin = k ? p->ends[k - 1] : 0;
       q.tiles = p->d_tiles + begin;
       q.n_tiles = p->ends[k] - begin;
-      e = launch_muon_product(q, p->maps, p->pairs, false, s);
+      e = launch_muon_product(q, p->maps, p->pairs, s);
     }
   }
   return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);

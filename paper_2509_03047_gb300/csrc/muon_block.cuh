@@ -14,6 +14,12 @@ __device__ __forceinline__ uint64_t chunk_at(uint32_t col_blocks, uint32_t r, ui
   return block * kBlockBytes + (r % kBlockRows) * 128 + (((c % 8) ^ (r % 8)) * 16);
 }
 
+// The same of the second halves.
+__device__ __forceinline__ uint64_t low_at(uint32_t col_blocks, uint32_t r, uint32_t c) {
+  const uint64_t block = static_cast<uint64_t>(r / kBlockRows) * col_blocks + c / 8;
+  return block * kBlockBytes + ((c % 8) * kBlockRows + r % kBlockRows) * 16;
+}
+
 __device__ __forceinline__ uint32_t half2_bits(float x, float y) {
   const __half2 h = __floats2half2_rn(x, y);
   return reinterpret_cast<const uint32_t&>(h);

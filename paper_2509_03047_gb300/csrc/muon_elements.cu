@@ -205,9 +205,8 @@ __global__ void __launch_bounds__(kElementThreads) iterate_kernel(const __grid_c
     for (int j = 0; j < 8; ++j) x[j] = j < left ? (x[j] * to_one) * factor : 0.0f;
     uint4 hi, lo;
     split(x, hi, lo);
-    const uint64_t to = chunk_at(d.col_blocks, r, at.chunk);
-    *reinterpret_cast<uint4*>(p.work + d.x[0] + to) = hi;
-    if (p.low) *reinterpret_cast<uint4*>(p.work + d.low + to) = lo;
+    *reinterpret_cast<uint4*>(p.work + d.x[0] + chunk_at(d.col_blocks, r, at.chunk)) = hi;
+    if (p.low) *reinterpret_cast<uint4*>(p.work + d.low + low_at(d.col_blocks, r, at.chunk)) = lo;
   }
 }
 

@@ -8,8 +8,7 @@
 // of tensor memory.  The blocks lie in memory as the tensor cores read them, by rows
 // or by columns, so X X^T, X^T X and products from either side need no
 // transposition, and results leave as they come, by bulk copies.  Of the symmetric
-// products the tiles on and below the diagonal are computed, and those below written
-// a second time, transposed.
+// products the tiles on and below the diagonal are computed, and read both ways.
 #include <algorithm>
 
 #include "kernels.h"
@@ -21,18 +20,19 @@ namespace frk {
 
 namespace {
 
-constexpr int kStages = 5;
+constexpr int kStages = 6;
 constexpr int kFactorBytes = 16384;  // 128 rows or columns of a factor, 64 of the contraction
 constexpr int kHalf = 8192;
 constexpr int kStageBytes = 2 * kFactorBytes;
-constexpr int kGroups = 2;           // of four warps, one of 64 columns each
-constexpr int kThreads = 64 + kGroups * 128;
-constexpr int kStaging = 2 * kBlockBytes;  // per group
+constexpr int kWarps = 8;            // that turn sums into blocks: a quarter of the rows, every other 64 columns
+constexpr int kThreads = 64 + kWarps * 32;
+constexpr int kStaging = kBlockBytes / 4;  // per warp
 constexpr int kTensorColumns = 512;
-constexpr size_t kShared = 1024 + kStages * kStageBytes + kGroups * kStaging;
+constexpr size_t kShared = 1024 + kStages * kStageBytes + kWarps * kStaging;
+static_assert(kSignals == 2 * kWarps, "one per warp");
 
 struct Control {
-  uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2], in[kGroups];
+  uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
   uint32_t tensor;
   uint32_t gave_up;
 };
@@ -86,18 +86,6 @@ struct Ring {
   }
 };
 
-__device__ __forceinline__ void group_sync(int group) { asm volatile("bar.sync %0, 128;" ::"r"(group + 1) : "memory"); }
-
-// The same, and whether `ok` is true of every thread: nobody leaves a group alone.
-__device__ __forceinline__ bool group_agrees(int group, bool ok) {
-  uint32_t all;
-  asm volatile("{\n\t.reg .pred a, b;\n\tsetp.ne.u32 a, %2, 0;\n\tbarrier.cta.red.and.pred b, %1, 128, a;\n\tselp.u32 %0, 1, 0, b;\n\t}"
-               : "=r"(all)
-               : "r"(group + 1), "r"(static_cast<uint32_t>(ok))
-               : "memory");
-  return all != 0;
-}
-
 __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps, uint32_t ring_at, Control& c, uint32_t rank) {
   Ring r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]);
@@ -107,11 +95,19 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
     Place a = {static_cast<int32_t>((rank ? t.a[1] : t.a[0]) + (t.flags & kAIterate ? tiles.iterate(0) : 0)), 0, static_cast<int32_t>(t.a_next), a_columns};
     Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? tiles.iterate(0) : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
                static_cast<int32_t>(t.b_next), b_columns};
-    const CUtensorMap *const a_map = a_columns ? &maps.columns : &maps.rows, *const b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
-    if (!wait_count(p.done + t.needs, tiles.count(), &c.gave_up)) return let_copies_land();
+    const CUtensorMap *a_map = a_columns ? &maps.columns : &maps.rows, *b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
+    if (p.waits && !wait_count(p.done + t.needs, tiles.count(), &c.gave_up)) return let_copies_land();
     const uint32_t bytes = 2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < t.depth; ++k) {
+      if (k == t.a_switch) {
+        a = {static_cast<int32_t>(rank ? t.a_after[1] : t.a_after[0]), 0, static_cast<int32_t>(t.square), 1};
+        a_map = &maps.columns;
+      }
+      if (k == t.b_switch) {
+        b = {static_cast<int32_t>(rank ? t.b_after[1] : t.b_after[0]), 0, static_cast<int32_t>(t.square), 1};
+        b_map = &maps.columns;
+      }
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
       if (!wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up)) return let_copies_land();
       if (rank == 0) expect_bytes(full, bytes);
@@ -130,14 +126,27 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
   uint32_t n = 0;
   for (Tiles tiles(p); tiles.take(); ++n) {
     const MuonTile& t = tiles.now;
-    const bool a_columns = t.flags & kAColumns, b_columns = t.flags & kBColumns;
-    const uint32_t half = n % 2, kind = product_kind(a_columns, b_columns, t.flags & kNarrow ? 128 : 256), depth = t.depth;
-    const uint32_t a_step = a_columns ? 2048 >> 4 : 32 >> 4, b_step = b_columns ? 2048 >> 4 : 32 >> 4;
-    const uint64_t a0 = factor(ring_at, a_columns, kHalf), b0 = factor(ring_at + kFactorBytes, b_columns, kHalf);
+    bool a_columns = t.flags & kAColumns, b_columns = t.flags & kBColumns;
+    const uint32_t half = n % 2, columns = t.flags & kNarrow ? 128 : 256, depth = t.depth, a_switch = t.a_switch, b_switch = t.b_switch;
+    uint32_t kind, a_step, b_step;
+    uint64_t a0, b0;
+    auto set = [&] {
+      kind = product_kind(a_columns, b_columns, columns);
+      a_step = a_columns ? 2048 >> 4 : 32 >> 4;
+      b_step = b_columns ? 2048 >> 4 : 32 >> 4;
+      a0 = factor(ring_at, a_columns, kHalf);
+      b0 = factor(ring_at + kFactorBytes, b_columns, kHalf);
+    };
+    set();
     if (!wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up)) return let_copies_land();
     tensor_fence_after();
     const uint32_t sums = tensor + half * 256;
     for (uint32_t k = 0; k < depth; ++k) {
+      if (k == a_switch || k == b_switch) {
+        a_columns |= k == a_switch;
+        b_columns |= k == b_switch;
+        set();
+      }
       if (!wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up)) return let_copies_land();
       tensor_fence_after();
       const uint64_t a = a0 + r.stage * (kStageBytes >> 4), b = b0 + r.stage * (kStageBytes >> 4);
@@ -150,135 +159,121 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
   }
 }
 
-// What sums of a product, the thread's row and 64 columns of it, become, in shared memory:
+// What is added to a row's 64 sums: of S, whose chunks lie as in the factors, or of second halves, whose chunks lie a block's rows apart.  (Not
+// from this SM's first-level cache: other SMs have written it during this launch.)
+struct Addend {
+  uint4 x[8];
+  __device__ __forceinline__ void of_square(const uint8_t* block, uint32_t row) {
+#pragma unroll
+    for (uint32_t c = 0; c < 8; ++c) x[c] = __ldcg(reinterpret_cast<const uint4*>(block + row * 128 + ((c ^ (row % 8)) * 16)));
+  }
+  __device__ __forceinline__ void of_low(const uint8_t* block, uint32_t row) {
+#pragma unroll
+    for (uint32_t c = 0; c < 8; ++c) x[c] = __ldcg(reinterpret_cast<const uint4*>(block + (c * kBlockRows + row) * 16));
+  }
+};
+
+// What sums of a product, the thread's row and 64 columns of it, become:
 //   S = X X^T             sums in X's scale twice
 //   P = a I + b S + c S^2
 //   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part
-// `one`: block of S or P, or of second halves (what the result adds is there); `two`: the transposed block, or the first halves.
+// rounded to fp16, for the factors in shared memory; what X's rounding leaves, to `low` if that is not null.
 template <int kPhase>
-__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t row, uint32_t diagonal, float (&v)[64], uint8_t* one, uint8_t* two, bool transpose,
-                                           bool low_before, bool low_after) {
+__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diagonal, const float (&v)[64], const Addend& in, bool adds, uint8_t* staging,
+                                           uint32_t row, uint8_t* low) {
 #pragma unroll
   for (uint32_t c = 0; c < 8; ++c) {
     float x[8], y[8];
+    if (kPhase == kPoly || (kPhase == kNext && adds)) floats(in.x[c], y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = v[8 * c + j];
-    const uint32_t at = row * 128 + ((c ^ (row % 8)) * 16);
-    uint4* const q = reinterpret_cast<uint4*>(one + at);
-    if (kPhase == kGram) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= kScaleS / (kScaleX * kScaleX);
-      *q = halves(x);
-    } else if (kPhase == kPoly) {
-      floats(*q, y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
+    for (uint32_t j = 0; j < 8; ++j) {
+      const float sum = v[8 * c + j];
+      if (kPhase == kGram) {
+        x[j] = sum * (kScaleS / (kScaleX * kScaleX));
+      } else if (kPhase == kPoly) {
         const float own = diagonal == 8 * c + j ? coef[0] * kScaleP : 0.0f;
-        x[j] = own + y[j] * (coef[1] * (kScaleP / kScaleS)) + x[j] * (coef[2] * (kScaleP / (kScaleS * kScaleS)));
+        x[j] = own + y[j] * (coef[1] * (kScaleP / kScaleS)) + sum * (coef[2] * (kScaleP / (kScaleS * kScaleS)));
+      } else {
+        x[j] = sum * (1.0f / kScaleP);
+        if (adds) x[j] += coef[0] * y[j];
       }
-      *q = halves(x);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= 1.0f / kScaleP;
-      if (low_before) {
-        floats(*q, y);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] += coef[0] * y[j];
-      }
-      uint4* const r = reinterpret_cast<uint4*>(two + at);
-      if (low_after)
-        split(x, *r, *q);
-      else
-        *r = halves(x);
     }
-    if (kPhase != kNext && transpose) {
-      // (neighbouring threads write neighbouring columns: no bank is met twice)
-#pragma unroll
-      for (uint32_t j = 0; j < 8; ++j)
-        *reinterpret_cast<__half*>(two + row / 64 * kHalf + (8 * c + j) * 128 + (((row % 64 / 8) ^ j) * 16) + row % 8 * 2) = __float2half_rn(x[j]);
+    uint4* const to = reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16));
+    if (kPhase == kNext && low != nullptr) {
+      uint4 lo;
+      split(x, *to, lo);
+      *reinterpret_cast<uint4*>(low + (c * kBlockRows + row) * 16) = lo;
+    } else {
+      *to = halves(x);
     }
   }
 }
 
+// One of the eight warps.  Each by itself: what it adds is on its way while the products run, its 32 rows of 64 columns leave by one copy.
 __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* staging, Control& c, uint32_t rank) {
-  const int group = (threadIdx.x - 64) / 128;
-  const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + threadIdx.x % 32;  // a warp reads the quarter of its index
-  const bool one_thread = threadIdx.x % 128 == 64;  // of the group
-  uint8_t *const one = staging + group * kStaging, *const two = one + kBlockBytes;
-  const uint32_t one_at = shared_address(one), two_at = shared_address(two), in = shared_address(&c.in[group]);
-  const uint64_t low = 2ull * p.x_blocks * kBlockBytes, square = static_cast<uint64_t>(p.p_blocks) * kBlockBytes;
-  uint32_t n = 0, phase = 0;
-  bool ok = true;
+  const uint32_t warp = threadIdx.x / 32 - 2, lane = threadIdx.x % 32;
+  const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + lane;  // a warp reads the quarter of its index
+  staging += warp * kStaging;
+  const uint32_t staging_at = shared_address(staging);
+  const uint64_t to_low = 2ull * p.x_blocks * kBlockBytes, to_square = static_cast<uint64_t>(p.p_blocks) * kBlockBytes;
+  uint32_t n = 0;
   for (Tiles tiles(p); tiles.take(); ++n) {
     const MuonTile& t = tiles.now;
     const uint32_t half = n % 2, parts = t.flags & kNarrow ? 2 : 4;
-    const bool mine = rank == 0 || t.flags & kSecond, transpose = t.flags & kTransposed;
-    const bool low_before = p.low >> tiles.round & 1, low_after = p.low >> (tiles.round + 1) & 1;
-    const bool adds = t.phase == kPoly || (t.phase == kNext && low_before);
+    const bool mine = rank == 0 || t.flags & kSecond;
+    const bool low_after = p.low >> (tiles.round + 1) & 1, adds = t.phase == kPoly || (t.phase == kNext && p.low >> tiles.round & 1);
     const float coef[3] = {p.coef[tiles.round][0], p.coef[tiles.round][1], p.coef[tiles.round][2]};
-    if (one_thread && adds) ok = wait_count(p.done + t.needs, tiles.count(), &c.gave_up);
-    for (uint32_t q = group; q < parts; q += kGroups) {
-      uint8_t* const at = p.work + (static_cast<uint64_t>(t.out) + rank * t.across + q) * kBlockBytes;
-      if (mine && one_thread) {
-        wait_stores_read();  // of the blocks before
-        if (adds) {
-          expect_bytes(in, kBlockBytes);
-          load_bytes(one_at, at + (t.phase == kPoly ? square : low), kBlockBytes, in);
-        }
-      }
-      if (q == static_cast<uint32_t>(group)) {
-        ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up) && ok;
-        tensor_fence_after();
-      }
-      __syncwarp();
+    uint8_t* const first = p.work + (static_cast<uint64_t>(t.out) + rank * t.across) * kBlockBytes;
+    Addend in;
+    auto fetch = [&](uint32_t q) {
+      if (t.phase == kPoly)
+        in.of_square(first + q * kBlockBytes + to_square, row);
+      else
+        in.of_low(first + q * kBlockBytes + to_low, row);
+    };
+    bool ok = true;
+    if (mine && adds) {
+      ok = !p.waits || wait_count(p.done + t.needs, tiles.count(), &c.gave_up);
+      fetch(warp / 4);
+    }
+    ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up) && ok;
+    if (!__all_sync(0xFFFFFFFFu, ok)) return let_copies_land();
+    tensor_fence_after();
+    for (uint32_t q = warp / 4; q < parts; q += 2) {
       float v[64];
       const uint32_t from = c.tensor + (quarter * 32 << 16) + half * 256 + q * 64;
       tensor_load(from, v);
       tensor_load(from + 32, v + 32);
       tensor_load_wait();
-      if (q + kGroups >= parts) tensor_fence_before();
-      if (mine) {
-        if (adds) {
-          ok = wait_phase(in, phase, &c.gave_up) && ok;
-          phase ^= 1;
-        } else {
-          group_sync(group);
-        }
-        if (t.phase == kGram) {
-          finish_row<kGram>(coef, row, 0, v, one, two, transpose, false, false);
-        } else if (t.phase == kPoly) {
-          // (the diagonal's column of this row among the block's)
-          finish_row<kPoly>(coef, row, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, one, two, transpose, false, false);
-        } else {
-          finish_row<kNext>(coef, row, 0, v, one, two, false, low_before, low_after);
-        }
-        before_copies();
+      if (q + 2 >= parts) {
+        tensor_fence_before();
+        __syncwarp();
+        if (lane == 0) arrive_in_first(shared_address(&c.sums_empty[half]));
       }
+      if (!mine) continue;
+      if (lane == 0) wait_stores_read();  // of the rows before
       __syncwarp();
-      if (!group_agrees(group, ok)) return let_copies_land();
-      if (one_thread) {
-        if (q + kGroups >= parts) arrive_in_first(shared_address(&c.sums_empty[half]));
-        if (mine) {
-          if (t.phase == kNext) {
-            if (low_after) store_bytes(at + low, one_at, kBlockBytes);
-            store_bytes(at + static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes, two_at, kBlockBytes);
-          } else {
-            store_bytes(at, one_at, kBlockBytes);
-            if (transpose) {
-              uint8_t* const other = p.work + (static_cast<uint64_t>(t.other) + q / 2 * t.across + 2 * rank) * kBlockBytes + q % 2 * kHalf;
-              store_bytes(other, two_at, kHalf);
-              store_bytes(other + kBlockBytes, two_at + kHalf, kHalf);
-            }
-          }
-          end_stores();
-        }
+      uint8_t* const block = first + q * kBlockBytes;
+      if (t.phase == kGram)
+        finish_row<kGram>(coef, 0, v, in, false, staging, row, nullptr);
+      else if (t.phase == kPoly)  // (the diagonal's column of this row among the block's)
+        finish_row<kPoly>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, true, staging, row, nullptr);
+      else
+        finish_row<kNext>(coef, 0, v, in, adds, staging, row, low_after ? block + to_low : nullptr);
+      if (adds && q + 2 < parts) fetch(q + 2);
+      before_copies();
+      __syncwarp();
+      if (lane == 0) {
+        store_bytes(block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes : 0) + quarter * kStaging, staging_at, kStaging);
+        end_stores();
       }
     }
-    if (one_thread) {
+    if (p.waits && lane == 0) {
       wait_stores();
       add_to_count(p.done + t.done);
     }
   }
+  if (lane == 0) wait_stores();
 }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
@@ -295,9 +290,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       barrier_init(shared_address(&c.sums_full[i]), 1);
-      barrier_init(shared_address(&c.sums_empty[i]), 2 * kGroups);
+      barrier_init(shared_address(&c.sums_empty[i]), 2 * kWarps);
     }
-    for (int i = 0; i < kGroups; ++i) barrier_init(shared_address(&c.in[i]), 1);
     c.gave_up = 0;
     barrier_init_done();
   }
@@ -355,8 +349,8 @@ cudaError_t muon_pairs(uint32_t* pairs) {
   return e != cudaSuccess ? e : n > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
 }
 
-cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, bool waits, cudaStream_t s) {
-  if (!waits) return launch_chained(product_kernel, static_cast<int>(2 * std::min(pairs, p.n_tiles)), kThreads, kShared, s, p, maps);
+cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, cudaStream_t s) {
+  if (!p.waits) return launch_chained(product_kernel, static_cast<int>(2 * std::min(pairs, p.n_tiles)), kThreads, kShared, s, p, maps);
   cudaLaunchAttribute attrs[1] = {};
   const cudaLaunchConfig_t c = config(pairs, s, attrs);
   cudaLaunchKernelEx(&c, product_kernel, p, maps);

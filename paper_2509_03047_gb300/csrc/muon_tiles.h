@@ -9,33 +9,37 @@
 
 namespace frk {
 
-// A factor of a product: a matrix of the workspace by its rows or by its columns.
+// A factor of a product: a matrix of the workspace by its rows or by its columns, S and P by either.
 struct Factor {
   uint32_t block, col_blocks;
   bool by_columns, iterate;
   uint32_t first(uint32_t b) const { return block + (by_columns ? 2 * b : b * col_blocks); }
+  // S and P: where the factor's 256 rows from block b on leave the tiles that exist, and what they meet there on the other side.
+  uint32_t switch_at(uint32_t b, uint32_t depth) const { return iterate ? depth : std::min(depth, 2 * (b + 2)); }
+  uint32_t after(uint32_t b, uint32_t mine) const { return iterate ? 0 : block + (b + 2) * col_blocks + 2 * mine; }
 };
 
 // A phase's product for a matrix.
 struct ProductOf {
   Factor a, b;
-  uint32_t depth;
+  uint32_t depth, square;
   uint32_t out, rows, cols;  // rows and columns in blocks of 128
 
   ProductOf(int phase, const MuonDesc& d) {
     const uint32_t x = static_cast<uint32_t>(d.x[0] / kBlockBytes), s = static_cast<uint32_t>(d.s / kBlockBytes), p = static_cast<uint32_t>(d.p / kBlockBytes);
     const uint32_t side = d.side_blocks;
+    square = 2 * side;
     if (phase == kGram) {
       a = b = {x, d.col_blocks, d.tall != 0, true};
       depth = d.tall ? 2 * d.row_blocks : d.col_blocks;
     } else if (phase == kPoly) {
-      a = b = {s, 2 * side, false, false};
-      depth = 2 * side;
+      a = b = {s, square, false, false};
+      depth = square;
     } else {
-      const Factor q = {p, 2 * side, false, false};
+      const Factor q = {p, square, false, false};
       a = d.tall ? Factor{x, d.col_blocks, false, true} : q;
       b = d.tall ? q : Factor{x, d.col_blocks, true, true};
-      depth = 2 * side;
+      depth = square;
     }
     out = phase == kGram ? s : phase == kPoly ? p : x;
     rows = phase == kNext ? d.row_blocks : side;
@@ -55,15 +59,20 @@ struct ProductOf {
     t.b[0] = b.first(c);
     // (a narrow tile's CTAs have 64 rows or columns each, of rows the halves of a block)
     t.b[1] = !narrow ? b.first(c + 1) : b.first(c) + (b.by_columns ? 1 : 0);
+    t.a_switch = a.switch_at(r, depth);
+    t.b_switch = b.switch_at(c, depth);
+    for (uint32_t k = 0; k < 2; ++k) {
+      t.a_after[k] = a.after(r, second ? r + k : r);
+      t.b_after[k] = b.after(c, c + k);  // (a narrow tile is the last one, whose blocks do not change sides)
+    }
     t.a_next = a.by_columns ? a.col_blocks : 1;
     t.b_next = b.by_columns ? b.col_blocks : 1;
+    t.square = square;
     t.depth = depth;
-    const bool transposed = phase != kNext && r != c;
     t.flags = (narrow ? kNarrow : 0) | (a.by_columns ? kAColumns : 0) | (b.by_columns ? kBColumns : 0) | (second ? kSecond : 0) |
-              (transposed ? kTransposed : 0) | (a.iterate ? kAIterate : 0) | (b.iterate ? kBIterate : 0);
+              (a.iterate ? kAIterate : 0) | (b.iterate ? kBIterate : 0);
     t.across = 2 * cols;
     t.out = out + r * t.across + 2 * c;
-    t.other = out + c * t.across + 2 * r;
     t.row = static_cast<uint16_t>(r);
     t.col = static_cast<uint16_t>(c);
     return t;
