@@ -96,7 +96,7 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
     Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? tiles.iterate(0) : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
                static_cast<int32_t>(t.b_next), b_columns};
     const CUtensorMap *a_map = a_columns ? &maps.columns : &maps.rows, *b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
-    if (p.waits && !wait_count(p.done + t.needs, tiles.count(), &c.gave_up)) return let_copies_land();
+    if (p.waits && !__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
     const uint32_t bytes = 2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < t.depth; ++k) {
@@ -109,10 +109,13 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
         b_map = &maps.columns;
       }
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
-      if (!wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up)) return let_copies_land();
-      if (rank == 0) expect_bytes(full, bytes);
-      load_blocks(to, a_map, a.half, a.block, full);
-      load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
+      if (!__all_sync(0xFFFFFFFFu, wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up))) return let_copies_land();
+      if (one_lane()) {
+        if (rank == 0) expect_bytes(full, bytes);
+        load_blocks(to, a_map, a.half, a.block, full);
+        load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
+      }
+      __syncwarp();
       a.advance();
       b.advance();
       r.next();
@@ -138,7 +141,7 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
       b0 = factor(ring_at + kFactorBytes, b_columns, kHalf);
     };
     set();
-    if (!wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up)) return let_copies_land();
+    if (!__all_sync(0xFFFFFFFFu, wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up))) return let_copies_land();
     tensor_fence_after();
     const uint32_t sums = tensor + half * 256;
     for (uint32_t k = 0; k < depth; ++k) {
@@ -147,15 +150,19 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
         b_columns |= k == b_switch;
         set();
       }
-      if (!wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up)) return let_copies_land();
+      if (!__all_sync(0xFFFFFFFFu, wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up))) return let_copies_land();
       tensor_fence_after();
       const uint64_t a = a0 + r.stage * (kStageBytes >> 4), b = b0 + r.stage * (kStageBytes >> 4);
+      if (one_lane()) {
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + j * b_step, kind, k + j > 0);
-      arrive_after_products(empty0 + r.stage * 8);
+        for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + j * b_step, kind, k + j > 0);
+        arrive_after_products(empty0 + r.stage * 8);
+      }
+      __syncwarp();
       r.next();
     }
-    arrive_after_products(shared_address(&c.sums_full[half]));
+    if (one_lane()) arrive_after_products(shared_address(&c.sums_full[half]));
+    __syncwarp();
   }
 }
 
@@ -303,9 +310,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   wait_for_kernel_before();
   if (p.clip == nullptr || p.clip->nonfinite == 0) {
     if (warp == 0) {
-      if (threadIdx.x == 0) bring(p, maps, ring_at, c, rank);
+      bring(p, maps, ring_at, c, rank);
     } else if (warp == 1) {
-      if (rank == 0 && threadIdx.x == 32) multiply_tiles(p, ring_at, c);
+      if (rank == 0) multiply_tiles(p, ring_at, c);
     } else {
       finish_tiles(p, staging, c, rank);
     }

@@ -24,6 +24,13 @@ __device__ __forceinline__ uint32_t rank_in_pair() {
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
 }
+// One lane of the warp, all of which call.  (A warp that goes together and lets one lane issue keeps addresses in uniform registers, which these
+// instructions take them from.)
+__device__ __forceinline__ bool one_lane() {
+  uint32_t mine;
+  asm volatile("{\n\t.reg .pred q;\n\telect.sync _|q, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, q;\n\t}" : "=r"(mine));
+  return mine != 0;
+}
 __device__ __forceinline__ void pair_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -45,7 +52,7 @@ __device__ __forceinline__ void arrive_in_first(uint32_t bar) {
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
   asm volatile(
-      "{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 q, [%1], %2;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      "{\n\t.reg .pred q;\n\tmbarrier.try_wait.parity.shared::cta.b64 q, [%1], %2;\n\tselp.u32 %0, 1, 0, q;\n\t}"
       : "=r"(done)
       : "r"(bar), "r"(parity)
       : "memory");
