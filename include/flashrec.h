@@ -610,7 +610,7 @@ typedef struct fr_embed_s* fr_embed;
 /* Plan for batches of up to `max_tokens` tokens, bound to the current device; it
  * allocates here and nowhere else, and one stream at a time may use it for
  * fr_embed_grad (fr_embed_lookup uses no memory of it).  Device memory: 8 to 16
- * bytes per token, a byte per row, and workspace of up to 30 MB.
+ * bytes per token and a workspace of a few MB.
  * rows, max_tokens < 2^31, dim <= 2^20, first <= 2^62; rows * dim and max_tokens *
  * dim <= 2^40.  Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
 fr_status fr_embed_create(uint64_t rows, uint64_t dim, uint64_t max_tokens, uint64_t first, fr_embed* out);

@@ -51,10 +51,11 @@ struct Met {  // a token of the batch
   uint32_t row, at;
 };
 constexpr int kSortThreads = 1024, kSortEach = 4, kSortTile = kSortThreads * kSortEach;
+constexpr uint64_t kCompareTokens = 8192;  // a batch of up to this many is sorted by comparing each with all
 constexpr uint32_t kSortCluster = 16;  // CTAs that sort a batch of up to a tile for each in one launch
 constexpr uint64_t kClusterTokens = static_cast<uint64_t>(kSortCluster) * kSortTile;
 constexpr uint32_t kSortCtas = 128;    // of a larger batch's launches
-constexpr int kMostDigit = 11;         // bits of a pass
+constexpr int kMostDigit = 9;          // bits of a pass
 
 struct SortPlan {
   int passes, bits;  // bits of a pass
@@ -72,7 +73,6 @@ struct SortParams {
   uint32_t* counts; // per CTA and bin
   uint32_t* found;  // tokens of the slice
   uint32_t* n_long; // set to zero
-  uint8_t* met;     // per row: set to 1 where a token meets it, or null
   uint64_t share;   // tokens per CTA
   uint32_t ctas;
   int each;         // tokens per thread and tile
@@ -87,38 +87,32 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
 
 // Vectors of a token's row that a lane has, 32 vectors apart.
 constexpr int lane_vectors(int v) { return v >= 8 ? 1 : v == 4 ? 2 : 4; }
-// The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns.
+// The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns; a multiple of what a CTA has.
 constexpr uint32_t kSumWarps = 8;
-#ifndef FR_RANGE_WARPS
-#define FR_RANGE_WARPS 80
-#endif
-#ifndef FR_LEAST_RANGE
-#define FR_LEAST_RANGE 16
-#endif
-constexpr uint32_t kRangeWarps = kSms * FR_RANGE_WARPS;  // ranges times column tiles, about
-constexpr uint32_t kLeastRange = FR_LEAST_RANGE;
+constexpr uint32_t kRangeWarps = kSms * 48;  // ranges times column tiles, about
+constexpr uint32_t kLeastRange = 16;
 inline uint32_t column_tiles(uint64_t dim, int v) {
   const uint64_t width = 32 * v * lane_vectors(v);
   return static_cast<uint32_t>((dim + width - 1) / width);
 }
 inline uint32_t ranges_of(uint64_t n, uint32_t tiles) {
   const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = (kRangeWarps + tiles - 1) / tiles;
-  return static_cast<uint32_t>(most < fill ? most : fill);
+  return static_cast<uint32_t>(((most < fill ? most : fill) + kSumWarps - 1) / kSumWarps * kSumWarps);
 }
 struct SumParams {
   const Met* sorted;
   const uint32_t* found;
-  uint32_t* n_long;  // rows in several ranges' parts
-  uint32_t* longs;   // the range where each starts
-  float* parts;      // two rows per range
-  uint8_t* met;      // null: accumulating
+  uint32_t* n_long;  // rows in several CTAs' parts
+  uint32_t* longs;   // the CTA where each begins
+  float* parts;      // two rows per CTA
   const void* out;
   void* grad;
   uint64_t dim, rows;
   float scale;
   uint32_t ranges, tiles;
   uint32_t sum_ctas, zero_ctas;
-  uint32_t rows_per_zero_cta;
+  uint32_t rows_per_zero_warp;
+  uint32_t accumulate;
   uint32_t bf16_out, bf16_grad;
   int v;
 };

@@ -24,7 +24,6 @@ struct fr_embed_s {
   uint32_t* d_longs = nullptr;
   float* d_parts = nullptr;
   uint32_t* d_numbers = nullptr;  // found, n_long
-  uint8_t* d_met = nullptr;       // zeros between calls
 };
 
 namespace {
@@ -43,19 +42,15 @@ fr_status fill_embed(fr_embed p) {
     const uint64_t ranges = ranges_of(n, column_tiles(p->dim, v));
     p->ranges = std::max(p->ranges, ranges);
   }
-  elems = 2 * p->ranges * p->dim;
+  elems = 2 * (p->ranges / kSumWarps) * p->dim;
   mem.scratch(&p->d_sorted[0], n);
   if (p->sort.passes > 1) mem.scratch(&p->d_sorted[1], n);
   if (n > kClusterTokens) mem.scratch(&p->d_counts, static_cast<uint64_t>(kSortCtas) * p->sort.bins());
-  mem.scratch(&p->d_longs, p->ranges);
+  mem.scratch(&p->d_longs, p->ranges / kSumWarps);
   mem.scratch(&p->d_parts, elems);
   mem.scratch(&p->d_numbers, 2);
-  mem.scratch(&p->d_met, p->rows);
   p->device_bytes = mem.scratch_bytes();
   cudaError_t e = mem.commit(&p->d_memory);
-  if (e == cudaSuccess) e = cudaMemset(p->d_memory, 0, std::max<uint64_t>(p->device_bytes, 1));
-  // (a call on a non-blocking stream is not ordered after the legacy stream's)
-  if (e == cudaSuccess) e = cudaStreamSynchronize(cudaStreamLegacy);
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   e = configure_sort();
   return e == cudaSuccess ? FR_OK : report_cuda("shared memory of the sort", e);
@@ -174,7 +169,6 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   sp.counts = p->d_counts;
   sp.found = p->d_numbers;
   sp.n_long = p->d_numbers + 1;
-  sp.met = accumulate ? nullptr : p->d_met;
   int last = 0;
   cudaError_t e = launch_sort(sp, p->sort, &last, s);
   if (e != cudaSuccess) return report_cuda("sort kernel launch", e);
@@ -184,7 +178,7 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.n_long = sp.n_long;
   q.longs = p->d_longs;
   q.parts = p->d_parts;
-  q.met = sp.met;
+  q.accumulate = accumulate;
   q.out = out;
   q.grad = grad;
   q.dim = p->dim;
@@ -192,13 +186,14 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.scale = scale;
   q.v = vector_elems(p->dim, out, type_bytes(out_dtype), grad, type_bytes(grad_dtype));
   q.tiles = column_tiles(p->dim, q.v);
-  q.ranges = std::max(1u, ranges_of(n, q.tiles));
-  q.sum_ctas = n == 0 ? 0 : static_cast<uint32_t>((static_cast<uint64_t>(q.ranges) * q.tiles + kSumWarps - 1) / kSumWarps);
+  q.ranges = std::max(kSumWarps, ranges_of(n, q.tiles));
+  q.sum_ctas = n == 0 ? 0 : q.ranges / kSumWarps * q.tiles;
   if (!accumulate) {
-    // about 64 KiB per CTA
+    // about 64 KiB per warp
     const uint64_t row_bytes = p->dim * type_bytes(grad_dtype);
-    q.rows_per_zero_cta = static_cast<uint32_t>(std::max<uint64_t>({1, (64 << 10) / row_bytes, (p->rows + (1u << 20) - 1) >> 20}));
-    q.zero_ctas = static_cast<uint32_t>((p->rows + q.rows_per_zero_cta - 1) / q.rows_per_zero_cta);
+    q.rows_per_zero_warp = static_cast<uint32_t>(std::min<uint64_t>(32, std::max<uint64_t>(1, (64 << 10) / row_bytes)));
+    const uint32_t per_cta = q.rows_per_zero_warp * kSumWarps;
+    q.zero_ctas = static_cast<uint32_t>((p->rows + per_cta - 1) / per_cta);
   }
   q.bf16_out = out_dtype == FR_DT_BF16;
   q.bf16_grad = grad_dtype == FR_DT_BF16;

@@ -1,13 +1,13 @@
 // embed_sort.cu -- the tokens of a batch that fall into the slice, sorted by row
 // and, within a row, in the batch's order.
 //
-// Counting sort by digits of up to 11 bits, the lowest first.  A pass counts each
+// Counting sort by digits of up to 9 bits, the lowest first.  A pass counts each
 // CTA's digits, then every CTA finds its places by adding up the counts of the
 // CTAs before it, and a token's among its CTA's by warps in turn: a warp's tokens
 // of one digit are found by a vote, those of the warps before by a table of counts
 // per warp and digit.  Nothing depends on the order in which anything runs.
 //
-// A batch of up to 65,536 tokens is sorted in one launch, by a cluster of CTAs that
+// A batch of up to 8,192 tokens is sorted by comparing each with all, one of up to 65,536 in one launch, by a cluster of CTAs that
 // read each other's counts from shared memory; a larger one by two launches per pass.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -62,21 +62,39 @@ struct Shared {
 };
 size_t shared_bytes(uint32_t bins) { return bins * (8 + kWarps * 2) + kWarps * 4; }
 
+// The lanes with this lane's digit (kAll: no token), for each of its tokens: a vote per bit, the tokens' votes side by side.
+__device__ __forceinline__ void same_digit(const uint32_t (&digit)[kSortEach], int bits, uint32_t (&same)[kSortEach]) {
+#pragma unroll
+  for (int k = 0; k < kSortEach; ++k) {
+    const uint32_t there = __ballot_sync(kAll, digit[k] != kAll);
+    same[k] = digit[k] != kAll ? there : ~there;
+  }
+  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+    for (int k = 0; k < kSortEach; ++k) {
+      const bool set = digit[k] >> b & 1;
+      const uint32_t ones = __ballot_sync(kAll, set);
+      same[k] &= set ? ones : ~ones;
+    }
+  }
+}
+
 // Each token's place among the tile's of its digit, and the tile's counts per warp, then sums over the warps before in their place, and totals.
 // digit >= bins: no token.  A warp's tokens are consecutive, the lanes' in turn.
-__device__ __forceinline__ void rank_tile(const Shared& sh, uint32_t bins, int each, const uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach]) {
+__device__ __forceinline__ void rank_tile(const Shared& sh, uint32_t bins, int bits, int each, const uint32_t (&digit)[kSortEach], uint32_t (&rank)[kSortEach]) {
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   uint16_t* mine = sh.before + warp * bins;
   for (uint32_t i = lane; i < bins / 2; i += 32) reinterpret_cast<uint32_t*>(mine)[i] = 0;
+  uint32_t same[kSortEach];
+  same_digit(digit, bits, same);
   __syncwarp();
 #pragma unroll
   for (int k = 0; k < kSortEach; ++k) {
     if (k >= each) break;
-    const uint32_t same = __match_any_sync(kAll, digit[k]);
     const uint32_t earlier = digit[k] < bins ? mine[digit[k]] : 0;
-    rank[k] = earlier + __popc(same & ((1u << lane) - 1));
+    rank[k] = earlier + __popc(same[k] & ((1u << lane) - 1));
     __syncwarp();
-    if (digit[k] < bins && lane == 31 - __clz(same)) mine[digit[k]] = static_cast<uint16_t>(rank[k] + 1);
+    if (digit[k] < bins && lane == 31 - __clz(same[k])) mine[digit[k]] = static_cast<uint16_t>(rank[k] + 1);
     __syncwarp();
   }
   __syncthreads();
@@ -119,9 +137,8 @@ __device__ __forceinline__ void take_tile(const SortParams& p, const Shared& sh,
     const uint64_t i = begin + tile_index(p.each, k);
     m[k] = k < p.each && i < end ? get<First>(p, pass, i) : Met{kAll, 0};
     digit[k] = digit_of(p, pass, m[k].row);
-    if (First && p.met != nullptr && m[k].row != kAll) p.met[m[k].row] = 1;
   }
-  rank_tile(sh, bins, p.each, digit, rank);
+  rank_tile(sh, bins, p.bits, p.each, digit, rank);
 }
 __device__ __forceinline__ void put_tile(const SortParams& p, const Shared& sh, uint32_t bins, int pass, const Met (&m)[kSortEach],
                                          const uint32_t (&digit)[kSortEach], const uint32_t (&rank)[kSortEach]) {
@@ -146,11 +163,11 @@ __global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_consta
       digit[k] = digit_of(p, p.pass, i < end ? get<First>(p, p.pass, i).row : kAll);
     }
     // (one addition for a warp's tokens of one digit: a third of a batch may be the same)
+    uint32_t same[kSortEach];
+    same_digit(digit, p.bits, same);
 #pragma unroll
-    for (int k = 0; k < kSortEach; ++k) {
-      const uint32_t same = __match_any_sync(kAll, digit[k]);
-      if (digit[k] != kAll && threadIdx.x % 32 == 31 - __clz(same)) atomicAdd(counts + digit[k], static_cast<uint32_t>(__popc(same)));
-    }
+    for (int k = 0; k < kSortEach; ++k)
+      if (digit[k] != kAll && threadIdx.x % 32 == 31 - __clz(same[k])) atomicAdd(counts + digit[k], static_cast<uint32_t>(__popc(same[k])));
   }
   if (First && blockIdx.x == 0 && threadIdx.x == 0) *p.n_long = 0;
   __syncthreads();
@@ -163,7 +180,7 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   const uint32_t bins = 1u << p.bits;
   const Shared sh(raw, bins);
   wait_for_kernel_before();
-  // (up to two digits per thread)
+  // (a digit per thread)
   uint32_t before[2] = {0, 0};
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
@@ -243,6 +260,47 @@ __global__ void __launch_bounds__(kSortThreads) cluster_kernel(const __grid_cons
   }
 }
 
+// A small batch: a token's place is the number of tokens of lower rows, and of its row before it.  16 threads count for each.
+constexpr uint32_t kCompareEach = 16, kCompareShare = kSortThreads / kCompareEach;
+__global__ void __launch_bounds__(kSortThreads) compare_kernel(const __grid_constant__ SortParams p) {
+  __shared__ __align__(16) uint32_t rows[kCompareTokens];
+  wait_for_kernel_before();
+  const uint32_t n = static_cast<uint32_t>(p.tokens.n), whole = (n + 3) / 4;
+  uint32_t found = 0;
+  for (uint32_t i = threadIdx.x; i < 4 * whole; i += kSortThreads) {
+    rows[i] = i < n ? get<true>(p, 0, i).row : kAll;
+    found += rows[i] != kAll;
+  }
+  if (blockIdx.x == 0) {
+    __shared__ uint32_t all;
+    if (threadIdx.x == 0) all = 0;
+    __syncthreads();
+    found = __reduce_add_sync(kAll, found);
+    if (threadIdx.x % 32 == 0) atomicAdd(&all, found);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      *p.found = all;
+      *p.n_long = 0;
+    }
+  }
+  __syncthreads();
+  const uint32_t i = blockIdx.x * kCompareShare + threadIdx.x / kCompareEach, row = i < n ? rows[i] : kAll;
+  uint32_t place = 0;
+#pragma unroll 4
+  for (uint32_t v = threadIdx.x % kCompareEach; v < whole; v += kCompareEach) {
+    const uint4 r = reinterpret_cast<const uint4*>(rows)[v];
+    const uint32_t least = row + (4 * v < i);  // below it: of a lower row, or of this one and before
+    if (v == i / 4) {
+      place += (r.x < row + (4 * v < i)) + (r.y < row + (4 * v + 1 < i)) + (r.z < row + (4 * v + 2 < i)) + (r.w < row);
+    } else {
+      place += (r.x < least) + (r.y < least) + (r.z < least) + (r.w < least);
+    }
+  }
+#pragma unroll
+  for (uint32_t k = kCompareEach / 2; k > 0; k /= 2) place += __shfl_xor_sync(kAll, place, k);
+  if (threadIdx.x % kCompareEach == 0 && row != kAll) p.sorted[0][place] = {row, i};
+}
+
 cudaError_t launch_cluster(const SortParams& p, int passes, size_t shared, cudaStream_t s) {
   cudaLaunchAttribute a[2] = {};
   a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -276,10 +334,14 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
   p.bits = plan.bits;
   *last = (plan.passes - 1) % 2;
   const uint64_t n = p.tokens.n;
+  if (n <= kCompareTokens) {
+    *last = 0;
+    return launch_chained(compare_kernel, n == 0 ? 1 : static_cast<int>((n + kCompareShare - 1) / kCompareShare), kSortThreads, 0, s, p);
+  }
   if (n <= kClusterTokens) {
     p.ctas = 1;
     while (p.ctas < kSortCluster && p.ctas * static_cast<uint64_t>(kSortThreads) < n) p.ctas *= 2;
-    p.each = n == 0 ? 1 : static_cast<int>((n + p.ctas * kSortThreads - 1) / (p.ctas * kSortThreads));
+    p.each = static_cast<int>((n + p.ctas * kSortThreads - 1) / (p.ctas * kSortThreads));
     p.share = static_cast<uint64_t>(p.each) * kSortThreads;
     return launch_cluster(p, plan.passes, shared_bytes(plan.bins()), s);
   }
