@@ -85,18 +85,22 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
 
 // ---- the gradient
 
-// Vectors of a token's row that a lane has, 32 vectors apart.
-constexpr int lane_vectors(int v) { return v >= 8 ? 1 : v == 4 ? 2 : 4; }
+// How a warp's lanes share a tile of columns.  Vectors of 8, 4, 2, 1 elements, 32 vectors apart; kOdd: rows that do not start on vectors'
+// boundaries, by the 16-byte granules around them.
+constexpr int kOdd = 0;
+constexpr int vector_of(int v) { return v == kOdd ? 1 : v; }
+constexpr int lane_vectors(int v) { return v == kOdd ? 12 : v >= 8 ? 1 : v == 4 ? 2 : 4; }
+constexpr int tile_width(int v) { return 32 * vector_of(v) * lane_vectors(v); }
 // The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns; a multiple of what a CTA has.
 constexpr uint32_t kSumWarps = 8;
-constexpr uint32_t kRangeWarps = kSms * 48;  // ranges times column tiles, about
-constexpr uint32_t kLeastRange = 16;
-inline uint32_t column_tiles(uint64_t dim, int v) {
-  const uint64_t width = 32 * v * lane_vectors(v);
-  return static_cast<uint32_t>((dim + width - 1) / width);
-}
-inline uint32_t ranges_of(uint64_t n, uint32_t tiles) {
-  const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = (kRangeWarps + tiles - 1) / tiles;
+// Ranges times column tiles, about.  A range has its fixed cost (the tokens at its borders, its part), some 5 us; one wave of them is best where
+// a token costs little of a warp's time, three where rows' writes are spread unevenly.  GB300, per SM 16, 24, 32, 48, 72 warps, us: 500,001 tokens
+// x 321 fp32 155, 159, 173, 182, 215; 32,768 x 768 accumulating 45.6, 48.3, 48.0, 48.5, 48.0; 65,536 x 4,096 137, 153, -, 129, 129.
+constexpr uint32_t kFewRangeWarps = kSms * 16, kRangeWarps = kSms * 48;
+constexpr uint32_t kLeastRange = 32;
+inline uint32_t column_tiles(uint64_t dim, int v) { return static_cast<uint32_t>((dim + tile_width(v) - 1) / tile_width(v)); }
+inline uint32_t ranges_of(uint64_t n, uint32_t tiles, bool few) {
+  const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = ((few ? kFewRangeWarps : kRangeWarps) + tiles - 1) / tiles;
   return static_cast<uint32_t>(((most < fill ? most : fill) + kSumWarps - 1) / kSumWarps * kSumWarps);
 }
 struct SumParams {
@@ -113,9 +117,11 @@ struct SumParams {
   uint32_t sum_ctas, zero_ctas;
   uint32_t rows_per_zero_warp;
   uint32_t accumulate;
+  uint32_t configure;  // 1: no launch, the kernel's shared-memory size is set
   uint32_t bf16_out, bf16_grad;
   int v;
 };
+cudaError_t configure_sum();
 cudaError_t launch_sum(const SumParams& p, cudaStream_t s);
 
 }  // namespace frk

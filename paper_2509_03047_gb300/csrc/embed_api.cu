@@ -32,14 +32,17 @@ bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) %
 bool is_float(uint32_t dtype) { return dtype == FR_DT_BF16 || dtype == FR_DT_F32; }
 uint32_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
 
+// Rows of odd length up to this go element by element, a lane's four at most.
+constexpr uint64_t kOddLeast = 128;
+
 constexpr uint64_t kMostRows = (1ull << 31) - 1, kMostDim = 1ull << 20, kMostElems = 1ull << 40, kMostFirst = 1ull << 62;
 
 fr_status fill_embed(fr_embed p) {
   PlanMemory mem;
   const uint64_t n = p->max_tokens;
   uint64_t elems = 0;
-  for (int v = 1; v <= 8; v *= 2) {
-    const uint64_t ranges = ranges_of(n, column_tiles(p->dim, v));
+  for (int v : {kOdd, 1, 2, 4, 8}) {
+    const uint64_t ranges = ranges_of(n, column_tiles(p->dim, v), false);
     p->ranges = std::max(p->ranges, ranges);
   }
   elems = 2 * (p->ranges / kSumWarps) * p->dim;
@@ -53,7 +56,8 @@ fr_status fill_embed(fr_embed p) {
   cudaError_t e = mem.commit(&p->d_memory);
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   e = configure_sort();
-  return e == cudaSuccess ? FR_OK : report_cuda("shared memory of the sort", e);
+  if (e == cudaSuccess) e = configure_sum();
+  return e == cudaSuccess ? FR_OK : report_cuda("shared memory of the gradient's kernels", e);
 }
 
 // What both calls ask of their arguments.
@@ -185,8 +189,9 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.rows = p->rows;
   q.scale = scale;
   q.v = vector_elems(p->dim, out, type_bytes(out_dtype), grad, type_bytes(grad_dtype));
+  if (q.v == 1 && p->dim > kOddLeast) q.v = kOdd;
   q.tiles = column_tiles(p->dim, q.v);
-  q.ranges = std::max(kSumWarps, ranges_of(n, q.tiles));
+  q.ranges = std::max(kSumWarps, ranges_of(n, q.tiles, q.v == kOdd || accumulate));
   q.sum_ctas = n == 0 ? 0 : q.ranges / kSumWarps * q.tiles;
   if (!accumulate) {
     // about 64 KiB per warp

@@ -106,18 +106,68 @@ __device__ __forceinline__ void clear_rows(const SumParams& p, uint32_t found, u
   }
 }
 
-// Tokens whose vectors are on their way together: what 32 registers hold of them and, where they are added to, of the rows.
-constexpr int tokens_ahead(int elems, bool bf16_out, bool bf16_grad, bool add) {
-  const int words = (elems * (bf16_out ? 2 : 4) + (add ? elems * (bf16_grad ? 2 : 4) : 0) + 3) / 4;
-  return 32 / words >= 8 ? 8 : 32 / words >= 4 ? 4 : 2;
-}
+// A warp's ring in shared memory: the tokens whose vectors, and where they are added to, rows, are on their way.  kRing: tokens, in four
+// batches, three of them under way while one is added.  A lane copies what it reads, or with kOdd the warp the granules around a tile's row.
+template <int Kind, bool Bf16Out, bool Bf16Grad, bool Add>
+struct Ring {
+  static constexpr int V = vector_of(Kind), kVectors = lane_vectors(Kind), kWidth = tile_width(Kind);
+  static constexpr int kSpare = Kind == kOdd ? 16 : 0;
+  static constexpr int kIn = kWidth * (Bf16Out ? 2 : 4) + kSpare, kOld = Add ? kWidth * (Bf16Grad ? 2 : 4) + kSpare : 0;
+  static constexpr int kMost = Kind == kOdd ? 13 << 10 : Add ? 6 << 10 : 8 << 10;
+  static constexpr int kRing = 16 * (kIn + kOld) <= kMost ? 16 : 8 * (kIn + kOld) <= kMost ? 8 : 4, kBatch = kRing / 4;
+  static constexpr int kBytes = kRing * (kIn + kOld);
+  // a CTA's, and what its warps hand on
+  static constexpr int kParts = 2 * kSumWarps * kWidth * 4;
+  static constexpr int kShared = kSumWarps * kBytes > kParts ? kSumWarps * kBytes : kParts;
+  uint8_t* at;
+  uint32_t lane;
+  uint64_t first, dim;  // column of the tile, columns of a row
 
-template <int V, bool Bf16Out, bool Bf16Grad, bool Add>
-__global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant__ SumParams p) {
-  constexpr int kVectors = lane_vectors(V), kWidth = 32 * V * kVectors;
-  constexpr int kAhead = tokens_ahead(V * kVectors, Bf16Out, Bf16Grad, Add);
-  // What each warp has of the row that it starts in, if that ends there, and of the one that goes on after it.
-  __shared__ float heads[kSumWarps][kWidth], tails[kSumWarps][kWidth];
+  __device__ __forceinline__ uint64_t column(int c) const { return first + (c * 32 + lane) * V; }
+  __device__ __forceinline__ bool mine(int c) const { return column(c) < dim; }
+  __device__ __forceinline__ uint8_t* in_slot(uint32_t token) const { return at + token % kRing * kIn; }
+  __device__ __forceinline__ uint8_t* old_slot(uint32_t token) const { return at + kRing * kIn + token % kRing * kOld; }
+
+  template <bool Bf16>
+  __device__ __forceinline__ void copy(uint8_t* slot, const void* base, uint64_t row) const {
+    constexpr int kSize = Bf16 ? 2 : 4;
+    if constexpr (Kind == kOdd) {
+      const uint64_t from = reinterpret_cast<uint64_t>(base) + (row * dim + first) * kSize;
+      const uint32_t end = (static_cast<uint32_t>(from) & 15) + static_cast<uint32_t>(min(static_cast<uint64_t>(kWidth), dim - first)) * kSize;
+      const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slot)) + lane * 16;
+      const uint8_t* const begin = reinterpret_cast<const uint8_t*>(from & ~15ull) + lane * 16;
+#pragma unroll
+      for (int k = 0; k < (kWidth * kSize + 16 + 511) / 512; ++k)
+        if (lane * 16 + k * 512 < end) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + k * 512), "l"(begin + k * 512) : "memory");
+    } else {
+#pragma unroll
+      for (int c = 0; c < kVectors; ++c)
+        if (mine(c)) Raw<V, Bf16>::copy(slot + (c * 32 + lane) * V * kSize, base, row * dim + column(c));
+    }
+  }
+  template <bool Bf16>
+  __device__ __forceinline__ Raw<V, Bf16> get(const uint8_t* slot, const void* base, uint64_t row, int c) const {
+    constexpr int kSize = Bf16 ? 2 : 4;
+    // (where it starts in its granule: of the address's low bits alone)
+    const uint32_t shift =
+        Kind == kOdd ? (static_cast<uint32_t>(reinterpret_cast<uint64_t>(base)) + (static_cast<uint32_t>(row) * static_cast<uint32_t>(dim) + static_cast<uint32_t>(first)) * kSize) & 15u : 0;
+    Raw<V, Bf16> r;
+    r.load(slot + shift + (c * 32 + lane) * V * kSize, 0);
+    return r;
+  }
+  // Other lanes' copies, and reads before the next copies.
+  __device__ __forceinline__ void together() const {
+    if constexpr (Kind == kOdd) __syncwarp();
+  }
+};
+
+template <int Kind, bool Bf16Out, bool Bf16Grad, bool Add>
+__global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ SumParams p) {
+  using R = Ring<Kind, Bf16Out, Bf16Grad, Add>;
+  constexpr int V = R::V, kVectors = R::kVectors, kWidth = R::kWidth, kBatch = R::kBatch;
+  extern __shared__ __align__(16) uint8_t raw[];
+  // What each warp has of the row that it starts in, if that ends there, and of the one that goes on after it: in the ring's place, after it.
+  auto heads = reinterpret_cast<float(*)[kWidth]>(raw), tails = heads + kSumWarps;
   __shared__ uint32_t ended[kSumWarps], from_inside[kSumWarps], to_inside[kSumWarps];
   wait_for_kernel_before();
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, found = *p.found;
@@ -128,58 +178,65 @@ __global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant_
   const uint32_t span = span_of(found, p.ranges), cta = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
   const uint64_t b = (static_cast<uint64_t>(cta) * kSumWarps + warp) * span;
   const Border from = border(p.sorted, found, span, b, lane), to = border(p.sorted, found, span, b + span, lane);
-  const uint64_t first = static_cast<uint64_t>(tile) * kWidth + lane * V;
-  auto column = [&](int c) { return first + c * (32 * V); };
-  auto mine = [&](int c) { return column(c) < p.dim; };
   auto place = [&](int c, int j) { return (c * V + j) * 32 + lane; };
+  const R ring = {raw + warp * R::kBytes, lane, static_cast<uint64_t>(tile) * kWidth, p.dim};
   bool head = from.inside;  // the row at hand started in a range before
   uint32_t head_row = kAll;
-  float sum[kVectors][V] = {};
-  // (the next 32 tokens are on their way while these are added)
-  auto tokens = [&](uint32_t i) { return i < to.at ? p.sorted[i] : Met{kAll, 0}; };
-  auto row_after = [&](uint32_t i) { return i + 1 < found && i < to.at ? p.sorted[i + 1].row : kAll; };
-  Met m = tokens(from.at + lane);
-  uint32_t after = row_after(from.at + lane);
-  for (uint32_t i = from.at; i < to.at; i += 32) {
-    const uint32_t here = min(to.at - i, 32u);
-    const uint32_t ends = __ballot_sync(kAll, lane < here && m.row != after);
-    const Met now = m;
-    m = tokens(i + 32 + lane);
-    after = row_after(i + 32 + lane);
-    for (uint32_t k = 0; k < here; k += kAhead) {
-      Raw<V, Bf16Out> in[kAhead][kVectors];
-      Raw<V, Bf16Grad> old[Add ? kAhead : 1][kVectors];
+  float sum[kVectors][V] = {}, head_sum[kVectors][V] = {};
+  // 32 tokens, those after them, and on their way the next ones
+  struct Group {
+    Met m;
+    uint32_t after;
+  };
+  auto fetch = [&](uint32_t i) {
+    i += lane;
+    return Group{i < to.at ? p.sorted[i] : Met{kAll, 0}, i + 1 < found && i < to.at ? p.sorted[i + 1].row : kAll};
+  };
+  auto ends_of = [&](const Group& g) { return __ballot_sync(kAll, g.m.row != kAll && g.m.row != g.after); };
+  const uint32_t count = to.at - from.at;
+  Group now = fetch(from.at), next = fetch(from.at + 32), later = fetch(from.at + 64);
+  uint32_t ends = ends_of(now), next_ends = ends_of(next);
+  // the copies of batch k + ... of this group, or the next
+  auto issue = [&](uint32_t base, uint32_t k) {
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        const uint64_t at = static_cast<uint64_t>(__shfl_sync(kAll, now.at, k + u)) * p.dim;
-        const uint64_t row = Add ? static_cast<uint64_t>(__shfl_sync(kAll, now.row, k + u)) * p.dim : 0;
-        if (k + u >= here) continue;
+    for (int u = 0; u < kBatch; ++u) {
+      const uint32_t j = k + u, i = j % 32;
+      const uint32_t token = __shfl_sync(kAll, j < 32 ? now.m.at : next.m.at, i);
+      const uint32_t row = Add ? __shfl_sync(kAll, j < 32 ? now.m.row : next.m.row, i) : 0;
+      if (base + j >= count) continue;
+      ring.template copy<Bf16Out>(ring.in_slot(base + j), p.out, token);
+      if (Add && (j < 32 ? ends : next_ends) >> i & 1) ring.template copy<Bf16Grad>(ring.old_slot(base + j), p.grad, row);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  for (int k = 0; k < 3; ++k) issue(0, k * kBatch);
+  for (uint32_t base = 0; base < count; base += 32) {
+    for (uint32_t k = 0; k < 32 && base + k < count; k += kBatch) {
+      ring.together();
+      issue(base, k + 3 * kBatch);
+      asm volatile("cp.async.wait_group 3;" ::: "memory");
+      ring.together();
 #pragma unroll
-        for (int c = 0; c < kVectors; ++c)
-          if (mine(c)) in[u][c].load(p.out, at + column(c));
-        if (!Add || !(ends >> (k + u) & 1)) continue;
-#pragma unroll
-        for (int c = 0; c < kVectors; ++c)
-          if (mine(c)) old[u][c].load(p.grad, row + column(c));
-      }
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) {
-        if (k + u >= here) break;
+      for (int u = 0; u < kBatch; ++u) {
+        if (base + k + u >= count) break;
+        const uint32_t token = Kind == kOdd ? __shfl_sync(kAll, now.m.at, k + u) : 0;
 #pragma unroll
         for (int c = 0; c < kVectors; ++c) {
           float x[V];
-          in[u][c].get(x);
+          ring.template get<Bf16Out>(ring.in_slot(base + k + u), p.out, token, c).get(x);
           add(sum[c], x);
         }
         if (!(ends >> (k + u) & 1)) continue;
-        const uint32_t row = __shfl_sync(kAll, now.row, k + u);
+        const uint32_t row = __shfl_sync(kAll, now.m.row, k + u);
 #pragma unroll
         for (int c = 0; c < kVectors; ++c) {
           if (head) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) heads[warp][place(c, j)] = sum[c][j];
-          } else if (mine(c)) {
-            finish<V, Bf16Grad, Add>(p.grad, static_cast<uint64_t>(row) * p.dim + column(c), p.scale, sum[c], old[Add ? u : 0][c]);
+            for (int j = 0; j < V; ++j) head_sum[c][j] = sum[c][j];
+          } else if (ring.mine(c)) {
+            Raw<V, Bf16Grad> old;
+            if (Add) old = ring.template get<Bf16Grad>(ring.old_slot(base + k + u), p.grad, row, c);
+            finish<V, Bf16Grad, Add>(p.grad, row * p.dim + ring.column(c), p.scale, sum[c], old);
           }
 #pragma unroll
           for (int j = 0; j < V; ++j) sum[c][j] = 0.0f;
@@ -188,6 +245,19 @@ __global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant_
         head = false;
       }
     }
+    now = next;
+    next = later;
+    later = fetch(from.at + base + 96);
+    ends = next_ends;
+    next_ends = ends_of(next);
+  }
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  __syncthreads();
+  if (from.inside && !head) {
+#pragma unroll
+    for (int c = 0; c < kVectors; ++c)
+#pragma unroll
+      for (int j = 0; j < V; ++j) heads[warp][place(c, j)] = head_sum[c][j];
   }
   if (to.inside) {
 #pragma unroll
@@ -221,16 +291,16 @@ __global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant_
       if (end == 0)
 #pragma unroll
         for (int j = 0; j < V; ++j) total[j] = __fadd_rn(total[j], heads[warp][place(c, j)]);
-      if (!mine(c)) continue;
+      if (!ring.mine(c)) continue;
       if (end == 0 && !before) {
-        const uint64_t at = static_cast<uint64_t>(head_row) * p.dim + column(c);
+        const uint64_t at = static_cast<uint64_t>(head_row) * p.dim + ring.column(c);
         Raw<V, Bf16Grad> old;
         if (Add) old.load(p.grad, at);
         finish<V, Bf16Grad, Add>(p.grad, at, p.scale, total, old);
       } else {
         Raw<V, false> part;
         part.set(total);
-        part.store(p.parts, (2ull * cta + !before) * p.dim + column(c));
+        part.store(p.parts, (2ull * cta + !before) * p.dim + ring.column(c));
       }
     }
     if (end == 1 && !before && tile == 0 && lane == 0) p.longs[atomicAdd(p.n_long, 1u)] = cta;
@@ -239,9 +309,9 @@ __global__ void __launch_bounds__(kThreads, 3) sum_kernel(const __grid_constant_
 
 // A long row's parts: the second of the CTA where it begins, the first of the CTAs after it that begin inside it.  (The list's order is any;
 // each row has its place.)
-template <int V, bool Bf16Grad, bool Add>
+template <int Kind, bool Bf16Grad, bool Add>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ SumParams p) {
-  constexpr int kVectors = lane_vectors(V), kWarps = kJoinThreads / 32, kWidth = 32 * V * kVectors;
+  constexpr int V = vector_of(Kind), kVectors = lane_vectors(Kind), kWarps = kJoinThreads / 32, kWidth = tile_width(Kind);
   __shared__ float sums[kWarps][kWidth];
   wait_for_kernel_before();
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -277,13 +347,13 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
 #pragma unroll
       for (int j = 0; j < V; ++j) sums[warp][(c * V + j) * 32 + lane] = sum[c][j];
     __syncthreads();
-    if (warp < kVectors) {  // a vector of columns each
-      const uint64_t column = first + (warp * 32 + lane) * V;
+    for (int c = warp; c < kVectors; c += kWarps) {  // a vector of columns each
+      const uint64_t column = first + (c * 32 + lane) * V;
       if (column < p.dim) {
         float total[V] = {};
         for (int w = 0; w < kWarps; ++w)
 #pragma unroll
-          for (int j = 0; j < V; ++j) total[j] = __fadd_rn(total[j], sums[w][(warp * V + j) * 32 + lane]);
+          for (int j = 0; j < V; ++j) total[j] = __fadd_rn(total[j], sums[w][(c * V + j) * 32 + lane]);
         Raw<V, Bf16Grad> old;
         if (Add) old.load(p.grad, row * p.dim + column);
         finish<V, Bf16Grad, Add>(p.grad, row * p.dim + column, p.scale, total, old);
@@ -293,29 +363,46 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
   }
 }
 
-template <int V, bool Bf16Out, bool Bf16Grad, bool Add>
+template <int Kind, bool Bf16Out, bool Bf16Grad, bool Add>
 cudaError_t launch(const SumParams& p, cudaStream_t s) {
-  cudaError_t e = launch_chained(sum_kernel<V, Bf16Out, Bf16Grad, Add>, static_cast<int>(p.sum_ctas + p.zero_ctas), kThreads, 0, s, p);
-  if (e == cudaSuccess) e = launch_chained(join_kernel<V, Bf16Grad, Add>, static_cast<int>(kSms * 2), kJoinThreads, 0, s, p);
+  constexpr int kShared = Ring<Kind, Bf16Out, Bf16Grad, Add>::kShared;
+  if (p.configure) return cudaFuncSetAttribute(sum_kernel<Kind, Bf16Out, Bf16Grad, Add>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+  cudaError_t e = launch_chained(sum_kernel<Kind, Bf16Out, Bf16Grad, Add>, static_cast<int>(p.sum_ctas + p.zero_ctas), kThreads, kShared, s, p);
+  if (e == cudaSuccess) e = launch_chained(join_kernel<Kind, Bf16Grad, Add>, static_cast<int>(kSms * 2), kJoinThreads, 0, s, p);
   return e;
 }
-template <int V, bool Bf16Out>
+template <int Kind, bool Bf16Out>
 cudaError_t launch_typed(const SumParams& p, cudaStream_t s) {
-  if (p.accumulate) return p.bf16_grad ? launch<V, Bf16Out, true, true>(p, s) : launch<V, Bf16Out, false, true>(p, s);
-  return p.bf16_grad ? launch<V, Bf16Out, true, false>(p, s) : launch<V, Bf16Out, false, false>(p, s);
+  if (p.accumulate) return p.bf16_grad ? launch<Kind, Bf16Out, true, true>(p, s) : launch<Kind, Bf16Out, false, true>(p, s);
+  return p.bf16_grad ? launch<Kind, Bf16Out, true, false>(p, s) : launch<Kind, Bf16Out, false, false>(p, s);
 }
-template <int V>
+template <int Kind>
 cudaError_t launch_wide(const SumParams& p, cudaStream_t s) {
-  return p.bf16_out ? launch_typed<V, true>(p, s) : launch_typed<V, false>(p, s);
+  return p.bf16_out ? launch_typed<Kind, true>(p, s) : launch_typed<Kind, false>(p, s);
 }
 
 }  // namespace
+
+cudaError_t configure_sum() {
+  SumParams p = {};
+  p.configure = 1;
+  for (int k = 0; k < 40; ++k) {
+    p.v = k / 8 == 4 ? kOdd : 1 << k / 8;
+    p.bf16_out = k & 1;
+    p.bf16_grad = k >> 1 & 1;
+    p.accumulate = k >> 2 & 1;
+    const cudaError_t e = launch_sum(p, nullptr);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
 
 cudaError_t launch_sum(const SumParams& p, cudaStream_t s) {
   switch (p.v) {
     case 8: return launch_wide<8>(p, s);
     case 4: return launch_wide<4>(p, s);
     case 2: return launch_wide<2>(p, s);
+    case kOdd: return launch_wide<kOdd>(p, s);
     default: return launch_wide<1>(p, s);
   }
 }

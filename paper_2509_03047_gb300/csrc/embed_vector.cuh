@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 
 #include <cstdint>
+#include <cstring>
 
 namespace frk {
 
@@ -28,6 +29,21 @@ struct Raw {
     const T* at = reinterpret_cast<const T*>(static_cast<const uint8_t*>(base) + element * (Bf16 ? 2 : 4));
 #pragma unroll
     for (int k = 0; k < kPieces; ++k) w[k] = at[k];
+  }
+  // To shared memory, asynchronously where a piece has four bytes or more.
+  static __device__ __forceinline__ void copy(void* shared, const void* base, uint64_t element) {
+    const T* at = reinterpret_cast<const T*>(static_cast<const uint8_t*>(base) + element * (Bf16 ? 2 : 4));
+    T* const to = static_cast<T*>(shared);
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(to + k));
+      if constexpr (kPiece == 16)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(a), "l"(at + k) : "memory");
+      else if constexpr (kPiece >= 4)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(a), "l"(at + k), "n"(kPiece) : "memory");
+      else
+        to[k] = at[k];
+    }
   }
   __device__ __forceinline__ void store(void* base, uint64_t element) const {
     T* at = reinterpret_cast<T*>(static_cast<uint8_t*>(base) + element * (Bf16 ? 2 : 4));
