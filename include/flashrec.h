@@ -515,12 +515,15 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  * (for more rows than columns with X^T X on the other side: the same matrix).
  * A zero matrix gives zeros, one with an Inf or NaN NaNs everywhere.
  *
- * Precision.  X is held as two fp16 numbers, 22 bits, and enters the products by
- * the first, as X X^T and the polynomial of it do by their roundings to fp16 (each
- * scaled so that fp16 holds it; sums in fp32).  The rounding of X alone would grow
- * with every iteration, by a, in the parts of small singular values.  With the usual coefficients
- * and 5 iterations O is off by 0.1 to 0.2% (2-norm over 2-norm) for any spectrum,
- * by up to 0.5% where a side has fewer than 16 elements.
+ * Precision.  All factors of the products are fp16 numbers, scaled so that fp16 holds
+ * them, their sums in fp32.  A matrix with an fp32 output (weight, master or update)
+ * has each factor as two of them, 22 bits, and three products for one: O is off by some
+ * 2^-19 (2-norm over 2-norm).  Others, and with FR_MUON_ONE all, enter X, X X^T and the
+ * polynomial in it by one rounding each: with the usual coefficients and 5 iterations O is
+ * off by 0.1 to 0.2% for any spectrum, by up to 0.5% where a side has fewer than 16 elements, less
+ * than a bf16 output's own rounding (0.4% at most).  (The rounding of X
+ * alone would grow with every iteration, by a, in the parts of small singular values:
+ * what it leaves is kept, and added to the product as it is.)
  *
  * One fr_muon_tensor is one matrix, rows * cols elements, row after row, in each
  * of its buffers.  fr_muon_step needs the weights, gradients and momenta,
@@ -545,8 +548,9 @@ typedef struct fr_muon_plan_s* fr_muon_plan;
 /* Plan over `n_tensors` matrices (host array, copied; one without elements is
  * allowed).  As with fr_opt_create the plan is bound to the current device and the
  * buffers' addresses, allocates here and nowhere else, and one stream at a time
- * may use it.  Its device memory: about 6 bytes per element and 4 per element of a square
- * of the smaller side, sides rounded up to multiples of 128.
+ * may use it.  Its device memory: about 6 bytes per element (8 with
+ * an fp32 output) and 4 (8) per element of a square of the smaller side, sides rounded up to
+ * multiples of 128.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT, FR_ERR_CUDA. */
 fr_status fr_muon_create(const fr_muon_tensor* tensors, uint64_t n_tensors, fr_muon_plan* out);
 
@@ -558,6 +562,9 @@ void fr_muon_destroy(fr_muon_plan plan);
 
 #define FR_MUON_MOST 10            /* iterations */
 #define FR_MUON_MOST_SIDE (1u << 20) /* rows, columns */
+
+/* Products of both halves for matrices with fp32 outputs, or of one for all. */
+typedef enum { FR_MUON_BY_TYPE = 0, FR_MUON_ONE = 1 } fr_muon_products;
 
 /* One step's numbers.  lr, weight_decay and their products with the factors as in
  * fr_adamw; 0 <= beta < 1; 1 to FR_MUON_MOST iterations with their (a, b, c),
@@ -571,7 +578,7 @@ typedef struct {
   uint32_t iterations;
   uint32_t nesterov;    /* 0 or 1 */
   uint32_t rounding;    /* fr_rounding, of bf16 weights without masters */
-  uint32_t reserved;    /* 0 */
+  uint32_t products;    /* fr_muon_products */
 } fr_muon;
 
 /* The step, per matrix with h = scale * gradient:

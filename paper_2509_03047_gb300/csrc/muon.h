@@ -8,8 +8,12 @@
 // from shared memory, with the row as the contraction's index or the column, so a
 // block goes there as it is and serves X X^T, X^T X, and products from
 // either side without a transposition.  The square matrices of the smaller side,
-// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike.  A plan's workspace
-// has all matrices' x[0], then all x[1], all second halves, all P, all S, in the same order.
+// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike. 
+//
+// A matrix with an fp32 output (split) has second halves of everything, in blocks like
+// the first ones, which enter the products too.  Its part of the workspace is apart:
+// all x[0], x[1], second halves of either, P, S, second halves of either; the others'
+// x[0], x[1], second halves, P, S.
 //
 // Scales: X 2^14, S 2^13, P 2^11, so that fp16 holds what the bounds on the
 // polynomials (flashrec.h) allow: |X| <= 2, |S| <= 4, |P| <= 16 in the spectral
@@ -38,7 +42,7 @@ struct MuonDesc {        // one matrix that has elements
   void* update;
   uint64_t rows, cols;
   uint64_t x[2];         // bytes in the workspace: the iterate's first halves, old and new
-  uint64_t low;          // its second halves
+  uint64_t low[2];       // its second halves (split: a place for each, else one)
   uint64_t s, p;
   uint32_t row_blocks, col_blocks;  // of 128 rows, of 64 columns (an even number)
   uint32_t side_blocks;  // of 128, of the smaller side
@@ -47,6 +51,7 @@ struct MuonDesc {        // one matrix that has elements
   uint32_t first_block;  // of all blocks of the plan's iterates
   uint32_t tensor;       // index in the plan
   uint32_t bf16_weight, bf16_grad, bf16_update;
+  uint32_t split;        // products of both halves
   float lr_scale, decay_scale, update_scale;
 };
 
@@ -83,6 +88,7 @@ struct MuonParams {
   uint64_t key;            // as in StepParams
   uint32_t last;           // which of x[] holds the last iterate
   uint32_t low;            // 1: the first iterate has second halves
+  uint32_t one;            // 1: products of first halves for all
   uint32_t* done;          // the products' counters, set to zero
 };
 cudaError_t launch_muon_norm(const MuonParams& p, cudaStream_t s);
@@ -131,8 +137,9 @@ struct MuonProduct {
   const fr_clip* clip;
   uint32_t* status;         // set to 1 by a kernel that gave up a wait
   uint32_t* done;           // counters, zero at the start
-  uint32_t x_blocks;        // of all iterates: from x[0] to x[1] and to the second halves
-  uint32_t p_blocks;        // from P to S
+  uint32_t x_blocks;        // of all iterates: from x[0] to x[1], from either to its second halves twice as far
+  uint32_t p_blocks;        // from P to S, the same
+  uint32_t split;
   float coef[FR_MUON_MOST][3];
   uint32_t low;             // bit i: the iterate before iteration i has second halves
   uint32_t waits;           // 1: tiles of several phases

@@ -24,14 +24,16 @@ struct fr_muon_plan_s {
   uint64_t n_tensors = 0, n_elems = 0, device_bytes = 0;
   bool params = true, updates = true;       // every matrix with elements has what the step, fr_orthogonalize needs
   float most_lr = 0.0f, most_decay = 0.0f;  // the largest |lr_scale| and |decay_scale|
-  uint64_t x_blocks = 0, p_blocks = 0;      // of all iterates, all squares
-  uint32_t n_units = 0, n_blocks = 0;
-  uint32_t ends[kPhases] = {};               // of each phase's tiles
-  uint32_t pairs = 0, most_tiles = 0;        // CTAs that are resident, two each; the most tiles of a phase
+  uint32_t n_units = 0, n_blocks = 0, pairs = 0;  // pairs of CTAs that are resident together
+  struct Part {                              // the matrices that are not split, and those that are
+    uint64_t x_blocks = 0, p_blocks = 0;     // of all iterates, all squares
+    uint32_t ends[kPhases] = {};             // of each phase's tiles
+    uint32_t most_tiles = 0;                 // of a phase
+    MuonTile* d_tiles = nullptr;
+  } parts[2];
   MuonDesc* d_tensors = nullptr;
   uint32_t* d_units = nullptr;
   uint32_t* d_blocks = nullptr;
-  MuonTile* d_tiles = nullptr;
   uint32_t* d_done = nullptr;
   MuonPartial* d_partials = nullptr;
   MuonNorm* d_norms = nullptr;
@@ -84,6 +86,7 @@ MuonDesc describe(const fr_muon_tensor& x, uint64_t index) {
   d.bf16_weight = x.weight && x.weight_dtype == FR_DT_BF16;
   d.bf16_grad = x.grad && x.grad_dtype == FR_DT_BF16;
   d.bf16_update = x.update && x.update_dtype == FR_DT_BF16;
+  d.split = x.master || (x.weight && !d.bf16_weight) || (x.update && !d.bf16_update);
   d.lr_scale = x.lr_scale;
   d.decay_scale = x.decay_scale;
   d.update_scale = x.update_scale;
@@ -112,7 +115,6 @@ cudaError_t make_maps(MuonMaps* maps, void* at, uint64_t bytes) {
 fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_tensors) {
   std::vector<MuonDesc> descs;
   std::vector<uint32_t> units, blocks;
-  std::vector<MuonTile> tiles;
   p->n_tensors = n_tensors;
   for (uint64_t t = 0; t < n_tensors; ++t) {
     const fr_muon_tensor& x = tensors[t];
@@ -124,10 +126,11 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     p->most_decay = std::max(p->most_decay, std::fabs(x.decay_scale));
     MuonDesc d = describe(x, t);
     const uint64_t n = static_cast<uint64_t>(d.row_blocks) * d.col_blocks;
-    d.x[0] = p->x_blocks * kBlockBytes;
-    d.p = p->p_blocks * kBlockBytes;
-    p->x_blocks += n;
-    p->p_blocks += square_blocks(d);
+    auto& part = p->parts[d.split];
+    d.x[0] = part.x_blocks * kBlockBytes;
+    d.p = part.p_blocks * kBlockBytes;
+    part.x_blocks += n;
+    part.p_blocks += square_blocks(d);
     d.first_unit = static_cast<uint32_t>(units.size());
     d.first_block = static_cast<uint32_t>(blocks.size());
     const uint32_t me = static_cast<uint32_t>(descs.size());
@@ -135,20 +138,32 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     blocks.insert(blocks.end(), n, me);
     descs.push_back(d);
   }
-  const uint64_t x_bytes = p->x_blocks * kBlockBytes, p_bytes = p->p_blocks * kBlockBytes, bytes = 3 * x_bytes + 2 * p_bytes;
-  for (MuonDesc& d : descs) {
-    d.x[1] = d.x[0] + x_bytes;
-    d.low = d.x[1] + x_bytes;
-    d.p += 3 * x_bytes;
-    d.s = d.p + p_bytes;
+  uint64_t bytes = 0;
+  for (uint32_t k = 0; k < 2; ++k) {
+    const auto& part = p->parts[k];
+    const uint64_t x_bytes = part.x_blocks * kBlockBytes, p_bytes = part.p_blocks * kBlockBytes;
+    for (MuonDesc& d : descs) {
+      if (d.split != k) continue;
+      d.x[0] += bytes;
+      d.x[1] = d.x[0] + x_bytes;
+      d.low[0] = d.x[1] + x_bytes;
+      d.low[1] = d.low[0] + (k ? x_bytes : 0);
+      d.p += bytes + (k ? 4 : 3) * x_bytes;
+      d.s = d.p + p_bytes;
+    }
+    bytes += k ? 4 * (x_bytes + p_bytes) : 3 * x_bytes + 2 * p_bytes;
   }
-  plan_tiles(descs, tiles, p->ends);
-  for (int k = 0; k < kPhases; ++k) p->most_tiles = std::max(p->most_tiles, p->ends[k] - (k ? p->ends[k - 1] : 0));
   PlanMemory mem;
   mem.table(&p->d_tensors, descs);
   mem.table(&p->d_units, units);
   mem.table(&p->d_blocks, blocks);
-  mem.table(&p->d_tiles, tiles);
+  for (uint32_t k = 0; k < 2; ++k) {
+    auto& part = p->parts[k];
+    std::vector<MuonTile> tiles;
+    plan_tiles(descs, k != 0, tiles, part.ends);
+    for (int phase = 0; phase < kPhases; ++phase) part.most_tiles = std::max(part.most_tiles, part.ends[phase] - (phase ? part.ends[phase - 1] : 0));
+    mem.table(&part.d_tiles, tiles);
+  }
   mem.scratch(&p->d_done, descs.size() * kPhases);
   mem.table(&p->d_norms, std::vector<MuonNorm>(descs.size(), MuonNorm{}));
   mem.scratch(&p->d_partials, units.size());
@@ -186,6 +201,7 @@ double most(F f, double top, double q2, double q1, double q0) {
 }
 
 const char* check_iterations(const fr_muon& h) {
+  if (h.products > FR_MUON_ONE) return "unknown choice of products";
   if (h.iterations < 1 || h.iterations > FR_MUON_MOST) return "iterations must be 1 to FR_MUON_MOST";
   double top = 1.0;
   for (uint32_t i = 0; i < h.iterations; ++i) {
@@ -209,6 +225,29 @@ const char* check_iterations(const fr_muon& h) {
 #endif
 constexpr uint32_t kTogether = FR_TOGETHER;
 
+cudaError_t launch_products(fr_muon_plan p, const fr_muon& h, MuonProduct q, const fr_muon_plan_s::Part& part, cudaStream_t s) {
+  q.x_blocks = static_cast<uint32_t>(part.x_blocks);
+  q.p_blocks = static_cast<uint32_t>(part.p_blocks);
+  if (part.most_tiles <= kTogether * p->pairs) {
+    q.tiles = part.d_tiles;
+    q.n_tiles = part.ends[kPhases - 1];
+    q.iterations = h.iterations;
+    q.waits = 1;
+    return launch_muon_product(q, p->maps, std::min(p->pairs, part.most_tiles), s);
+  }
+  for (q.first = 0; q.first < h.iterations; ++q.first) {
+    q.iterations = q.first + 1;
+    for (int phase = 0; phase < kPhases; ++phase) {
+      const uint32_t begin = phase ? part.ends[phase - 1] : 0;
+      q.tiles = part.d_tiles + begin;
+      q.n_tiles = part.ends[phase] - begin;
+      const cudaError_t e = launch_muon_product(q, p->maps, p->pairs, s);
+      if (e != cudaSuccess) return e;
+    }
+  }
+  return cudaSuccess;
+}
+
 // X through all iterations, in the plan's workspace.
 fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t s) {
   MuonProduct q = {};
@@ -216,9 +255,8 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   q.clip = mp.clip;
   q.status = p->d_status;
   q.done = p->d_done;
-  q.x_blocks = static_cast<uint32_t>(p->x_blocks);
-  q.p_blocks = static_cast<uint32_t>(p->p_blocks);
-  // An iterate keeps its second halves if the iterations after it raise small singular values, and a rounding among them, by more than 4.
+  // Of first halves alone: an iterate keeps its second ones if the iterations after it raise small singular values, and a rounding among them, by
+  // more than 4.
   double gain = 1.0;
   for (uint32_t i = h.iterations; i-- > 0;) {
     for (int j = 0; j < 3; ++j) q.coef[i][j] = static_cast<float>(h.coef[i][j]);
@@ -227,25 +265,13 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   }
   mp.low = q.low & 1;
   mp.last = h.iterations % 2;
+  mp.one = h.products == FR_MUON_ONE;
   cudaError_t e = launch_muon_norm(mp, s);
   if (e == cudaSuccess) e = launch_muon_iterate(mp, s);
   if (e != cudaSuccess) return report_cuda("element kernel launch", e);
-  if (p->most_tiles <= kTogether * p->pairs) {
-    q.tiles = p->d_tiles;
-    q.n_tiles = p->ends[kPhases - 1];
-    q.iterations = h.iterations;
-    q.waits = 1;
-    e = launch_muon_product(q, p->maps, std::min(p->pairs, p->most_tiles), s);
-    return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);
-  }
-  for (q.first = 0; q.first < h.iterations && e == cudaSuccess; ++q.first) {
-    q.iterations = q.first + 1;
-    for (int k = 0; k < kPhases && e == cudaSuccess; ++k) {
-      const uint32_t begin = k ? p->ends[k - 1] : 0;
-      q.tiles = p->d_tiles + begin;
-      q.n_tiles = p->ends[k] - begin;
-      e = launch_muon_product(q, p->maps, p->pairs, s);
-    }
+  for (uint32_t k = 0; k < 2 && e == cudaSuccess; ++k) {
+    q.split = k && !mp.one;
+    if (p->parts[k].most_tiles > 0) e = launch_products(p, h, q, p->parts[k], s);
   }
   return e == cudaSuccess ? FR_OK : report_cuda("product kernel launch", e);
 }
@@ -344,7 +370,6 @@ fr_status fr_muon_step(fr_muon_plan p, const fr_muon* h, const fr_clip* clip_dev
   if (h->nesterov > 1) return report_invalid(me, "nesterov must be 0 or 1");
   if (h->step == 0) return report_invalid(me, "step counts from 1");
   if (h->rounding > FR_ROUND_RANDOM) return report_invalid(me, "unknown rounding");
-  if (h->reserved != 0) return report_invalid(me, "reserved must be 0");
   if (const char* what = check_iterations(*h)) return report_invalid(me, what);
   if (clip_dev != nullptr && !on(clip_dev, 8)) return report_invalid(me, "clip_dev is not 8-byte aligned");
   if (p->n_blocks == 0) return FR_OK;

@@ -17,6 +17,7 @@ namespace {
 constexpr int kWarps = kElementThreads / 32;
 
 __device__ __forceinline__ bool skipped(const MuonParams& p) { return p.clip != nullptr && p.clip->nonfinite != 0; }
+__device__ __forceinline__ bool is_split(const MuonParams& p, const MuonDesc& d) { return d.split && !p.one; }
 __device__ __forceinline__ float grad_scale(const MuonParams& p) { return p.clip != nullptr ? p.clip->scale : 1.0f; }
 
 // Eight consecutive elements of an fp32 or bf16 buffer from element i, `left` of them there; zeros after them.
@@ -206,13 +207,23 @@ __global__ void __launch_bounds__(kElementThreads) iterate_kernel(const __grid_c
     uint4 hi, lo;
     split(x, hi, lo);
     *reinterpret_cast<uint4*>(p.work + d.x[0] + chunk_at(d.col_blocks, r, at.chunk)) = hi;
-    if (p.low) *reinterpret_cast<uint4*>(p.work + d.low + low_at(d.col_blocks, r, at.chunk)) = lo;
+    if (is_split(p, d))
+      *reinterpret_cast<uint4*>(p.work + d.low[0] + chunk_at(d.col_blocks, r, at.chunk)) = lo;
+    else if (p.low)
+      *reinterpret_cast<uint4*>(p.work + d.low[0] + low_at(d.col_blocks, r, at.chunk)) = lo;
   }
 }
 
-// (the last iterate has no second halves)
+// (without products of them the last iterate has no second halves)
 __device__ __forceinline__ void last_iterate(const MuonParams& p, const MuonDesc& d, uint32_t r, uint32_t c, float (&o)[8]) {
-  floats(*reinterpret_cast<const uint4*>(p.work + d.x[p.last] + chunk_at(d.col_blocks, r, c)), o);
+  const uint64_t at = chunk_at(d.col_blocks, r, c);
+  floats(*reinterpret_cast<const uint4*>(p.work + d.x[p.last] + at), o);
+  if (is_split(p, d)) {
+    float lo[8];
+    floats(*reinterpret_cast<const uint4*>(p.work + d.low[p.last] + at), lo);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] += lo[j];
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) o[j] *= 1.0f / kScaleX;
 }

@@ -20,19 +20,24 @@ namespace frk {
 
 namespace {
 
-constexpr int kStages = 6;
 constexpr int kFactorBytes = 16384;  // 128 rows or columns of a factor, 64 of the contraction
 constexpr int kHalf = 8192;
-constexpr int kStageBytes = 2 * kFactorBytes;
+// The products of a step: first halves; or with second halves first times second and second times first as well, for 22 bits of each factor.
+template <bool kSplit>
+struct Stages {
+  static constexpr int kCount = kSplit ? 3 : 6, kBytes = (kSplit ? 4 : 2) * kFactorBytes;
+};
+constexpr int kRingBytes = 12 * kFactorBytes, kMostStages = 6;
+static_assert(Stages<true>::kCount * Stages<true>::kBytes == kRingBytes && Stages<false>::kCount * Stages<false>::kBytes == kRingBytes, "one size");
 constexpr int kWarps = 8;            // that turn sums into blocks: a quarter of the rows, every other 64 columns
 constexpr int kThreads = 64 + kWarps * 32;
 constexpr int kStaging = kBlockBytes / 4;  // per warp
 constexpr int kTensorColumns = 512;
-constexpr size_t kShared = 1024 + kStages * kStageBytes + kWarps * kStaging;
+constexpr size_t kShared = 1024 + kRingBytes + kWarps * kStaging;
 static_assert(kSignals == 2 * kWarps, "one per warp");
 
 struct Control {
-  uint64_t full[kStages], empty[kStages], sums_full[2], sums_empty[2];
+  uint64_t full[kMostStages], empty[kMostStages], sums_full[2], sums_empty[2];
   uint32_t tensor;
   uint32_t gave_up;
 };
@@ -76,18 +81,21 @@ struct Tiles {
 };
 
 // Where a stage and its phase stand.
+template <bool kSplit>
 struct Ring {
   uint32_t stage = 0, phase = 0;
   __device__ __forceinline__ void next() {
-    if (++stage == kStages) {
+    if (++stage == Stages<kSplit>::kCount) {
       stage = 0;
       phase ^= 1;
     }
   }
 };
 
+template <bool kSplit>
 __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps, uint32_t ring_at, Control& c, uint32_t rank) {
-  Ring r;
+  constexpr int kStageBytes = Stages<kSplit>::kBytes;
+  Ring<kSplit> r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]);
   for (Tiles tiles(p); tiles.take();) {
     const MuonTile& t = tiles.now;
@@ -97,7 +105,9 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
                static_cast<int32_t>(t.b_next), b_columns};
     const CUtensorMap *a_map = a_columns ? &maps.columns : &maps.rows, *b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
     if (p.waits && !__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
-    const uint32_t bytes = 2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes);
+    const uint32_t bytes = (kSplit ? 2 : 1) * (2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes));
+    const int32_t a_low = 2 * static_cast<int32_t>(t.flags & kAIterate ? p.x_blocks : p.p_blocks),
+                  b_low = 2 * static_cast<int32_t>(t.flags & kBIterate ? p.x_blocks : p.p_blocks);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
     for (uint32_t k = 0; k < t.depth; ++k) {
       if (k == t.a_switch) {
@@ -114,6 +124,10 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
         if (rank == 0) expect_bytes(full, bytes);
         load_blocks(to, a_map, a.half, a.block, full);
         load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
+        if (kSplit) {
+          load_blocks(to + 2 * kFactorBytes, a_map, a.half, a.block + a_low, full);
+          load_blocks(to + 3 * kFactorBytes, b_map, b.half, b.block + b_low, full);
+        }
       }
       __syncwarp();
       a.advance();
@@ -123,8 +137,10 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
   }
 }
 
+template <bool kSplit>
 __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ring_at, Control& c) {
-  Ring r;
+  constexpr int kStageBytes = Stages<kSplit>::kBytes;
+  Ring<kSplit> r;
   const uint32_t full0 = shared_address(&c.full[0]), empty0 = shared_address(&c.empty[0]), tensor = c.tensor;
   uint32_t n = 0;
   for (Tiles tiles(p); tiles.take(); ++n) {
@@ -156,6 +172,13 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
       if (one_lane()) {
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + j * b_step, kind, k + j > 0);
+        if (kSplit) {
+          constexpr uint32_t kLow = 2 * kFactorBytes >> 4;
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + j * a_step, b + kLow + j * b_step, kind, true);
+#pragma unroll
+          for (uint32_t j = 0; j < 4; ++j) multiply(sums, a + kLow + j * a_step, b + j * b_step, kind, true);
+        }
         arrive_after_products(empty0 + r.stage * 8);
       }
       __syncwarp();
@@ -183,15 +206,21 @@ struct Addend {
 // What sums of a product, the thread's row and 64 columns of it, become:
 //   S = X X^T             sums in X's scale twice
 //   P = a I + b S + c S^2
-//   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part
-// rounded to fp16, for the factors in shared memory; what X's rounding leaves, to `low` if that is not null.
-template <int kPhase>
-__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diagonal, const float (&v)[64], const Addend& in, bool adds, uint8_t* staging,
-                                           uint32_t row, uint8_t* low) {
+//   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part.  (kSplit: X = P X, all of it)
+// rounded to fp16, for the factors in shared memory; what the rounding leaves in `rest` (kSplit), or X's to `low` if that is not null.
+template <int kPhase, bool kSplit>
+__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diagonal, const float (&v)[64], const Addend& in, const Addend& in_low, bool adds,
+                                           uint8_t* staging, uint32_t row, uint8_t* low, Addend& rest) {
 #pragma unroll
   for (uint32_t c = 0; c < 8; ++c) {
     float x[8], y[8];
-    if (kPhase == kPoly || (kPhase == kNext && adds)) floats(in.x[c], y);
+    if (kPhase == kPoly || (kPhase == kNext && !kSplit && adds)) floats(in.x[c], y);
+    if (kPhase == kPoly && kSplit) {
+      float z[8];
+      floats(in_low.x[c], z);
+#pragma unroll
+      for (uint32_t j = 0; j < 8; ++j) y[j] += z[j];
+    }
 #pragma unroll
     for (uint32_t j = 0; j < 8; ++j) {
       const float sum = v[8 * c + j];
@@ -202,11 +231,13 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
         x[j] = own + y[j] * (coef[1] * (kScaleP / kScaleS)) + sum * (coef[2] * (kScaleP / (kScaleS * kScaleS)));
       } else {
         x[j] = sum * (1.0f / kScaleP);
-        if (adds) x[j] += coef[0] * y[j];
+        if (!kSplit && adds) x[j] += coef[0] * y[j];
       }
     }
     uint4* const to = reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16));
-    if (kPhase == kNext && low != nullptr) {
+    if (kSplit) {
+      split(x, *to, rest.x[c]);
+    } else if (kPhase == kNext && low != nullptr) {
       uint4 lo;
       split(x, *to, lo);
       *reinterpret_cast<uint4*>(low + (c * kBlockRows + row) * 16) = lo;
@@ -216,7 +247,18 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
   }
 }
 
+// The warp's rows from shared memory to their block.
+__device__ __forceinline__ void store_rows(uint8_t* to, uint32_t staging_at, uint32_t lane) {
+  before_copies();
+  __syncwarp();
+  if (lane == 0) {
+    store_bytes(to, staging_at, kStaging);
+    end_stores();
+  }
+}
+
 // One of the eight warps.  Each by itself: what it adds is on its way while the products run, its 32 rows of 64 columns leave by one copy.
+template <bool kSplit>
 __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* staging, Control& c, uint32_t rank) {
   const uint32_t warp = threadIdx.x / 32 - 2, lane = threadIdx.x % 32;
   const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + lane;  // a warp reads the quarter of its index
@@ -228,15 +270,17 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
     const MuonTile& t = tiles.now;
     const uint32_t half = n % 2, parts = t.flags & kNarrow ? 2 : 4;
     const bool mine = rank == 0 || t.flags & kSecond;
-    const bool low_after = p.low >> (tiles.round + 1) & 1, adds = t.phase == kPoly || (t.phase == kNext && p.low >> tiles.round & 1);
+    const bool low_after = !kSplit && p.low >> (tiles.round + 1) & 1, adds = t.phase == kPoly || (!kSplit && t.phase == kNext && p.low >> tiles.round & 1);
     const float coef[3] = {p.coef[tiles.round][0], p.coef[tiles.round][1], p.coef[tiles.round][2]};
     uint8_t* const first = p.work + (static_cast<uint64_t>(t.out) + rank * t.across) * kBlockBytes;
-    Addend in;
+    Addend in, in_low, rest;
     auto fetch = [&](uint32_t q) {
-      if (t.phase == kPoly)
+      if (t.phase == kPoly) {
         in.of_square(first + q * kBlockBytes + to_square, row);
-      else
+        if (kSplit) in_low.of_square(first + q * kBlockBytes + 3 * to_square, row);
+      } else {
         in.of_low(first + q * kBlockBytes + to_low, row);
+      }
     };
     bool ok = true;
     if (mine && adds) {
@@ -262,17 +306,20 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       __syncwarp();
       uint8_t* const block = first + q * kBlockBytes;
       if (t.phase == kGram)
-        finish_row<kGram>(coef, 0, v, in, false, staging, row, nullptr);
+        finish_row<kGram, kSplit>(coef, 0, v, in, in_low, false, staging, row, nullptr, rest);
       else if (t.phase == kPoly)  // (the diagonal's column of this row among the block's)
-        finish_row<kPoly>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, true, staging, row, nullptr);
+        finish_row<kPoly, kSplit>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, in_low, true, staging, row, nullptr, rest);
       else
-        finish_row<kNext>(coef, 0, v, in, adds, staging, row, low_after ? block + to_low : nullptr);
+        finish_row<kNext, kSplit>(coef, 0, v, in, in_low, adds, staging, row, low_after ? block + to_low : nullptr, rest);
       if (adds && q + 2 < parts) fetch(q + 2);
-      before_copies();
-      __syncwarp();
-      if (lane == 0) {
-        store_bytes(block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes : 0) + quarter * kStaging, staging_at, kStaging);
-        end_stores();
+      uint8_t* const to = block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes : 0) + quarter * kStaging;
+      store_rows(to, staging_at, lane);
+      if (kSplit) {
+        if (lane == 0) wait_stores_read();
+        __syncwarp();
+#pragma unroll
+        for (uint32_t c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16)) = rest.x[c];
+        store_rows(to + (t.phase == kNext ? to_low : 2 * to_square), staging_at, lane);
       }
     }
     if (p.waits && lane == 0) {
@@ -283,15 +330,16 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
   if (lane == 0) wait_stores();
 }
 
+template <bool kSplit>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
     product_kernel(const __grid_constant__ MuonProduct p, const __grid_constant__ MuonMaps maps) {
   extern __shared__ uint8_t raw[];
   __shared__ Control c;
   const uint32_t ring_at = (shared_address(raw) + 1023) & ~1023u;
-  uint8_t* const staging = raw + (ring_at - shared_address(raw)) + kStages * kStageBytes;
+  uint8_t* const staging = raw + (ring_at - shared_address(raw)) + kRingBytes;
   const uint32_t rank = rank_in_pair(), warp = threadIdx.x / 32;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kMostStages; ++i) {
       barrier_init(shared_address(&c.full[i]), 1);
       barrier_init(shared_address(&c.empty[i]), 1);
     }
@@ -310,11 +358,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   wait_for_kernel_before();
   if (p.clip == nullptr || p.clip->nonfinite == 0) {
     if (warp == 0) {
-      bring(p, maps, ring_at, c, rank);
+      bring<kSplit>(p, maps, ring_at, c, rank);
     } else if (warp == 1) {
-      if (rank == 0) multiply_tiles(p, ring_at, c);
+      if (rank == 0) multiply_tiles<kSplit>(p, ring_at, c);
     } else {
-      finish_tiles(p, staging, c, rank);
+      finish_tiles<kSplit>(p, staging, c, rank);
     }
   }
   // Neither CTA frees or leaves while the other's products or arrivals may still reach it.
@@ -343,24 +391,27 @@ cudaLaunchConfig_t config(uint32_t pairs, cudaStream_t s, cudaLaunchAttribute (&
 }  // namespace
 
 cudaError_t configure_muon_product() {
-  return cudaFuncSetAttribute(product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
+  const cudaError_t e = cudaFuncSetAttribute(product_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(product_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
 }
 
 cudaError_t muon_pairs(uint32_t* pairs) {
   cudaLaunchAttribute attrs[1] = {};
   cudaLaunchConfig_t c = config(kSms / 2, nullptr, attrs);
   c.numAttrs = 0;
-  int n = 0;
-  const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, product_kernel, &c);
-  *pairs = static_cast<uint32_t>(n);
-  return e != cudaSuccess ? e : n > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
+  int n = 0, m = 0;
+  cudaError_t e = cudaOccupancyMaxActiveClusters(&n, product_kernel<false>, &c);
+  if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&m, product_kernel<true>, &c);
+  *pairs = static_cast<uint32_t>(std::min(n, m));
+  return e != cudaSuccess ? e : *pairs > 0 ? cudaSuccess : cudaErrorLaunchOutOfResources;
 }
 
 cudaError_t launch_muon_product(const MuonProduct& p, const MuonMaps& maps, uint32_t pairs, cudaStream_t s) {
-  if (!p.waits) return launch_chained(product_kernel, static_cast<int>(2 * std::min(pairs, p.n_tiles)), kThreads, kShared, s, p, maps);
+  auto* const kernel = p.split ? product_kernel<true> : product_kernel<false>;
+  if (!p.waits) return launch_chained(kernel, static_cast<int>(2 * std::min(pairs, p.n_tiles)), kThreads, kShared, s, p, maps);
   cudaLaunchAttribute attrs[1] = {};
   const cudaLaunchConfig_t c = config(pairs, s, attrs);
-  cudaLaunchKernelEx(&c, product_kernel, p, maps);
+  cudaLaunchKernelEx(&c, kernel, p, maps);
   return cudaGetLastError();
 }
 

@@ -2,7 +2,6 @@
 #pragma once
 
 #include <algorithm>
-#include <numeric>
 #include <vector>
 
 #include "muon.h"
@@ -79,13 +78,14 @@ struct ProductOf {
   }
 };
 
-// The tiles of an iteration: S of all matrices, then P, then X, in each those with the longest contraction first.  ends: where each phase's end.
-inline void plan_tiles(const std::vector<MuonDesc>& descs, std::vector<MuonTile>& tiles, uint32_t (&ends)[kPhases]) {
+// The tiles of an iteration over the matrices that are split, or those that are not: S of all, then P, then X, in each those with the longest contraction first.  ends: where each phase's end.
+inline void plan_tiles(const std::vector<MuonDesc>& descs, bool split, std::vector<MuonTile>& tiles, uint32_t (&ends)[kPhases]) {
   for (int phase = 0; phase < kPhases; ++phase) {
     std::vector<ProductOf> all;
     for (const MuonDesc& d : descs) all.emplace_back(phase, d);
-    std::vector<uint32_t> order(descs.size());
-    std::iota(order.begin(), order.end(), 0u);
+    std::vector<uint32_t> order;
+    for (uint32_t m = 0; m < descs.size(); ++m)
+      if ((descs[m].split != 0) == split) order.push_back(m);
     std::stable_sort(order.begin(), order.end(), [&](uint32_t x, uint32_t y) { return all[x].depth > all[y].depth; });
     for (uint32_t m : order) {
       const ProductOf& q = all[m];

@@ -32,6 +32,7 @@ FP_ENTRY_BYTES = 16
 FR_OPT_BLOCK = 256
 FR_ROUND_NEAREST, FR_ROUND_RANDOM = 0, 1
 FR_MUON_MOST, FR_MUON_MOST_SIDE = 10, 1 << 20
+FR_MUON_BY_TYPE, FR_MUON_ONE = 0, 1
 CLIP_BYTES = 16
 
 _TORCH_TO_FR = {torch.bfloat16: FR_DT_BF16, torch.float32: FR_DT_F32, torch.uint8: FR_DT_BYTES,
@@ -76,7 +77,7 @@ class fr_muon(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_double), ("beta", ctypes.c_double), ("weight_decay", ctypes.c_double),
                 ("coef", ctypes.c_double * 3 * FR_MUON_MOST), ("step", ctypes.c_uint64), ("seed", ctypes.c_uint64),
                 ("iterations", ctypes.c_uint32), ("nesterov", ctypes.c_uint32), ("rounding", ctypes.c_uint32),
-                ("reserved", ctypes.c_uint32)]
+                ("products", ctypes.c_uint32)]
 
 
 class FlashrecError(RuntimeError):
@@ -520,11 +521,13 @@ MUON_COEFFICIENTS = ((3.4445, -4.7750, 2.0315),) * 5
 
 
 def muon(lr: float = 0.0, beta: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
-         coefficients=MUON_COEFFICIENTS, step: int = 1, seed: int = 0, rounding: int = FR_ROUND_NEAREST) -> fr_muon:
+         coefficients=MUON_COEFFICIENTS, step: int = 1, seed: int = 0, rounding: int = FR_ROUND_NEAREST,
+         products: int = FR_MUON_BY_TYPE) -> fr_muon:
     """The numbers of a step: one (a, b, c) per iteration."""
     if not 1 <= len(coefficients) <= FR_MUON_MOST:
         raise ValueError("1 to %d iterations, not %d" % (FR_MUON_MOST, len(coefficients)))
-    h = fr_muon(lr, beta, weight_decay, step=step, seed=seed, iterations=len(coefficients), nesterov=bool(nesterov), rounding=rounding)
+    h = fr_muon(lr, beta, weight_decay, step=step, seed=seed, iterations=len(coefficients), nesterov=bool(nesterov), rounding=rounding,
+                products=products)
     for i, abc in enumerate(coefficients):
         h.coef[i][:] = abc
     return h

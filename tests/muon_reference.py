@@ -6,6 +6,8 @@ USUAL = ((3.4445, -4.7750, 2.0315),) * 5
 # relative size of one in what it enters and passed on with a gain of about one (the parts that would grow go in unrounded):
 # the worst case adds them up.
 ROUNDING = 3 * 2.0 ** -11
+# Two fp16 numbers hold what one leaves to 2^-11 of that, and the product of the second ones, left out, is as small.
+SPLIT_ROUNDING = 3 * 2 * 2.0 ** -22
 
 
 def orthogonal(g, coefficients=USUAL):
@@ -25,9 +27,11 @@ def orthogonal(g, coefficients=USUAL):
     return x.T if tall else x
 
 
-def bound(coefficients=USUAL):
-    """Of |error| / |O|, 2-norms over all elements."""
-    return ROUNDING * len(coefficients)
+def bound(coefficients=USUAL, split=False, shape=(0, 0)):
+    """Of |error| / |O|, 2-norms over all elements.  split: products of both halves; the tensor cores add 16 products at a time,
+    each sum off by 2^-23 at most (it may be cut off), in the three products of an iteration."""
+    each = SPLIT_ROUNDING + 3 * (3 * (max(shape) // 16 + 8)) * 2.0 ** -23 if split else ROUNDING
+    return each * len(coefficients)
 
 
 def matrix(rng, rows, cols, kind="half"):

@@ -34,21 +34,23 @@ def _near(got, want, rel, note):
     assert err <= rel * np.linalg.norm(want.ravel()) + 1e-300, (note, err / np.linalg.norm(want.ravel()), rel)
 
 
-def _orthogonalize(gs, grad="f32", update="f32", shift=0, coefficients=mref.USUAL, **more):
+def _orthogonalize(gs, grad="f32", update="f32", shift=0, coefficients=mref.USUAL, products=0, **more):
     """(gradients as the library reads them, its updates)"""
     shapes = [g.shape for g in gs]
     flat = [g.ravel() if grad == "f32" else ref.f32_to_bf16(g.ravel()) for g in gs]
     b = Buffers(flat, shift)
     u = Buffers([np.zeros(g.size, np.float32 if update == "f32" else np.uint16) for g in gs], shift)
     plan = fr.MuonPlan(grads=_views(b, shapes), updates=_views(u, shapes), **more)
-    plan.orthogonalize(fr.muon(coefficients=coefficients))
+    plan.orthogonalize(fr.muon(coefficients=coefficients, products=products))
     torch.cuda.synchronize()
     b.check()
     return [_wide(x).reshape(s) for x, s in zip(flat, shapes)], [_wide(x).reshape(s) for x, s in zip(u.get(), shapes)]
 
 
-def _output_rounding(kind):
-    return 2.0 ** -8 if kind == "bf16" else 2.0 ** -24
+def _bound(kind, shape, coefficients=mref.USUAL, products=0):
+    """Of O in an output of this type, its own rounding included."""
+    split = kind == "f32" and products == fr.FR_MUON_BY_TYPE
+    return mref.bound(coefficients, split, shape) + (2.0 ** -8 if kind == "bf16" else 2.0 ** -24)
 
 
 @pytest.mark.parametrize("shift", [0, 1])
@@ -59,15 +61,39 @@ def test_orthogonalize_is_its_definition(grad, update, shift):
     gs, got = _orthogonalize([mref.matrix(rng, *s) for s in SHAPES], grad, update, shift, update_scale=scale)
     for g, o, x in zip(gs, got, scale):
         if g.size:
-            _near(o, x * mref.orthogonal(g), mref.bound() + _output_rounding(update), g.shape)
+            _near(o, x * mref.orthogonal(g), _bound(update, g.shape), g.shape)
 
 
+@pytest.mark.parametrize("products", [0, 1])
 @pytest.mark.parametrize("kind", ["lowrank", "decay", "spiky"])
-def test_hard_spectra(kind):
+def test_hard_spectra(kind, products):
     rng = np.random.default_rng(6)
-    gs, got = _orthogonalize([mref.matrix(rng, *s, kind) for s in [(128, 128), (300, 700), (700, 300), (512, 512)]])
+    gs, got = _orthogonalize([mref.matrix(rng, *s, kind) for s in [(128, 128), (300, 700), (700, 300), (512, 512)]], products=products)
     for g, o in zip(gs, got):
-        _near(o, mref.orthogonal(g), mref.bound(), (kind, g.shape))
+        _near(o, mref.orthogonal(g), _bound("f32", g.shape, products=products), (kind, g.shape))
+
+
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+def test_products_of_one_half(grad):
+    rng = np.random.default_rng(5)
+    gs, got = _orthogonalize([mref.matrix(rng, *s) for s in SHAPES], grad, products=fr.FR_MUON_ONE)
+    for g, o in zip(gs, got):
+        if g.size:
+            _near(o, mref.orthogonal(g), _bound("f32", g.shape, products=fr.FR_MUON_ONE), g.shape)
+
+
+def test_a_list_of_both_kinds():
+    """Matrices with fp32 outputs and others in one plan: each as alone."""
+    rng = np.random.default_rng(18)
+    shapes = [(200, 300), (300, 130), (64, 64), (257, 256)]
+    gs = [torch.from_numpy(mref.matrix(rng, *s)).cuda() for s in shapes]
+    kinds = [torch.float32, torch.bfloat16, torch.bfloat16, torch.float32]
+    outs = [torch.zeros(s, dtype=k, device="cuda") for s, k in zip(shapes, kinds)]
+    fr.MuonPlan(grads=gs, updates=outs).orthogonalize()
+    for g, o in zip(gs, outs):
+        alone = torch.zeros_like(o)
+        fr.MuonPlan(grads=[g], updates=[alone]).orthogonalize()
+        assert torch.equal(alone, o)
 
 
 @pytest.mark.parametrize("coefficients", [((1.5, -0.5, 0.0),) * 10, ((2.0, -1.5, 0.5),), ((3.4445, -4.7750, 2.0315),) * 2,
@@ -76,7 +102,7 @@ def test_other_polynomials(coefficients):
     rng = np.random.default_rng(7)
     gs, got = _orthogonalize([mref.matrix(rng, *s) for s in [(130, 300), (300, 130), (64, 64)]], coefficients=coefficients)
     for g, o in zip(gs, got):
-        _near(o, mref.orthogonal(g, coefficients), mref.bound(coefficients), (coefficients, g.shape))
+        _near(o, mref.orthogonal(g, coefficients), _bound("f32", g.shape, coefficients), (coefficients, g.shape))
 
 
 def test_scales_of_a_matrix_and_its_empty_and_nonfinite_ones():
@@ -97,7 +123,7 @@ def test_scales_of_a_matrix_and_its_empty_and_nonfinite_ones():
     _, got = _orthogonalize(gs)
     for g, o in zip(gs, got):
         if np.isfinite(g).all():
-            _near(o, mref.orthogonal(g), mref.bound(), float(np.abs(g).max()))
+            _near(o, mref.orthogonal(g), _bound("f32", g.shape), float(np.abs(g).max()))
         else:
             assert np.isnan(o).all()
 
@@ -155,7 +181,8 @@ class Step:
                 new = ref.bf16_to_f32(new)
             # the update's own error, the sum's in fp32 (products, sums and lr: four roundings), a bf16 weight's rounding
             # (at random: a whole step)
-            slack = p["lr"] * f["lr_scale"] * mref.bound() * np.linalg.norm(u) + 4 * 2.0 ** -24 * np.linalg.norm(old)
+            bound = mref.bound(split=self.param != "bf16" and not p.get("products"), shape=s)
+            slack = p["lr"] * f["lr_scale"] * bound * np.linalg.norm(u) + 4 * 2.0 ** -24 * np.linalg.norm(old)
             if self.param == "bf16":
                 slack += (2.0 ** -7 if p.get("rounding") else 2.0 ** -8) * np.linalg.norm(want)
             assert np.linalg.norm(new.astype(np.float64) - want) <= slack, (s, np.linalg.norm(new - want) / slack)
@@ -175,6 +202,14 @@ def test_step_is_its_definition(param, grad, nesterov, shift):
     s.check(0.37109375)
 
 
+@pytest.mark.parametrize("param", ["master", "f32"])
+def test_step_with_products_of_one_half(param):
+    s = Step(SHAPES, param, "bf16", products=fr.FR_MUON_ONE)
+    s.plan.step(s.hyper(), _record(0.5))
+    torch.cuda.synchronize()
+    s.check(0.5)
+
+
 def test_step_without_a_record_and_without_momentum():
     s = Step(SMALL, "master", "f32", beta=0.0, nesterov=False)
     s.plan.step(s.hyper())
@@ -188,8 +223,8 @@ def test_random_rounding_of_weights_is_near_and_unbiased(shift):
     s.plan.step(s.hyper(), _record(1.0))
     torch.cuda.synchronize()
     s.check(1.0)
-    # the same step with fp32 weights gives what was rounded
-    f = Step([(256, 512), (3, 5)], "f32", "bf16", shift)
+    # the same step with fp32 weights, by the same products, gives what was rounded
+    f = Step([(256, 512), (3, 5)], "f32", "bf16", shift, products=fr.FR_MUON_ONE)
     for t, x in zip(f.b["weight"].tensors, s.host["weight"]):
         t.copy_(torch.from_numpy(ref.bf16_to_f32(x)))
     f.plan.step(f.hyper(), _record(1.0))
@@ -284,7 +319,14 @@ def test_two_plans_on_two_streams():
 def test_long_and_large(shape):
     rng = np.random.default_rng(15)
     gs, got = _orthogonalize([mref.matrix(rng, *shape, "half" if min(shape) > 2 else "plain")], "bf16", "bf16")
-    _near(got[0], mref.orthogonal(gs[0]), mref.bound() + 2.0 ** -8, shape)
+    _near(got[0], mref.orthogonal(gs[0]), _bound("bf16", shape), shape)
+
+
+@pytest.mark.parametrize("shape", [(1, 1 << 20), (1500, 3000), (2049, 1025)])
+def test_long_and_large_in_fp32(shape):
+    rng = np.random.default_rng(16)
+    gs, got = _orthogonalize([mref.matrix(rng, *shape, "half" if min(shape) > 2 else "plain")])
+    _near(got[0], mref.orthogonal(gs[0]), _bound("f32", shape), shape)
 
 
 def test_empty_lists_do_nothing():
