@@ -30,7 +30,7 @@
 
 namespace frk {
 
-constexpr int kBlockRows = 128, kBlockCols = 64, kBlockBytes = kBlockRows * kBlockCols * 2;
+constexpr int kBlockRows = 128, kBlockCols = 64, kMuonBlockBytes = kBlockRows * kBlockCols * 2;
 constexpr float kScaleX = 0x1p14f, kScaleS = 0x1p13f, kScaleP = 0x1p11f;
 constexpr double kMostX = 2.0, kMostP = 15.0;
 
@@ -98,7 +98,7 @@ cudaError_t launch_muon_update(const MuonParams& p, cudaStream_t s);    // fr_or
 
 // ---- products
 
-enum : int { kGram = 0, kPoly = 1, kNext = 2 };  // S, P, the next X
+enum : int { kGram = 0, kPolynomial = 1, kNext = 2 };  // S, P, the next X
 constexpr int kPhases = 3;
 
 // D[i][j] = sum over k of A(i, k) B(j, k): a tile of it, 256 x 256 or 256 x 128, by a pair of CTAs.  All that a CTA needs of it in one record, so

@@ -101,7 +101,7 @@ cudaError_t make_maps(MuonMaps* maps, void* at, uint64_t bytes) {
   const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
   if (e != cudaSuccess) return e;
   if (found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
-  const cuuint64_t sizes[4] = {kBlockCols, kBlockRows / 2, 2, bytes / kBlockBytes}, strides[3] = {128, kBlockBytes / 2, kBlockBytes};
+  const cuuint64_t sizes[4] = {kBlockCols, kBlockRows / 2, 2, bytes / kMuonBlockBytes}, strides[3] = {128, kMuonBlockBytes / 2, kMuonBlockBytes};
   const cuuint32_t steps[4] = {1, 1, 1, 1};
   auto make = [&](CUtensorMap* map, cuuint32_t halves, cuuint32_t blocks) {
     const cuuint32_t box[4] = {kBlockCols, kBlockRows / 2, halves, blocks};
@@ -127,8 +127,8 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     MuonDesc d = describe(x, t);
     const uint64_t n = static_cast<uint64_t>(d.row_blocks) * d.col_blocks;
     auto& part = p->parts[d.split];
-    d.x[0] = part.x_blocks * kBlockBytes;
-    d.p = part.p_blocks * kBlockBytes;
+    d.x[0] = part.x_blocks * kMuonBlockBytes;
+    d.p = part.p_blocks * kMuonBlockBytes;
     part.x_blocks += n;
     part.p_blocks += square_blocks(d);
     d.first_unit = static_cast<uint32_t>(units.size());
@@ -141,7 +141,7 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   uint64_t bytes = 0;
   for (uint32_t k = 0; k < 2; ++k) {
     const auto& part = p->parts[k];
-    const uint64_t x_bytes = part.x_blocks * kBlockBytes, p_bytes = part.p_blocks * kBlockBytes;
+    const uint64_t x_bytes = part.x_blocks * kMuonBlockBytes, p_bytes = part.p_blocks * kMuonBlockBytes;
     for (MuonDesc& d : descs) {
       if (d.split != k) continue;
       d.x[0] += bytes;

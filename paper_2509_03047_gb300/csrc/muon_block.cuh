@@ -11,13 +11,13 @@ namespace frk {
 // Byte offset of the 16-byte chunk of columns 8 c ... 8 c + 7 of row r in a matrix of `col_blocks` blocks per block row.
 __device__ __forceinline__ uint64_t chunk_at(uint32_t col_blocks, uint32_t r, uint32_t c) {
   const uint64_t block = static_cast<uint64_t>(r / kBlockRows) * col_blocks + c / 8;
-  return block * kBlockBytes + (r % kBlockRows) * 128 + (((c % 8) ^ (r % 8)) * 16);
+  return block * kMuonBlockBytes + (r % kBlockRows) * 128 + (((c % 8) ^ (r % 8)) * 16);
 }
 
 // The same of the second halves.
 __device__ __forceinline__ uint64_t low_at(uint32_t col_blocks, uint32_t r, uint32_t c) {
   const uint64_t block = static_cast<uint64_t>(r / kBlockRows) * col_blocks + c / 8;
-  return block * kBlockBytes + ((c % 8) * kBlockRows + r % kBlockRows) * 16;
+  return block * kMuonBlockBytes + ((c % 8) * kBlockRows + r % kBlockRows) * 16;
 }
 
 __device__ __forceinline__ uint32_t half2_bits(float x, float y) {

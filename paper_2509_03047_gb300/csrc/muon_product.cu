@@ -31,7 +31,7 @@ constexpr int kRingBytes = 12 * kFactorBytes, kMostStages = 6;
 static_assert(Stages<true>::kCount * Stages<true>::kBytes == kRingBytes && Stages<false>::kCount * Stages<false>::kBytes == kRingBytes, "one size");
 constexpr int kWarps = 8;            // that turn sums into blocks: a quarter of the rows, every other 64 columns
 constexpr int kThreads = 64 + kWarps * 32;
-constexpr int kStaging = kBlockBytes / 4;  // per warp
+constexpr int kStaging = kMuonBlockBytes / 4;  // per warp
 constexpr int kTensorColumns = 512;
 constexpr size_t kShared = 1024 + kRingBytes + kWarps * kStaging;
 static_assert(kSignals == 2 * kWarps, "one per warp");
@@ -214,8 +214,8 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
 #pragma unroll
   for (uint32_t c = 0; c < 8; ++c) {
     float x[8], y[8];
-    if (kPhase == kPoly || (kPhase == kNext && !kSplit && adds)) floats(in.x[c], y);
-    if (kPhase == kPoly && kSplit) {
+    if (kPhase == kPolynomial || (kPhase == kNext && !kSplit && adds)) floats(in.x[c], y);
+    if (kPhase == kPolynomial && kSplit) {
       float z[8];
       floats(in_low.x[c], z);
 #pragma unroll
@@ -226,7 +226,7 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
       const float sum = v[8 * c + j];
       if (kPhase == kGram) {
         x[j] = sum * (kScaleS / (kScaleX * kScaleX));
-      } else if (kPhase == kPoly) {
+      } else if (kPhase == kPolynomial) {
         const float own = diagonal == 8 * c + j ? coef[0] * kScaleP : 0.0f;
         x[j] = own + y[j] * (coef[1] * (kScaleP / kScaleS)) + sum * (coef[2] * (kScaleP / (kScaleS * kScaleS)));
       } else {
@@ -264,22 +264,22 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
   const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + lane;  // a warp reads the quarter of its index
   staging += warp * kStaging;
   const uint32_t staging_at = shared_address(staging);
-  const uint64_t to_low = 2ull * p.x_blocks * kBlockBytes, to_square = static_cast<uint64_t>(p.p_blocks) * kBlockBytes;
+  const uint64_t to_low = 2ull * p.x_blocks * kMuonBlockBytes, to_square = static_cast<uint64_t>(p.p_blocks) * kMuonBlockBytes;
   uint32_t n = 0;
   for (Tiles tiles(p); tiles.take(); ++n) {
     const MuonTile& t = tiles.now;
     const uint32_t half = n % 2, parts = t.flags & kNarrow ? 2 : 4;
     const bool mine = rank == 0 || t.flags & kSecond;
-    const bool low_after = !kSplit && p.low >> (tiles.round + 1) & 1, adds = t.phase == kPoly || (!kSplit && t.phase == kNext && p.low >> tiles.round & 1);
+    const bool low_after = !kSplit && p.low >> (tiles.round + 1) & 1, adds = t.phase == kPolynomial || (!kSplit && t.phase == kNext && p.low >> tiles.round & 1);
     const float coef[3] = {p.coef[tiles.round][0], p.coef[tiles.round][1], p.coef[tiles.round][2]};
-    uint8_t* const first = p.work + (static_cast<uint64_t>(t.out) + rank * t.across) * kBlockBytes;
+    uint8_t* const first = p.work + (static_cast<uint64_t>(t.out) + rank * t.across) * kMuonBlockBytes;
     Addend in, in_low, rest;
     auto fetch = [&](uint32_t q) {
-      if (t.phase == kPoly) {
-        in.of_square(first + q * kBlockBytes + to_square, row);
-        if (kSplit) in_low.of_square(first + q * kBlockBytes + 3 * to_square, row);
+      if (t.phase == kPolynomial) {
+        in.of_square(first + q * kMuonBlockBytes + to_square, row);
+        if (kSplit) in_low.of_square(first + q * kMuonBlockBytes + 3 * to_square, row);
       } else {
-        in.of_low(first + q * kBlockBytes + to_low, row);
+        in.of_low(first + q * kMuonBlockBytes + to_low, row);
       }
     };
     bool ok = true;
@@ -304,15 +304,15 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       if (!mine) continue;
       if (lane == 0) wait_stores_read();  // of the rows before
       __syncwarp();
-      uint8_t* const block = first + q * kBlockBytes;
+      uint8_t* const block = first + q * kMuonBlockBytes;
       if (t.phase == kGram)
         finish_row<kGram, kSplit>(coef, 0, v, in, in_low, false, staging, row, nullptr, rest);
-      else if (t.phase == kPoly)  // (the diagonal's column of this row among the block's)
-        finish_row<kPoly, kSplit>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, in_low, true, staging, row, nullptr, rest);
+      else if (t.phase == kPolynomial)  // (the diagonal's column of this row among the block's)
+        finish_row<kPolynomial, kSplit>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, in_low, true, staging, row, nullptr, rest);
       else
         finish_row<kNext, kSplit>(coef, 0, v, in, in_low, adds, staging, row, low_after ? block + to_low : nullptr, rest);
       if (adds && q + 2 < parts) fetch(q + 2);
-      uint8_t* const to = block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kBlockBytes : 0) + quarter * kStaging;
+      uint8_t* const to = block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kMuonBlockBytes : 0) + quarter * kStaging;
       store_rows(to, staging_at, lane);
       if (kSplit) {
         if (lane == 0) wait_stores_read();

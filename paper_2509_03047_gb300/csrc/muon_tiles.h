@@ -25,13 +25,13 @@ struct ProductOf {
   uint32_t out, rows, cols;  // rows and columns in blocks of 128
 
   ProductOf(int phase, const MuonDesc& d) {
-    const uint32_t x = static_cast<uint32_t>(d.x[0] / kBlockBytes), s = static_cast<uint32_t>(d.s / kBlockBytes), p = static_cast<uint32_t>(d.p / kBlockBytes);
+    const uint32_t x = static_cast<uint32_t>(d.x[0] / kMuonBlockBytes), s = static_cast<uint32_t>(d.s / kMuonBlockBytes), p = static_cast<uint32_t>(d.p / kMuonBlockBytes);
     const uint32_t side = d.side_blocks;
     square = 2 * side;
     if (phase == kGram) {
       a = b = {x, d.col_blocks, d.tall != 0, true};
       depth = d.tall ? 2 * d.row_blocks : d.col_blocks;
-    } else if (phase == kPoly) {
+    } else if (phase == kPolynomial) {
       a = b = {s, square, false, false};
       depth = square;
     } else {
@@ -40,7 +40,7 @@ struct ProductOf {
       b = d.tall ? q : Factor{x, d.col_blocks, true, true};
       depth = square;
     }
-    out = phase == kGram ? s : phase == kPoly ? p : x;
+    out = phase == kGram ? s : phase == kPolynomial ? p : x;
     rows = phase == kNext ? d.row_blocks : side;
     cols = phase == kNext ? d.col_blocks / 2 : side;
   }
