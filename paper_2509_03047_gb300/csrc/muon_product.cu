@@ -116,7 +116,7 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
       }
       if (k == t.b_switch) {
         b = {static_cast<int32_t>(rank ? t.b_after[1] : t.b_after[0]), 0, static_cast<int32_t>(t.square), 1};
-        b_map = &maps.columns;
+        b_map = narrow ? &maps.half : &maps.columns;
       }
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
       if (!__all_sync(0xFFFFFFFFu, wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up))) return let_copies_land();

@@ -93,7 +93,8 @@ void check_tile(const MuonTile& t, const MuonDesc& d) {
   const bool narrow = t.flags & kNarrow, second = t.flags & kSecond;
   const uint32_t rows = phase == kNext ? d.row_blocks : side, cols = phase == kNext ? d.col_blocks / 2 : side;
   CHECK(t.row < rows && t.col < cols && second == (t.row + 1u < rows));
-  CHECK(narrow || t.col + 1u < cols);
+  CHECK(narrow || (t.col % 2 == 0 && t.col + 1u < cols));
+  CHECK(t.row % 2 == 0);
   CHECK(t.depth == (phase == kGram ? (d.tall ? 2 * d.row_blocks : d.col_blocks) : 2 * side));
   const bool a_x = phase == kGram || (phase == kNext && d.tall), b_x = phase == kGram || (phase == kNext && !d.tall);
   CHECK(a_x == ((t.flags & kAIterate) != 0) && b_x == ((t.flags & kBIterate) != 0));

@@ -336,3 +336,14 @@ def test_empty_lists_do_nothing():
     plan.step(fr.muon(lr=1.0))
     assert plan.n_elems == 0
     torch.cuda.synchronize()
+
+
+def test_a_matrix_gives_the_same_bits_in_a_long_list():
+    """One whose phases fill the SMs has wider tiles."""
+    rng = np.random.default_rng(19)
+    g = mref.matrix(rng, 700, 520)
+    for update in ("bf16", "f32"):
+        _, alone = _orthogonalize([g], update=update)
+        _, among = _orthogonalize([g] * 40, update=update)
+        for o in among:
+            assert alone[0].tobytes() == o.tobytes()
