@@ -247,12 +247,21 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
   }
 }
 
-// The warp's rows from shared memory to their block.
-__device__ __forceinline__ void store_rows(uint8_t* to, uint32_t staging_at, uint32_t lane) {
+// The warp's rows from shared memory to their block.  Where tiles of a launch wait for one another, by ordinary stores, 512 bytes at a time: another
+// SM sees them sooner.  Else by a bulk copy, which costs the warp nothing.
+__device__ __forceinline__ void store_rows(uint8_t* to, const uint8_t* staging, uint32_t lane, bool soon) {
+  if (soon) {
+    __syncwarp();
+#pragma unroll
+    for (uint32_t k = 0; k < kStaging / 512; ++k)
+      *reinterpret_cast<uint4*>(to + k * 512 + lane * 16) = *reinterpret_cast<const uint4*>(staging + k * 512 + lane * 16);
+    __syncwarp();
+    return;
+  }
   before_copies();
   __syncwarp();
   if (lane == 0) {
-    store_bytes(to, staging_at, kStaging);
+    store_bytes(to, shared_address(staging), kStaging);
     end_stores();
   }
 }
@@ -263,7 +272,6 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
   const uint32_t warp = threadIdx.x / 32 - 2, lane = threadIdx.x % 32;
   const uint32_t quarter = threadIdx.x / 32 % 4, row = quarter * 32 + lane;  // a warp reads the quarter of its index
   staging += warp * kStaging;
-  const uint32_t staging_at = shared_address(staging);
   const uint64_t to_low = 2ull * p.x_blocks * kMuonBlockBytes, to_square = static_cast<uint64_t>(p.p_blocks) * kMuonBlockBytes;
   uint32_t n = 0;
   for (Tiles tiles(p); tiles.take(); ++n) {
@@ -296,11 +304,7 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       tensor_load(from, v);
       tensor_load(from + 32, v + 32);
       tensor_load_wait();
-      if (q + 2 >= parts) {
-        tensor_fence_before();
-        __syncwarp();
-        if (lane == 0) arrive_in_first(shared_address(&c.sums_empty[half]));
-      }
+      if (q + 2 >= parts) tensor_fence_before();
       if (!mine) continue;
       if (lane == 0) wait_stores_read();  // of the rows before
       __syncwarp();
@@ -313,18 +317,19 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
         finish_row<kNext, kSplit>(coef, 0, v, in, in_low, adds, staging, row, low_after ? block + to_low : nullptr, rest);
       if (adds && q + 2 < parts) fetch(q + 2);
       uint8_t* const to = block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kMuonBlockBytes : 0) + quarter * kStaging;
-      store_rows(to, staging_at, lane);
+      store_rows(to, staging, lane, p.waits);
       if (kSplit) {
         if (lane == 0) wait_stores_read();
         __syncwarp();
 #pragma unroll
         for (uint32_t c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16)) = rest.x[c];
-        store_rows(to + (t.phase == kNext ? to_low : 2 * to_square), staging_at, lane);
+        store_rows(to + (t.phase == kNext ? to_low : 2 * to_square), staging, lane, p.waits);
       }
     }
-    if (p.waits && lane == 0) {
-      wait_stores();
-      add_to_count(p.done + t.done);
+    __syncwarp();
+    if (lane == 0) {
+      if (p.waits) add_to_count(p.done + t.done);
+      arrive_in_first(shared_address(&c.sums_empty[half]));
     }
   }
   if (lane == 0) wait_stores();

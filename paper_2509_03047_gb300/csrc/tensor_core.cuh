@@ -85,9 +85,9 @@ __device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t cou
   asm volatile("fence.proxy.async;" ::: "memory");
   return true;
 }
-// After this thread's copies to memory have ended.
+// After this thread's writes, and those of the warp's others before its last barrier.
 __device__ __forceinline__ void add_to_count(uint32_t* counter) {
-  asm volatile("fence.proxy.async;\n\tred.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
+  asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
 }
 // The part of a role that has given up: its copies in flight land meanwhile.
 __device__ __forceinline__ void let_copies_land() {
