@@ -104,7 +104,10 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
     Place b = {static_cast<int32_t>((rank ? t.b[1] : t.b[0]) + (t.flags & kBIterate ? tiles.iterate(0) : 0)), narrow && !b_columns ? static_cast<int32_t>(rank) : 0,
                static_cast<int32_t>(t.b_next), b_columns};
     const CUtensorMap *a_map = a_columns ? &maps.columns : &maps.rows, *b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
-    if (p.waits && !__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
+    if (p.waits) {
+      if (!__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
+      before_reading_copies();
+    }
     const uint32_t bytes = (kSplit ? 2 : 1) * (2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes));
     const int32_t a_low = 2 * static_cast<int32_t>(t.flags & kAIterate ? p.x_blocks : p.p_blocks),
                   b_low = 2 * static_cast<int32_t>(t.flags & kBIterate ? p.x_blocks : p.p_blocks);

@@ -44,10 +44,10 @@ __device__ __forceinline__ void barrier_init_done() { asm volatile("fence.mbarri
 __device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// (Released to this CTA alone: what it tells the other one is that loads from tensor memory have ended, no writes.  A wider release waits for
+// every write on its way, 3,000 clocks.)
 __device__ __forceinline__ void arrive_in_first(uint32_t bar) {
-  asm volatile(
-      "{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar)
-      : "memory");
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
   uint32_t done;
@@ -70,7 +70,7 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   }
   return true;
 }
-// Until a counter in memory has reached `count`; with it the writes before its additions are visible, to copies too.
+// Until a counter in memory has reached `count`; with it the writes before its additions are visible (to copies after before_reading_copies).
 __device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t count, volatile uint32_t* gave_up) {
   const long long start = clock64();
   for (;;) {
@@ -82,9 +82,9 @@ __device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t cou
       return false;
     }
   }
-  asm volatile("fence.proxy.async;" ::: "memory");
   return true;
 }
+__device__ __forceinline__ void before_reading_copies() { asm volatile("fence.proxy.async;" ::: "memory"); }
 // After this thread's writes, and those of the warp's others before its last barrier.
 __device__ __forceinline__ void add_to_count(uint32_t* counter) {
   asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(counter) : "memory");
