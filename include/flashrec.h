@@ -517,13 +517,14 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  *
  * Precision.  All factors of the products are fp16 numbers, scaled so that fp16 holds
  * them, their sums in fp32.  A matrix with an fp32 output (weight, master or update)
- * has each factor as two of them, 22 bits, and three products for one: O is off by some
- * 2^-19 (2-norm over 2-norm).  Others, and with FR_MUON_ONE all, enter X, X X^T and the
- * polynomial in it by one rounding each: with the usual coefficients and 5 iterations O is
- * off by 0.1 to 0.2% for any spectrum, by up to 0.5% where a side has fewer than 16 elements, less
- * than a bf16 output's own rounding (0.4% at most).  (The rounding of X
- * alone would grow with every iteration, by a, in the parts of small singular values:
- * what it leaves is kept, and added to the product as it is.)
+ * has each factor as two of them, 22 bits, and three products for one: O is off by
+ * 2^-16 to 2^-14 (2-norm over 2-norm; sides of 256 to 4,096), what the tensor cores' additions
+ * lose.  Others, and with FR_MUON_ONE all, enter X, X X^T and the polynomial in it by one
+ * rounding each: with the usual coefficients and 5 iterations O is off by 0.1 to 0.2% for
+ * any spectrum, by up to 0.5% where a side has fewer than 16 elements; a bf16 output's own rounding is
+ * 0.17% (0.4% at most).  (The rounding of X alone would grow with every iteration, by a, in
+ * the parts of small singular values: what it leaves is kept, and added to the product
+ * as it is, until the iterations left raise it by no more than 4.)
  *
  * One fr_muon_tensor is one matrix, rows * cols elements, row after row, in each
  * of its buffers.  fr_muon_step needs the weights, gradients and momenta,

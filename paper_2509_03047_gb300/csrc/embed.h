@@ -51,10 +51,11 @@ struct Met {  // a token of the batch
   uint32_t row, at;
 };
 constexpr int kSortThreads = 1024, kSortEach = 4, kSortTile = kSortThreads * kSortEach;
-constexpr uint64_t kCompareTokens = 8192;  // a batch of up to this many is sorted by comparing each with all
+constexpr uint64_t kCompareTokens = 4096;  // a batch of up to this many is sorted by comparing each with all
 constexpr uint32_t kSortCluster = 16;  // CTAs that sort a batch of up to a tile for each in one launch
 constexpr uint64_t kClusterTokens = static_cast<uint64_t>(kSortCluster) * kSortTile;
 constexpr uint32_t kSortCtas = 128;    // of a larger batch's launches
+constexpr uint64_t kFillShare = 128 << 10;  // bytes per CTA
 constexpr int kMostDigit = 9;          // bits of a pass
 
 struct SortPlan {
@@ -75,6 +76,8 @@ struct SortParams {
   uint32_t* n_long; // set to zero
   uint64_t share;   // tokens per CTA
   uint32_t ctas;
+  uint8_t* fill;    // zeros go here, by CTAs of the first launch beyond the sort's: the gradient's rows before some are written
+  uint64_t fill_bytes;
   int each;         // tokens per thread and tile
   int bits;
   int pass;
@@ -93,9 +96,10 @@ constexpr int lane_vectors(int v) { return v == kOdd ? 12 : v >= 8 ? 1 : v == 4 
 constexpr int tile_width(int v) { return 32 * vector_of(v) * lane_vectors(v); }
 // The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns; a multiple of what a CTA has.
 constexpr uint32_t kSumWarps = 8;
-// Ranges times column tiles, about.  A range has its fixed cost (the tokens at its borders, its part), some 5 us; one wave of them is best where
-// a token costs little of a warp's time, three where rows' writes are spread unevenly.  GB300, per SM 16, 24, 32, 48, 72 warps, us: 500,001 tokens
-// x 321 fp32 155, 159, 173, 182, 215; 32,768 x 768 accumulating 45.6, 48.3, 48.0, 48.5, 48.0; 65,536 x 4,096 137, 153, -, 129, 129.
+// Ranges times column tiles, about.  A range has its fixed cost (the tokens at its borders, its part), some 5 us: one wave of them is best for odd
+// rows and for wide ones that are added to, three where a token costs a warp little or rows' writes are spread unevenly.  GB300, per SM 16, 24,
+// 32, 48, 72 warps, us: 500,001 tokens x 321 fp32 155, 159, 173, 182, 215; 32,768 x 768 accumulating 45.6, 48.3, 48.0, 48.5, 48.0; 300,000 x 8
+// accumulating 88, -, -, 72, -; 65,536 x 4,096 137, 153, -, 129, 129.
 constexpr uint32_t kFewRangeWarps = kSms * 16, kRangeWarps = kSms * 48;
 constexpr uint32_t kLeastRange = 32;
 inline uint32_t column_tiles(uint64_t dim, int v) { return static_cast<uint32_t>((dim + tile_width(v) - 1) / tile_width(v)); }
@@ -114,7 +118,7 @@ struct SumParams {
   uint64_t dim, rows;
   float scale;
   uint32_t ranges, tiles;
-  uint32_t sum_ctas, zero_ctas;
+  uint32_t ctas, zero_ctas;
   uint32_t rows_per_zero_warp;
   uint32_t accumulate;
   uint32_t configure;  // 1: no launch, the kernel's shared-memory size is set

@@ -7,7 +7,7 @@
 // of one digit are found by a vote, those of the warps before by a table of counts
 // per warp and digit.  Nothing depends on the order in which anything runs.
 //
-// A batch of up to 8,192 tokens is sorted by comparing each with all, one of up to 65,536 in one launch, by a cluster of CTAs that
+// A batch of up to 4,096 tokens is sorted by comparing each with all, one of up to 65,536 in one launch, by a cluster of CTAs that
 // read each other's counts from shared memory; a larger one by two launches per pass.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
@@ -147,12 +147,25 @@ __device__ __forceinline__ void put_tile(const SortParams& p, const Shared& sh, 
     if (digit[k] != kAll) p.sorted[pass % 2][sh.base[digit[k]] + sh.before[threadIdx.x / 32 * bins + digit[k]] + rank[k]] = m[k];
 }
 
+// Zeros: share `index` of the bytes.  (While the sort waits for latencies on some SMs, the others write.)
+__device__ __forceinline__ void fill_share(const SortParams& p, uint64_t index) {
+  const uint64_t begin = index * kFillShare, end = min(begin + kFillShare, p.fill_bytes);
+  if (begin >= end) return;
+  uint8_t* const to = p.fill + begin;
+  const uint32_t head = static_cast<uint32_t>(min((16 - reinterpret_cast<uint64_t>(to) % 16) % 16, end - begin));
+  const uint32_t whole = static_cast<uint32_t>((end - begin - head) / 16), tail = static_cast<uint32_t>(end - begin - head) % 16;
+  for (uint32_t i = threadIdx.x; i < whole; i += kSortThreads) reinterpret_cast<uint4*>(to + head)[i] = make_uint4(0, 0, 0, 0);
+  if (threadIdx.x < head / 2) reinterpret_cast<uint16_t*>(to)[threadIdx.x] = 0;
+  if (threadIdx.x < tail / 2) reinterpret_cast<uint16_t*>(to + head + 16ull * whole)[threadIdx.x] = 0;
+}
+
 template <bool First>
 __global__ void __launch_bounds__(kSortThreads) count_kernel(const __grid_constant__ SortParams p) {
   __shared__ uint32_t counts[1 << kMostDigit];
   const uint32_t bins = 1u << p.bits;
   for (uint32_t i = threadIdx.x; i < bins; i += kSortThreads) counts[i] = 0;
   wait_for_kernel_before();
+  if (First && blockIdx.x >= p.ctas) return fill_share(p, blockIdx.x - p.ctas);
   __syncthreads();
   const uint64_t n = First ? p.tokens.n : *p.found, begin = blockIdx.x * p.share, end = min(begin + p.share, n);
   for (uint64_t at = begin; at < end; at += kSortTile) {
@@ -221,6 +234,7 @@ __global__ void __launch_bounds__(kSortThreads) cluster_kernel(const __grid_cons
   const uint32_t bins = 1u << p.bits, me = cluster.block_rank();
   const Shared sh(raw, bins);
   wait_for_kernel_before();
+  if (blockIdx.x >= p.ctas) return fill_share(p, blockIdx.x - p.ctas);  // (other clusters than the first)
   uint64_t n = p.tokens.n;
   for (int pass = 0; pass < passes; ++pass) {
     Met m[kSortEach];
@@ -265,6 +279,7 @@ constexpr uint32_t kCompareEach = 16, kCompareShare = kSortThreads / kCompareEac
 __global__ void __launch_bounds__(kSortThreads) compare_kernel(const __grid_constant__ SortParams p) {
   __shared__ __align__(16) uint32_t rows[kCompareTokens];
   wait_for_kernel_before();
+  if (blockIdx.x >= p.ctas) return fill_share(p, blockIdx.x - p.ctas);
   const uint32_t n = static_cast<uint32_t>(p.tokens.n), whole = (n + 3) / 4;
   uint32_t found = 0;
   for (uint32_t i = threadIdx.x; i < 4 * whole; i += kSortThreads) {
@@ -301,6 +316,8 @@ __global__ void __launch_bounds__(kSortThreads) compare_kernel(const __grid_cons
   if (threadIdx.x % kCompareEach == 0 && row != kAll) p.sorted[0][place] = {row, i};
 }
 
+uint32_t fill_ctas(const SortParams& p) { return static_cast<uint32_t>((p.fill_bytes + kFillShare - 1) / kFillShare); }
+
 cudaError_t launch_cluster(const SortParams& p, int passes, size_t shared, cudaStream_t s) {
   cudaLaunchAttribute a[2] = {};
   a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -309,7 +326,7 @@ cudaError_t launch_cluster(const SortParams& p, int passes, size_t shared, cudaS
   a[1].val.clusterDim.x = p.ctas;
   a[1].val.clusterDim.y = a[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t c = {};
-  c.gridDim = dim3(p.ctas);
+  c.gridDim = dim3((fill_ctas(p) + p.ctas - 1) / p.ctas * p.ctas + p.ctas);
   c.blockDim = dim3(kSortThreads);
   c.dynamicSmemBytes = shared;
   c.stream = s;
@@ -336,7 +353,8 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
   const uint64_t n = p.tokens.n;
   if (n <= kCompareTokens) {
     *last = 0;
-    return launch_chained(compare_kernel, n == 0 ? 1 : static_cast<int>((n + kCompareShare - 1) / kCompareShare), kSortThreads, 0, s, p);
+    p.ctas = n == 0 ? 1 : static_cast<uint32_t>((n + kCompareShare - 1) / kCompareShare);
+    return launch_chained(compare_kernel, static_cast<int>(p.ctas + fill_ctas(p)), kSortThreads, 0, s, p);
   }
   if (n <= kClusterTokens) {
     p.ctas = 1;
@@ -349,7 +367,8 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
   p.share = ((n + kSortCtas - 1) / kSortCtas + kSortTile - 1) / kSortTile * kSortTile;
   p.ctas = static_cast<uint32_t>((n + p.share - 1) / p.share);
   for (p.pass = 0; p.pass < plan.passes; ++p.pass) {
-    cudaError_t e = launch_chained(p.pass == 0 ? count_kernel<true> : count_kernel<false>, static_cast<int>(p.ctas), kSortThreads, 0, s, p);
+    cudaError_t e = launch_chained(p.pass == 0 ? count_kernel<true> : count_kernel<false>, static_cast<int>(p.ctas + (p.pass == 0 ? fill_ctas(p) : 0)),
+                                   kSortThreads, 0, s, p);
     if (e == cudaSuccess)
       e = launch_chained(p.pass == 0 ? place_kernel<true> : place_kernel<false>, static_cast<int>(p.ctas), kSortThreads, shared_bytes(plan.bins()), s, p);
     if (e != cudaSuccess) return e;

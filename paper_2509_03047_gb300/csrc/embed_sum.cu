@@ -7,7 +7,8 @@
 // token.  A range's border inside a row moves to the row's start if the row has no
 // more tokens than a range.  A longer row's parts are added in the ranges' order by
 // the CTA where it ends, or, if it began in another, by a second launch, from the
-// workspace.  Ranges follow from the batch alone, so a repeated call gives the same bits.
+// workspace.  Rows that no token meets are
+// filled with zeros by CTAs of their own, or have been, beside the sort.  Ranges follow from the batch alone, so a repeated call gives the same bits.
 #include <cuda_runtime.h>
 
 #include "embed.h"
@@ -171,8 +172,8 @@ __global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ S
   __shared__ uint32_t ended[kSumWarps], from_inside[kSumWarps], to_inside[kSumWarps];
   wait_for_kernel_before();
   const uint32_t lane = threadIdx.x % 32, warp = threadIdx.x / 32, found = *p.found;
-  if (blockIdx.x >= p.sum_ctas) {
-    if (!Add) clear_rows<V, Bf16Grad>(p, found, (blockIdx.x - p.sum_ctas) * kSumWarps + warp, lane);
+  if (blockIdx.x >= p.ctas) {
+    if (!Add) clear_rows<V, Bf16Grad>(p, found, (blockIdx.x - p.ctas) * kSumWarps + warp, lane);
     return;
   }
   const uint32_t span = span_of(found, p.ranges), cta = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
@@ -367,7 +368,7 @@ template <int Kind, bool Bf16Out, bool Bf16Grad, bool Add>
 cudaError_t launch(const SumParams& p, cudaStream_t s) {
   constexpr int kShared = Ring<Kind, Bf16Out, Bf16Grad, Add>::kShared;
   if (p.configure) return cudaFuncSetAttribute(sum_kernel<Kind, Bf16Out, Bf16Grad, Add>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
-  cudaError_t e = launch_chained(sum_kernel<Kind, Bf16Out, Bf16Grad, Add>, static_cast<int>(p.sum_ctas + p.zero_ctas), kThreads, kShared, s, p);
+  cudaError_t e = launch_chained(sum_kernel<Kind, Bf16Out, Bf16Grad, Add>, static_cast<int>(p.ctas + p.zero_ctas), kThreads, kShared, s, p);
   if (e == cudaSuccess) e = launch_chained(join_kernel<Kind, Bf16Grad, Add>, static_cast<int>(kSms * 2), kJoinThreads, 0, s, p);
   return e;
 }

@@ -8,7 +8,10 @@
 // from shared memory, with the row as the contraction's index or the column, so a
 // block goes there as it is and serves X X^T, X^T X, and products from
 // either side without a transposition.  The square matrices of the smaller side,
-// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike. 
+// S = X X^T (or X^T X) and P = a I + b S + c S^2, are held alike, of them the tiles of
+// 256 x 256 on and below the diagonal.  What X's rounding to fp16 leaves, which no
+// product reads, has blocks of its own kind: chunk c of row r at c * 128 + r, so that
+// a warp's 32 rows of a chunk are 512 bytes.
 //
 // A matrix with an fp32 output (split) has second halves of everything, in blocks like
 // the first ones, which enter the products too.  Its part of the workspace is apart:

@@ -1,14 +1,31 @@
-// muon_product.cu -- the products of the orthogonalised update, all iterations of all
-// matrices of a list in one launch.
+// muon_product.cu -- the products of the orthogonalised update: X X^T, the polynomial
+// in it, the next X, of all matrices of a list.
 //
 // D[i][j] = sum over k of A(i, k) B(j, k), tiles of 256 x 256 by pairs of CTAs, one
 // pair per two SMs, each taking every n-th tile of the list.  A warp brings the
-// factors' blocks, 64 of the contraction at a time; a thread multiplies; eight warps
+// factors' blocks, 64 of the contraction at a time; another multiplies; eight warps
 // turn the sums into fp16 blocks, while the next tile's products fill the other half
 // of tensor memory.  The blocks lie in memory as the tensor cores read them, by rows
 // or by columns, so X X^T, X^T X and products from either side need no
-// transposition, and results leave as they come, by bulk copies.  Of the symmetric
-// products the tiles on and below the diagonal are computed, and read both ways.
+// transposition.  Of the symmetric products the tiles on and below the diagonal are
+// computed, and read both ways.
+//
+// What bounds it, GB300:
+//   products of first halves: the way from L2 to an SM.  A step is 512 clocks of
+//     products and 32 KiB per SM, which take 570 (57 bytes a clock; a tile of 256 x
+//     128, 24 KiB for 256 clocks, 404).  A tile has 500 to 1,000 clocks more before its
+//     first step, a launch some 5 us.  Back to back the power limit counts: 14336 x
+//     4096 five iterations 2.8 ms, 1,400 TFLOP/s of the needed work (half of a symmetric
+//     product), 1,550 with the tiles' upper halves, at 1,550 MHz;
+//   products of both halves: the tensor cores, three times the work for twice the
+//     bytes: 1,670 TFLOP/s of it, at the power limit;
+//   iterates of narrow matrices: HBM, 6 to 8 bytes an element each iteration;
+//   small lists: 8,000 clocks a phase for its way through L2 (stores 1,900 until they
+//     are seen, the wait 1,300, the first copies 1,000 to 3,000).
+// Pairs of 256 x 256, not CTAs of 128 x 256 (22 TB/s from L2 at full rate) or 128 x
+// 128 (29).  Six stages of 32 KiB and 4 KiB per finishing warp, not five and 8: 24
+// layers of width 1024 6.44 -> 5.96 ms.  Second halves go past shared memory, each
+// lane's own.
 #include <algorithm>
 
 #include "kernels.h"
@@ -269,7 +286,7 @@ __device__ __forceinline__ void store_rows(uint8_t* to, const uint8_t* staging, 
   }
 }
 
-// One of the eight warps.  Each by itself: what it adds is on its way while the products run, its 32 rows of 64 columns leave by one copy.
+// One of the eight warps.  Each by itself: what it adds is on its way while the products run, its 32 rows of 64 columns leave together.
 template <bool kSplit>
 __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* staging, Control& c, uint32_t rank) {
   const uint32_t warp = threadIdx.x / 32 - 2, lane = threadIdx.x % 32;

@@ -102,10 +102,6 @@ __device__ __forceinline__ void load_blocks(uint32_t to, const CUtensorMap* map,
                "l"(map), "r"(0), "r"(half), "r"(block), "r"(in_first(bar))
                : "memory");
 }
-__device__ __forceinline__ void load_bytes(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar)
-               : "memory");
-}
 __device__ __forceinline__ void store_bytes(void* to, uint32_t from, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(to), "r"(from), "r"(bytes) : "memory");
 }

@@ -41,19 +41,19 @@ int main() {
     sorts.clear(), sums.clear(), lookups.clear();
     CHECK(fr_embed_grad(p, place(out), out_type, place(1 << 22), 4, n, 0.5f, place(grad), grad_type, accumulate, nullptr) == FR_OK);
     const bool runs = rows && dim && (n || !accumulate);
-    CHECK(sorts.size() == (runs ? 1u : 0u) && sums.size() == sorts.size());
-    if (runs) {
+    CHECK(sorts.size() == (runs ? 1u : 0u) && sums.size() == (runs && n ? 1u : 0u));
+    const bool fill = !accumulate && n < rows;
+    if (runs) CHECK(sorts[0].fill_bytes == (fill ? rows * dim * type_bytes(grad_type) : 0) && (!fill || sorts[0].fill == place(grad)));
+    if (runs && n) {
       const SumParams& q = sums[0];
       const int v = vector_of(q.v);
       CHECK(dim % v == 0 && out % std::min<uint64_t>(16, v * type_bytes(out_type)) == 0 && grad % std::min<uint64_t>(16, v * type_bytes(grad_type)) == 0);
       CHECK(static_cast<uint64_t>(q.tiles) * tile_width(q.v) >= dim && static_cast<uint64_t>(q.tiles - 1) * tile_width(q.v) < dim);
-      CHECK(q.ranges % kSumWarps == 0 && q.ranges >= kSumWarps && (n == 0 || q.ranges <= p->ranges));
-      CHECK(q.sum_ctas == (n ? q.ranges / kSumWarps * q.tiles : 0) && q.sum_ctas + q.zero_ctas > 0);
-      if (accumulate)
-        CHECK(q.zero_ctas == 0);
-      else
+      CHECK(q.ranges % kSumWarps == 0 && q.ranges >= kSumWarps && q.ranges <= p->ranges);
+      CHECK(q.ctas == q.ranges / kSumWarps * q.tiles && (q.zero_ctas == 0) == (accumulate || fill));
+      if (q.zero_ctas)
         CHECK(static_cast<uint64_t>(q.zero_ctas) * kSumWarps * q.rows_per_zero_warp >= rows && q.rows_per_zero_warp >= 1 && q.rows_per_zero_warp <= 32);
-      CHECK(q.sorted == p->d_sorted[(p->sort.passes - 1) % 2] && (q.sorted != nullptr || n == 0));
+      CHECK(q.sorted == p->d_sorted[(p->sort.passes - 1) % 2] && q.sorted != nullptr);
       CHECK(sorts[0].counts != nullptr || n <= kClusterTokens);
     }
     CHECK(fr_embed_lookup(p, place(grad), grad_type, place(1 << 22), 8, n, 2.0f, place(out), out_type, nullptr) == FR_OK);

@@ -130,12 +130,23 @@ def test_gradient_is_its_definition(out, grad, index, dim, shift, accumulate):
     (1, 1, 5, "mixed"), (1, 5000, 40, "mixed"), (2, 4096, 8, "mixed"), (3, 4097, 8, 0.9), (2047, 4096, 16, "zipf"),
     (2048, 8192, 24, "zipf"), (2049, 8193, 16, "zipf"), (2050, 60000, 33, 0.3), (50257, 32768, 64, "zipf"), (50257, 3, 64, "zipf"),
     (130000, 300001, 8, "zipf"), (259, 500001, 21, 0.33), (5000000, 20000, 4, "zipf"), (400, 70000, 2048, 0.6),
-    (9, 100000, 512, 1.0), (1 << 23, 9000, 1, "mixed"), (100, 12000, 4104, "zipf")])
+    (9, 100000, 512, 1.0), (1 << 23, 9000, 1, "mixed"), (100, 12000, 4104, "zipf"), (100000, 70000, 3, "zipf"),
+    (70001, 300, 1, "zipf"), (20000, 6000, 131, "mixed")])
 def test_batches_and_slices_of_many_sizes(rows, n, dim, how, accumulate):
     rng = np.random.default_rng(rows + n)
     tokens = _tokens(rng, n, 5, rows, np.int32, how)
     o, old, got = _gradient(rng, rows, 5, dim, tokens, "bf16", "f32", accumulate, -1.5)
     _check(rows, 5, tokens, o, old, got, accumulate, -1.5)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("dim", DIMS)
+@pytest.mark.parametrize("grad", ["bf16", "f32"])
+def test_gradient_of_fewer_tokens_than_rows(grad, dim, shift):
+    rng = np.random.default_rng(dim + 2)
+    tokens = _tokens(rng, 300, 1000, 1500, np.int64)
+    o, old, got = _gradient(rng, 1500, 1000, dim, tokens, "bf16", grad, False, 0.7, shift)
+    _check(1500, 1000, tokens, o, old, got, False, 0.7)
 
 
 @pytest.mark.parametrize("accumulate", [False, True])
