@@ -213,9 +213,19 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
 // from this SM's first-level cache: other SMs have written it during this launch.)
 struct Addend {
   uint4 x[8];
-  __device__ __forceinline__ void of_square(const uint8_t* block, uint32_t row) {
+  // The warp's 32 rows as they lie, whole lines at a time; to_rows() afterwards.  (Each lane its row's chunks: 32 lines for a load, and the factors'
+  // copies wait behind them, 3,000 clocks instead of 1,000.)
+  __device__ __forceinline__ void of_square(const uint8_t* rows, uint32_t lane) {
 #pragma unroll
-    for (uint32_t c = 0; c < 8; ++c) x[c] = __ldcg(reinterpret_cast<const uint4*>(block + row * 128 + ((c ^ (row % 8)) * 16)));
+    for (uint32_t k = 0; k < 8; ++k) x[k] = __ldcg(reinterpret_cast<const uint4*>(rows + k * 512 + lane * 16));
+  }
+  __device__ __forceinline__ void to_rows(uint8_t* staging, uint32_t lane) {
+#pragma unroll
+    for (uint32_t k = 0; k < 8; ++k) *reinterpret_cast<uint4*>(staging + k * 512 + lane * 16) = x[k];
+    __syncwarp();
+#pragma unroll
+    for (uint32_t c = 0; c < 8; ++c) x[c] = *reinterpret_cast<const uint4*>(staging + lane * 128 + ((c ^ (lane % 8)) * 16));
+    __syncwarp();
   }
   __device__ __forceinline__ void of_low(const uint8_t* block, uint32_t row) {
 #pragma unroll
@@ -227,10 +237,11 @@ struct Addend {
 //   S = X X^T             sums in X's scale twice
 //   P = a I + b S + c S^2
 //   X = P X1 + a X2       X1, X2 the halves of the old X; a I in P has the first one's part.  (kSplit: X = P X, all of it)
-// rounded to fp16, for the factors in shared memory; what the rounding leaves in `rest` (kSplit), or X's to `low` if that is not null.
+// rounded to fp16, for the factors in shared memory; what the rounding leaves in `in_low` (kSplit), whose S has been used, or X's to `low` if that is
+// not null.
 template <int kPhase, bool kSplit>
-__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diagonal, const float (&v)[64], const Addend& in, const Addend& in_low, bool adds,
-                                           uint8_t* staging, uint32_t row, uint8_t* low, Addend& rest) {
+__device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diagonal, const float (&v)[64], const Addend& in, Addend& in_low, bool adds,
+                                           uint8_t* staging, uint32_t row, uint8_t* low) {
 #pragma unroll
   for (uint32_t c = 0; c < 8; ++c) {
     float x[8], y[8];
@@ -256,7 +267,7 @@ __device__ __forceinline__ void finish_row(const float (&coef)[3], uint32_t diag
     }
     uint4* const to = reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16));
     if (kSplit) {
-      split(x, *to, rest.x[c]);
+      split(x, *to, in_low.x[c]);
     } else if (kPhase == kNext && low != nullptr) {
       uint4 lo;
       split(x, *to, lo);
@@ -301,11 +312,12 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
     const bool low_after = !kSplit && p.low >> (tiles.round + 1) & 1, adds = t.phase == kPolynomial || (!kSplit && t.phase == kNext && p.low >> tiles.round & 1);
     const float coef[3] = {p.coef[tiles.round][0], p.coef[tiles.round][1], p.coef[tiles.round][2]};
     uint8_t* const first = p.work + (static_cast<uint64_t>(t.out) + rank * t.across) * kMuonBlockBytes;
-    Addend in, in_low, rest;
+    Addend in, in_low;
     auto fetch = [&](uint32_t q) {
       if (t.phase == kPolynomial) {
-        in.of_square(first + q * kMuonBlockBytes + to_square, row);
-        if (kSplit) in_low.of_square(first + q * kMuonBlockBytes + 3 * to_square, row);
+        const uint8_t* const rows = first + q * kMuonBlockBytes + to_square + quarter * kStaging;
+        in.of_square(rows, lane);
+        if (kSplit) in_low.of_square(rows + 2 * to_square, lane);
       } else {
         in.of_low(first + q * kMuonBlockBytes + to_low, row);
       }
@@ -328,21 +340,26 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
       if (!mine) continue;
       if (lane == 0) wait_stores_read();  // of the rows before
       __syncwarp();
+      if (t.phase == kPolynomial) {
+        in.to_rows(staging, lane);
+        if (kSplit) in_low.to_rows(staging, lane);
+      }
       uint8_t* const block = first + q * kMuonBlockBytes;
       if (t.phase == kGram)
-        finish_row<kGram, kSplit>(coef, 0, v, in, in_low, false, staging, row, nullptr, rest);
+        finish_row<kGram, kSplit>(coef, 0, v, in, in_low, false, staging, row, nullptr);
       else if (t.phase == kPolynomial)  // (the diagonal's column of this row among the block's)
-        finish_row<kPolynomial, kSplit>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, in_low, true, staging, row, nullptr, rest);
+        finish_row<kPolynomial, kSplit>(coef, (t.row + rank) * kBlockRows + row - (2 * t.col + q) * kBlockCols, v, in, in_low, true, staging, row, nullptr);
       else
-        finish_row<kNext, kSplit>(coef, 0, v, in, in_low, adds, staging, row, low_after ? block + to_low : nullptr, rest);
-      if (adds && q + 2 < parts) fetch(q + 2);
+        finish_row<kNext, kSplit>(coef, 0, v, in, in_low, adds, staging, row, low_after ? block + to_low : nullptr);
+      if (!kSplit && adds && q + 2 < parts) fetch(q + 2);
       uint8_t* const to = block + (t.phase == kNext ? static_cast<uint64_t>(tiles.iterate(1)) * kMuonBlockBytes : 0) + quarter * kStaging;
       store_rows(to, staging, lane, p.waits);
       if (kSplit) {
         if (lane == 0) wait_stores_read();
         __syncwarp();
 #pragma unroll
-        for (uint32_t c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16)) = rest.x[c];
+        for (uint32_t c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(staging + row % 32 * 128 + ((c ^ (row % 8)) * 16)) = in_low.x[c];
+        if (adds && q + 2 < parts) fetch(q + 2);
         store_rows(to + (t.phase == kNext ? to_low : 2 * to_square), staging, lane, p.waits);
       }
     }
