@@ -89,10 +89,10 @@ cudaError_t launch_sort(SortParams p, const SortPlan& plan, int* last, cudaStrea
 // ---- the gradient
 
 // How a warp's lanes share a tile of columns.  Vectors of 8, 4, 2, 1 elements, 32 vectors apart; kOdd: rows that do not start on vectors'
-// boundaries, by the 16-byte granules around them.
-constexpr int kOdd = 0;
-constexpr int vector_of(int v) { return v == kOdd ? 1 : v; }
-constexpr int lane_vectors(int v) { return v == kOdd ? 12 : v >= 8 ? 1 : v == 4 ? 2 : 4; }
+// boundaries, by the 16-byte granules around them.  kWide: two vectors of 8.
+constexpr int kOdd = 0, kWide = 16;
+constexpr int vector_of(int v) { return v == kOdd ? 1 : v == kWide ? 8 : v; }
+constexpr int lane_vectors(int v) { return v == kOdd ? 12 : v == kWide ? 2 : v == 8 ? 1 : v == 4 ? 2 : 4; }
 constexpr int tile_width(int v) { return 32 * vector_of(v) * lane_vectors(v); }
 // The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns; a multiple of what a CTA has.
 constexpr uint32_t kSumWarps = 8;
@@ -101,11 +101,14 @@ constexpr uint32_t kSumWarps = 8;
 // 32, 48, 72 warps, us: 500,001 tokens x 321 fp32 155, 159, 173, 182, 215; 32,768 x 768 accumulating 45.6, 48.3, 48.0, 48.5, 48.0; 300,000 x 8
 // accumulating 88, -, -, 72, -; 65,536 x 4,096 137, 153, -, 129, 129.
 constexpr uint32_t kFewRangeWarps = kSms * 16, kRangeWarps = kSms * 48;
-constexpr uint32_t kLeastRange = 32;
+constexpr uint32_t kLeastRange = 32, kShortRange = 8;  // tokens: of a range, of one where a wave of them is not full
 inline uint32_t column_tiles(uint64_t dim, int v) { return static_cast<uint32_t>((dim + tile_width(v) - 1) / tile_width(v)); }
 inline uint32_t ranges_of(uint64_t n, uint32_t tiles, bool few) {
-  const uint64_t most = (n + kLeastRange - 1) / kLeastRange, fill = ((few ? kFewRangeWarps : kRangeWarps) + tiles - 1) / tiles;
-  return static_cast<uint32_t>(((most < fill ? most : fill) + kSumWarps - 1) / kSumWarps * kSumWarps);
+  auto share = [](uint64_t x, uint64_t of) { return (x + of - 1) / of; };
+  const uint64_t wave = share(kFewRangeWarps, tiles), fill = few ? wave : share(kRangeWarps, tiles), whole = share(n, kLeastRange),
+                 brief = share(n, kShortRange) < wave ? share(n, kShortRange) : wave;
+  const uint64_t most = whole > brief ? whole : brief;
+  return static_cast<uint32_t>(share(most < fill ? most : fill, kSumWarps) * kSumWarps);
 }
 struct SumParams {
   const Met* sorted;

@@ -34,6 +34,8 @@ uint32_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
 
 // Rows of odd length up to this go element by element, a lane's four at most.
 constexpr uint64_t kOddLeast = 128;
+// From here on a warp takes 1 KiB or more of a row, not half of it: 65,536 tokens of 4,096 130 -> 123 us (of 768 45 -> 52).
+constexpr uint64_t kWideLeast = 1024;
 
 // With fewer tokens than rows all rows are filled with zeros beside the sort, with more those that no token meets, once they are known: rows that
 // are met are written once then.  (50,257 rows, 8,000 tokens of 768 41 us, by rows 83, 32,768 57 and 84, 131,072 122 and 117; 16,032 rows, 65,536
@@ -46,7 +48,7 @@ fr_status fill_embed(fr_embed p) {
   PlanMemory mem;
   const uint64_t n = p->max_tokens;
   uint64_t elems = 0;
-  for (int v : {kOdd, 1, 2, 4, 8}) {
+  for (int v : {kOdd, 1, 2, 4, 8, kWide}) {
     for (bool few : {false, true}) p->ranges = std::max<uint64_t>(p->ranges, ranges_of(n, column_tiles(p->dim, v), few));
   }
   elems = 2 * (p->ranges / kSumWarps) * p->dim;
@@ -198,6 +200,7 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.scale = scale;
   q.v = vector_elems(p->dim, out, type_bytes(out_dtype), grad, type_bytes(grad_dtype));
   if (q.v == 1 && p->dim > kOddLeast) q.v = kOdd;
+  if (q.v == 8 && p->dim >= kWideLeast) q.v = kWide;
   q.tiles = column_tiles(p->dim, q.v);
   q.ranges = std::max(kSumWarps, ranges_of(n, q.tiles, q.v == kOdd || (accumulate && q.tiles > 1)));
   q.ctas = q.ranges / kSumWarps * q.tiles;

@@ -25,7 +25,7 @@ constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ uint32_t span_of(uint32_t found, uint32_t ranges) {
   const uint32_t share = (found + ranges - 1) / ranges;
-  return share < kLeastRange ? kLeastRange : share;
+  return share < kShortRange ? kShortRange : share;
 }
 
 // The first place in [lo, hi) whose row is `row` or above, or hi; 32 places are looked at together.
@@ -387,8 +387,8 @@ cudaError_t launch_wide(const SumParams& p, cudaStream_t s) {
 cudaError_t configure_sum() {
   SumParams p = {};
   p.configure = 1;
-  for (int k = 0; k < 40; ++k) {
-    p.v = k / 8 == 4 ? kOdd : 1 << k / 8;
+  for (int k = 0; k < 48; ++k) {
+    p.v = k / 8 == 5 ? kOdd : 1 << k / 8;
     p.bf16_out = k & 1;
     p.bf16_grad = k >> 1 & 1;
     p.accumulate = k >> 2 & 1;
@@ -404,6 +404,7 @@ cudaError_t launch_sum(const SumParams& p, cudaStream_t s) {
     case 4: return launch_wide<4>(p, s);
     case 2: return launch_wide<2>(p, s);
     case kOdd: return launch_wide<kOdd>(p, s);
+    case kWide: return launch_wide<kWide>(p, s);
     default: return launch_wide<1>(p, s);
   }
 }
