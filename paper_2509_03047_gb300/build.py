@@ -51,6 +51,11 @@ KERNEL_FILES = ["sweep_fp.cu", "sweep_pack.cu", "sweep_unpack.cu", "sweep_unpack
 OPTIM_KERNEL_FILES = ["optim_clip.cu", "optim_step.cu", "optim_convert.cu", "optim_block.cuh", "optim_math.cuh", "optim.h",
                       "kernels.h"]
 
+# Those of the orthogonalised update and of the embedding.
+MUON_KERNEL_FILES = ["muon_elements.cu", "muon_product.cu", "muon_block.cuh", "muon_tiles.h", "tensor_core.cuh", "muon.h", "optim_math.cuh", "optim.h",
+                     "kernels.h"]
+EMBED_KERNEL_FILES = ["embed_lookup.cu", "embed_sort.cu", "embed_sum.cu", "embed_vector.cuh", "embed.h", "optim.h", "kernels.h"]
+
 
 def _code_only(text: str) -> str:
     """`text` without its C/C++ comments, trailing blanks and blank lines:
@@ -88,6 +93,15 @@ def source_digest(kernels_only: bool = False) -> str:
 def optim_digest() -> str:
     """The same of the optimizer step's device-kernel files."""
     return _digest(OPTIM_KERNEL_FILES)
+
+
+def muon_digest() -> str:
+    """And of the orthogonalised update's, with the file that cuts its products into tiles."""
+    return _digest(MUON_KERNEL_FILES)
+
+
+def embed_digest() -> str:
+    return _digest(EMBED_KERNEL_FILES)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:

@@ -254,6 +254,11 @@ int main() {
   clear();
   CHECK(fr_muon_step(p, &h, nullptr, nullptr) == FR_OK && products[0].p.low == 0x0F && iterates[0].low == 1 && applies[0].last == 1);
 
+  // a wait that a kernel gave up is reported once
+  CHECK(fr_muon_sync_status(p, nullptr) == FR_OK);
+  *p->d_status = 1;
+  CHECK(fr_muon_sync_status(p, nullptr) == FR_ERR_DEVICE_TIMEOUT && fr_muon_sync_status(p, nullptr) == FR_OK && *p->d_status == 0);
+
   // refusals launch nothing
   clear();
   auto refuses = [&](auto change) {

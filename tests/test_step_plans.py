@@ -7,6 +7,7 @@ import pytest
 import torch
 
 from host_tests import build_host_test
+from paper_2509_03047_gb300 import build
 
 fr = pytest.importorskip("paper_2509_03047_gb300.flashrec")
 
@@ -56,3 +57,20 @@ def test_numbers_of_a_step():
     h = fr.muon(lr=0.5, coefficients=[(1, 2, 3), (4, 5, 6)], nesterov=False, step=7, seed=9, rounding=1, products=1)
     assert (h.lr, h.beta, h.iterations, h.nesterov, h.step, h.seed, h.rounding, h.products) == (0.5, 0.95, 2, 0, 7, 9, 1, 1)
     assert list(h.coef[1]) == [4.0, 5.0, 6.0] and list(h.coef[2]) == [0.0, 0.0, 0.0]
+
+
+@pytest.mark.parametrize("files,digest", [(build.MUON_KERNEL_FILES, build.muon_digest), (build.EMBED_KERNEL_FILES, build.embed_digest)])
+def test_a_digest_changes_with_its_own_sources(files, digest, monkeypatch, tmp_path):
+    csrc = tmp_path / "csrc"
+    shutil.copytree(build.CSRC, csrc)
+    monkeypatch.setattr(build, "CSRC", str(csrc))
+    before = digest()
+    for name in build.SOURCES + build.HEADERS:
+        path = csrc / name
+        text = path.read_text()
+        path.write_text(text + "\n// a comment\n")
+        assert digest() == before
+        path.write_text(text + "\nint more;\n")
+        assert (digest() != before) == (name in files), name
+        path.write_text(text)
+    assert digest() == before
