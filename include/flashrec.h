@@ -587,7 +587,7 @@ typedef struct {
  *   G  = m, or with nesterov beta m + (1 - beta) h
  *   p <- p - lr lr_scale (update_scale O(G) + weight_decay decay_scale p)
  * `clip_dev`: as in fr_adamw_step; if it counts a non-finite gradient the step leaves
- * every byte as it is.
+ * every byte as it is.  In a CUDA graph the numbers in `hyper` are those of the capture.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_CUDA. */
 fr_status fr_muon_step(fr_muon_plan plan, const fr_muon* hyper, const fr_clip* clip_dev, void* stream);
 
@@ -638,8 +638,10 @@ fr_status fr_embed_lookup(fr_embed plan, const void* table, uint32_t table_dtype
 
 /* grad[r] = scale * (the sum of out[i] over the tokens i of row first + r), all
  * `rows` rows, or with `accumulate` 1 added to what is there, where rows that no
- * token meets are not touched.  Sums are in fp32, parts of at most n / 12,000 (or n *
- * dim / 3 million, or 8) tokens one after the other, rounded once at the end.  `out` is read only.
+ * token meets are not touched.  Sums are in fp32: a row's tokens in the batch's
+ * order, those of long rows in parts that are added one after the other;
+ * the product with scale, and what is there, are rounded once.  `out` is read only; no
+ * buffers may overlap.
  * Errors: as fr_embed_lookup. */
 fr_status fr_embed_grad(fr_embed plan, const void* out, uint32_t out_dtype, const void* tokens, uint32_t token_bytes,
                         uint64_t n, float scale, void* grad, uint32_t grad_dtype, uint32_t accumulate, void* stream);

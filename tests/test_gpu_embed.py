@@ -131,7 +131,7 @@ def test_gradient_is_its_definition(out, grad, index, dim, shift, accumulate):
     (2048, 8192, 24, "zipf"), (2049, 8193, 16, "zipf"), (2050, 60000, 33, 0.3), (50257, 32768, 64, "zipf"), (50257, 3, 64, "zipf"),
     (130000, 300001, 8, "zipf"), (259, 500001, 21, 0.33), (5000000, 20000, 4, "zipf"), (400, 70000, 2048, 0.6),
     (9, 100000, 512, 1.0), (1 << 23, 9000, 1, "mixed"), (100, 12000, 4104, "zipf"), (100000, 70000, 3, "zipf"),
-    (70001, 300, 1, "zipf"), (20000, 6000, 131, "mixed")])
+    (70001, 300, 1, "zipf"), (20000, 6000, 131, "mixed"), (300000, 70000, 4, "mixed")])
 def test_batches_and_slices_of_many_sizes(rows, n, dim, how, accumulate):
     rng = np.random.default_rng(rows + n)
     tokens = _tokens(rng, n, 5, rows, np.int32, how)
@@ -268,3 +268,49 @@ def test_offsets_past_32_bits():
     assert torch.equal(table[tokens[0]].float(), want[0].bfloat16().float())
     assert torch.equal(table[tokens[1:3]].float(), want[1:3])
     assert int(torch.count_nonzero(table[1:rows - 2])) == 0
+
+
+def test_an_empty_slice_and_empty_rows():
+    plan = fr.EmbedPlan(0, 6, 100, first=50)
+    tokens = torch.arange(40, 60, device="cuda")
+    table = torch.empty(0, 6, device="cuda")
+    out = plan.lookup(table, tokens, out=torch.full((20, 6), 7.0, device="cuda"))
+    assert not out.any()
+    assert plan.grad(out, tokens).shape == (0, 6)
+    empty = fr.EmbedPlan(4, 0, 100)
+    assert empty.lookup(torch.empty(4, 0, device="cuda"), tokens).shape == (20, 0)
+    assert empty.grad(torch.empty(20, 0, device="cuda"), tokens).shape == (4, 0)
+    torch.cuda.synchronize()
+
+
+def test_calls_that_the_binding_refuses():
+    plan = fr.EmbedPlan(10, 4, 8)
+    table, tokens = torch.zeros(10, 4, device="cuda"), torch.zeros(5, dtype=torch.int64, device="cuda")
+    out = torch.zeros(5, 4, device="cuda")
+    for bad in (lambda: plan.lookup(table[:9], tokens), lambda: plan.lookup(table, tokens, out=out[:4]), lambda: plan.lookup(table.half(), tokens),
+                lambda: plan.lookup(table, tokens.short()), lambda: plan.lookup(table, tokens.cpu()), lambda: plan.lookup(table.cpu(), tokens),
+                lambda: plan.lookup(torch.zeros(4, 10, device="cuda").t(), tokens), lambda: plan.grad(out, tokens, table[:, :3]),
+                lambda: plan.grad(out, tokens, accumulate=True), lambda: plan.grad(out[:4], tokens)):
+        with pytest.raises(ValueError):
+            bad()
+    many = torch.zeros(9, dtype=torch.int32, device="cuda")
+    with pytest.raises(fr.FlashrecError, match="more tokens"):
+        plan.lookup(table, many)
+    with pytest.raises(fr.FlashrecError, match="scale"):
+        plan.lookup(table, tokens, scale=float("nan"))
+    with pytest.raises(fr.FlashrecError, match="scale"):
+        plan.grad(out, tokens, scale=1e39)
+    torch.cuda.synchronize()
+
+
+def test_a_batch_among_two_streams():
+    """Lookups of one plan on two streams at once (they use no memory of it)."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    table = torch.randn(500, 64, generator=gen, device="cuda")
+    plan, streams = fr.EmbedPlan(500, 64, 30000), [torch.cuda.Stream() for _ in range(2)]
+    tokens = [torch.randint(0, 500, (30000,), generator=gen, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [plan.lookup(table, t, stream=s) for t, s in zip(tokens, streams)]
+    torch.cuda.synchronize()
+    for t, o in zip(tokens, got):
+        assert torch.equal(o, table[t])

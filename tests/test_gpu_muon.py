@@ -347,3 +347,41 @@ def test_a_matrix_gives_the_same_bits_in_a_long_list():
         _, among = _orthogonalize([g] * 40, update=update)
         for o in among:
             assert alone[0].tobytes() == o.tobytes()
+
+
+@pytest.mark.parametrize("param", ["master", "bf16"])
+def test_a_long_list_from_a_graph(param):
+    """More tiles than go through all iterations in one launch."""
+    shapes = [(600, 700)] * 30 + [(1024, 1100)] * 12 + [(300, 200)] * 40
+    eager, graphed = (Step(shapes, param, "bf16") for _ in range(2))
+    record, graph = _record(0.5), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        graphed.plan.step(graphed.hyper(), record)
+    eager.plan.step(eager.hyper(), record)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert eager.plan.sync_status() == graphed.plan.sync_status() == fr.FR_OK
+    a, b = eager.get(), graphed.get()
+    for k in a:
+        for x, y in zip(a[k], b[k]):
+            assert x.tobytes() == y.tobytes()
+    eager.check(0.5)
+
+
+def test_refused_calls_leave_everything():
+    s = Step(SMALL, "bf16", "bf16")
+    before = s.get()
+    for change in (dict(lr=-1.0), dict(lr=float("nan")), dict(beta=1.0), dict(step=0), dict(coefficients=[(16.0, 0.0, 0.0)]), dict(rounding=2),
+                   dict(products=2), dict(weight_decay=float("inf"))):
+        with pytest.raises(fr.FlashrecError):
+            s.plan.step(s.hyper(**change))
+    with pytest.raises(fr.FlashrecError, match="update"):
+        s.plan.orthogonalize()
+    with pytest.raises(ValueError):
+        s.plan.step(s.hyper(), torch.zeros(2, dtype=torch.int64))
+    torch.cuda.synchronize()
+    after = s.get()
+    for k in before:
+        for x, y in zip(before[k], after[k]):
+            assert x.tobytes() == y.tobytes()
