@@ -18,7 +18,7 @@ struct fr_embed_s {
   void* d_memory = nullptr;
   uint64_t rows = 0, dim = 0, max_tokens = 0, first = 0, device_bytes = 0;
   SortPlan sort;
-  uint64_t ranges = 0;  // the most that any vector width has
+  uint64_t ranges = 0;  // the most that a call has
   Met* d_sorted[2] = {};
   uint32_t* d_counts = nullptr;
   uint32_t* d_longs = nullptr;
@@ -32,11 +32,6 @@ bool on(const void* p, uint64_t bytes) { return reinterpret_cast<uintptr_t>(p) %
 bool is_float(uint32_t dtype) { return dtype == FR_DT_BF16 || dtype == FR_DT_F32; }
 uint32_t type_bytes(uint32_t dtype) { return dtype == FR_DT_F32 ? 4 : 2; }
 
-// Rows of odd length up to this go element by element, a lane's four at most.
-constexpr uint64_t kOddLeast = 128;
-// From here on a warp takes 1 KiB or more of a row, not half of it: 65,536 tokens of 4,096 130 -> 123 us (of 768 45 -> 52).
-constexpr uint64_t kWideLeast = 1024;
-
 // With fewer tokens than rows all rows are filled with zeros beside the sort, with more those that no token meets, once they are known: rows that
 // are met are written once then.  (50,257 rows, 8,000 tokens of 768 41 us, by rows 83, 32,768 57 and 84, 131,072 122 and 117; 16,032 rows, 65,536
 // tokens of 4,096 138 and 130.)
@@ -47,16 +42,12 @@ constexpr uint64_t kMostRows = (1ull << 31) - 1, kMostDim = 1ull << 20, kMostEle
 fr_status fill_embed(fr_embed p) {
   PlanMemory mem;
   const uint64_t n = p->max_tokens;
-  uint64_t elems = 0;
-  for (int v : {kOdd, 1, 2, 4, 8, kWide}) {
-    for (bool few : {false, true}) p->ranges = std::max<uint64_t>(p->ranges, ranges_of(n, column_tiles(p->dim, v), few));
-  }
-  elems = 2 * (p->ranges / kSumWarps) * p->dim;
+  if (p->dim > 0) p->ranges = std::max(ranges_of(n, p->dim, false), ranges_of(n, p->dim, true));
   mem.scratch(&p->d_sorted[0], n);
   if (p->sort.passes > 1) mem.scratch(&p->d_sorted[1], n);
   if (n > kClusterTokens) mem.scratch(&p->d_counts, static_cast<uint64_t>(kSortCtas) * p->sort.bins());
   mem.scratch(&p->d_longs, p->ranges / kSumWarps);
-  mem.scratch(&p->d_parts, elems);
+  mem.scratch(&p->d_parts, 2 * (p->ranges / kSumWarps) * p->dim);
   mem.scratch(&p->d_numbers, 2);
   p->device_bytes = mem.scratch_bytes();
   cudaError_t e = mem.commit(&p->d_memory);
@@ -198,11 +189,9 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.grad = grad;
   q.dim = p->dim;
   q.scale = scale;
-  q.v = vector_elems(p->dim, out, type_bytes(out_dtype), grad, type_bytes(grad_dtype));
-  if (q.v == 1 && p->dim > kOddLeast) q.v = kOdd;
-  if (q.v == 8 && p->dim >= kWideLeast) q.v = kWide;
+  q.v = kind_of(p->dim, vector_elems(p->dim, out, type_bytes(out_dtype), grad, type_bytes(grad_dtype)));
   q.tiles = column_tiles(p->dim, q.v);
-  q.ranges = std::max(kSumWarps, ranges_of(n, q.tiles, q.v == kOdd || (accumulate && q.tiles > 1)));
+  q.ranges = ranges_of(n, p->dim, accumulate);
   q.ctas = q.ranges / kSumWarps * q.tiles;
   q.rows = p->rows;
   if (!accumulate && !fill) {

@@ -7,8 +7,12 @@
 // of one digit are found by a vote, those of the warps before by a table of counts
 // per warp and digit.  Nothing depends on the order in which anything runs.
 //
-// A batch of up to 4,096 tokens is sorted by comparing each with all, one of up to 65,536 in one launch, by a cluster of CTAs that
-// read each other's counts from shared memory; a larger one by two launches per pass.
+// A batch of up to 4,096 tokens is sorted by comparing each with all, one of up to
+// 65,536 in one launch, by a cluster of CTAs that read each other's counts from shared
+// memory; a larger one by two launches per pass.
+//
+// Bound by latencies (a pass: tokens, votes, the counts of all CTAs, the places, 8
+// us): 32,768 tokens 18 us, 65,536 20, 500,001 of 259 rows 24.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 

@@ -7,8 +7,13 @@
 // token.  A range's border inside a row moves to the row's start if the row has no
 // more tokens than a range.  A longer row's parts are added in the ranges' order by
 // the CTA where it ends, or, if it began in another, by a second launch, from the
-// workspace.  Rows that no token meets are
-// filled with zeros by CTAs of their own, or have been, beside the sort.  Ranges follow from the batch alone, so a repeated call gives the same bits.
+// workspace.  Rows that no token meets are filled with zeros by CTAs of their own, or
+// have been, beside the sort.  Ranges follow from the batch and the sizes alone, so a
+// repeated call gives the same bits, at any addresses.
+//
+// Bound by gathering rows: 65,536 tokens of 4,096 in bf16 94 us, 5.4 TB/s (HBM 69%;
+// latencies, three batches of a range on their way); by instructions with odd rows:
+// 500,001 tokens of 321 in fp32 115 us, 5.7 TB/s.
 #include <cuda_runtime.h>
 
 #include "embed.h"
@@ -162,8 +167,9 @@ struct Ring {
   }
 };
 
+// (CTAs per SM: with three a wide row's registers spill, 124 -> 144 us; with them odd rows go from 138 to 125.)
 template <int Kind, bool Bf16Out, bool Bf16Grad, bool Add>
-__global__ void __launch_bounds__(kThreads) sum_kernel(const __grid_constant__ SumParams p) {
+__global__ void __launch_bounds__(kThreads, Kind == kWide ? 2 : 3) sum_kernel(const __grid_constant__ SumParams p) {
   using R = Ring<Kind, Bf16Out, Bf16Grad, Add>;
   constexpr int V = R::V, kVectors = R::kVectors, kWidth = R::kWidth, kBatch = R::kBatch;
   extern __shared__ __align__(16) uint8_t raw[];

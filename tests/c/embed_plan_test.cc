@@ -47,6 +47,7 @@ int main() {
     if (runs && n) {
       const SumParams& q = sums[0];
       const int v = vector_of(q.v);
+      CHECK(q.ranges == ranges_of(n, dim, accumulate));  // not of the addresses
       CHECK(dim % v == 0 && out % std::min<uint64_t>(16, v * type_bytes(out_type)) == 0 && grad % std::min<uint64_t>(16, v * type_bytes(grad_type)) == 0);
       CHECK(static_cast<uint64_t>(q.tiles) * tile_width(q.v) >= dim && static_cast<uint64_t>(q.tiles - 1) * tile_width(q.v) < dim);
       CHECK(q.ranges % kSumWarps == 0 && q.ranges >= kSumWarps && q.ranges <= p->ranges);

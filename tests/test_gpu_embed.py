@@ -168,12 +168,15 @@ def test_a_plan_s_next_calls_know_nothing_of_the_ones_before():
         _check(3000, 0, tokens, o, old, got, accumulate, 1.0)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("dim", [72, 264, 1032, 321])
 @pytest.mark.parametrize("how", ["zipf", 0.7])
-def test_repeated_calls_and_other_addresses_give_the_same_bits(how):
+def test_repeated_calls_and_other_addresses_give_the_same_bits(how, dim, accumulate):
+    """On and off the vectors' boundaries."""
     tokens = _tokens(np.random.default_rng(3), 50000, 0, 700, np.int64, how)
     first = None
-    for shift in (0, 0, 0, 8):  # (both places are on the vectors' boundaries; off them other columns share a warp, sums do not change)
-        _, _, got = _gradient(np.random.default_rng(4), 700, 0, 72, tokens, "f32", "f32", False, 1.0, shift)
+    for shift in (0, 0, 8, 1):
+        _, _, got = _gradient(np.random.default_rng(4), 700, 0, dim, tokens, "bf16", "f32", accumulate, 1.0, shift)
         first = got if first is None else first
         assert got.tobytes() == first.tobytes()
 
