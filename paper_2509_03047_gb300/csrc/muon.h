@@ -126,8 +126,9 @@ struct __attribute__((aligned(16))) MuonTile {
   uint32_t reserved[2];
 };
 static_assert(sizeof(MuonTile) == 96, "six loads of 16 bytes");
-// kNarrow: 128 columns.  kAColumns, kBColumns: a factor is read by its columns, else its rows.  kSecond: there are rows for the second CTA.
-enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kAIterate = 16, kBIterate = 32 };
+// kNarrow: 128 columns.  kAColumns, kBColumns: a factor is read by its columns, else its rows.  kSecond: there are rows for the second CTA.  kSame:
+// on the diagonal, both factors are the same blocks.
+enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kAIterate = 16, kBIterate = 32, kSame = 64 };
 constexpr uint32_t kSignals = 16;  // of a tile: two CTAs, eight warps
 
 // One launch takes a list through some iterations, or a phase of one: its tiles in order, iteration after iteration, each pair every n-th.  A tile waits until all

@@ -84,7 +84,7 @@ struct Tiles {
   }
   // How often the counter that the tile needs must have been added to.
   __device__ __forceinline__ uint32_t count() const { return now.count * (now.phase == kGram ? round : round + 1); }
-  // The place of the iterate before or after this round.
+  // The place of the iterate before or after this iteration.
   __device__ __forceinline__ uint32_t iterate(uint32_t after) const { return (round + after) % 2 ? p.x_blocks : 0; }
 
  private:
@@ -125,7 +125,8 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
       if (!__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
       before_reading_copies();
     }
-    const uint32_t bytes = (kSplit ? 2 : 1) * (2 * kFactorBytes + (narrow ? kFactorBytes : 2 * kFactorBytes));
+    const bool same = t.flags & kSame;
+    const uint32_t bytes = (kSplit ? 2 : 1) * (2 * kFactorBytes + (same ? 0 : narrow ? kFactorBytes : 2 * kFactorBytes));
     const int32_t a_low = 2 * static_cast<int32_t>(t.flags & kAIterate ? p.x_blocks : p.p_blocks),
                   b_low = 2 * static_cast<int32_t>(t.flags & kBIterate ? p.x_blocks : p.p_blocks);
     // (few instructions per step: one thread takes 4 to 6 clocks for each, and 512 clocks of products wait for it)
@@ -143,10 +144,10 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
       if (one_lane()) {
         if (rank == 0) expect_bytes(full, bytes);
         load_blocks(to, a_map, a.half, a.block, full);
-        load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
+        if (!same) load_blocks(to + kFactorBytes, b_map, b.half, b.block, full);
         if (kSplit) {
           load_blocks(to + 2 * kFactorBytes, a_map, a.half, a.block + a_low, full);
-          load_blocks(to + 3 * kFactorBytes, b_map, b.half, b.block + b_low, full);
+          if (!same) load_blocks(to + 3 * kFactorBytes, b_map, b.half, b.block + b_low, full);
         }
       }
       __syncwarp();
@@ -174,7 +175,7 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
       a_step = a_columns ? 2048 >> 4 : 32 >> 4;
       b_step = b_columns ? 2048 >> 4 : 32 >> 4;
       a0 = factor(ring_at, a_columns, kHalf);
-      b0 = factor(ring_at + kFactorBytes, b_columns, kHalf);
+      b0 = factor(ring_at + (t.flags & kSame ? 0 : kFactorBytes), b_columns, kHalf);
     };
     set();
     if (!__all_sync(0xFFFFFFFFu, wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up))) return let_copies_land();

@@ -87,7 +87,7 @@ struct ProductOf {
     t.square = square;
     t.depth = depth;
     t.flags = (narrow ? kNarrow : 0) | (a.by_columns ? kAColumns : 0) | (b.by_columns ? kBColumns : 0) | (second ? kSecond : 0) |
-              (a.iterate ? kAIterate : 0) | (b.iterate ? kBIterate : 0);
+              (a.iterate ? kAIterate : 0) | (b.iterate ? kBIterate : 0) | (phase != kNext && r == c && !narrow ? kSame : 0);
     t.across = 2 * cols;
     t.out = out + r * t.across + 2 * c;
     t.row = static_cast<uint16_t>(r);

@@ -109,6 +109,11 @@ void check_tile(const MuonTile& t, const MuonDesc& d) {
     check_factor(walk(t.b[rank], half, t.b_next, b_cols, t.b_switch, t.b_after[rank], t.square, t.depth), b_x ? x : sq,
                  b_x ? d.col_blocks : 2 * side, b_cols, !b_x, narrow ? t.col : t.col + rank, rank, narrow);
   }
+  const bool same = t.flags & kSame;
+  CHECK(same == (phase != kNext && t.row == t.col && !narrow));
+  if (same)
+    for (uint32_t rank = 0; rank < 2; ++rank)
+      CHECK(t.a[rank] == t.b[rank] && t.a_after[rank] == t.b_after[rank] && t.a_switch == t.b_switch && t.a_next == t.b_next && a_cols == b_cols && second);
   CHECK(t.across == 2 * cols && t.out == (phase == kGram ? s : phase == kPolynomial ? q : x) + t.row * t.across + 2 * t.col);
 }
 
