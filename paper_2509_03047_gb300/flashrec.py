@@ -627,14 +627,14 @@ _TOKENS = {torch.int32: 4, torch.int64: 8}
 
 def _buffer(name: str, t: torch.Tensor, allowed):
     """(address, code of the type) of a contiguous CUDA tensor"""
-    if t.numel() and not t.is_cuda:
-        raise ValueError("%s is not on a CUDA device" % name)
-    if not t.is_contiguous():
-        raise ValueError("%s is not contiguous" % name)
     code = allowed.get(t.dtype)
     if code is None:
         raise ValueError("%s: unsupported dtype %s" % (name, t.dtype))
-    return (t.data_ptr() if t.numel() else None), code
+    if not t.is_cuda and t.numel():
+        raise ValueError("%s is not on a CUDA device" % name)
+    if not t.is_contiguous():
+        raise ValueError("%s is not contiguous" % name)
+    return t.data_ptr(), code  # (of an empty tensor 0, NULL)
 
 
 def fr_embed_create(rows: int, dim: int, max_tokens: int, first: int = 0):
@@ -904,9 +904,9 @@ class EmbedPlan:
             pass
 
     def _here(self, name: str, t: torch.Tensor, shape) -> None:
-        if t.numel() and t.device != self.device:
+        if t.get_device() != self.device.index and t.numel():
             raise ValueError("%s is on %s, the plan on %s" % (name, t.device, self.device))
-        if shape is not None and tuple(t.shape) != tuple(shape):
+        if shape is not None and t.shape != shape:
             raise ValueError("%s has the shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
 
     def lookup(self, table: torch.Tensor, tokens: torch.Tensor, scale: float = 1.0, out: Optional[torch.Tensor] = None,
