@@ -3,6 +3,11 @@
 //
 // Every operation is written as the one rounding that it is, as in
 // optim_math.cuh, so both passes over the momentum see the same G.
+//
+// Bound by memory, at two thirds of its rate: 88 million elements in bf16 with their
+// momenta, norm 165 us (10 bytes an element, 5.3 TB/s; each CTA waits for its stores
+// before it is counted), X from it 169 (10), weights 106 (6).  More loads at a time, shorter and longer CTAs,
+// and lists cut into parts that L2 holds are slower or equal.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
