@@ -81,6 +81,8 @@ def train(steps=60, quiet=False):
         adamw.step = muon.step = step + 1
         for rank in ranks:
             rank.step(mean, adamw, muon)
+        if any(rank.muon.sync_status() != fr.FR_OK for rank in ranks):
+            raise RuntimeError("a wait was given up in step %d: its replica is to be restored" % step)
         n = fr.diff(ranks[0].plan.fingerprint(), ranks[1].plan.fingerprint())[1]
         if n:
             raise RuntimeError("the replicas differ in %d chunks after step %d" % (n, step))

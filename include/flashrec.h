@@ -597,8 +597,12 @@ fr_status fr_muon_step(fr_muon_plan plan, const fr_muon* hyper, const fr_clip* c
 fr_status fr_orthogonalize(fr_muon_plan plan, const fr_muon* hyper, void* stream);
 
 /* Synchronize `stream`, then return and clear the condition that the plan's kernels
- * recorded: FR_ERR_DEVICE_TIMEOUT, a wait inside a kernel given up after seconds (weights
- * and updates are left as they were, then and until this call), else FR_OK. */
+ * recorded: FR_ERR_DEVICE_TIMEOUT, a wait inside a kernel given up after seconds, else
+ * FR_OK.  The step that gave up left weights, masters and updates as they were, but its
+ * momenta are those after it: restore the state (from a replica, as after any other failure of
+ * a rank) rather than repeat the step, which would count its gradient twice.  The plan's
+ * calls after it leave every byte, and return FR_OK all the same, until this call: ask before
+ * the state is used, saved or sent. */
 fr_status fr_muon_sync_status(fr_muon_plan plan, void* stream);
 
 /* ---------------------------------------------------------------- embeddings */

@@ -82,7 +82,7 @@ struct MuonParams {
   MuonNorm* norms;
   uint8_t* work;
   const fr_clip* clip;     // may be null
-  const uint32_t* status;  // not zero: a product gave up, nothing is written
+  const uint32_t* status;  // not zero: a product gave up, no momentum, weight or update is written
   float beta, beta_rest;   // beta, 1 - beta
   float lr, decay;
   uint32_t momentum;       // 0: G is the gradient
@@ -130,6 +130,7 @@ static_assert(sizeof(MuonTile) == 96, "six loads of 16 bytes");
 // on the diagonal, both factors are the same blocks.
 enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kAIterate = 16, kBIterate = 32, kSame = 64 };
 constexpr uint32_t kSignals = 16;  // of a tile: two CTAs, eight warps
+constexpr int64_t kWaitClocks = 4ll << 30;  // some two seconds
 
 // One launch takes a list through some iterations, or a phase of one: its tiles in order, iteration after iteration, each pair every n-th.  A tile waits until all
 // those that it reads from have counted; they come before it in that order, and all CTAs are resident, so every wait ends.
@@ -140,6 +141,7 @@ struct MuonProduct {
   uint8_t* work;
   const fr_clip* clip;
   uint32_t* status;         // set to 1 by a kernel that gave up a wait
+  int64_t wait_clocks;      // after which it does
   uint32_t* done;           // counters, zero at the start
   uint32_t x_blocks;        // of all iterates: from x[0] to x[1], from either to its second halves twice as far
   uint32_t p_blocks;        // from P to S, the same

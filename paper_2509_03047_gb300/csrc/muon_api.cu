@@ -39,6 +39,7 @@ struct fr_muon_plan_s {
   MuonNorm* d_norms = nullptr;
   uint8_t* d_work = nullptr;
   uint32_t* d_status = nullptr;
+  int64_t wait_clocks = kWaitClocks;
   MuonMaps maps;
 };
 
@@ -253,6 +254,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   q.work = p->d_work;
   q.clip = mp.clip;
   q.status = p->d_status;
+  q.wait_clocks = p->wait_clocks;
   q.done = p->d_done;
   // Of first halves alone: an iterate keeps its second ones if the iterations after it raise small singular values, and a rounding among them, by
   // more than 4.

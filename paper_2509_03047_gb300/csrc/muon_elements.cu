@@ -100,7 +100,9 @@ __global__ void __launch_bounds__(kElementThreads) norm_kernel(const __grid_cons
   const uint32_t t = p.units[blockIdx.x], lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const MuonDesc& d = p.tensors[t];
   wait_for_kernel_before();
-  if (skipped(p)) return;
+  // (after a wait that was given up momenta stay too, as long as nobody has asked)
+  const bool stopped = p.momentum && *p.status != 0;
+  if (skipped(p) || stopped) return;
   const float scale = grad_scale(p);
   const uint64_t n = d.rows * d.cols, first = static_cast<uint64_t>(blockIdx.x - d.first_unit) * kUnit;
   constexpr int kEach = kUnit / (8 * kElementThreads);

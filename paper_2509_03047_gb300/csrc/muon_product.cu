@@ -122,7 +122,7 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
                static_cast<int32_t>(t.b_next), b_columns};
     const CUtensorMap *a_map = a_columns ? &maps.columns : &maps.rows, *b_map = narrow ? &maps.half : b_columns ? &maps.columns : &maps.rows;
     if (p.waits) {
-      if (!__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), &c.gave_up))) return let_copies_land();
+      if (!__all_sync(0xFFFFFFFFu, wait_count(p.done + t.needs, tiles.count(), p.wait_clocks, &c.gave_up))) return let_copies_land();
       before_reading_copies();
     }
     const bool same = t.flags & kSame;
@@ -140,7 +140,7 @@ __device__ __forceinline__ void bring(const MuonProduct& p, const MuonMaps& maps
         b_map = narrow ? &maps.half : &maps.columns;
       }
       const uint32_t full = full0 + r.stage * 8, to = ring_at + r.stage * kStageBytes;
-      if (!__all_sync(0xFFFFFFFFu, wait_phase(empty0 + r.stage * 8, r.phase ^ 1, &c.gave_up))) return let_copies_land();
+      if (!__all_sync(0xFFFFFFFFu, wait_phase(empty0 + r.stage * 8, r.phase ^ 1, p.wait_clocks, &c.gave_up))) return let_copies_land();
       if (one_lane()) {
         if (rank == 0) expect_bytes(full, bytes);
         load_blocks(to, a_map, a.half, a.block, full);
@@ -178,7 +178,7 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
       b0 = factor(ring_at + (t.flags & kSame ? 0 : kFactorBytes), b_columns, kHalf);
     };
     set();
-    if (!__all_sync(0xFFFFFFFFu, wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, &c.gave_up))) return let_copies_land();
+    if (!__all_sync(0xFFFFFFFFu, wait_phase(shared_address(&c.sums_empty[half]), (n / 2 + 1) % 2, p.wait_clocks, &c.gave_up))) return let_copies_land();
     tensor_fence_after();
     const uint32_t sums = tensor + half * 256;
     for (uint32_t k = 0; k < depth; ++k) {
@@ -187,7 +187,7 @@ __device__ __forceinline__ void multiply_tiles(const MuonProduct& p, uint32_t ri
         b_columns |= k == b_switch;
         set();
       }
-      if (!__all_sync(0xFFFFFFFFu, wait_phase(full0 + r.stage * 8, r.phase, &c.gave_up))) return let_copies_land();
+      if (!__all_sync(0xFFFFFFFFu, wait_phase(full0 + r.stage * 8, r.phase, p.wait_clocks, &c.gave_up))) return let_copies_land();
       tensor_fence_after();
       const uint64_t a = a0 + r.stage * (kStageBytes >> 4), b = b0 + r.stage * (kStageBytes >> 4);
       if (one_lane()) {
@@ -325,10 +325,10 @@ __device__ __forceinline__ void finish_tiles(const MuonProduct& p, uint8_t* stag
     };
     bool ok = true;
     if (mine && adds) {
-      ok = !p.waits || wait_count(p.done + t.needs, tiles.count(), &c.gave_up);
+      ok = !p.waits || wait_count(p.done + t.needs, tiles.count(), p.wait_clocks, &c.gave_up);
       fetch(warp / 4);
     }
-    ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, &c.gave_up) && ok;
+    ok = wait_phase(shared_address(&c.sums_full[half]), n / 2 % 2, p.wait_clocks, &c.gave_up) && ok;
     if (!__all_sync(0xFFFFFFFFu, ok)) return let_copies_land();
     tensor_fence_after();
     for (uint32_t q = warp / 4; q < parts; q += 2) {
@@ -399,7 +399,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
   pair_sync();
   tensor_fence_after();
   wait_for_kernel_before();
-  if (p.clip == nullptr || p.clip->nonfinite == 0) {
+  // (Once a product has given up a wait, those after it do nothing.  A pair whose CTAs disagree, because one of this launch gives up just now, ends by
+  // its waits' limit.)
+  const bool stopped = *static_cast<volatile uint32_t*>(p.status) != 0;
+  if (!stopped && (p.clip == nullptr || p.clip->nonfinite == 0)) {
     if (warp == 0) {
       bring<kSplit>(p, maps, ring_at, c, rank);
     } else if (warp == 1) {

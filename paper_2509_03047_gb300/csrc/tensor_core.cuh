@@ -58,12 +58,12 @@ __device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return done != 0;
 }
-// Until the barrier's phase of this parity is over: false after some two seconds, or if somebody else in the CTA has given up.
-__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+// Until the barrier's phase of this parity is over: false after `limit` clocks, or if somebody else in the CTA has given up.
+__device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, int64_t limit, volatile uint32_t* gave_up) {
   if (try_wait(bar, parity)) return true;
   const long long start = clock64();
   while (!try_wait(bar, parity)) {
-    if (*gave_up || clock64() - start > (4ll << 30)) {
+    if (*gave_up || clock64() - start > limit) {
       *gave_up = 1;
       return false;
     }
@@ -71,13 +71,13 @@ __device__ __forceinline__ bool wait_phase(uint32_t bar, uint32_t parity, volati
   return true;
 }
 // Until a counter in memory has reached `count`; with it the writes before its additions are visible (to copies after before_reading_copies).
-__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t count, volatile uint32_t* gave_up) {
+__device__ __forceinline__ bool wait_count(const uint32_t* counter, uint32_t count, int64_t limit, volatile uint32_t* gave_up) {
   const long long start = clock64();
   for (;;) {
     uint32_t now;
     asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(counter) : "memory");
     if (now >= count) break;
-    if (*gave_up || clock64() - start > (4ll << 30)) {
+    if (*gave_up || clock64() - start > limit) {
       *gave_up = 1;
       return false;
     }

@@ -875,6 +875,7 @@ class MuonPlan:
         fr_muon_step(self.handle, hyper, clip, stream)
 
     def sync_status(self, stream=None) -> int:
+        """FR_OK, or FR_ERR_DEVICE_TIMEOUT once: a step was left half done, and nothing has been written since."""
         return fr_muon_sync_status(self.handle, stream)
 
     def orthogonalize(self, hyper: Optional[fr_muon] = None, stream=None) -> None:
