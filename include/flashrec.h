@@ -518,10 +518,12 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  * Precision.  All factors of the products are fp16 numbers, scaled so that fp16 holds
  * them, their sums in fp32.  A matrix with an fp32 output (weight, master or update)
  * has each factor as two of them, 22 bits, and three products for one: O is off by
- * 2^-16 to 2^-14 (2-norm over 2-norm; sides of 256 to 4,096), what the tensor cores' additions
- * lose.  Others, and with FR_MUON_ONE all, enter X, X X^T and the polynomial in it by one
- * rounding each: with the usual coefficients and 5 iterations O is off by 0.1 to 0.2% for
- * any spectrum, by up to 0.5% where a side has fewer than 16 elements; a bf16 output's own rounding is
+ * 2^-17 to 2^-12 (roots of sums of squares over all elements; most where both sides have thousands,
+ * or the rank is low), whatever the sides, mostly what the tensor cores' additions cut
+ * off: they add 4,096 terms at most, longer sums are put together in fp32 (32,768 with one
+ * product).  Others, and with FR_MUON_ONE all, enter X, X X^T and the polynomial in it by one
+ * rounding each: with the usual coefficients and 5 iterations O is off by 0.05 to 0.2%,
+ * by up to 0.5% where fewer than 16 singular values are not zero; a bf16 output's own rounding is
  * 0.17% (0.4% at most).  (The rounding of X alone would grow with every iteration, by a, in
  * the parts of small singular values: what it leaves is kept, and added to the product
  * as it is, until the iterations left raise it by no more than 4.)
@@ -551,7 +553,7 @@ typedef struct fr_muon_plan_s* fr_muon_plan;
  * buffers' addresses, allocates here and nowhere else, and one stream at a time
  * may use it.  Its device memory: about 6 bytes per element (8 with
  * an fp32 output) and 4 (8) per element of a square of the smaller side, sides rounded up to
- * multiples of 128.
+ * multiples of 128, and 20 MB where sums are put together.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT, FR_ERR_CUDA. */
 fr_status fr_muon_create(const fr_muon_tensor* tensors, uint64_t n_tensors, fr_muon_plan* out);
 

@@ -131,6 +131,12 @@ static_assert(sizeof(MuonTile) == 96, "six loads of 16 bytes");
 enum : uint32_t { kNarrow = 1, kAColumns = 2, kBColumns = 4, kSecond = 8, kAIterate = 16, kBIterate = 32, kSame = 64 };
 constexpr uint32_t kSignals = 16;  // of a tile: two CTAs, eight warps
 constexpr int64_t kWaitClocks = 4ll << 30;  // some two seconds
+// The tensor cores cut their sums off to fp32 with every 16 products, always towards zero: of long contractions that adds up.  So after this many steps of
+// 64 the sums go to fp32 numbers in memory, and new ones begin in tensor memory.  (2^20 terms in one go: O off by 8e-3, with products of both halves
+// as with one.)  Products of both halves lose up to 1.9e-4 by what a part of 4,096 terms is cut off; in one product a part of 32,768 is far below the
+// factors' own rounding.
+constexpr uint32_t part_steps(bool split) { return split ? 64 : 512; }
+constexpr int kPartBytes = 128 * 256 * 4;  // of a CTA
 
 // One launch takes a list through some iterations, or a phase of one: its tiles in order, iteration after iteration, each pair every n-th.  A tile waits until all
 // those that it reads from have counted; they come before it in that order, and all CTAs are resident, so every wait ends.
@@ -143,6 +149,8 @@ struct MuonProduct {
   uint32_t* status;         // set to 1 by a kernel that gave up a wait
   int64_t wait_clocks;      // after which it does
   uint32_t* done;           // counters, zero at the start
+  uint32_t parts;           // 1: a tile's contraction is longer than a part
+  uint8_t* sums;            // then kPartBytes for each CTA: of a tile's parts but the last
   uint32_t x_blocks;        // of all iterates: from x[0] to x[1], from either to its second halves twice as far
   uint32_t p_blocks;        // from P to S, the same
   uint32_t split;

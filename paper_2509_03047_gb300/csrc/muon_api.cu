@@ -29,6 +29,7 @@ struct fr_muon_plan_s {
     uint64_t x_blocks = 0, p_blocks = 0;     // of all iterates, all squares
     uint32_t ends[kPhases] = {};             // of each phase's tiles
     uint32_t most_tiles = 0;                 // of a phase
+    uint32_t deepest = 0;                    // steps of a contraction
     MuonTile* d_tiles = nullptr;
   } parts[2];
   MuonDesc* d_tensors = nullptr;
@@ -38,6 +39,7 @@ struct fr_muon_plan_s {
   MuonPartial* d_partials = nullptr;
   MuonNorm* d_norms = nullptr;
   uint8_t* d_work = nullptr;
+  uint8_t* d_sums = nullptr;                 // where a contraction is longer than a part
   uint32_t* d_status = nullptr;
   int64_t wait_clocks = kWaitClocks;
   MuonMaps maps;
@@ -154,6 +156,9 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     }
     bytes += k ? 4 * (x_bytes + p_bytes) : 3 * x_bytes + 2 * p_bytes;
   }
+  cudaError_t e = descs.empty() ? cudaSuccess : configure_muon_product();
+  if (e == cudaSuccess && !descs.empty()) e = muon_pairs(&p->pairs);
+  if (e != cudaSuccess) return report_cuda("the product kernels' shared memory", e);
   PlanMemory mem;
   mem.table(&p->d_tensors, descs);
   mem.table(&p->d_units, units);
@@ -163,6 +168,7 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
     std::vector<MuonTile> tiles;
     plan_tiles(descs, k != 0, tiles, part.ends);
     for (int phase = 0; phase < kPhases; ++phase) part.most_tiles = std::max(part.most_tiles, part.ends[phase] - (phase ? part.ends[phase - 1] : 0));
+    for (const MuonTile& t : tiles) part.deepest = std::max(part.deepest, t.depth);
     mem.table(&part.d_tiles, tiles);
   }
   mem.scratch(&p->d_done, descs.size() * kPhases);
@@ -170,15 +176,15 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   mem.scratch(&p->d_partials, units.size());
   mem.table(&p->d_status, std::vector<uint32_t>(1, 0));
   mem.scratch(&p->d_work, bytes);
+  // (products of one half for all have longer parts)
+  if (p->parts[0].deepest > part_steps(false) || p->parts[1].deepest > part_steps(true)) mem.scratch(&p->d_sums, 2ull * p->pairs * kPartBytes);
   p->n_units = static_cast<uint32_t>(units.size());
   p->n_blocks = static_cast<uint32_t>(blocks.size());
   p->device_bytes = bytes;
-  cudaError_t e = mem.commit(&p->d_memory);
+  e = mem.commit(&p->d_memory);
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   if (bytes == 0) return FR_OK;
-  e = configure_muon_product();
-  if (e == cudaSuccess) e = muon_pairs(&p->pairs);
-  if (e == cudaSuccess) e = make_maps(&p->maps, p->d_work, bytes);
+  e = make_maps(&p->maps, p->d_work, bytes);
   return e == cudaSuccess ? FR_OK : report_cuda("tensor maps of the workspace", e);
 }
 
@@ -228,6 +234,7 @@ constexpr uint32_t kTogether = 4;
 cudaError_t launch_products(fr_muon_plan p, const fr_muon& h, MuonProduct q, const fr_muon_plan_s::Part& part, cudaStream_t s) {
   q.x_blocks = static_cast<uint32_t>(part.x_blocks);
   q.p_blocks = static_cast<uint32_t>(part.p_blocks);
+  q.parts = part.deepest > part_steps(q.split);
   if (part.most_tiles <= kTogether * p->pairs) {
     q.tiles = part.d_tiles;
     q.n_tiles = part.ends[kPhases - 1];
@@ -256,6 +263,7 @@ fr_status iterate(fr_muon_plan p, const fr_muon& h, MuonParams& mp, cudaStream_t
   q.status = p->d_status;
   q.wait_clocks = p->wait_clocks;
   q.done = p->d_done;
+  q.sums = p->d_sums;
   // Of first halves alone: an iterate keeps its second ones if the iterations after it raise small singular values, and a rounding among them, by
   // more than 4.
   double gain = 1.0;
