@@ -94,6 +94,27 @@ constexpr int kOdd = 0, kWide = 16;
 constexpr int vector_of(int v) { return v == kOdd ? 1 : v == kWide ? 8 : v; }
 constexpr int lane_vectors(int v) { return v == kOdd ? 12 : v == kWide ? 2 : v == 8 ? 1 : v == 4 ? 2 : 4; }
 constexpr int tile_width(int v) { return 32 * vector_of(v) * lane_vectors(v); }
+// The granules around a row's columns from `first` on, `width` of them at most: 16 bytes at `begin` and so on, as many as `bytes` reaches into.
+struct Granules {
+  uint64_t begin;
+  uint32_t bytes;
+#ifdef __CUDACC__
+  __host__ __device__ __forceinline__
+#endif
+  Granules(uint64_t base, uint64_t row, uint64_t dim, uint64_t first, uint32_t width, uint32_t size) {
+    const uint64_t from = base + (row * dim + first) * size, left = dim - first;
+    begin = from & ~15ull;
+    bytes = (static_cast<uint32_t>(from) & 15) + static_cast<uint32_t>(left < width ? left : width) * size;
+  }
+};
+// Whether they lie in a buffer of `rows` rows: those of its first and last row may reach beyond it, where memory is somebody else's.  (A row has
+// more than kOddLeast elements, so no other row's do.)
+#ifdef __CUDACC__
+__host__ __device__ __forceinline__
+#else
+inline
+#endif
+bool by_granules(uint64_t row, uint64_t rows) { return row != 0 && row + 1 != rows; }
 // The sorted tokens are cut into ranges of equal length, one for a warp per tile of columns; a multiple of what a CTA has.
 constexpr uint32_t kSumWarps = 8;
 // Ranges times column tiles, about.  A range has its fixed cost (the tokens at its borders, its part), some 5 us: one wave of them is best for odd
@@ -128,7 +149,7 @@ struct SumParams {
   float* parts;      // two rows per CTA
   const void* out;
   void* grad;
-  uint64_t dim, rows;
+  uint64_t dim, rows, n;  // n rows of out
   float scale;
   uint32_t ranges, tiles;
   uint32_t ctas, zero_ctas;

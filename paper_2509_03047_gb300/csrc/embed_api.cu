@@ -194,6 +194,7 @@ fr_status fr_embed_grad(fr_embed p, const void* out, uint32_t out_dtype, const v
   q.ranges = ranges_of(n, p->dim, accumulate);
   q.ctas = q.ranges / kSumWarps * q.tiles;
   q.rows = p->rows;
+  q.n = n;
   if (!accumulate && !fill) {
     // about 64 KiB per warp
     const uint64_t row_bytes = p->dim * type_bytes(grad_dtype);

@@ -134,17 +134,25 @@ struct Ring {
   __device__ __forceinline__ uint8_t* in_slot(uint32_t token) const { return at + token % kRing * kIn; }
   __device__ __forceinline__ uint8_t* old_slot(uint32_t token) const { return at + kRing * kIn + token % kRing * kOld; }
 
+  // Row `row` of a buffer of `rows`.
   template <bool Bf16>
-  __device__ __forceinline__ void copy(uint8_t* slot, const void* base, uint64_t row) const {
+  __device__ __forceinline__ void copy(uint8_t* slot, const void* base, uint64_t row, uint64_t rows) const {
     constexpr int kSize = Bf16 ? 2 : 4;
     if constexpr (Kind == kOdd) {
-      const uint64_t from = reinterpret_cast<uint64_t>(base) + (row * dim + first) * kSize;
-      const uint32_t end = (static_cast<uint32_t>(from) & 15) + static_cast<uint32_t>(min(static_cast<uint64_t>(kWidth), dim - first)) * kSize;
-      const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slot)) + lane * 16;
-      const uint8_t* const begin = reinterpret_cast<const uint8_t*>(from & ~15ull) + lane * 16;
+      const Granules g(reinterpret_cast<uint64_t>(base), row, dim, first, kWidth, kSize);
+      if (by_granules(row, rows)) {
+        const uint32_t to = static_cast<uint32_t>(__cvta_generic_to_shared(slot)) + lane * 16;
+        const uint8_t* const begin = reinterpret_cast<const uint8_t*>(g.begin) + lane * 16;
 #pragma unroll
-      for (int k = 0; k < (kWidth * kSize + 16 + 511) / 512; ++k)
-        if (lane * 16 + k * 512 < end) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + k * 512), "l"(begin + k * 512) : "memory");
+        for (int k = 0; k < (kWidth * kSize + 16 + 511) / 512; ++k)
+          if (lane * 16 + k * 512 < g.bytes) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + k * 512), "l"(begin + k * 512) : "memory");
+      } else {
+        using T = typename Words<kSize>::T;
+        const uint64_t from = reinterpret_cast<uint64_t>(base) + (row * dim + first) * kSize;
+        T* const to = reinterpret_cast<T*>(slot + (from & 15));
+        const uint64_t width = min(static_cast<uint64_t>(kWidth), dim - first);
+        for (uint32_t i = lane; i < width; i += 32) to[i] = reinterpret_cast<const T*>(from)[i];
+      }
     } else {
 #pragma unroll
       for (int c = 0; c < kVectors; ++c)
@@ -211,8 +219,8 @@ __global__ void __launch_bounds__(kThreads, Kind == kWide ? 2 : 3) sum_kernel(co
       const uint32_t token = __shfl_sync(kAll, j < 32 ? now.m.at : next.m.at, i);
       const uint32_t row = Add ? __shfl_sync(kAll, j < 32 ? now.m.row : next.m.row, i) : 0;
       if (base + j >= count) continue;
-      ring.template copy<Bf16Out>(ring.in_slot(base + j), p.out, token);
-      if (Add && (j < 32 ? ends : next_ends) >> i & 1) ring.template copy<Bf16Grad>(ring.old_slot(base + j), p.grad, row);
+      ring.template copy<Bf16Out>(ring.in_slot(base + j), p.out, token, p.n);
+      if (Add && (j < 32 ? ends : next_ends) >> i & 1) ring.template copy<Bf16Grad>(ring.old_slot(base + j), p.grad, row, p.rows);
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
