@@ -658,21 +658,44 @@ def fr_embed_destroy(plan) -> None:
         lib.fr_embed_destroy(plan)
 
 
-def fr_embed_lookup(plan, table: torch.Tensor, tokens: torch.Tensor, scale: float, out: torch.Tensor, stream=None) -> None:
-    """`out`: as many rows as `tokens` (int32 or int64) has elements."""
+def _embed_sizes(plan, name: str, table: torch.Tensor, tokens: torch.Tensor, out: torch.Tensor) -> None:
+    """The library takes addresses alone: a table of another size than the plan's, or another number of rows than tokens, would
+    be read and written beyond its end."""
+    rows, dim, _, _ = fr_embed_info(plan)
+    if table.numel() != rows * dim:
+        raise ValueError("%s holds %d elements, not %d rows of %d" % (name, table.numel(), rows, dim))
+    if out.numel() != tokens.numel() * dim:
+        raise ValueError("out holds %d elements, not %d rows of %d" % (out.numel(), tokens.numel(), dim))
+    devices = {t.get_device() for t in (table, tokens, out) if t.numel()}
+    if len(devices) > 1:
+        raise ValueError("%s, tokens and out are on several devices" % name)
+
+
+def _embed_lookup(plan, table, tokens, scale, out, stream) -> None:
     w, wt = _buffer("table", table, _FLOATS)
     t, tb = _buffer("tokens", tokens, _TOKENS)
     o, ot = _buffer("out", out, _FLOATS)
     _check(lib.fr_embed_lookup(plan, w, wt, t, tb, tokens.numel(), scale, o, ot, _stream(stream)), "fr_embed_lookup")
 
 
-def fr_embed_grad(plan, out: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
-                  stream=None) -> None:
-    """The table's gradient `grad` from the rows' gradients `out`."""
+def _embed_grad(plan, out, tokens, grad, scale, accumulate, stream) -> None:
     o, ot = _buffer("out", out, _FLOATS)
     t, tb = _buffer("tokens", tokens, _TOKENS)
     g, gt = _buffer("grad", grad, _FLOATS)
     _check(lib.fr_embed_grad(plan, o, ot, t, tb, tokens.numel(), scale, g, gt, int(bool(accumulate)), _stream(stream)), "fr_embed_grad")
+
+
+def fr_embed_lookup(plan, table: torch.Tensor, tokens: torch.Tensor, scale: float, out: torch.Tensor, stream=None) -> None:
+    """`out`: as many rows as `tokens` (int32 or int64) has elements."""
+    _embed_sizes(plan, "table", table, tokens, out)
+    _embed_lookup(plan, table, tokens, scale, out, stream)
+
+
+def fr_embed_grad(plan, out: torch.Tensor, tokens: torch.Tensor, grad: torch.Tensor, scale: float = 1.0, accumulate: bool = False,
+                  stream=None) -> None:
+    """The table's gradient `grad` from the rows' gradients `out`."""
+    _embed_sizes(plan, "grad", grad, tokens, out)
+    _embed_grad(plan, out, tokens, grad, scale, accumulate, stream)
 
 
 # ---------------------------------------------------------------- convenience
@@ -919,7 +942,7 @@ class EmbedPlan:
             with _allocating_on(stream, self.device):
                 out = torch.empty(*tokens.shape, self.dim, dtype=table.dtype, device=self.device)
         self._here("out", out, (*tokens.shape, self.dim))
-        fr_embed_lookup(self.handle, table, tokens, scale, out, stream)
+        _embed_lookup(self.handle, table, tokens, scale, out, stream)  # (sizes and devices are looked at above)
         return out
 
     def grad(self, out: torch.Tensor, tokens: torch.Tensor, grad: Optional[torch.Tensor] = None, scale: float = 1.0,
@@ -934,5 +957,5 @@ class EmbedPlan:
             with _allocating_on(stream, self.device):
                 grad = torch.empty(self.rows, self.dim, dtype=torch.float32, device=self.device)
         self._here("grad", grad, (self.rows, self.dim))
-        fr_embed_grad(self.handle, out, tokens, grad, scale, accumulate, stream)
+        _embed_grad(self.handle, out, tokens, grad, scale, accumulate, stream)
         return grad
