@@ -528,6 +528,9 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  * the parts of small singular values: what it leaves is kept, and added to the product
  * as it is, until the iterations left raise it by no more than 4.)
  *
+ * FR_MUON_BOTH_HALVES in a matrix's flags gives one with bf16 outputs what one with an fp32
+ * output has.
+ *
  * One fr_muon_tensor is one matrix, rows * cols elements, row after row, in each
  * of its buffers.  fr_muon_step needs the weights, gradients and momenta,
  * fr_orthogonalize the gradients and updates; a pointer that no call needs is
@@ -540,11 +543,13 @@ typedef struct {
   void* update;      /* FR_DT_BF16 or FR_DT_F32: what fr_orthogonalize writes       */
   uint64_t rows, cols;
   uint32_t weight_dtype, grad_dtype, update_dtype;
-  uint32_t flags;    /* 0 */
+  uint32_t flags;    /* 0 or FR_MUON_BOTH_HALVES                                    */
   float lr_scale, decay_scale; /* the matrix's factors, as in fr_opt_tensor          */
   float update_scale;          /* on O: 0.2 sqrt(max(rows, cols)), or as one likes   */
   uint32_t reserved; /* 0 */
 } fr_muon_tensor;
+
+#define FR_MUON_BOTH_HALVES 2u
 
 typedef struct fr_muon_plan_s* fr_muon_plan;
 
@@ -552,7 +557,7 @@ typedef struct fr_muon_plan_s* fr_muon_plan;
  * allowed).  As with fr_opt_create the plan is bound to the current device and the
  * buffers' addresses, allocates here and nowhere else, and one stream at a time
  * may use it.  Its device memory: about 6 bytes per element (8 with
- * an fp32 output) and 4 (8) per element of a square of the smaller side, sides rounded up to
+ * both halves) and 4 (8) per element of a square of the smaller side, sides rounded up to
  * multiples of 128, and 20 MB where sums are put together.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT, FR_ERR_CUDA. */
 fr_status fr_muon_create(const fr_muon_tensor* tensors, uint64_t n_tensors, fr_muon_plan* out);
@@ -566,7 +571,7 @@ void fr_muon_destroy(fr_muon_plan plan);
 #define FR_MUON_MOST 10            /* iterations */
 #define FR_MUON_MOST_SIDE (1u << 20) /* rows, columns */
 
-/* Products of both halves for matrices with fp32 outputs, or of one for all. */
+/* Products of both halves for matrices with fp32 outputs or FR_MUON_BOTH_HALVES, or of one for all. */
 typedef enum { FR_MUON_BY_TYPE = 0, FR_MUON_ONE = 1 } fr_muon_products;
 
 /* One step's numbers.  lr, weight_decay and their products with the factors as in

@@ -13,7 +13,7 @@
 // product reads, has blocks of its own kind: chunk c of row r at c * 128 + r, so that
 // a warp's 32 rows of a chunk are 512 bytes.
 //
-// A matrix with an fp32 output (split) has second halves of everything, in blocks like
+// A matrix with an fp32 output, or whose caller asks for it, (split) has second halves of everything, in blocks like
 // the first ones, which enter the products too.  Its part of the workspace is apart:
 // all x[0], x[1], second halves of either, P, S, second halves of either; the others'
 // x[0], x[1], second halves, P, S.

@@ -56,7 +56,7 @@ bool is_float(uint32_t dtype) { return dtype == FR_DT_BF16 || dtype == FR_DT_F32
 
 const char* check(const fr_muon_tensor& x, bool& misaligned) {
   misaligned = false;
-  if (x.flags != 0 || x.reserved != 0) return "tensor flags and reserved must be 0";
+  if ((x.flags & ~FR_MUON_BOTH_HALVES) != 0 || x.reserved != 0) return "unknown tensor flags, or reserved is not 0";
   if (x.rows > kMostSide || x.cols > kMostSide) return "a matrix has too many rows or columns";
   if (!std::isfinite(x.lr_scale) || !std::isfinite(x.decay_scale) || !std::isfinite(x.update_scale)) return "a matrix's factors must be finite";
   if (x.weight && !is_float(x.weight_dtype)) return "weights are bf16 or fp32";
@@ -89,7 +89,7 @@ MuonDesc describe(const fr_muon_tensor& x, uint64_t index) {
   d.bf16_weight = x.weight && x.weight_dtype == FR_DT_BF16;
   d.bf16_grad = x.grad && x.grad_dtype == FR_DT_BF16;
   d.bf16_update = x.update && x.update_dtype == FR_DT_BF16;
-  d.split = x.master || (x.weight && !d.bf16_weight) || (x.update && !d.bf16_update);
+  d.split = (x.flags & FR_MUON_BOTH_HALVES) || x.master || (x.weight && !d.bf16_weight) || (x.update && !d.bf16_update);
   d.lr_scale = x.lr_scale;
   d.decay_scale = x.decay_scale;
   d.update_scale = x.update_scale;

@@ -33,6 +33,7 @@ FR_OPT_BLOCK = 256
 FR_ROUND_NEAREST, FR_ROUND_RANDOM = 0, 1
 FR_MUON_MOST, FR_MUON_MOST_SIDE = 10, 1 << 20
 FR_MUON_BY_TYPE, FR_MUON_ONE = 0, 1
+FR_MUON_BOTH_HALVES = 2
 CLIP_BYTES = 16
 
 _TORCH_TO_FR = {torch.bfloat16: FR_DT_BF16, torch.float32: FR_DT_F32, torch.uint8: FR_DT_BYTES,
@@ -533,7 +534,7 @@ def muon(lr: float = 0.0, beta: float = 0.95, weight_decay: float = 0.0, nestero
     return h
 
 
-def _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale):
+def _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale, both_halves=False):
     """(fr_muon_tensor array, its length)"""
     lists = [("weights", "weight", weights, _FLOATS), ("grads", "grad", grads, _FLOATS), ("masters", "master", masters, _F32),
              ("momenta", "momentum", momenta, _F32), ("updates", "update", updates, _FLOATS)]
@@ -583,14 +584,18 @@ def _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale
             raise ValueError("%d factors for %d matrices" % (len(x), count))
         for i, v in enumerate(x):
             setattr(arr[i], field, v)
+    for i in range(count):
+        arr[i].flags = FR_MUON_BOTH_HALVES if both_halves else 0
     return arr, count
 
 
 def fr_muon_create(weights=None, grads=None, momenta=None, masters=None, updates=None, lr_scale=None, decay_scale=None,
-                   update_scale=None):
+                   update_scale=None, both_halves=False):
     """Plan over lists of contiguous two-dimensional CUDA tensors on the current device (a list, or an entry, may be None;
-    factors default to 1).  Momenta and masters are fp32, the others bf16 or fp32.  Returns the opaque handle (int)."""
-    arr, count = _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale)
+    factors default to 1).  Momenta and masters are fp32, the others bf16 or fp32.  `both_halves`: matrices with bf16 outputs get
+    the products that those with fp32 ones have, in 2.5 times the time (see include/flashrec.h).  Returns the opaque handle
+    (int)."""
+    arr, count = _muon_array(weights, grads, momenta, masters, updates, lr_scale, decay_scale, update_scale, both_halves)
     h = ctypes.c_void_p()
     _check(lib.fr_muon_create(arr, count, ctypes.byref(h)), "fr_muon_create")
     return h.value
@@ -872,13 +877,14 @@ class MuonPlan:
     clip record comes from an OptPlan over all gradients."""
 
     def __init__(self, weights=None, grads=None, momenta=None, masters=None, updates=None, lr_scale=None, decay_scale=None,
-                 update_scale=None):
+                 update_scale=None, both_halves=False):
         lists = [weights, grads, momenta, masters, updates]
         self.buffers = [None if x is None else list(x) for x in lists]  # the plan holds their addresses
         first = next((t for x in self.buffers if x for t in x if t is not None and t.numel()), None)
         self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
         self.handle = None
-        self.handle = fr_muon_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale, update_scale=update_scale)
+        self.handle = fr_muon_create(*self.buffers, lr_scale=lr_scale, decay_scale=decay_scale, update_scale=update_scale,
+                                     both_halves=both_halves)
         self.n_tensors, self.n_elems, self.device_bytes = fr_muon_info(self.handle)
 
     def close(self) -> None:

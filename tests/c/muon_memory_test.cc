@@ -102,6 +102,23 @@ int main() {
     CHECK((p->d_sums != nullptr) == longer);
     fr_muon_destroy(p);
   }
+  // a matrix with bf16 outputs has products of both halves if its flag asks for them, and not with FR_MUON_ONE; other flags are refused
+  resident = 76;
+  for (uint32_t flags : {0u, 1u, FR_MUON_BOTH_HALVES, FR_MUON_BOTH_HALVES | 1, 4u, 0x80000000u}) {
+    fr_muon_tensor x = matrix(100, 200, false);
+    x.flags = flags;
+    fr_muon_plan p = nullptr;
+    const bool known = (flags & ~FR_MUON_BOTH_HALVES) == 0;
+    CHECK(fr_muon_create(&x, 1, &p) == (known ? FR_OK : FR_ERR_INVALID_ARG) && (p != nullptr) == known);
+    if (!known) continue;
+    fake::finish_all();
+    for (uint32_t how : {FR_MUON_BY_TYPE, FR_MUON_ONE}) {
+      products.clear();
+      h.products = how;
+      CHECK(fr_orthogonalize(p, &h, nullptr) == FR_OK && products.size() == 1 && products[0].p.split == (flags != 0 && how == FR_MUON_BY_TYPE));
+    }
+    fr_muon_destroy(p);
+  }
   for (int split = 0; split < 2; ++split)
     for (int parts = 0; parts < 2; ++parts) CHECK(seen[split][parts] > 5);
   std::printf("muon_memory ok\n");

@@ -62,6 +62,28 @@ def test_precision_does_not_fall_with_the_sides(shape, kind):
     assert both <= one / 4, (both, one)
 
 
+def test_bf16_outputs_by_products_of_both_halves():
+    """They are the fp32 ones, rounded once: updates, and the weights of a step."""
+    gs = [_matrix(s, "plain") for s in [(200, 300), (700, 130), (64, 64), (90, 5000)]]
+    wide = [_orthogonal(g, fr.FR_MUON_BY_TYPE) for g in gs]
+    outs = [torch.zeros_like(g, dtype=torch.bfloat16) for g in gs]
+    plan = fr.MuonPlan(grads=gs, updates=outs, both_halves=True)
+    plan.orthogonalize()
+    for o, w in zip(outs, wide):
+        assert torch.equal(o, w.bfloat16())
+    plan.orthogonalize(fr.muon(products=fr.FR_MUON_ONE))
+    one = [torch.zeros_like(o) for o in outs]
+    fr.MuonPlan(grads=gs, updates=one).orthogonalize()
+    for o, w in zip(outs, one):
+        assert torch.equal(o, w)
+    weights = [(w * 0.1).bfloat16() for w in wide]
+    masters = [w.float() for w in weights]
+    for w, both in ((weights, True), (masters, False)):
+        fr.MuonPlan(w, gs, [torch.zeros_like(g) for g in gs], both_halves=both).step(fr.muon(lr=0.02, weight_decay=0.1))
+    for w, m in zip(weights, masters):
+        assert torch.equal(w, m.bfloat16())
+
+
 @pytest.mark.parametrize("products", [fr.FR_MUON_BY_TYPE, fr.FR_MUON_ONE])
 def test_a_long_matrix_gives_the_same_bits_in_any_list(products):
     """Of many parts, the last one short; among others that have one; in a list that goes phase by phase."""
