@@ -26,11 +26,13 @@ namespace {
 constexpr int kWarps = kSortThreads / 32;
 constexpr uint32_t kAll = 0xFFFFFFFFu;
 
-// Exclusive sums over `n` (a power of two, at most 2 kSortThreads) counts in shared memory; every thread calls.
+static_assert((1 << kMostDigit) <= kSortThreads, "a thread has a digit");
+
+// Exclusive sums over `n` (at most kSortThreads) counts in shared memory; every thread calls.
 __device__ __forceinline__ uint32_t scan(uint32_t* x, uint32_t n, uint32_t* warps) {
   const uint32_t t = threadIdx.x, lane = t % 32;
-  const uint32_t a = 2 * t < n ? x[2 * t] : 0, b = 2 * t + 1 < n ? x[2 * t + 1] : 0;
-  uint32_t sum = a + b;
+  const uint32_t a = t < n ? x[t] : 0;
+  uint32_t sum = a;
 #pragma unroll
   for (int k = 1; k < 32; k *= 2) {
     const uint32_t y = __shfl_up_sync(kAll, sum, k);
@@ -48,9 +50,7 @@ __device__ __forceinline__ uint32_t scan(uint32_t* x, uint32_t n, uint32_t* warp
     warps[t] = w;
   }
   __syncthreads();
-  const uint32_t before = (t >= 32 ? warps[t / 32 - 1] : 0) + sum - a - b;
-  if (2 * t < n) x[2 * t] = before;
-  if (2 * t + 1 < n) x[2 * t + 1] = before + a;
+  if (t < n) x[t] = (t >= 32 ? warps[t / 32 - 1] : 0) + sum - a;
   const uint32_t total = warps[kWarps - 1];
   __syncthreads();
   return total;
@@ -197,25 +197,19 @@ __global__ void __launch_bounds__(kSortThreads) place_kernel(const __grid_consta
   const uint32_t bins = 1u << p.bits;
   const Shared sh(raw, bins);
   wait_for_kernel_before();
-  // (a digit per thread)
-  uint32_t before[2] = {0, 0};
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const uint32_t i = threadIdx.x + j * kSortThreads;
-    if (i >= bins) break;
+  uint32_t before = 0;
+  if (threadIdx.x < bins) {
     uint32_t total = 0;
 #pragma unroll 16
     for (uint32_t c = 0; c < p.ctas; ++c) {
-      if (c == blockIdx.x) before[j] = total;
-      total += p.counts[static_cast<uint64_t>(c) * bins + i];
+      if (c == blockIdx.x) before = total;
+      total += p.counts[static_cast<uint64_t>(c) * bins + threadIdx.x];
     }
-    sh.base[i] = total;
+    sh.base[threadIdx.x] = total;
   }
   __syncthreads();
   const uint32_t found = scan(sh.base, bins, sh.warps);
-#pragma unroll
-  for (int j = 0; j < 2; ++j)
-    if (threadIdx.x + j * kSortThreads < bins) sh.base[threadIdx.x + j * kSortThreads] += before[j];
+  if (threadIdx.x < bins) sh.base[threadIdx.x] += before;
   if (First && blockIdx.x == 0 && threadIdx.x == 0) *p.found = found;
   __syncthreads();
   const uint64_t n = First ? p.tokens.n : *p.found, begin = blockIdx.x * p.share, end = min(begin + p.share, n);
@@ -249,24 +243,19 @@ __global__ void __launch_bounds__(kSortThreads) cluster_kernel(const __grid_cons
     else
       take_tile<false>(p, sh, bins, pass, begin, end, m, digit, rank);
     cluster.sync();
-    uint32_t before[2] = {0, 0};
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const uint32_t i = threadIdx.x + j * kSortThreads;
-      if (i >= bins) break;
+    uint32_t before = 0;
+    if (threadIdx.x < bins) {
       uint32_t total = 0;
 #pragma unroll 16
       for (uint32_t c = 0; c < p.ctas; ++c) {
-        if (c == me) before[j] = total;
-        total += *cluster.map_shared_rank(sh.totals + i, c);
+        if (c == me) before = total;
+        total += *cluster.map_shared_rank(sh.totals + threadIdx.x, c);
       }
-      sh.base[i] = total;
+      sh.base[threadIdx.x] = total;
     }
     __syncthreads();
     n = scan(sh.base, bins, sh.warps);
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-      if (threadIdx.x + j * kSortThreads < bins) sh.base[threadIdx.x + j * kSortThreads] += before[j];
+    if (threadIdx.x < bins) sh.base[threadIdx.x] += before;
     __syncthreads();
     put_tile(p, sh, bins, pass, m, digit, rank);
     // the tokens for the next pass; and no CTA changes or leaves counts that others read
