@@ -49,7 +49,7 @@ fr_status fill_embed(fr_embed p) {
   mem.scratch(&p->d_longs, p->ranges / kSumWarps);
   mem.scratch(&p->d_parts, 2 * (p->ranges / kSumWarps) * p->dim);
   mem.scratch(&p->d_numbers, 2);
-  p->device_bytes = mem.scratch_bytes();
+  p->device_bytes = mem.bytes();
   cudaError_t e = mem.commit(&p->d_memory);
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   e = configure_sort();

@@ -180,7 +180,7 @@ fr_status fill_muon(fr_muon_plan p, const fr_muon_tensor* tensors, uint64_t n_te
   if (p->parts[0].deepest > part_steps(false) || p->parts[1].deepest > part_steps(true)) mem.scratch(&p->d_sums, 2ull * p->pairs * kPartBytes);
   p->n_units = static_cast<uint32_t>(units.size());
   p->n_blocks = static_cast<uint32_t>(blocks.size());
-  p->device_bytes = bytes;
+  p->device_bytes = mem.bytes();
   e = mem.commit(&p->d_memory);
   if (e != cudaSuccess) return report_cuda("plan device tables", e);
   if (bytes == 0) return FR_OK;

@@ -1,7 +1,7 @@
 // The device memory of a plan of the orthogonalised update (csrc/muon_api.cu) without a
 // GPU: a product whose contraction is longer than a part has a place for the sums of
 // its parts, for each CTA of the launch, within the plan's allocation and beside
-// everything else; one without has none.
+// everything else; one without has none; what fr_muon_info gives is the whole allocation.
 #include <cstdio>
 #include <random>
 
@@ -78,6 +78,9 @@ int main() {
     uint64_t bytes;
     CHECK(fr_muon_info(p, nullptr, nullptr, &bytes) == FR_OK);
     const uint8_t* const memory = static_cast<const uint8_t*>(p->d_memory);
+    const uint64_t work = (3 * p->parts[0].x_blocks + 2 * p->parts[0].p_blocks + 4 * p->parts[1].x_blocks + 4 * p->parts[1].p_blocks) * kMuonBlockBytes;
+    CHECK(p->d_work >= memory && p->d_work + work <= memory + bytes);
+    CHECK(reinterpret_cast<uint8_t*>(p->d_partials + p->n_units) <= memory + bytes && reinterpret_cast<uint8_t*>(p->d_blocks + p->n_blocks) <= memory + bytes);
     for (uint32_t how : {FR_MUON_BY_TYPE, FR_MUON_ONE}) {
       products.clear();
       h.products = how;
@@ -90,7 +93,7 @@ int main() {
         CHECK(parts || deepest <= part_steps(l.p.split));
         ++seen[l.p.split][parts];
         if (!parts) continue;
-        CHECK(l.p.sums != nullptr && l.p.sums >= l.p.work + bytes && l.p.sums >= memory);
+        CHECK(l.p.sums != nullptr && l.p.sums >= l.p.work + work && l.p.sums + 2ull * l.pairs * kPartBytes <= memory + bytes);
         CHECK(reinterpret_cast<uintptr_t>(l.p.sums) % 16 == reinterpret_cast<uintptr_t>(memory) % 16);
         // every byte of them is the plan's (the host's allocation takes the write)
         std::memset(l.p.sums, 0, 2ull * l.pairs * kPartBytes);
