@@ -514,6 +514,9 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  *   X <- a X + b (X X^T) X + c (X X^T)^2 X
  * (for more rows than columns with X^T X on the other side: the same matrix).
  * A zero matrix gives zeros, one with an Inf or NaN NaNs everywhere.
+ * G is a whole matrix.  Of a rank's shard of one (tensor parallelism, sharded states) the calls
+ * make the shard's own O: block-wise orthogonalisation, a variant in use, but another update
+ * than the shard of the matrix's O, which needs the whole matrix's gradient and momentum in one place.
  *
  * Precision.  All factors of the products are fp16 numbers, scaled so that fp16 holds
  * them, their sums in fp32.  A matrix with an fp32 output (weight, master or update)
@@ -641,8 +644,8 @@ fr_status fr_embed_info(fr_embed plan, uint64_t* rows, uint64_t* dim, uint64_t* 
 void fr_embed_destroy(fr_embed plan);
 
 /* out[i] = scale * table[tokens[i] - first], `n` rows of dim elements, multiplied in
- * fp32 and rounded once, to nearest even; zeros where the token is outside.  Types
- * are FR_DT_BF16 or FR_DT_F32; `scale` is finite.
+ * fp32, the product rounded to out's type, to nearest even; zeros where the token is
+ * outside.  Types are FR_DT_BF16 or FR_DT_F32; `scale` is finite.  No buffers may overlap.
  * Errors: FR_ERR_INVALID_ARG, FR_ERR_ALIGNMENT (any buffer off its element size), FR_ERR_CUDA. */
 fr_status fr_embed_lookup(fr_embed plan, const void* table, uint32_t table_dtype, const void* tokens, uint32_t token_bytes,
                           uint64_t n, float scale, void* out, uint32_t out_dtype, void* stream);
@@ -650,9 +653,10 @@ fr_status fr_embed_lookup(fr_embed plan, const void* table, uint32_t table_dtype
 /* grad[r] = scale * (the sum of out[i] over the tokens i of row first + r), all
  * `rows` rows, or with `accumulate` 1 added to what is there, where rows that no
  * token meets are not touched.  Sums are in fp32: a row's tokens in the batch's
- * order, those of long rows in parts that are added one after the other;
- * the product with scale, and what is there, are rounded once.  `out` is read only; no
- * buffers may overlap.
+ * order, a long row's in parts whose sums are added in an order that the batch and dim
+ * decide.  The product with scale, and what is there added to it in one operation, is
+ * rounded to fp32, and that to the gradient's type, both to nearest even.  `out` is read only;
+ * no buffers may overlap.
  * Errors: as fr_embed_lookup. */
 fr_status fr_embed_grad(fr_embed plan, const void* out, uint32_t out_dtype, const void* tokens, uint32_t token_bytes,
                         uint64_t n, float scale, void* grad, uint32_t grad_dtype, uint32_t accumulate, void* stream);

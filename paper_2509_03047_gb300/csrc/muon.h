@@ -19,7 +19,7 @@
 // x[0], x[1], second halves, P, S.
 //
 // Scales: X 2^14, S 2^13, P 2^11, so that fp16 holds what the bounds on the
-// polynomials (flashrec.h) allow: |X| <= 2, |S| <= 4, |P| <= 16 in the spectral
+// polynomials (flashrec.h) allow: |X| <= 2, |S| <= 4, |P| <= 15 in the spectral
 // norm, which no element exceeds; and elements down to 2^-28, 2^-27, 2^-25 of 1 are
 // normal numbers.
 #pragma once

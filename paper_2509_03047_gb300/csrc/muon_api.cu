@@ -218,7 +218,7 @@ const char* check_iterations(const fr_muon& h) {
     auto next = [&](double s) { return s * p(s); };
     // (a hair more than the bound, for the roundings of X)
     const double reach = top * 1.01;
-    // (one by one: a bound on P's parts keeps fp16 from overflow in b S and c S^2 alike)
+    // (P is rounded to fp16 as a whole; b S and c S^2 are fp32 numbers)
     if (!(most(p, reach, 0.0, 2.0 * c, b) <= kMostP)) return "a polynomial exceeds 15 on the singular values that it meets";
     top = most(next, reach, 5.0 * c, 3.0 * b, a);
     if (!(top <= kMostX)) return "an iteration takes a singular value above 2";
