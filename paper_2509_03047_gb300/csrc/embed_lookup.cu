@@ -4,7 +4,9 @@
 // apart: its tokens, then its table's vectors are on their way together.
 //
 // Bound by writing the output: 32,768 tokens of 4,096 in bf16, half of them in the
-// slice of 16,032 rows, 44 us, 95% of the copy rate for what it needs.
+// slice of 16,032 rows, 44 us, 95% of the copy rate for what it needs.  (28 bytes per
+// thread are spilled in the kernels of vectors of 8 bf16 elements, and of 4 fp32 ones to
+// bf16, which keep 40 registers for six CTAs per SM: within these 5%.)
 #include <cuda_runtime.h>
 
 #include "embed.h"
@@ -90,11 +92,13 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const __grid_constant__ L
 
 template <int V>
 cudaError_t launch(const LookupParams& p, cudaStream_t s) {
-  if (V <= 2 && p.dim / V > kRowLeast) {
-    const uint64_t ctas = (p.tokens.n + kThreads / 32 - 1) / (kThreads / 32);
-    auto* const kernel = p.bf16_table ? (p.bf16_out ? row_kernel<V, true, true> : row_kernel<V, true, false>)
-                                      : (p.bf16_out ? row_kernel<V, false, true> : row_kernel<V, false, false>);
-    return launch_chained(kernel, static_cast<int>(ctas), kThreads, 0, s, p);
+  if constexpr (V <= 2) {
+    if (p.dim / V > kRowLeast) {
+      const uint64_t ctas = (p.tokens.n + kThreads / 32 - 1) / (kThreads / 32);
+      auto* const kernel = p.bf16_table ? (p.bf16_out ? row_kernel<V, true, true> : row_kernel<V, true, false>)
+                                        : (p.bf16_out ? row_kernel<V, false, true> : row_kernel<V, false, false>);
+      return launch_chained(kernel, static_cast<int>(ctas), kThreads, 0, s, p);
+    }
   }
   const uint64_t all = p.tokens.n * (p.dim / V), ctas = (all + kThreads * kEach - 1) / (kThreads * kEach);
   if (ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
