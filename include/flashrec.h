@@ -520,13 +520,14 @@ fr_status fr_opt_convert(fr_opt src, fr_opt dst, uint32_t rounding, uint64_t see
  *
  * Precision.  All factors of the products are fp16 numbers, scaled so that fp16 holds
  * them, their sums in fp32.  A matrix with an fp32 output (weight, master or update)
- * has each factor as two of them, 22 bits, and three products for one: O is off by
- * 2^-17 to 2^-12 (roots of sums of squares over all elements; most where both sides have thousands,
- * or the rank is low), whatever the sides, mostly what the tensor cores' additions cut
- * off: they add 4,096 terms at most, longer sums are put together in fp32 (32,768 with one
- * product).  Others, and with FR_MUON_ONE all, enter X, X X^T and the polynomial in it by one
- * rounding each: with the usual coefficients and 5 iterations O is off by 0.05 to 0.2%,
- * by up to 0.5% where fewer than 16 singular values are not zero; a bf16 output's own rounding is
+ * has each factor as two of them, 22 bits, and three products for one: O is off (roots of
+ * sums of squares over all elements) by 2^-17 to 2^-12 for matrices like gradients, by up to 2^-10
+ * where one singular value is a thousand times thousands of others, and no more with
+ * longer sides: the tensor cores, whose additions cut sums off, add 4,096 terms at most
+ * (32,768 with one product), longer sums are put together in fp32.  Others, and with FR_MUON_ONE
+ * all, enter X, X X^T and the polynomial in it by one rounding each: with the usual
+ * coefficients and 5 iterations O is off by 0.05 to 0.2%, by up to 0.5% where singular values
+ * are few (below some 40), equal, or outweighed by one; a bf16 output's own rounding is
  * 0.17% (0.4% at most).  (The rounding of X alone would grow with every iteration, by a, in
  * the parts of small singular values: what it leaves is kept, and added to the product
  * as it is, until the iterations left raise it by no more than 4.)
